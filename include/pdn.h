@@ -58,7 +58,7 @@
 extern "C" {
 #endif
 
-#define PDN_ABI_VERSION 5
+#define PDN_ABI_VERSION 6
 
 typedef enum {
   PDN_OK = 0,
@@ -319,6 +319,100 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* problem, const pdn_inputs* in,
                                const void* dO, const float* dS_T, pdn_bwd_out* out,
                                void* ws, size_t ws_bytes, void* hip_stream,
                                void* const* stage_events, int n_events);
+
+/* ---------------------------------------------------------------- serving
+ * A server keeps the states of its sequences in a pool and runs ragged batches
+ * of them.  pdn_slot_fwd advances states over one or many tokens (decoding,
+ * prompts); pdn_slot_draft scores drafted tokens without moving the state and
+ * applies the ones a verification accepted in the next call's pass over the
+ * state; pdn_draft_verify is that verification.  All of it stays on the
+ * device: `accepted` of one is `accepted` of the other.
+ *
+ * Tokens of a batch are packed: q, k [tokens, Hk, dk], v, o [tokens, H, dv],
+ * beta, beta_p, g_p and a scalar g [tokens, H], a per-channel g
+ * [tokens, H, dk], ktilde [tokens, Hk, dk].  Value head h reads the query and
+ * key of head h / (H / Hk).  pdn_problem's B is the number of sequences, T the
+ * most tokens one of them has (a longer one is cut there), chunk is unused.
+ * The recurrence, its modes and the meaning of the other members are those of
+ * pdn_chunk_fwd; states and products are fp32 for both io types.
+ * Per-channel gate: of each eight tokens of a sequence (T > 1: counted from
+ * its first in the call) the log-decays of a channel must sum to more than -87.
+ *
+ * `starts`, `slot`, `slot_out`, `fresh`, `accepted` are device arrays, read by
+ * the kernels and not checked on the host; whatever they hold, accesses stay
+ * inside the declared tensors: row numbers are clamped to [0, tokens], and a
+ * sequence whose slot is outside [0, slots) is left out (its rows of o, and
+ * every slot, stay as they were: padding of a batch).  Rows of o that belong
+ * to no sequence stay as they were.
+ * A slot written by one sequence of a call must not be read or written by
+ * another of the same call; several may read one slot (forks of a state).
+ * Nothing checks it; the states concerned, and outputs of the readers, are
+ * then undefined. */
+typedef struct {
+  int64_t tokens;           /* rows of the packed token tensors                */
+  int64_t slots;            /* states in the pool                              */
+  int64_t Hk;               /* query / key heads, a divisor of H; 0: H         */
+  int64_t q_stride, k_stride, v_stride; /* elements from a token's row to the
+                               next (q, k, v may be slices of one projection's
+                               rows; whole multiples of 16 bytes); 0: dense    */
+  const int32_t* starts;    /* [B + 1] first row of each sequence, and the end of
+                               the last; NULL: B sequences of T rows           */
+  const int32_t* slot;      /* [B] slot a sequence's state is read from; NULL: its
+                               own number                                      */
+  const int32_t* slot_out;  /* [B] slot it is written to; NULL: slot           */
+  const int32_t* fresh;     /* [B] non-zero: start from a zero state (nothing is
+                               read from the slot); NULL: none does            */
+  float* S;                 /* [slots, H, dk, dv] S^T                          */
+  float* A;                 /* [slots, H, dk]; SQUASH, DIAG_SM, ATQ, else NULL */
+  /* pdn_slot_draft only (NULL and 0 in pdn_slot_fwd): */
+  float* tape;              /* [slots, tape_tokens, H, R] records of pending tokens,
+                               R = dk + dv + (per-channel gate: dk, else 4) + (A: dk):
+                               write key, correction e_t, log-decay summed from the first
+                               pending token (without the per-channel gate four
+                               times the same), A_t                            */
+  int64_t tape_tokens;      /* >= T                                            */
+  int32_t* pending;         /* [slots, H] records a slot has (of every head the
+                               same); zero at first                            */
+  const int32_t* accepted;  /* [B] pending tokens of the sequence that hold, first
+                               ones first; NULL: none                          */
+} pdn_slots;
+
+/* Advances each sequence's state over its tokens: reads it from `slot`, writes
+ * the state after the last token (S, A) to `slot_out`, and o.  in->S0 and in->A0
+ * must be NULL (PDN_ERR_VALUE).  One launch, no workspace.  Tokens pending
+ * on a tape are not looked at: apply or drop them first (pdn_slot_draft). */
+pdn_status pdn_slot_fwd(const pdn_problem* problem, const pdn_inputs* in,
+                        const pdn_slots* slots, void* o, void* hip_stream);
+
+/* Scores drafted tokens.  Of the tokens pending in `slot` the first
+ * min(accepted, pending) are applied to the state, the others dropped; the
+ * state then goes to `slot_out` (S, A), the new tokens' outputs to o, and the new
+ * tokens are left pending in slot_out's tape.  A sequence without rows only
+ * has its accepted tokens applied.  fresh: nothing is applied, the state is zero. */
+pdn_status pdn_slot_draft(const pdn_problem* problem, const pdn_inputs* in,
+                          const pdn_slots* slots, void* o, void* hip_stream);
+
+/* Verifies drafted tokens by the target's probabilities.  A sequence's rows are
+ * the tokens it was fed (ids): one that is certain, then the drafts.  p[row] is the
+ * target's distribution after that token, q[row] the distribution that token was
+ * drafted from (unused for a sequence's first; q NULL: each draft had
+ * probability one), both [rows, V] in `dtype`.  Draft t + 1 holds iff those before
+ * it do and u[t] q[t+1][x] < p[t][x], x its id (an id outside [0, V) does not
+ * hold).  accepted[n]: the tokens that hold, the first and the drafts.
+ * token[n]: drawn with r[n] by inversion (the first j whose running sum is
+ * over r times the whole) from max(p - q, 0) of the first refused draft (from p
+ * where that is zero everywhere), or from p after the last draft; -1 where no
+ * token has a positive weight.  A sequence without rows: 0 and -1.
+ * u: [rows] (a sequence's last is unused), r: [N], in [0, 1).  p and q need
+ * not be normalised; NaN counts as zero weight.  `starts` as in pdn_slots
+ * (NULL: rows / N rows each).  Sums are taken in 64 bits.
+ * `ws` must be 256-byte aligned, of pdn_draft_verify_workspace_size bytes. */
+pdn_status pdn_draft_verify_workspace_size(int64_t N, int64_t V, size_t* bytes);
+pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype,
+                            const void* p, const void* q, const int32_t* ids,
+                            const float* u, const float* r, const int32_t* starts,
+                            int32_t* accepted, int32_t* token, void* ws,
+                            size_t ws_bytes, void* hip_stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* pdn_status_string(pdn_status status);

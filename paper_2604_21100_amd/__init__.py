@@ -100,6 +100,15 @@ class BwdOut(ctypes.Structure):
                                    "dktilde")]
 
 
+class Slots(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("tokens", "slots", "Hk", "q_stride",
+                                               "k_stride", "v_stride")]
+                + [(n, _vp) for n in ("starts", "slot", "slot_out", "fresh",
+                                      "S", "A", "tape")]
+                + [("tape_tokens", ctypes.c_int64), ("pending", _vp),
+                   ("accepted", _vp)])
+
+
 _lib.pdn_workspace_size.argtypes = [ctypes.POINTER(Problem), ctypes.c_int,
                                     ctypes.POINTER(ctypes.c_size_t)]
 _lib.pdn_workspace_size.restype = ctypes.c_int
@@ -133,6 +142,17 @@ _lib.pdn_chunk_fwd_noalloc.argtypes = [
     ctypes.POINTER(Problem), ctypes.POINTER(Inputs), ctypes.POINTER(FwdOut),
     _vp]
 _lib.pdn_chunk_fwd_noalloc.restype = ctypes.c_int
+for _f in (_lib.pdn_slot_fwd, _lib.pdn_slot_draft):
+    _f.argtypes = [ctypes.POINTER(Problem), ctypes.POINTER(Inputs),
+                   ctypes.POINTER(Slots), _vp, _vp]
+    _f.restype = ctypes.c_int
+_lib.pdn_draft_verify.argtypes = [ctypes.c_int64, ctypes.c_int64,
+                                  ctypes.c_int64, ctypes.c_int, *[_vp] * 9,
+                                  ctypes.c_size_t, _vp]
+_lib.pdn_draft_verify.restype = ctypes.c_int
+_lib.pdn_draft_verify_workspace_size.argtypes = [
+    ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]
+_lib.pdn_draft_verify_workspace_size.restype = ctypes.c_int
 _lib.pdn_noalloc_scratch_bytes.argtypes = []
 _lib.pdn_noalloc_scratch_bytes.restype = ctypes.c_size_t
 _lib.pdn_status_string.argtypes = [ctypes.c_int]
@@ -143,7 +163,7 @@ _lib.pdn_scan_segments.argtypes = [ctypes.POINTER(Problem),
                                    ctypes.POINTER(ctypes.c_int)]
 _lib.pdn_scan_segments.restype = ctypes.c_int
 
-ABI_VERSION = 5   # PDN_ABI_VERSION: the struct layouts mirrored above
+ABI_VERSION = 6   # PDN_ABI_VERSION: the struct layouts mirrored above
 if _lib.pdn_abi_version() != ABI_VERSION:
     raise ImportError(f"{LIB_PATH} implements ABI version "
                       f"{_lib.pdn_abi_version()}, this binding mirrors "
@@ -153,7 +173,9 @@ EXPORTED = ("pdn_workspace_size", "pdn_chunk_fwd", "pdn_chunk_fwd_events",
             "pdn_chunk_bwd", "pdn_chunk_bwd_events", "pdn_chunk_fwd_train",
             "pdn_chunk_bwd_train", "pdn_chunk_fwd_noalloc",
             "pdn_noalloc_scratch_bytes", "pdn_status_string",
-            "pdn_abi_version", "pdn_scan_segments")
+            "pdn_abi_version", "pdn_scan_segments", "pdn_slot_fwd",
+            "pdn_slot_draft", "pdn_draft_verify",
+            "pdn_draft_verify_workspace_size")
 FWD_STAGE_EVENTS = 4   # PDN_FWD_STAGE_EVENTS
 BWD_STAGE_EVENTS = 7   # PDN_BWD_STAGE_EVENTS
 FWD_STAGES = ("precond", "chunk_prep", "chunk_scan")
@@ -428,3 +450,181 @@ def pdn_chunk_bwd(q, k, v, beta, dO, *, g=None, gate="none", precond="squash",
     if st != PDN_OK:
         raise PdnError(st, "pdn_chunk_bwd")
     return out
+
+
+# ------------------------------------------------------- states in a pool
+def _on(name, t, device, dtype=None, shape=None):
+    """A dense tensor the kernels read as `shape` and `dtype` on `device`."""
+    if t is None:
+        return None
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the state pool on {device}")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _token_rows(name, t, device, dtype, shape):
+    """A [tokens, heads, d] tensor with dense rows: its pointer and the elements
+    from one token to the next (0: dense)."""
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the state pool on {device}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
+    if t.stride(2) != 1 or t.stride(1) != shape[2]:
+        if shape[0] and shape[1] > 1 or t.stride(2) != 1:
+            raise ValueError(f"a token's row of {name} must be dense")
+    return t.data_ptr(), t.stride(0)
+
+
+def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
+               slots, slots_out, fresh, max_tokens, g, gate, precond, beta_p,
+               g_p, log_a_scale, A, ktilde, x, scale, ridge, knorm, o, stream):
+    if S.dim() != 4 or q.dim() != 3 or v.dim() != 3:
+        raise ValueError("S must be [slots, H, dk, dv], q, k [tokens, Hk, dk] "
+                         "and v [tokens, H, dv]")
+    P, H, dk, dv = S.shape
+    M, Hk, _ = q.shape
+    dev, f32, i32 = S.device, torch.float32, torch.int32
+    io = _io_of(q)
+    if starts is not None:
+        N = starts.numel() - 1
+        if N < 0:
+            raise ValueError("starts must hold one entry more than sequences")
+    elif slots is not None:
+        N = slots.numel()
+    else:
+        N = M // max_tokens if max_tokens else M
+    T = max_tokens
+    if T is None:   # without starts: rows shared out evenly
+        T = M if starts is not None else M // N if N else 0
+    gram = precond in GRAM_PRECONDS
+    prob = make_problem(N, T, H, dk, dv, io=io, gate=gate, precond=precond,
+                        x=x, scale=scale, ridge=ridge, knorm=knorm)
+    qp, qs = _token_rows("q", q, dev, q.dtype, (M, Hk, dk))
+    kp, ks = _token_rows("k", k, dev, q.dtype, (M, Hk, dk))
+    vp, vs = _token_rows("v", v, dev, q.dtype, (M, H, dv))
+    if o is None:
+        o = torch.empty((M, H, dv), dtype=q.dtype, device=dev)
+    inp = Inputs(qp, kp, vp, _on("beta", beta, dev, f32, (M, H)),
+                 _on("g", g, dev, f32,
+                     (M, H, dk) if gate == "channel" else (M, H)),
+                 _on("beta_p", beta_p, dev, f32, (M, H)),
+                 _on("g_p", g_p, dev, f32, (M, H)),
+                 _on("log_a_scale", log_a_scale, dev, f32, (H,)),
+                 None, None, _on("ktilde", ktilde, dev, q.dtype, (M, Hk, dk)))
+    sl = Slots(M, P, Hk, qs, ks, vs, _on("starts", starts, dev, i32, (N + 1,)),
+               _on("slots", slots, dev, i32, (N,)),
+               _on("slots_out", slots_out, dev, i32, (N,)),
+               _on("fresh", fresh, dev, i32, (N,)), _on("S", S, dev, f32),
+               _on("A", A, dev, f32, (P, H, dk)), None, 0, None, None)
+    if tape is not None:
+        sl.tape = _on("tape", tape, dev, f32,
+                      (P, tape.shape[1], H, pdn_tape_record(dk, dv, gate, precond)))
+        sl.tape_tokens = tape.shape[1]
+        sl.pending = _on("pending", pending, dev, i32, (P, H))
+        sl.accepted = _on("accepted", accepted, dev, i32, (N,))
+    with torch.cuda.device(dev):
+        st = fn(ctypes.byref(prob), ctypes.byref(inp), ctypes.byref(sl),
+                _on("o", o, dev, q.dtype, (M, H, dv)), _stream(stream, dev))
+    if st != PDN_OK:
+        raise PdnError(st, where)
+    return o
+
+
+def pdn_tape_record(dk, dv, gate="none", precond="squash") -> int:
+    """Elements of a pending token's record for one head (see pdn_slots)."""
+    return (dk + dv + (dk if gate == "channel" else 4)
+            + (dk if precond in GRAM_PRECONDS else 0))
+
+
+def pdn_slot_fwd(q, k, v, beta, S, *, starts=None, slots=None, slots_out=None,
+                 fresh=None, max_tokens=None, g=None, gate="none",
+                 precond="squash", beta_p=None, g_p=None, log_a_scale=None,
+                 A=None, ktilde=None, x=1.5, scale=1.0, ridge=1.0,
+                 knorm="none", o=None, stream=None):
+    """Advance states of a pool over packed sequences (pdn_slot_fwd of pdn.h).
+
+    q, k [tokens, Hk, dk] and v [tokens, H, dv], rows of any token stride
+    (slices of one projection); S [slots, H, dk, dv] and A [slots, H, dk] are
+    read and written in place.  starts [N + 1], slots, slots_out, fresh [N]:
+    int32 on the device.  Without starts the rows are shared evenly
+    by the sequences (one row each without slots too).  max_tokens: the most
+    rows a sequence has (default: unknown, at most all).  Returns o."""
+    return _slot_call(
+        _lib.pdn_slot_fwd, "pdn_slot_fwd", q, k, v, beta, S, None, None, None,
+        starts=starts, slots=slots, slots_out=slots_out, fresh=fresh,
+        max_tokens=max_tokens, g=g, gate=gate, precond=precond, beta_p=beta_p,
+        g_p=g_p, log_a_scale=log_a_scale, A=A, ktilde=ktilde, x=x, scale=scale,
+        ridge=ridge, knorm=knorm, o=o, stream=stream)
+
+
+def pdn_slot_draft(q, k, v, beta, S, tape, pending, *, accepted=None,
+                   starts=None, slots=None, slots_out=None, fresh=None,
+                   max_tokens=None, g=None, gate="none", precond="squash",
+                   beta_p=None, g_p=None, log_a_scale=None, A=None,
+                   ktilde=None, x=1.5, scale=1.0, ridge=1.0, knorm="none",
+                   o=None, stream=None):
+    """Score drafted tokens on states of a pool (pdn_slot_draft of pdn.h).
+
+    The tokens the last call left pending are applied as far as `accepted`
+    ([N] int32, e.g. of pdn_draft_verify) says, then the new ones are scored
+    and left pending.  tape: [slots, most tokens, H, pdn_tape_record(...)]
+    fp32; pending: [slots, H] int32, zero at first.  max_tokens defaults to what
+    the tape holds.  The rest as in pdn_slot_fwd.  Returns o."""
+    if tape.dim() != 4:
+        raise ValueError("tape must be [slots, tokens, H, record]")
+    if max_tokens is None and starts is not None:
+        max_tokens = tape.shape[1]
+    return _slot_call(
+        _lib.pdn_slot_draft, "pdn_slot_draft", q, k, v, beta, S, tape, pending,
+        accepted, starts=starts, slots=slots, slots_out=slots_out, fresh=fresh,
+        max_tokens=max_tokens, g=g, gate=gate, precond=precond, beta_p=beta_p,
+        g_p=g_p, log_a_scale=log_a_scale, A=A, ktilde=ktilde, x=x, scale=scale,
+        ridge=ridge, knorm=knorm, o=o, stream=stream)
+
+
+def pdn_draft_verify_workspace_size(N: int, V: int) -> int:
+    n = ctypes.c_size_t(0)
+    st = _lib.pdn_draft_verify_workspace_size(N, V, ctypes.byref(n))
+    if st != PDN_OK:
+        raise PdnError(st, "pdn_draft_verify_workspace_size")
+    return n.value
+
+
+def pdn_draft_verify(p, ids, u, r, *, q=None, starts=None, accepted=None,
+                     token=None, workspace=None, stream=None):
+    """Verify drafted tokens against the target's probabilities
+    (pdn_draft_verify of pdn.h).
+
+    p, q: [rows, V], fp32 or bf16; ids [rows] int32, the tokens fed; u [rows],
+    r [N] fp32 in [0, 1).  Returns (accepted, token), int32 [N]: the rows that hold
+    (what pdn_slot_draft applies) and the token after them."""
+    if p.dim() != 2:
+        raise ValueError("p must be [rows, V]")
+    M, V = p.shape
+    N, dev, f32, i32 = r.numel(), p.device, torch.float32, torch.int32
+    io = _io_of(p)
+    accepted = torch.empty(N, dtype=i32, device=dev) if accepted is None else accepted
+    token = torch.empty(N, dtype=i32, device=dev) if token is None else token
+    if workspace is None:
+        workspace = torch.empty(max(pdn_draft_verify_workspace_size(N, V), 1),
+                                dtype=torch.uint8, device=dev)
+    with torch.cuda.device(dev):
+        st = _lib.pdn_draft_verify(
+            N, M, V, PDN_BF16 if io == "bf16" else PDN_F32, _on("p", p, dev),
+            _on("q", q, dev, p.dtype, (M, V)), _on("ids", ids, dev, i32, (M,)),
+            _on("u", u, dev, f32, (M,)), _on("r", r, dev, f32, (N,)),
+            _on("starts", starts, dev, i32, (N + 1,)),
+            _on("accepted", accepted, dev, i32, (N,)),
+            _on("token", token, dev, i32, (N,)), _on("workspace", workspace, dev),
+            workspace.numel(), _stream(stream, dev))
+    if st != PDN_OK:
+        raise PdnError(st, "pdn_draft_verify")
+    return accepted, token

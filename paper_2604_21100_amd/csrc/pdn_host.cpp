@@ -152,6 +152,141 @@ pdn_status check_bwd_support(const pdn_problem* p) {
   return PDN_OK;
 }
 
+// ---- calls on a pool of states
+struct SlotSizes {
+  int64_t nq, nk, nv, no, nx;       // bytes the token tensors span
+  int64_t nscal, ngate, ngram;      // per-token fp32 tensors, bytes
+  int64_t nS, nA, ntape, npend, nseq;
+  int64_t qs, ks, vs;               // token strides
+};
+
+// rows x stride (the last row: its own width), in bytes
+bool span_ok(int64_t rows, int64_t stride, int64_t width, int esz, int64_t* out) {
+  if (rows == 0) {
+    *out = 0;
+    return true;
+  }
+  int64_t x;
+  if (!mul_ok(rows - 1, stride, &x) || x > INT64_MAX / 16 - width) return false;
+  *out = (x + width) * esz;
+  return true;
+}
+
+pdn_status check_slots(const pdn_problem* p, const pdn_slots* s, bool draft, SlotSizes* out) {
+  Sizes unused;
+  if (!p) return PDN_ERR_NULL;
+  pdn_problem one = *p;   // (the chunk is not used by these calls)
+  one.chunk = 64;
+  pdn_status st = check_problem(&one, &unused);
+  if (st != PDN_OK) return st;
+  if (!s) return PDN_ERR_NULL;
+  if (s->tokens < 0 || s->slots < 0 || s->Hk < 0) return PDN_ERR_SHAPE;
+  const int64_t Hk = s->Hk ? s->Hk : p->H;
+  if (p->H > 0 && p->H % Hk != 0) return PDN_ERR_SHAPE;
+  // row numbers and slots are 32-bit on the device; one workgroup a head
+  if (s->tokens > INT32_MAX || s->slots > INT32_MAX || unused.BH >= (int64_t)1 << 24) return PDN_ERR_SHAPE;
+  int64_t even;
+  if (!s->starts && (!mul_ok(p->B, p->T, &even) || even != s->tokens)) return PDN_ERR_SHAPE;
+  if (!s->slot && p->B > s->slots) return PDN_ERR_SHAPE;
+  SlotSizes z{};
+  const int esz = p->io == PDN_BF16 ? 2 : 4;
+  int64_t wq, wv, tok, slots_h, rec;
+  if (!mul_ok(Hk, p->dk, &wq) || !mul_ok(p->H, p->dv, &wv) || !mul_ok(s->tokens, p->H, &tok) ||
+      !mul_ok(s->slots, p->H, &slots_h))
+    return PDN_ERR_SHAPE;
+  z.qs = s->q_stride ? s->q_stride : wq;
+  z.ks = s->k_stride ? s->k_stride : wq;
+  z.vs = s->v_stride ? s->v_stride : wv;
+  if (z.qs < wq || z.ks < wq || z.vs < wv) return PDN_ERR_SHAPE;
+  if (z.qs * esz % 16 || z.ks * esz % 16 || z.vs * esz % 16) return PDN_ERR_ALIGN;
+  if (!span_ok(s->tokens, z.qs, wq, esz, &z.nq) || !span_ok(s->tokens, z.ks, wq, esz, &z.nk) ||
+      !span_ok(s->tokens, z.vs, wv, esz, &z.nv) || !span_ok(s->tokens, wv, wv, esz, &z.no) ||
+      !span_ok(s->tokens, wq, wq, esz, &z.nx) || !mul_ok(tok, 4 * 128, &z.nscal) ||
+      !mul_ok(slots_h, (int64_t)4 * 128 * 128, &z.nS))
+    return PDN_ERR_SHAPE;
+  z.nscal = tok * 4;
+  z.ngate = p->gate == PDN_GATE_NONE ? 0 : p->gate == PDN_GATE_SCALAR ? tok * 4 : tok * 4 * p->dk;
+  z.nS = slots_h * p->dk * p->dv * 4;
+  z.nA = slots_h * p->dk * 4;
+  z.nseq = p->B * 4;
+  if (draft) {
+    if (s->tape_tokens > INT32_MAX || p->T > s->tape_tokens || s->tape_tokens < 1) return PDN_ERR_SHAPE;
+    if (!mul_ok(slots_h, s->tape_tokens, &rec) || !mul_ok(rec, 4 * 512, &z.ntape)) return PDN_ERR_SHAPE;
+    z.ntape = rec * 4 * (p->dk + p->dv + (p->gate == PDN_GATE_CHANNEL ? p->dk : 4) +
+                         (pdn::has_gram(p->precond) ? p->dk : 0));
+    z.npend = slots_h * 4;
+  }
+  *out = z;
+  return PDN_OK;
+}
+
+pdn_status slot_call(const pdn_problem* p, const pdn_inputs* in, const pdn_slots* s, void* o, bool draft,
+                     void* hip_stream) {
+  SlotSizes z;
+  pdn_status st = check_slots(p, s, draft, &z);
+  if (st != PDN_OK) return st;
+  if (!in) return PDN_ERR_NULL;
+  const bool gram = pdn::has_gram(p->precond), some = s->tokens > 0 && p->H > 0;
+  const bool work = p->B > 0 && p->H > 0 && s->slots > 0;
+  if (some) {
+    if (!in->q || !in->k || !in->v || !in->beta || !o) return PDN_ERR_NULL;
+    if (p->gate != PDN_GATE_NONE && !in->g) return PDN_ERR_NULL;
+    if (gram && !in->beta_p) return PDN_ERR_NULL;
+    if (p->precond == PDN_PRECOND_EXTERNAL && !in->ktilde) return PDN_ERR_NULL;
+  }
+  if (work) {
+    if (!s->S || (gram && !s->A)) return PDN_ERR_NULL;
+    if (p->precond == PDN_PRECOND_SQUASH && !in->log_a_scale) return PDN_ERR_NULL;
+    if (draft && (!s->pending || !s->tape)) return PDN_ERR_NULL;
+  }
+  if (p->gate == PDN_GATE_NONE && in->g) return PDN_ERR_VALUE;
+  // the states are the pool's
+  if (in->S0 || in->A0) return PDN_ERR_VALUE;
+  if (!gram && s->A) return PDN_ERR_VALUE;
+  if (!draft && (s->tape || s->pending || s->accepted)) return PDN_ERR_VALUE;
+  std::vector<Buf> ins = {{in->q, z.nq}, {in->k, z.nk}, {in->v, z.nv}, {in->beta, z.nscal}, {in->g, z.ngate}};
+  if (gram) {
+    ins.push_back({in->beta_p, z.nscal});
+    ins.push_back({in->g_p, z.nscal});
+  }
+  if (p->precond == PDN_PRECOND_SQUASH) ins.push_back({in->log_a_scale, p->H * 4});
+  if (p->precond == PDN_PRECOND_EXTERNAL) ins.push_back({in->ktilde, z.nx});
+  const std::vector<Buf> lists = {{s->starts, (p->B + 1) * 4}, {s->slot, z.nseq}, {s->slot_out, z.nseq},
+                                  {s->fresh, z.nseq}, {s->accepted, z.nseq}};
+  const std::vector<Buf> outs = {{o, z.no}, {s->S, z.nS}, {s->A, z.nA}, {s->tape, z.ntape}, {s->pending, z.npend}};
+  for (const std::vector<Buf>& v : {ins, outs})
+    for (const Buf& x : v)
+      if (x.p && !aligned16(x.p)) return PDN_ERR_ALIGN;
+  for (const Buf& x : lists)
+    if (x.p && (reinterpret_cast<uintptr_t>(x.p) & 3u)) return PDN_ERR_ALIGN;
+  ins.insert(ins.end(), lists.begin(), lists.end());
+  if ((st = check_aliasing(ins, outs, Buf{nullptr, 0})) != PDN_OK) return st;
+  if (!work) return PDN_OK;
+
+  pdn::SlotArgs a{};
+  a.B = p->B; a.T = p->T; a.H = p->H; a.Hk = s->Hk ? s->Hk : p->H;
+  a.tokens = s->tokens; a.slots = s->slots;
+  a.q_stride = z.qs; a.k_stride = z.ks; a.v_stride = z.vs;
+  a.dk = p->dk; a.dv = p->dv;
+  a.gate = p->gate; a.precond = p->precond; a.knorm = p->knorm;
+  a.lnx = std::log(p->x);
+  a.scale = p->scale;
+  a.ridge = p->ridge;
+  a.q = in->q; a.k = in->k; a.v = in->v; a.ktilde = in->ktilde;
+  a.beta = in->beta; a.g = in->g; a.beta_p = in->beta_p; a.g_p = in->g_p;
+  a.log_a_scale = in->log_a_scale;
+  a.starts = s->starts; a.slot = s->slot; a.slot_out = s->slot_out; a.fresh = s->fresh;
+  a.S = s->S; a.A = s->A; a.o = o;
+  if (draft) {
+    a.tape = s->tape;
+    a.pending = s->pending;
+    a.accepted = s->accepted;
+    a.tape_tokens = s->tape_tokens;
+  }
+  return pdn::launch_slots(a, p->io == PDN_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PDN_OK
+                                                                                                     : PDN_ERR_HIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -454,6 +589,66 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* p, const pdn_inputs* in, const
   if (st != PDN_OK) return st;
   return chunk_bwd_impl(p, in, dO, dS_T, out, ws, ws_bytes, hip_stream,
                         reinterpret_cast<hipEvent_t const*>(stage_events), true);
+}
+
+pdn_status pdn_slot_fwd(const pdn_problem* p, const pdn_inputs* in, const pdn_slots* s, void* o,
+                        void* hip_stream) {
+  return slot_call(p, in, s, o, false, hip_stream);
+}
+
+pdn_status pdn_slot_draft(const pdn_problem* p, const pdn_inputs* in, const pdn_slots* s, void* o,
+                          void* hip_stream) {
+  return slot_call(p, in, s, o, true, hip_stream);
+}
+
+static pdn_status check_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype, bool even, int64_t* row_bytes,
+                               int64_t* ws_bytes) {
+  if (N < 0 || rows < 0 || V < 0) return PDN_ERR_SHAPE;
+  if (dtype != PDN_F32 && dtype != PDN_BF16) return PDN_ERR_DTYPE;
+  // ids and row numbers are 32-bit; a workgroup a segment and sequence
+  int64_t blocks, bytes;
+  if (N > INT32_MAX || rows > INT32_MAX || V > INT32_MAX || (V == 0 && rows > 0)) return PDN_ERR_SHAPE;
+  if (!mul_ok(N, pdn::verify_blocks(V), &blocks) || blocks >= (int64_t)1 << 24) return PDN_ERR_SHAPE;
+  if (!mul_ok(rows, V, &bytes) || !mul_ok(bytes, 4, &bytes)) return PDN_ERR_SHAPE;
+  if (even && N > 0 && rows % N != 0) return PDN_ERR_SHAPE;
+  *row_bytes = rows * V * (dtype == PDN_BF16 ? 2 : 4);
+  *ws_bytes = blocks * 16;
+  return PDN_OK;
+}
+
+pdn_status pdn_draft_verify_workspace_size(int64_t N, int64_t V, size_t* bytes) {
+  if (!bytes) return PDN_ERR_NULL;
+  int64_t rb, wb;
+  const pdn_status st = check_verify(N, V > 0 ? N : 0, V, PDN_F32, false, &rb, &wb);
+  if (st == PDN_OK) *bytes = static_cast<size_t>(wb);
+  return st;
+}
+
+pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype, const void* p, const void* q,
+                            const int32_t* ids, const float* u, const float* r, const int32_t* starts,
+                            int32_t* accepted, int32_t* token, void* ws, size_t ws_bytes, void* hip_stream) {
+  int64_t rb, wb;
+  pdn_status st = check_verify(N, rows, V, dtype, !starts, &rb, &wb);
+  if (st != PDN_OK) return st;
+  if (N > 0 && (!accepted || !token)) return PDN_ERR_NULL;
+  if (N > 0 && rows > 0 && (!p || !ids || !u || !r)) return PDN_ERR_NULL;
+  const std::vector<Buf> ins = {{p, rb}, {q, rb}, {ids, rows * 4}, {u, rows * 4}, {r, N * 4}, {starts, (N + 1) * 4}};
+  const std::vector<Buf> outs = {{accepted, N * 4}, {token, N * 4}};
+  for (const std::vector<Buf>& v : {ins, outs})   // (probabilities: to an element, as a row of an odd V is)
+    for (const Buf& x : v)
+      if (x.p && (reinterpret_cast<uintptr_t>(x.p) & (dtype == PDN_BF16 && (x.p == p || x.p == q) ? 1u : 3u)))
+        return PDN_ERR_ALIGN;
+  if ((st = check_aliasing(ins, outs, Buf{ws, N > 0 ? static_cast<int64_t>(ws_bytes) : 0})) != PDN_OK) return st;
+  if (N == 0) return PDN_OK;
+  if (wb > 0 && (!ws || ws_bytes < static_cast<size_t>(wb) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0))
+    return PDN_ERR_WORKSPACE;
+  pdn::VerifyArgs a{};
+  a.N = N; a.rows = rows; a.V = V;
+  a.p = p; a.q = q; a.ids = ids; a.u = u; a.r = r; a.starts = starts;
+  a.accepted = accepted; a.token = token;
+  a.sums = static_cast<double*>(ws);
+  return pdn::launch_verify(a, dtype == PDN_BF16, static_cast<hipStream_t>(hip_stream)) == hipSuccess ? PDN_OK
+                                                                                                      : PDN_ERR_HIP;
 }
 
 }  // extern "C"

@@ -229,6 +229,53 @@ inline bool step_form(const FwdArgs& a, bool io_bf16) {
 }
 hipError_t launch_step_tokens(const FwdArgs& a, int io_bf16, hipStream_t s);
 
+// The calls on a pool of states (pdn_slots.hip): see pdn_slots in pdn.h.
+struct SlotArgs {
+  int64_t B, T, H, Hk;   // sequences, most tokens of one, value heads, query / key heads
+  int64_t tokens, slots;
+  int64_t q_stride, k_stride, v_stride;   // elements from one token to the next
+  int dk, dv, gate, precond, knorm;
+  float lnx, scale, ridge;
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* ktilde;
+  const float* beta;
+  const float* g;
+  const float* beta_p;
+  const float* g_p;
+  const float* log_a_scale;
+  const int32_t* starts;
+  const int32_t* slot;
+  const int32_t* slot_out;
+  const int32_t* fresh;
+  float* S;
+  float* A;
+  void* o;
+  // drafts (NULL otherwise)
+  float* tape;           // [slots, tape_tokens, H, record]
+  int32_t* pending;      // [slots, H]
+  const int32_t* accepted;
+  int64_t tape_tokens;
+};
+hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s);
+
+// Verification of drafted tokens (pdn_verify.hip).
+struct VerifyArgs {
+  int64_t N, rows, V;
+  const void* p;
+  const void* q;
+  const int32_t* ids;
+  const float* u;
+  const float* r;
+  const int32_t* starts;
+  int32_t* accepted;
+  int32_t* token;
+  double* sums;          // [N, verify_blocks(V), 2]
+};
+int64_t verify_blocks(int64_t V);   // segments a row is summed in
+hipError_t launch_verify(const VerifyArgs& a, int io_bf16, hipStream_t s);
+
 struct WsLayout {
   size_t sumL, sumD, Abound, KtG, Tm, Pm, G, Qt, QL, KL, seg_end, seg_phi, seg_start, total;
   ScanSplit split;

@@ -1,0 +1,262 @@
+// Verification of drafted tokens against the target's probabilities, from
+// given random numbers.  Row t of a sequence is the target's distribution
+// after its token t; token t + 1 was drafted from row t + 1 of q:
+//   token t + 1 holds iff those before it do and u_t q_{t+1}(x) < p_t(x)
+//   w = max(p_n - q_{n+1}, 0) where draft n + 1 is refused (p_n where that is
+//   zero everywhere), p_n after the last draft
+//   the next token: the first j with w_0 + .. + w_j > r (w_0 + .. + w_{V-1})
+// Products, differences and sums in 64 bits: a product of two of the inputs'
+// numbers is exact, and a running sum over a large vocabulary has to be finer
+// than the steps between its tokens, which 32 bits are not.
+//
+// Two launches: the row the sequence stops at is summed in segments of 2048
+// tokens, a workgroup each (every one finds the row for itself: a few reads),
+// then one workgroup a sequence finds the segment, and in it the token.
+// Segment sums are added in one order, so the token does not depend on which
+// workgroup was first.
+#include "pdn_device.hpp"
+#include "pdn_internal.hpp"
+
+namespace pdn {
+
+namespace {
+
+constexpr int kThreads = 256, kVec = 8, kSeg = kThreads * kVec;
+
+inline __host__ __device__ int64_t segments(int64_t V) { return (V + kSeg - 1) / kSeg; }
+
+struct Span {
+  int64_t lo, n;   // first row, rows
+};
+__device__ __forceinline__ Span seq_span(const VerifyArgs& a, int64_t seq) {
+  int64_t lo = seq * (a.rows / a.N), hi = lo + a.rows / a.N;
+  if (a.starts) {
+    lo = a.starts[seq];
+    hi = a.starts[seq + 1];
+  }
+  lo = min(max(lo, (int64_t)0), a.rows);
+  return Span{lo, max(min(hi, a.rows) - lo, (int64_t)0)};
+}
+
+// drafts that hold, found by one wave (every lane returns it)
+template <typename T>
+__device__ __forceinline__ int64_t held(const VerifyArgs& a, const Span& s, int l) {
+  const T* p = static_cast<const T*>(a.p);
+  const T* q = static_cast<const T*>(a.q);
+  for (int64_t t0 = 0; t0 + 1 < s.n; t0 += kWave) {
+    const int64_t row = s.lo + t0 + l;
+    const bool draft = t0 + l + 1 < s.n;
+    bool ok = false;
+    if (draft) {
+      const int64_t x = a.ids[row + 1];
+      if (x >= 0 && x < a.V) {
+        const double px = to_f(p[row * a.V + x]), qx = q ? to_f(q[(row + 1) * a.V + x]) : 1.f;
+        ok = a.u[row] * qx < px;
+      }
+    }
+    const unsigned long long bad = __ballot(draft && !ok);
+    if (bad) return t0 + __ffsll(bad) - 1;
+  }
+  return max(s.n - 1, (int64_t)0);
+}
+
+// Eight tokens' weights from j0: p (kind 1), or what is left of it over q or
+// without the drafted token x (kind 0; x < 0 and q NULL: p).  No token past V,
+// no NaN, nothing below zero.
+template <typename T>
+struct Row {
+  const T* p;
+  const T* q;   // NULL: without the one token x
+  int64_t x;
+};
+template <typename T>
+__device__ __forceinline__ void ld_row(const T* p, int64_t j0, int64_t V, float (&v)[kVec]) {
+  T raw[kVec];
+  if (j0 + kVec <= V) {
+    __builtin_memcpy(raw, p + j0, sizeof raw);   // (rows of an odd V are aligned to an element only)
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) raw[i] = j0 + i < V ? p[j0 + i] : from_f<T>(0.f);
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = to_f(raw[i]);
+}
+template <typename T>
+__device__ __forceinline__ void weights(const Row<T>& r, int64_t j0, int64_t V, double (&w0)[kVec], double (&w1)[kVec]) {
+  float p[kVec], q[kVec];
+  ld_row(r.p, j0, V, p);
+  if (r.q) ld_row(r.q, j0, V, q);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const double x = p[i], y = r.q ? x - q[i] : (j0 + i == r.x ? 0.0 : x);
+    w1[i] = x > 0.0 ? x : 0.0;
+    w0[i] = y > 0.0 ? y : 0.0;
+  }
+}
+template <typename T>
+__device__ __forceinline__ Row<T> stop_row(const VerifyArgs& a, const Span& s, int64_t n) {
+  const int64_t row = s.lo + n;
+  Row<T> r{static_cast<const T*>(a.p) + row * a.V, nullptr, -1};
+  if (n + 1 < s.n) {   // a draft was refused
+    if (a.q) r.q = static_cast<const T*>(a.q) + (row + 1) * a.V;
+    else r.x = a.ids[row + 1];
+  }
+  return r;
+}
+
+__device__ __forceinline__ double wave_add(double x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+  return x;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
+  __shared__ double sW[2][kThreads / kWave];
+  const int64_t segs = segments(a.V), seq = blockIdx.x / segs, seg = blockIdx.x % segs;
+  const Span s = seq_span(a, seq);
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
+  if (s.n == 0) return;
+  const int64_t n = held<T>(a, s, l);
+  if (seg == 0 && tid == 0) a.accepted[seq] = static_cast<int>(n + 1);
+  double w0[kVec], w1[kVec], x0 = 0.0, x1 = 0.0;
+  weights(stop_row<T>(a, s, n), seg * kSeg + tid * kVec, a.V, w0, w1);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    x0 += w0[i];
+    x1 += w1[i];
+  }
+  x0 = wave_add(x0);
+  x1 = wave_add(x1);
+  if (l == 0) {
+    sW[0][w] = x0;
+    sW[1][w] = x1;
+  }
+  __syncthreads();
+  if (tid < 2) a.sums[blockIdx.x * 2 + tid] = ((sW[tid][0] + sW[tid][1]) + sW[tid][2]) + sW[tid][3];
+}
+
+// inclusive sums over the workgroup's threads, in order; every thread also
+// gets the whole sum
+__device__ __forceinline__ double block_scan(double x, double* sW, double* all) {
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const double y = __shfl_up(x, off, 64);
+    if (l >= off) x += y;
+  }
+  __syncthreads();
+  if (l == 63) sW[w] = x;
+  __syncthreads();
+  double before = 0.0, sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kThreads / kWave; ++i) {
+    if (i < w) before += sW[i];
+    sum += sW[i];
+  }
+  *all = sum;
+  return before + x;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void verify_pick(VerifyArgs a) {
+  __shared__ double sW[kThreads / kWave];
+  __shared__ double sTot[2];
+  __shared__ unsigned long long sFirst, sLast;   // the first position over the target; the last with a weight, plus one
+  __shared__ double sBefore;
+  const int64_t segs = segments(a.V), seq = blockIdx.x;
+  const Span s = seq_span(a, seq);
+  const int tid = threadIdx.x;
+  if (s.n == 0) {   // no rows
+    if (tid == 0) {
+      a.accepted[seq] = 0;
+      a.token[seq] = -1;
+    }
+    return;
+  }
+  const double* sums = a.sums + seq * segs * 2;
+  const int64_t n = a.accepted[seq] - 1;
+  double tot[2] = {0.0, 0.0};
+  for (int64_t b = 0; b < segs; b += kThreads)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      double all;
+      block_scan(b + tid < segs ? sums[2 * (b + tid) + k] : 0.0, sW, &all);
+      tot[k] += all;
+    }
+  const int kind = tot[0] > 0.0 ? 0 : 1;   // nothing left over q: p itself
+  const double target = a.r[seq] * tot[kind];
+  // the segment, then the token in it: the first whose running sum is over the
+  // target, else the last that has a weight
+  if (tid == 0) {
+    sFirst = ~0ull;
+    sLast = 0ull;
+    sBefore = 0.0;
+  }
+  double base = 0.0;
+  for (int64_t b = 0; b < segs; b += kThreads) {
+    const double x = b + tid < segs ? sums[2 * (b + tid) + kind] : 0.0;
+    double all;
+    const double cum = base + block_scan(x, sW, &all);
+    if (b + tid < segs && x > 0.0) {
+      atomicMax(&sLast, static_cast<unsigned long long>(b + tid) + 1);
+      if (cum > target) atomicMin(&sFirst, static_cast<unsigned long long>(b + tid));
+    }
+    __syncthreads();
+    const bool found = sFirst != ~0ull;
+    if (found && static_cast<unsigned long long>(b + tid) == sFirst) sBefore = cum - x;
+    __syncthreads();
+    if (found) break;
+    base += all;
+  }
+  const unsigned long long first = sFirst, last = sLast;
+  const double before = sBefore;
+  __syncthreads();
+  if (last == 0ull) {   // no token has a weight
+    if (tid == 0) a.token[seq] = -1;
+    return;
+  }
+  const int64_t seg = static_cast<int64_t>(first != ~0ull ? first : last - 1);
+  if (tid == 0) {
+    sFirst = ~0ull;
+    sLast = 0ull;
+  }
+  double w0[kVec], w1[kVec], x = 0.0, all;
+  const int64_t j0 = seg * kSeg + tid * kVec;
+  weights(stop_row<T>(a, s, n), j0, a.V, w0, w1);
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) x += kind ? w1[i] : w0[i];
+  double cum = before + (block_scan(x, sW, &all) - x);
+  unsigned long long f = ~0ull, g = 0ull;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const double v = kind ? w1[i] : w0[i];
+    cum += v;
+    if (v > 0.0) {
+      g = static_cast<unsigned long long>(j0 + i) + 1;
+      if (f == ~0ull && first != ~0ull && cum > target) f = static_cast<unsigned long long>(j0 + i);
+    }
+  }
+  if (f != ~0ull) atomicMin(&sFirst, f);
+  if (g) atomicMax(&sLast, g);
+  __syncthreads();
+  if (tid == 0) a.token[seq] = static_cast<int>(sFirst != ~0ull ? sFirst : sLast - 1);
+}
+
+template <typename T>
+hipError_t launch(const VerifyArgs& a, hipStream_t s) {
+  if (a.rows > 0)
+    hipLaunchKernelGGL((verify_sums<T>), dim3(static_cast<unsigned>(a.N * segments(a.V))), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((verify_pick<T>), dim3(static_cast<unsigned>(a.N)), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int64_t verify_blocks(int64_t V) { return segments(V); }
+
+hipError_t launch_verify(const VerifyArgs& a, int io_bf16, hipStream_t s) {
+  return io_bf16 ? launch<bf16>(a, s) : launch<float>(a, s);
+}
+
+}  // namespace pdn
