@@ -25,27 +25,11 @@
 // and written by the same call.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
+#include "pdn_slots.hpp"
 
 namespace pdn {
 
 namespace {
-
-template <typename T> struct Vec2;
-template <> struct Vec2<float> { typedef floatx2 type; };
-template <> struct Vec2<bf16> { typedef __bf16 type __attribute__((ext_vector_type(2))); };
-
-template <typename T>
-__device__ __forceinline__ floatx2 ld2(const T* p) {
-  const auto v = *reinterpret_cast<const typename Vec2<T>::type*>(p);
-  return floatx2{to_f(v[0]), to_f(v[1])};
-}
-template <typename T>
-__device__ __forceinline__ void st2(T* p, float x, float y) {
-  typename Vec2<T>::type v;
-  v[0] = from_f<T>(x);
-  v[1] = from_f<T>(y);
-  *reinterpret_cast<typename Vec2<T>::type*>(p) = v;
-}
 
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
@@ -54,22 +38,6 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 constexpr int kBlk = 8;   // tokens of a block
-
-// The rows of a sequence: [lo, hi) of the packed tensors.  What `starts` holds
-// is device data: whatever it is, the rows stay inside the tensors.
-struct Rows {
-  int64_t lo, n;
-};
-__device__ __forceinline__ Rows seq_rows(const SlotArgs& a, int64_t seq) {
-  int64_t lo = seq * a.T, hi = lo + a.T;
-  if (a.starts) {
-    lo = a.starts[seq];
-    hi = a.starts[seq + 1];
-  }
-  lo = min(max(lo, (int64_t)0), a.tokens);
-  hi = min(min(hi, a.tokens), lo + a.T);
-  return Rows{lo, max(hi - lo, (int64_t)0)};
-}
 
 // TB: tokens of a block, 1 (one-token calls: the products on the vector unit)
 // or kBlk.
@@ -85,7 +53,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
   const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
-  const Rows rows = seq_rows(a, seq);
+  const SlotRows rows = slot_rows(a, seq);
   const bool fresh = a.fresh && a.fresh[seq] != 0;
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lr = l & 15, lg = l >> 4;
   const int v0 = 32 * w + 2 * lr;
@@ -499,6 +467,7 @@ hipError_t launch_dims(const SlotArgs& a, hipStream_t s) {
 
 hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s) {
   if (a.B * a.H == 0) return hipSuccess;
+  if (slot_chunk_form(a, io_bf16)) return launch_slot_chunks(a, s);
   return io_bf16 ? launch_dims<bf16>(a, s) : launch_dims<float>(a, s);
 }
 
