@@ -267,7 +267,8 @@ hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s);
 // 32-bit offsets.)
 inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
   const int64_t far = (int64_t)1 << 25;
-  return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.q_stride < far && a.k_stride < far && a.Hk * a.dk < far && a.knorm == kKnormNone &&
+  return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.q_stride < far && a.k_stride < far && a.v_stride < far &&
+         a.Hk * a.dk < far && a.H * a.dv < far && a.knorm == kKnormNone &&
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
 }
 hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);

@@ -13,13 +13,15 @@
 // which is rounded to bf16, is taken as two numbers (2^-16).
 //
 // A workgroup holds one head's state for all of its sequence.  Its consumer waves
-// own 32 columns each: a lane has rows 32 kk + 8 g + 4 u + i (g = lane / 16) of
-// columns 2 (lane % 16) and the next, the rows of an accumulator tile (kk, u) being
-// so chosen that two tiles are the eight contraction elements of the next
-// product, so S, X and E never leave registers.  Four producer waves meanwhile
-// form the next chunk's operands in LDS: write keys and preconditioner state,
-// two channels a lane; L and P by matrix products; M from two 16 x 16 inverses by
-// substitution and M21 = -M22 L21 M11.
+// own 16 columns each: a lane has rows 32 kk + 8 g + 4 u + i (g = lane / 16) of
+// column lane % 16, the rows of an accumulator tile (kk, u) being so chosen that
+// two tiles are the eight contraction elements of the next product, so S, X and E
+// never leave registers.  Four producer waves meanwhile form the next chunk's
+// operands in LDS: write keys and preconditioner state, two channels and an
+// eighth or a quarter of the chunk a lane; L and P by matrix products; M from two
+// 16 x 16 inverses by substitution and M21 = -M22 L21 M11.
+#include <type_traits>
+
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 #include "pdn_slots.hpp"
@@ -31,25 +33,34 @@ namespace {
 
 constexpr int kC = 32;
 
-// the parts of an fp32 number: x = p[0] + p[1] + .., each bf16
+// two bf16 numbers in a register
+__device__ __forceinline__ floatx2 pair_f(uint32_t x) {
+  return floatx2{__builtin_bit_cast(float, x << 16), __builtin_bit_cast(float, x & 0xffff0000u)};
+}
+// The parts of two fp32 numbers: x = p[0] + p[1] + .., each bf16, in the halves of
+// a register (the conversion takes two at a time; said so, or it is made twice).
 template <int N>
-__device__ __forceinline__ void parts(float x, bf16 (&p)[N]) {
+__device__ __forceinline__ void parts(floatx2 x, uint32_t (&p)[N]) {
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    p[j] = static_cast<bf16>(x);
-    x -= static_cast<float>(p[j]);
+    p[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, typename Vec2<bf16>::type));
+    if (j + 1 < N) x -= pair_f(p[j]);
   }
 }
 // two accumulator tiles as the right operand of a slab
 template <int N>
 __device__ __forceinline__ void parts8(const floatx4& a, const floatx4& b, bf16x8 (&f)[N]) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  u32x4 r[N];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    bf16 p[N];
-    parts<N>(i < 4 ? a[i] : b[i - 4], p);
+  for (int i = 0; i < 4; ++i) {
+    uint32_t p[N];
+    parts<N>(i < 2 ? floatx2{a[2 * i], a[2 * i + 1]} : floatx2{b[2 * i - 4], b[2 * i - 3]}, p);
 #pragma unroll
-    for (int j = 0; j < N; ++j) f[j][i] = p[j];
+    for (int j = 0; j < N; ++j) r[j][i] = p[j];
   }
+#pragma unroll
+  for (int j = 0; j < N; ++j) f[j] = __builtin_bit_cast(bf16x8, r[j]);
 }
 // acc += (a[0] + a[1] + ..) (b[0] + b[1] + ..), small terms first, those of
 // part numbers past `most` left out
@@ -62,26 +73,26 @@ __device__ __forceinline__ void mma_parts(floatx4& acc, const bf16x8 (&a)[NA], c
       if (s <= most && s - i >= 0 && s - i < NB) acc = mfma(a[i], b[s - i], acc);
 }
 
-// LDS, byte offsets.  K and Q tiles three times (one in use, one that operands are
-// formed from, one on its way), what is formed from them twice; per-token
-// numbers three times.
-template <int DK, int NP>
+// LDS, byte offsets.  K and Q tiles and per-token numbers four times (the chunk in
+// use, and those one, two and three after it), what is formed from them twice.
+template <int DK, int DV, int NP>
 struct Lay {
-  static constexpr int kTile = kC * DK * 2, kMat = kC * kC * 2;
-  static constexpr int oK = 0, oQ = oK + 3 * kTile, oX = oQ + 3 * kTile;            // oX: external write keys
-  static constexpr int oT = oX + (NP == 0 ? 3 * kTile : 0);                         // write keys' parts
-  static constexpr int oM = oT + (NP == 3 ? 2 * 3 * kTile : 0), oP = oM + 2 * 3 * kMat;
+  static constexpr int kTile = kC * DK * 2, kVal = kC * DV * 2, kMat = kC * kC * 2;
+  static constexpr int oK = 0, oQ = oK + 4 * kTile, oX = oQ + 4 * kTile;            // oX: external write keys
+  static constexpr int oT = oX + (NP == 0 ? 4 * kTile : 0);                         // write keys' parts
+  static constexpr int oV = oT + (NP == 3 ? 2 * 3 * kTile : 0);
+  static constexpr int oO = oV + kVal, oM = oO + kVal, oP = oM + 3 * kMat;
   static constexpr int oL = oP + 2 * 2 * kMat, kL = kC * (kC + 4) * 4, oF = oL + kL;   // L, M in fp32
-  static constexpr int oS = oF + kL, kS = 7 * kC * 4;   // beta, lam, w, gain, decay, G (64 bits)
-  static constexpr int total = oS + 3 * kS;
+  static constexpr int oA = oF + kL;                                                // per segment and channel, sums of bp k^2
+  static constexpr int oS = oA + (NP == 3 ? 512 * 4 : 0), kS = 8 * kC * 4;          // see load_scalars
+  static constexpr int total = oS + 4 * kS;
 };
 
 // NP: the write keys' parts, 3 (SQUASH); 1: they are the keys; 0: the caller's
 template <int DK, int DV, int NP>
-__global__ __launch_bounds__(DV * 2 + 256) void slot_chunks(SlotArgs a) {
-  using L = Lay<DK, NP>;
-  constexpr int NC = DV / 32, KK = DK / 32, NCH = DK / 8, RK = DK * 2, NT = NP == 3 ? 3 : 1;
-  constexpr int UNITS = kC * NCH / 64;   // 1 KB copies of a tile
+__global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
+  using L = Lay<DK, DV, NP>;
+  constexpr int NC = DV / 16, KK = DK / 32, NCH = DK / 8, RK = DK * 2, NT = NP == 3 ? 3 : 1;
   __shared__ __attribute__((aligned(1024))) char smem[L::total];
   lds_char* const sm = (lds_char*)smem;
   const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
@@ -93,340 +104,445 @@ __global__ __launch_bounds__(DV * 2 + 256) void slot_chunks(SlotArgs a) {
   const int r0 = 8 * (m >> 2) + (m & 3);   // left-operand row of this lane, then + 4 u
   const int nch = static_cast<int>((rows.n + kC - 1) / kC);
   auto kt_tile = [&](int it, int p) {   // part p of chunk it's write keys
-    return sm + (NP == 3 ? L::oT + ((it & 1) * 3 + p) * L::kTile : (NP == 1 ? L::oK : L::oX) + (it % 3) * L::kTile);
+    return sm + (NP == 3 ? L::oT + ((it & 1) * 3 + p) * L::kTile : (NP == 1 ? L::oK : L::oX) + (it & 3) * L::kTile);
   };
-  auto mat = [&](int o, int n, int it, int p) { return sm + o + ((it & 1) * n + p) * L::kMat; };
-  auto scal = [&](int it, int x) { return sm + L::oS + (it % 3) * L::kS + x * kC * 4; };
+  auto mat_m = [&](int p) { return sm + L::oM + p * L::kMat; };
+  auto mat_p = [&](int it, int p) { return sm + L::oP + ((it & 1) * 2 + p) * L::kMat; };
+  auto scal = [&](int it, int x) { return sm + L::oS + (it & 3) * L::kS + x * kC * 4; };
+
+  typedef __attribute__((address_space(3))) bf16 lds_bf16;
 
   if (w < NC) {
     // ------------------------------------------------------------ consumers
-    const int v0 = 32 * w + 2 * m;
-    floatx4 S[KK][2][2];
+    const int v0 = 16 * w + m;
+    floatx4 S[KK][2];
     {
       const float* sp = a.S + (src * a.H + h) * (DK * DV) + 8 * g * DV + v0;
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          const floatx2 x = fresh ? floatx2{0.f, 0.f} : *reinterpret_cast<const floatx2*>(sp + (32 * kk + r) * DV);
-          S[kk][r / 4][0][r % 4] = x[0];
-          S[kk][r / 4][1][r % 4] = x[1];
-        }
+        for (int r = 0; r < 8; ++r) S[kk][r / 4][r % 4] = fresh ? 0.f : sp[(32 * kk + r) * DV];
     }
-    const bf16* vb = static_cast<const bf16*>(a.v) + h * DV + v0;
-    bf16* ob = static_cast<bf16*>(a.o) + h * DV + v0;
-    uint32_t vv[8];
-    auto load_v = [&](int ch) {
-      const int64_t t0 = static_cast<int64_t>(ch) * kC;
-#pragma unroll
-      for (int r = 0; r < 8; ++r)
-        vv[r] = *reinterpret_cast<const uint32_t*>(vb + (rows.lo + min(t0 + 8 * g + r, rows.n - 1)) * a.v_stride);
-    };
-    if (nch > 0) load_v(0);
     lds_sync();
-    for (int it = 0; it <= nch; ++it) {
-      const int ch = it - 1;
-      if (ch < 0) {
-        lds_sync();
-        lds_sync();
-        lds_sync();
-        continue;
-      }
-      const int64_t t0 = static_cast<int64_t>(ch) * kC;
-      const int n = static_cast<int>(min<int64_t>(kC, rows.n - t0));
+    lds_sync();
+    lds_sync();   // (the first chunk is being formed)
+    lds_sync();
+    for (int ch = 0; ch < nch; ++ch) {
       // ---- K S^T and Q S^T
-      floatx4 y[2][2], z[2][2], e[2][2];
+      floatx4 y[2], z[2], e[2];
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) y[u][b] = z[u][b] = e[u][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 2; ++u) y[u] = z[u] = e[u] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
-        bf16x8 k1[2][1], q1[2][1], sp[2][3];
-        reads_done();   // (a slab at a time: all slabs' parts at once do not fit the registers)
+        bf16x8 k1[2][1], q1[2][1], sp[3];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const int off = (ch % 3) * L::kTile + tile_off<NCH>(r0, 4 * kk + g) + 4 * u * RK;
+          const int off = (ch & 3) * L::kTile + tile_off<NCH>(r0, 4 * kk + g) + 4 * u * RK;
           k1[u][0] = lds_frag(sm + L::oK + off);
           q1[u][0] = lds_frag(sm + L::oQ + off);
         }
+        parts8<3>(S[kk][0], S[kk][1], sp);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) parts8<3>(S[kk][0][b], S[kk][1][b], sp[b]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            mma_parts(y[u][b], k1[u], sp[b], 2);
-            mma_parts(z[u][b], q1[u], sp[b], 1);
-          }
+        for (int u = 0; u < 2; ++u) {
+          mma_parts(y[u], k1[u], sp, 2);
+          mma_parts(z[u], q1[u], sp, 1);
+        }
       }
-      lds_sync();   // A
-      // ---- X, E = M X
+      // ---- X
+      bf16x8 xp[3];
       {
-        floatx4 x[2][2];
+        const bf16x8 v8 = lds_frag_t(sm + L::oV + tile_off<DV / 8>(8 * g + (m >> 2), 2 * w + ((m & 3) >> 1)) + (m & 1) * 8,
+                                     4 * DV * 2);
+        floatx4 x[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const floatx4 be = lds_f4(scal(ch, 0) + (8 * g + 4 * u) * 4), lam = lds_f4(scal(ch, 1) + (8 * g + 4 * u) * 4);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t v = vv[4 * u + i];
-            const float v2[2] = {__builtin_bit_cast(float, v << 16), __builtin_bit_cast(float, v & 0xffff0000u)};
-#pragma unroll
-            for (int b = 0; b < 2; ++b)
-              x[u][b][i] = 8 * g + 4 * u + i < n ? be[i] * (v2[b] - lam[i] * y[u][b][i]) : 0.f;
-          }
-          z[u][0] *= lam;
-          z[u][1] *= lam;
+          for (int i = 0; i < 4; ++i)   // (a row past the end has no strength, and no value that could spoil that)
+            x[u][i] = be[i] * (static_cast<float>(v8[4 * u + i]) - lam[i] * y[u][i]);
+          z[u] *= lam;
         }
-        if (ch + 1 < nch) load_v(ch + 1);
-        bf16x8 mp[2][3], xp[2][3];
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int p = 0; p < 3; ++p) mp[u][p] = lds_frag(mat(L::oM, 3, ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
-#pragma unroll
-        for (int b = 0; b < 2; ++b) parts8<3>(x[0][b], x[1][b], xp[b]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int b = 0; b < 2; ++b) mma_parts(e[u][b], mp[u], xp[b], 2);
+        parts8<3>(x[0], x[1], xp);
       }
-      lds_sync();   // B
-      // ---- the state after the chunk, and O
+      lds_sync();   // A
+      // ---- E = M X, the state after the chunk
+      bf16x8 ep[2], wp[3];
       {
-        bf16x8 ep[2][2], wp[2][3];
-        const floatx4 w0 = lds_f4(scal(ch, 2) + 8 * g * 4), w1 = lds_f4(scal(ch, 2) + (8 * g + 4) * 4);
-        const float lc = lds_f4(scal(ch, 1) + (kC - 4) * 4)[3];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          parts8<3>(w0 * e[0][b], w1 * e[1][b], wp[b]);
-          parts8<2>(e[0][b], e[1][b], ep[b]);
-        }
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            bf16x8 tp[NT];
-            reads_done();
-#pragma unroll
-            for (int p = 0; p < NT; ++p)
-              tp[p] = lds_frag_t(kt_tile(ch, p) + tile_off<NCH>(8 * g + (m >> 2), 4 * kk + (m & 3)) + u * 8, 4 * RK);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-              S[kk][u][b] *= lc;
-              mma_parts(S[kk][u][b], tp, wp[b], 2);
-            }
-          }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          bf16x8 pp[2];
+          bf16x8 mp[3];
 #pragma unroll
-          for (int p = 0; p < 2; ++p) pp[p] = lds_frag(mat(L::oP, 2, ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
-#pragma unroll
-          for (int b = 0; b < 2; ++b) mma_parts(z[u][b], pp, ep[b], 1);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int t = 8 * g + 4 * u + i;
-            if (t < n) st2<bf16>(ob + (rows.lo + t0 + t) * a.H * DV, a.scale * z[u][0][i], a.scale * z[u][1][i]);
-          }
+          for (int p = 0; p < 3; ++p) mp[p] = lds_frag(mat_m(p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
+          mma_parts(e[u], mp, xp, 2);
         }
+        const floatx4 w0 = lds_f4(scal(ch, 2) + 8 * g * 4), w1 = lds_f4(scal(ch, 2) + (8 * g + 4) * 4);
+        parts8<3>(w0 * e[0], w1 * e[1], wp);
+        parts8<2>(e[0], e[1], ep);
       }
-      lds_sync();   // C
+      const float lc = lds_f4(scal(ch, 1) + (kC - 4) * 4)[3];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bf16x8 tp[NT];
+#pragma unroll
+          for (int p = 0; p < NT; ++p)
+            tp[p] = lds_frag_t(kt_tile(ch, p) + tile_off<NCH>(8 * g + (m >> 2), 4 * kk + (m & 3)) + u * 8, 4 * RK);
+          S[kk][u] *= lc;
+          mma_parts(S[kk][u], tp, wp, 2);
+        }
+      // ---- O, which the producers store
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        bf16x8 pp[2];
+#pragma unroll
+        for (int p = 0; p < 2; ++p) pp[p] = lds_frag(mat_p(ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
+        mma_parts(z[u], pp, ep, 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<lds_bf16*>(sm + L::oO + tile_off<DV / 8>(8 * g + 4 * u + i, v0 >> 3) + (v0 & 7) * 2) =
+              static_cast<bf16>(a.scale * z[u][i]);
+      }
+      lds_sync();   // B
     }
-    float* sp = a.S + (dst * a.H + h) * (DK * DV) + 8 * g * DV + v0;
+    int at = 8 * g * DV + v0;
+    asm volatile("" : "+v"(at));   // (or these addresses are formed at the start and held throughout)
+    float* sp = a.S + (dst * a.H + h) * (DK * DV) + at;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-      for (int r = 0; r < 8; ++r)
-        *reinterpret_cast<floatx2*>(sp + (32 * kk + r) * DV) = floatx2{S[kk][r / 4][0][r % 4], S[kk][r / 4][1][r % 4]};
+      for (int r = 0; r < 8; ++r) sp[(32 * kk + r) * DV] = S[kk][r / 4][r % 4];
   } else {
     // ------------------------------------------------------------ producers
     constexpr int PAIRS = DK / 2, SEGS = 256 / PAIRS, TOK = kC / SEGS;   // channel pairs; tokens a lane forms keys of
-    const int pw = w - NC, pt = pw * 64 + l;
-    const int cp = pt % PAIRS, seg = pt / PAIRS;
+    typedef __attribute__((address_space(3))) floatx2 lds_floatx2;
+    typedef __attribute__((address_space(3))) double lds_double;
+    typedef __attribute__((address_space(3))) uint32_t lds_u32;
+    typedef __attribute__((address_space(3))) uint16_t lds_u16;
+    const int pw = w - NC, pt0 = pw * 64 + l;
+    // The lane's number, made anew for each phase: what is formed from it, LDS
+    // addresses above all, is then formed where it is used (held throughout, all of
+    // them together take more registers than there are).
+    int ll = l;
+    __builtin_amdgcn_s_setprio(3);   // (a step ends with the slowest producer)
+    auto anew = [&]() { asm volatile("" : "+v"(ll)); };
     const bool gram = NP == 3;
     const float mu = gram ? fast_exp(a.log_a_scale[h]) : 0.f;
     floatx2 A = {0.f, 0.f};
-    float* const ap = gram ? a.A + h * DK + 2 * cp : nullptr;
+    float* const ap = gram ? a.A + h * DK + 2 * (pt0 % PAIRS) : nullptr;
     if (gram && !fresh) A = *reinterpret_cast<const floatx2*>(ap + src * a.H * DK);
-    // a chunk's rows into LDS; those past the sequence's end read as zeros
-    auto copy_rows = [&](int ch) {
+    // A chunk's rows, through registers (16 bytes a lane and piece of a tile) into
+    // LDS; those past the sequence's end read as zeros.
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    auto load_tile = [&](int ch, const void* p, int64_t stride, int64_t first, auto width, u32x4* to) {
+      constexpr int W = decltype(width)::value, N = W / 8;
       const int64_t row = rows.lo + static_cast<int64_t>(ch) * kC;
       const int n = static_cast<int>(min<int64_t>(kC, rows.n - static_cast<int64_t>(ch) * kC));
-      const int buf = (ch % 3) * L::kTile;
-      auto tile = [&](const void* p, int64_t stride, int o) {
-        const __amdgpu_buffer_rsrc_t r =
-            buf_rsrc(static_cast<const char*>(p) + (row * stride + hk * DK) * 2, static_cast<uint32_t>(((n - 1) * stride + DK) * 2));
+      const __amdgpu_buffer_rsrc_t r = buf_rsrc(static_cast<const char*>(p) + (row * stride + first) * 2,
+                                                static_cast<uint32_t>(((n - 1) * stride + W) * 2));
 #pragma unroll
-        for (int x = 0; x < UNITS / 4; ++x) {
-          const int unit = UNITS / 4 * pw + x;
-          unit_copy(r, unit_src<NCH>(unit, l, static_cast<uint32_t>(stride * 2)), sm + o + buf + unit * 1024);
-        }
-      };
-      tile(a.k, a.k_stride, L::oK);
-      tile(a.q, a.q_stride, L::oQ);
-      if (NP == 0) tile(a.ktilde, a.Hk * DK, L::oX);
+      for (int x = 0; x < kC * N / 256; ++x) {
+        const uint32_t at = pw * 64 + ll + 256 * x;
+        to[x] = __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(at / N * static_cast<uint32_t>(stride * 2) + at % N * 16), 0, 0);
+      }
     };
-    // its per-token numbers, a lane a token
+    auto put_tile = [&](auto width, const u32x4* from, int o) {
+      constexpr int N = decltype(width)::value / 8;
+#pragma unroll
+      for (int x = 0; x < kC * N / 256; ++x) {
+        const uint32_t at = pw * 64 + ll + 256 * x;
+        lds_put(sm + o + tile_off<N>(at / N, at % N), __builtin_bit_cast(bf16x8, from[x]));
+      }
+    };
+    // a chunk's outputs (rows past the end are past the buffer's range)
+    auto store_o = [&](int ch) {
+      constexpr int N = DV / 8;
+      const int64_t HV = a.H * DV;
+      const int n = static_cast<int>(min<int64_t>(kC, rows.n - static_cast<int64_t>(ch) * kC));
+      const __amdgpu_buffer_rsrc_t r =
+          buf_rsrc(static_cast<const char*>(a.o) + ((rows.lo + static_cast<int64_t>(ch) * kC) * HV + h * DV) * 2,
+                   static_cast<uint32_t>(((n - 1) * HV + DV) * 2));
+#pragma unroll
+      for (int x = 0; x < kC * N / 256; ++x) {
+        const uint32_t at = pw * 64 + ll + 256 * x;
+        buf_put16(r, at / N * static_cast<uint32_t>(HV * 2) + at % N * 16, lds_frag(sm + L::oO + tile_off<N>(at / N, at % N)));
+      }
+    };
+    constexpr std::integral_constant<int, DK> wk;
+    constexpr std::integral_constant<int, DV> wv;
+    u32x4 rk[DK / 64], rq[DK / 64], rx[DK / 64], rv[DV / 64];
+    auto load_keys = [&](int ch) {
+      load_tile(ch, a.k, a.k_stride, hk * DK, wk, rk);
+      load_tile(ch, a.q, a.q_stride, hk * DK, wk, rq);
+      if (NP == 0) load_tile(ch, a.ktilde, a.Hk * DK, hk * DK, wk, rx);
+    };
+    auto put_keys = [&](int ch) {
+      const int buf = (ch & 3) * L::kTile;
+      put_tile(wk, rk, L::oK + buf);
+      put_tile(wk, rq, L::oQ + buf);
+      if (NP == 0) put_tile(wk, rx, L::oX + buf);
+    };
+    // Its per-token numbers, a lane a token: 0 write strength, 1 lam, 2 w, 3 gain
+    // and 4 decay of the preconditioner, 5 that decay over a segment, 6 log-decay
+    // from the chunk's start (64 bits: the decay between two tokens is a difference
+    // of two of these)
+    // (each read whether it is used or not: a branch here would wait for the loads)
+    const float *const gb = a.gate == kGateScalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
+                *const gpb = gram && a.g_p ? a.g_p : a.beta;
+    float s_be = 0.f, s_g = 0.f, s_bp = 0.f, s_gp = 0.f;
     auto load_scalars = [&](int ch) {
-      const int64_t t0 = static_cast<int64_t>(ch) * kC;
-      const int n = static_cast<int>(min<int64_t>(kC, rows.n - t0)), t = l & 31;
-      const int64_t sc = (rows.lo + t0 + min(t, n - 1)) * a.H + h;
-      const float be = a.beta[sc], gt = a.gate == kGateScalar && t < n ? a.g[sc] : 0.f;
-      const float bp = gram ? a.beta_p[sc] : 0.f, gp = gram && a.g_p ? a.g_p[sc] : 0.f;
-      double to = gt;   // (64 bits: the decay between two tokens is a difference of two of these)
+      const int64_t sc = (rows.lo + min(static_cast<int64_t>(ch) * kC + (ll & 31), rows.n - 1)) * a.H + h;
+      s_be = a.beta[sc];
+      s_g = gb[sc];
+      s_bp = bpb[sc];
+      s_gp = gpb[sc];
+    };
+    auto put_scalars = [&](int ch) {
+      const int t = ll & 31;
+      const bool in = static_cast<int64_t>(ch) * kC + t < rows.n;
+      const float be = in ? s_be : 0.f, bp = in ? s_bp : 0.f, gp = in && a.g_p ? s_gp : 0.f;
+      double to = in && a.gate == kGateScalar ? s_g : 0.f;
 #pragma unroll
       for (int off = 1; off < kC; off <<= 1) {
         const double x = __shfl_up(to, off, kC);
         if (t >= off) to += x;
       }
       const double end = __shfl(to, kC - 1, kC);
-      if (l < kC) {
+      const float dp = fast_exp(gp);
+      float ds = dp;
+#pragma unroll
+      for (int off = 1; off < TOK; off <<= 1) ds *= __shfl_xor(ds, off, kC);
+      if (ll < kC) {
         auto put = [&](int x, float v) { *reinterpret_cast<lds_float*>(scal(ch, x) + t * 4) = v; };
-        put(0, t < n ? be : 0.f);
+        put(0, be);
         put(1, fast_exp(static_cast<float>(to)));
         put(2, fast_exp(static_cast<float>(end - to)));
-        put(3, t < n ? bp : 0.f);
-        put(4, t < n ? fast_exp(gp) : 1.f);
-        *reinterpret_cast<__attribute__((address_space(3))) double*>(scal(ch, 5) + t * 8) = to;
+        put(3, bp);
+        put(4, dp);
+        if (t % TOK == 0) *reinterpret_cast<lds_float*>(scal(ch, 5) + t / TOK * 4) = ds;
+        *reinterpret_cast<lds_double*>(scal(ch, 6) + t * 8) = to;
       }
     };
     auto fl = [&](int o, int t, int x) { return reinterpret_cast<lds_float*>(sm + o + (t * (kC + 4) + x) * 4); };
-    auto put16 = [&](lds_char* tile, int t, int x, bf16 v) {
-      *reinterpret_cast<__attribute__((address_space(3))) bf16*>(tile + tile_off<4>(t, x >> 3) + (x & 7) * 2) = v;
+    auto seg_sum = [&](int sg, int cp) { return reinterpret_cast<lds_floatx2*>(sm + L::oA + (sg * DK + 2 * cp) * 4); };
+    // what this lane's tokens add to the preconditioner state of its two channels
+    auto put_sums = [&](int ch) {
+      const int pt = pw * 64 + ll, cp = pt % PAIRS, seg = pt / PAIRS;
+      const lds_char* kp = sm + L::oK + (ch & 3) * L::kTile + (cp % 4) * 4;
+      uint32_t x[TOK];
+      floatx4 bp[TOK / 4], dp[TOK / 4];
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) x[j] = *reinterpret_cast<const lds_u32*>(kp + tile_off<NCH>(seg * TOK + j, cp / 4));
+#pragma unroll
+      for (int j = 0; j < TOK / 4; ++j) {
+        bp[j] = lds_f4(scal(ch, 3) + (seg * TOK + 4 * j) * 4);
+        dp[j] = lds_f4(scal(ch, 4) + (seg * TOK + 4 * j) * 4);
+      }
+      reads_done();
+      floatx2 sum = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        const floatx2 k = pair_f(x[j]);
+        sum = dp[j / 4][j % 4] * sum + bp[j / 4][j % 4] * k * k;
+      }
+      *seg_sum(seg, cp) = sum;
+    };
+    // its tokens' write keys; A: to the chunk's end
+    auto put_write_keys = [&](int ch) {
+      const int pt = pw * 64 + ll, cp = pt % PAIRS, seg = pt / PAIRS;
+      const lds_char* kp = sm + L::oK + (ch & 3) * L::kTile + (cp % 4) * 4;
+      uint32_t x[TOK];
+      floatx4 bp[TOK / 4], dp[TOK / 4], ds[SEGS / 4];
+      floatx2 sum[SEGS];
+#pragma unroll
+      for (int j = 0; j < SEGS; ++j) sum[j] = *seg_sum(j, cp);
+#pragma unroll
+      for (int j = 0; j < SEGS / 4; ++j) ds[j] = lds_f4(scal(ch, 5) + 16 * j);
+#pragma unroll
+      for (int j = 0; j < TOK / 4; ++j) {
+        bp[j] = lds_f4(scal(ch, 3) + (seg * TOK + 4 * j) * 4);
+        dp[j] = lds_f4(scal(ch, 4) + (seg * TOK + 4 * j) * 4);
+      }
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) x[j] = *reinterpret_cast<const lds_u32*>(kp + tile_off<NCH>(seg * TOK + j, cp / 4));
+      reads_done();
+      floatx2 s = A;
+#pragma unroll
+      for (int j = 0; j < SEGS; ++j) {
+        if (j == seg) s = A;
+        A = ds[j / 4][j % 4] * A + sum[j];
+      }
+#pragma unroll
+      for (int j = 0; j < TOK; ++j) {
+        const floatx2 k = pair_f(x[j]);
+        s = dp[j / 4][j % 4] * s + bp[j / 4][j % 4] * k * k;
+        uint32_t p[3];
+        parts<3>(floatx2{squash_gain(s[0], mu, a.lnx) * k[0], squash_gain(s[1], mu, a.lnx) * k[1]}, p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+          *reinterpret_cast<lds_u32*>(kt_tile(ch, q) + tile_off<NCH>(seg * TOK + j, cp / 4) + (cp % 4) * 4) = p[q];
+      }
+    };
+    // L and P: a wave the rows 8 g + 4 u + i and columns r0 + 4 c of K Kt^T and Q Kt^T
+    auto put_products = [&](int ch) {
+      const int u = pw >> 1, c = pw & 1, m = ll & 15, g = ll >> 4, r0 = 8 * (m >> 2) + (m & 3);
+      floatx4 kk4 = {0.f, 0.f, 0.f, 0.f}, qk4 = kk4;
+      const int tile = (ch & 3) * L::kTile, s = r0 + 4 * c;
+      const double Gs = *reinterpret_cast<const lds_double*>(scal(ch, 6) + s * 8);
+      double Gt[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) Gt[i] = *reinterpret_cast<const lds_double*>(scal(ch, 6) + (8 * g + 4 * u + i) * 8);
+      const floatx4 be = lds_f4(scal(ch, 0) + (8 * g + 4 * u) * 4);
+#pragma unroll
+      for (int k2 = 0; k2 < KK; k2 += 2) {
+        bf16x8 k1[2][1], q1[2][1], tp[2][NT];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int off = tile_off<NCH>(r0, 4 * (k2 + x) + g);
+          k1[x][0] = lds_frag(sm + L::oK + tile + off + 4 * u * RK);
+          q1[x][0] = lds_frag(sm + L::oQ + tile + off + 4 * u * RK);
+#pragma unroll
+          for (int p = 0; p < NT; ++p) tp[x][p] = lds_frag(kt_tile(ch, p) + off + 4 * c * RK);
+        }
+        reads_done();
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          mma_parts(kk4, k1[x], tp[x], 2);
+          mma_parts(qk4, q1[x], tp[x], 1);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        floatx2 pr;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const int t = 8 * g + 4 * u + i + b;
+          const float d = fast_exp(static_cast<float>(Gt[i + b] - Gs));
+          *fl(L::oL, t, s) = s < t ? be[i + b] * d * kk4[i + b] : 0.f;
+          pr[b] = s <= t ? d * qk4[i + b] : 0.f;
+        }
+        uint32_t p[2];
+        parts<2>(pr, p);
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int b = 0; b < 2; ++b)
+            *reinterpret_cast<lds_u16*>(mat_p(ch, q) + tile_off<4>(8 * g + 4 * u + i + b, s >> 3) + (s & 7) * 2) =
+                static_cast<uint16_t>(b ? p[q] >> 16 : p[q]);
+      }
+    };
+    // M, by two waves: a lane a row of a 16 x 16 block, from M (I + L) = I, column
+    // after column from the last, in both; then one puts the blocks into place, the
+    // other forms M21.
+    auto put_inverse = [&]() {
+      const int m = ll & 15, g = ll >> 4, b0 = ll & 16;   // lanes 0-15 the first block, 16-31 the second
+      float x[16];
+#pragma unroll
+      for (int c = 0; c < 16; ++c) x[c] = m == c ? 1.f : 0.f;
+      // (rows of L two at a time, two such groups ahead of their use)
+      floatx4 lt[8][2][4];
+      auto load_l = [&](int j2) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int c = 0; c <= j2 / 2; ++c) lt[j2][j][c] = *reinterpret_cast<lds_floatx4*>(fl(L::oL, b0 + 2 * j2 + j, b0 + 4 * c));
+        reads_done();
+      };
+      load_l(7);
+      load_l(6);
+#pragma unroll
+      for (int j2 = 7; j2 >= 0; --j2) {
+        if (j2 >= 2) load_l(j2 - 2);
+#pragma unroll
+        for (int j = 2 * j2 + 1; j >= 2 * j2; --j)
+#pragma unroll
+          for (int c = 0; c < j; ++c) x[c] -= x[j] * lt[j2][j & 1][c / 4][c % 4];
+      }
+      if (pw == 0) {
+        if (ll < 32)
+#pragma unroll
+          for (int c = 0; c < 16; c += 8) {
+            bf16x8 f8[3];
+            parts8<3>(floatx4{x[c], x[c + 1], x[c + 2], x[c + 3]}, floatx4{x[c + 4], x[c + 5], x[c + 6], x[c + 7]}, f8);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) lds_put(mat_m(q) + tile_off<4>(b0 + m, (b0 + c) / 8), f8[q]);
+          }
+        return;
+      }
+      if (ll < 32)
+#pragma unroll
+        for (int c = 0; c < 16; c += 4)
+          *reinterpret_cast<lds_floatx4*>(fl(L::oF, b0 + m, b0 + c)) = floatx4{x[c], x[c + 1], x[c + 2], x[c + 3]};
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      // M21 transposed, a lane four columns of a row: M11^T ((M22 L21)^T)
+      floatx4 t1 = {0.f, 0.f, 0.f, 0.f}, m21 = t1;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) mma4(t1, *fl(L::oL, 16 + 4 * j + g, m), *fl(L::oF, 16 + m, 16 + 4 * j + g));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma4(m21, *fl(L::oF, 4 * g + i, m), t1[i]);
+      uint32_t p[2][3];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) parts<3>(floatx2{-m21[2 * i], -m21[2 * i + 1]}, p[i]);
+      typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+      typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        *reinterpret_cast<lds_u32x2*>(mat_m(q) + tile_off<4>(16 + m, g >> 1) + (g & 1) * 8) = u32x2{p[0][q], p[1][q]};
     };
     // (M's upper right block stays zero)
-    for (int x = pt; x < 2 * 3 * L::kMat / 16; x += 256) lds_put(sm + L::oM + x * 16, bf16x8{});
-    if (nch > 0) {
-      copy_rows(0);
-      if (pw == 3) load_scalars(0);
+    for (int x = pt0; x < 3 * L::kMat / 16; x += 256) lds_put(sm + L::oM + x * 16, bf16x8{});
+    for (int ch = 0; ch < min(nch, 2); ++ch) {
+      load_keys(ch);
+      put_keys(ch);
+      if (pw == 3) {
+        load_scalars(ch);
+        put_scalars(ch);
+      }
     }
-    wait_loads<0>();
     lds_sync();
+    if (gram && nch > 0) put_sums(0);
+    lds_sync();
+    // A step of two phases: the write keys of chunk it beside M of the one before,
+    // which the consumers hold already; then the L and P of chunk it.  Loads are
+    // issued when a step begins and waited for when it ends.
     for (int it = 0; it <= nch; ++it) {
       const bool live = it < nch;
-      if (it + 1 < nch) copy_rows(it + 1);
-      if (gram && live) {
-        // ---- preconditioner state of two channels over the chunk, and this lane's tokens' write keys
-        const lds_char* kp = sm + L::oK + (it % 3) * L::kTile;
-        floatx2 At[TOK], kt[TOK];
-#pragma unroll
-        for (int t4 = 0; t4 < kC; t4 += 4) {
-          const floatx4 bp = lds_f4(scal(it, 3) + t4 * 4), dp = lds_f4(scal(it, 4) + t4 * 4);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int t = t4 + j;
-            const uint32_t x = *reinterpret_cast<const __attribute__((address_space(3))) uint32_t*>(
-                kp + tile_off<NCH>(t, cp / 4) + (cp % 4) * 4);
-            const floatx2 k = {__builtin_bit_cast(float, x << 16), __builtin_bit_cast(float, x & 0xffff0000u)};
-            A = dp[j] * A + bp[j] * k * k;
-            if (seg == t / TOK) {
-              At[t % TOK] = A;
-              kt[t % TOK] = k;
-            }
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-          bf16 p[2][3];
-#pragma unroll
-          for (int b = 0; b < 2; ++b) parts<3>(squash_gain(At[j][b], mu, a.lnx) * kt[j][b], p[b]);
-#pragma unroll
-          for (int q = 0; q < 3; ++q) {
-            typename Vec2<bf16>::type v;
-            v[0] = p[0][q];
-            v[1] = p[1][q];
-            *reinterpret_cast<__attribute__((address_space(3))) typename Vec2<bf16>::type*>(
-                kt_tile(it, q) + tile_off<NCH>(seg * TOK + j, cp / 4) + (cp % 4) * 4) = v;
-          }
-        }
+      anew();
+      if (it > 0 && pw < 2) put_inverse();
+      anew();
+      if (live) load_tile(it, a.v, a.v_stride, h * DV, wv, rv);
+      if (it > 0 && it + 1 < nch && pw == 3) put_scalars(it + 1);
+      if (it + 2 < nch) {
+        load_keys(it + 2);
+        if (pw == 3) load_scalars(it + 2);
       }
+      if (it > 1) store_o(it - 2);
+      anew();
+      if (gram && live) put_write_keys(it);
       lds_sync();   // A
-      if (live) {
-        // ---- a wave the rows 8 g + 4 u + i and columns r0 + 4 c of K Kt^T and Q Kt^T
-        const int u = pw >> 1, c = pw & 1;
-        floatx4 kk4 = {0.f, 0.f, 0.f, 0.f}, qk4 = kk4;
-        const int tile = (it % 3) * L::kTile;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          const int off = tile_off<NCH>(r0, 4 * kk + g);
-          bf16x8 k1[1], q1[1], tp[NT];
-          k1[0] = lds_frag(sm + L::oK + tile + off + 4 * u * RK);
-          q1[0] = lds_frag(sm + L::oQ + tile + off + 4 * u * RK);
-#pragma unroll
-          for (int p = 0; p < NT; ++p) tp[p] = lds_frag(kt_tile(it, p) + off + 4 * c * RK);
-          mma_parts(kk4, k1, tp, 2);
-          mma_parts(qk4, q1, tp, 1);
-        }
-        const int s = r0 + 4 * c;
-        typedef __attribute__((address_space(3))) double lds_double;
-        const double Gs = *reinterpret_cast<const lds_double*>(scal(it, 5) + s * 8);
-        const floatx4 be = lds_f4(scal(it, 0) + (8 * g + 4 * u) * 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int t = 8 * g + 4 * u + i;
-          const float d = fast_exp(static_cast<float>(*reinterpret_cast<const lds_double*>(scal(it, 5) + t * 8) - Gs));
-          *fl(L::oL, t, s) = s < t ? be[i] * d * kk4[i] : 0.f;
-          bf16 p[2];
-          parts<2>(s <= t ? d * qk4[i] : 0.f, p);
-          put16(mat(L::oP, 2, it, 0), t, s, p[0]);
-          put16(mat(L::oP, 2, it, 1), t, s, p[1]);
-        }
-      }
+      anew();
+      if (live) put_products(it);
+      anew();
+      if (gram && it + 1 < nch) put_sums(it + 1);
+      anew();
+      if (live) put_tile(wv, rv, L::oV);   // (the consumers have used theirs)
+      if (it + 2 < nch) put_keys(it + 2);
+      // No load is under way any more.  Said outright (vmcnt 0), or the compiler,
+      // which does not see that a load's branch and its use's go together, waits
+      // for loads just issued before it reuses a register in the next step.
+      __builtin_amdgcn_s_waitcnt(0x0f70);
       lds_sync();   // B
-      if (live && pw == 0) {
-        // ---- M: a lane a column of a 16 x 16 block, row after row
-        const int b0 = l & 16;   // lanes 0-15 the first block, 16-31 the second
-        float x[16];
-#pragma unroll
-        for (int t = 0; t < 16; ++t) {
-          x[t] = t == m ? 1.f : 0.f;
-#pragma unroll
-          for (int j = 0; j < t; j += 4) {
-            const floatx4 f = *reinterpret_cast<lds_floatx4*>(fl(L::oL, b0 + t, b0 + j));
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (j + i < t) x[t] -= f[i] * x[j + i];
-          }
-        }
-        if (l < 32)
-#pragma unroll
-          for (int t = 0; t < 16; ++t) *fl(L::oF, b0 + t, b0 + m) = x[t];
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        floatx4 t1 = {0.f, 0.f, 0.f, 0.f}, m21 = t1;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mma4(t1, *fl(L::oL, 16 + m, 4 * j + g), *fl(L::oF, 4 * j + g, m));   // L21 M11
-        const floatx4 m22 = *reinterpret_cast<lds_floatx4*>(fl(L::oF, 16 + m, 16 + 4 * g));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mma4(m21, m22[i], t1[i]);
-        bf16 p[3];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          parts<3>(-m21[i], p);
-#pragma unroll
-          for (int q = 0; q < 3; ++q) put16(mat(L::oM, 3, it, q), 16 + 4 * g + i, m, p[q]);
-        }
-        if (l < 32)
-#pragma unroll
-          for (int t = 0; t < 16; ++t) {
-            parts<3>(x[t], p);
-#pragma unroll
-            for (int q = 0; q < 3; ++q) put16(mat(L::oM, 3, it, q), b0 + t, b0 + m, p[q]);
-          }
-      }
-      if (it + 1 < nch && pw == 3) load_scalars(it + 1);
-      wait_loads<0>();
-      lds_sync();   // C
     }
-    if (gram && seg == 0) *reinterpret_cast<floatx2*>(ap + dst * a.H * DK) = A;
+    if (nch > 0) store_o(nch - 1);
+    if (gram && pt0 < PAIRS) *reinterpret_cast<floatx2*>(ap + dst * a.H * DK) = A;
   }
 }
 
 template <int DK, int DV, int NP>
 hipError_t launch(const SlotArgs& a, hipStream_t st) {
-  static_assert(Lay<DK, NP>::total <= 160 * 1024, "a chunk's operands must fit the LDS of a compute unit");
-  hipLaunchKernelGGL((slot_chunks<DK, DV, NP>), dim3(static_cast<unsigned>(a.B * a.H)), dim3(DV * 2 + 256), 0, st, a);
+  static_assert(Lay<DK, DV, NP>::total <= 160 * 1024, "a chunk's operands must fit the LDS of a compute unit");
+  hipLaunchKernelGGL((slot_chunks<DK, DV, NP>), dim3(static_cast<unsigned>(a.B * a.H)), dim3(DV * 4 + 256), 0, st, a);
   return hipGetLastError();
 }
 
