@@ -128,76 +128,93 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
     lds_sync();   // (the first chunk is being formed)
     lds_sync();
     for (int ch = 0; ch < nch; ++ch) {
-      // ---- K S^T and Q S^T
-      floatx4 y[2], z[2], e[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) y[u] = z[u] = e[u] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) {
-        bf16x8 k1[2][1], q1[2][1], sp[3];
+      // ---- K S^T and Q S^T (operands are read one slab ahead of their use)
+      floatx4 y[2], z[2], e[2], be[2], lam[2];
+      bf16x8 kq[2][2][2][1];
+      auto load_kq = [&](int kk) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int off = (ch & 3) * L::kTile + tile_off<NCH>(r0, 4 * kk + g) + 4 * u * RK;
-          k1[u][0] = lds_frag(sm + L::oK + off);
-          q1[u][0] = lds_frag(sm + L::oQ + off);
+          kq[kk & 1][0][u][0] = lds_frag(sm + L::oK + off);
+          kq[kk & 1][1][u][0] = lds_frag(sm + L::oQ + off);
         }
+      };
+      load_kq(0);
+      const bf16x8 v8 = lds_frag_t(sm + L::oV + tile_off<DV / 8>(8 * g + (m >> 2), 2 * w + ((m & 3) >> 1)) + (m & 1) * 8,
+                                   4 * DV * 2);
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        y[u] = z[u] = e[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        be[u] = lds_f4(scal(ch, 0) + (8 * g + 4 * u) * 4);
+        lam[u] = lds_f4(scal(ch, 1) + (8 * g + 4 * u) * 4);
+      }
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        if (kk + 1 < KK) load_kq(kk + 1);
+        reads_done();
+        bf16x8 sp[3];
         parts8<3>(S[kk][0], S[kk][1], sp);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          mma_parts(y[u], k1[u], sp, 2);
-          mma_parts(z[u], q1[u], sp, 1);
+          mma_parts(y[u], kq[kk & 1][0][u], sp, 2);
+          mma_parts(z[u], kq[kk & 1][1][u], sp, 1);
         }
       }
       // ---- X
+      bf16x8 tp[2][NT];
+      auto load_t = [&](int x) {   // the write keys' columns of tile x = 2 kk + u
+#pragma unroll
+        for (int p = 0; p < NT; ++p)
+          tp[x & 1][p] = lds_frag_t(kt_tile(ch, p) + tile_off<NCH>(8 * g + (m >> 2), 4 * (x >> 1) + (m & 3)) + (x & 1) * 8, 4 * RK);
+      };
+      load_t(0);
+      reads_done();
       bf16x8 xp[3];
       {
-        const bf16x8 v8 = lds_frag_t(sm + L::oV + tile_off<DV / 8>(8 * g + (m >> 2), 2 * w + ((m & 3) >> 1)) + (m & 1) * 8,
-                                     4 * DV * 2);
         floatx4 x[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          const floatx4 be = lds_f4(scal(ch, 0) + (8 * g + 4 * u) * 4), lam = lds_f4(scal(ch, 1) + (8 * g + 4 * u) * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i)   // (a row past the end has no strength, and no value that could spoil that)
-            x[u][i] = be[i] * (static_cast<float>(v8[4 * u + i]) - lam[i] * y[u][i]);
-          z[u] *= lam;
+            x[u][i] = be[u][i] * (static_cast<float>(v8[4 * u + i]) - lam[u][i] * y[u][i]);
+          z[u] *= lam[u];
         }
         parts8<3>(x[0], x[1], xp);
       }
       lds_sync();   // A
       // ---- E = M X, the state after the chunk
-      bf16x8 ep[2], wp[3];
-      {
+      bf16x8 ep[2], wp[3], mp[2][3];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          bf16x8 mp[3];
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-          for (int p = 0; p < 3; ++p) mp[p] = lds_frag(mat_m(p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
-          mma_parts(e[u], mp, xp, 2);
-        }
-        const floatx4 w0 = lds_f4(scal(ch, 2) + 8 * g * 4), w1 = lds_f4(scal(ch, 2) + (8 * g + 4) * 4);
-        parts8<3>(w0 * e[0], w1 * e[1], wp);
-        parts8<2>(e[0], e[1], ep);
-      }
+        for (int p = 0; p < 3; ++p) mp[u][p] = lds_frag(mat_m(p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
+      const floatx4 w0 = lds_f4(scal(ch, 2) + 8 * g * 4), w1 = lds_f4(scal(ch, 2) + (8 * g + 4) * 4);
       const float lc = lds_f4(scal(ch, 1) + (kC - 4) * 4)[3];
+      reads_done();
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
+      for (int u = 0; u < 2; ++u) mma_parts(e[u], mp[u], xp, 2);
+      parts8<3>(w0 * e[0], w1 * e[1], wp);
+      bf16x8 pp[2][2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          bf16x8 tp[NT];
+      for (int x = 0; x < 2 * KK; ++x) {
+        if (x + 1 < 2 * KK) {
+          load_t(x + 1);
+        } else {
 #pragma unroll
-          for (int p = 0; p < NT; ++p)
-            tp[p] = lds_frag_t(kt_tile(ch, p) + tile_off<NCH>(8 * g + (m >> 2), 4 * kk + (m & 3)) + u * 8, 4 * RK);
-          S[kk][u] *= lc;
-          mma_parts(S[kk][u], tp, wp, 2);
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int p = 0; p < 2; ++p) pp[u][p] = lds_frag(mat_p(ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
         }
+        reads_done();
+        floatx4& t = S[x >> 1][x & 1];
+        t *= lc;
+        mma_parts(t, tp[x & 1], wp, 2);
+      }
+      parts8<2>(e[0], e[1], ep);
       // ---- O, which the producers store
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        bf16x8 pp[2];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) pp[p] = lds_frag(mat_p(ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
-        mma_parts(z[u], pp, ep, 1);
+        mma_parts(z[u], pp[u], ep, 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           *reinterpret_cast<lds_bf16*>(sm + L::oO + tile_off<DV / 8>(8 * g + 4 * u + i, v0 >> 3) + (v0 & 7) * 2) =
