@@ -10,6 +10,7 @@ fails loudly if the library has not been built.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -453,34 +454,48 @@ def pdn_chunk_bwd(q, k, v, beta, dO, *, g=None, gate="none", precond="squash",
 
 
 # ------------------------------------------------------- states in a pool
-def _on(name, t, device, dtype=None, shape=None):
-    """A dense tensor the kernels read as `shape` and `dtype` on `device`."""
+def _on(name, t, device, dtype, shape):
+    """Pointer of a dense tensor of this dtype and shape on `device` (None: NULL)."""
     if t is None:
         return None
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the state pool on {device}")
-    if dtype is not None and t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    return _ptr(t)
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
 def _token_rows(name, t, device, dtype, shape):
     """A [tokens, heads, d] tensor with dense rows: its pointer and the elements
     from one token to the next (0: dense)."""
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the state pool on {device}")
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not on {device}")
     if t.is_contiguous():
         return t.data_ptr(), 0
-    if t.stride(2) != 1 or t.stride(1) != shape[2]:
-        if shape[0] and shape[1] > 1 or t.stride(2) != 1:
-            raise ValueError(f"a token's row of {name} must be dense")
-    return t.data_ptr(), t.stride(0)
+    s0, s1, s2 = t.stride()
+    if s2 != 1 or s1 != shape[2] and shape[1] > 1:
+        raise ValueError(f"a token's row of {name} must be dense")
+    return t.data_ptr(), s0
+
+
+def _call_on(device, stream, fn, *args):
+    """fn(*args, stream) with `device` current."""
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(device.index)
+    else:
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == device.index:
+        return fn(*args, raw)
+    with torch.cuda.device(device):
+        return fn(*args, raw)
 
 
 def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
@@ -491,8 +506,9 @@ def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
                          "and v [tokens, H, dv]")
     P, H, dk, dv = S.shape
     M, Hk, _ = q.shape
-    dev, f32, i32 = S.device, torch.float32, torch.int32
-    io = _io_of(q)
+    dev, f32, i32, dt = S.device, torch.float32, torch.int32, q.dtype
+    if dev.type != "cuda":
+        raise ValueError(f"S is on {dev}")
     if starts is not None:
         N = starts.numel() - 1
         if N < 0:
@@ -504,35 +520,32 @@ def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
     T = max_tokens
     if T is None:   # without starts: rows shared out evenly
         T = M if starts is not None else M // N if N else 0
-    gram = precond in GRAM_PRECONDS
-    prob = make_problem(N, T, H, dk, dv, io=io, gate=gate, precond=precond,
-                        x=x, scale=scale, ridge=ridge, knorm=knorm)
-    qp, qs = _token_rows("q", q, dev, q.dtype, (M, Hk, dk))
-    kp, ks = _token_rows("k", k, dev, q.dtype, (M, Hk, dk))
-    vp, vs = _token_rows("v", v, dev, q.dtype, (M, H, dv))
+    prob = Problem(N, T, H, dk, dv, 64, PDN_BF16 if _io_of(q) == "bf16" else PDN_F32,
+                   GATES[gate], PRECONDS[precond], x, scale, ridge, KNORMS[knorm])
+    qp, qs = _token_rows("q", q, dev, dt, (M, Hk, dk))
+    kp, ks = _token_rows("k", k, dev, dt, (M, Hk, dk))
+    vp, vs = _token_rows("v", v, dev, dt, (M, H, dv))
     if o is None:
-        o = torch.empty((M, H, dv), dtype=q.dtype, device=dev)
-    inp = Inputs(qp, kp, vp, _on("beta", beta, dev, f32, (M, H)),
-                 _on("g", g, dev, f32,
-                     (M, H, dk) if gate == "channel" else (M, H)),
-                 _on("beta_p", beta_p, dev, f32, (M, H)),
-                 _on("g_p", g_p, dev, f32, (M, H)),
+        o = torch.empty((M, H, dv), dtype=dt, device=dev)
+    scalars, seqs = (M, H), (N,)
+    inp = Inputs(qp, kp, vp, _on("beta", beta, dev, f32, scalars),
+                 _on("g", g, dev, f32, (M, H, dk) if gate == "channel" else scalars),
+                 _on("beta_p", beta_p, dev, f32, scalars),
+                 _on("g_p", g_p, dev, f32, scalars),
                  _on("log_a_scale", log_a_scale, dev, f32, (H,)),
-                 None, None, _on("ktilde", ktilde, dev, q.dtype, (M, Hk, dk)))
+                 None, None, _on("ktilde", ktilde, dev, dt, (M, Hk, dk)))
     sl = Slots(M, P, Hk, qs, ks, vs, _on("starts", starts, dev, i32, (N + 1,)),
-               _on("slots", slots, dev, i32, (N,)),
-               _on("slots_out", slots_out, dev, i32, (N,)),
-               _on("fresh", fresh, dev, i32, (N,)), _on("S", S, dev, f32),
-               _on("A", A, dev, f32, (P, H, dk)), None, 0, None, None)
+               _on("slots", slots, dev, i32, seqs),
+               _on("slots_out", slots_out, dev, i32, seqs),
+               _on("fresh", fresh, dev, i32, seqs), _on("S", S, dev, f32, S.shape),
+               _on("A", A, dev, f32, (P, H, dk)))
     if tape is not None:
         sl.tape = _on("tape", tape, dev, f32,
                       (P, tape.shape[1], H, pdn_tape_record(dk, dv, gate, precond)))
         sl.tape_tokens = tape.shape[1]
         sl.pending = _on("pending", pending, dev, i32, (P, H))
-        sl.accepted = _on("accepted", accepted, dev, i32, (N,))
-    with torch.cuda.device(dev):
-        st = fn(ctypes.byref(prob), ctypes.byref(inp), ctypes.byref(sl),
-                _on("o", o, dev, q.dtype, (M, H, dv)), _stream(stream, dev))
+        sl.accepted = _on("accepted", accepted, dev, i32, seqs)
+    st = _call_on(dev, stream, fn, prob, inp, sl, _on("o", o, dev, dt, (M, H, dv)))
     if st != PDN_OK:
         raise PdnError(st, where)
     return o
@@ -590,6 +603,7 @@ def pdn_slot_draft(q, k, v, beta, S, tape, pending, *, accepted=None,
         ridge=ridge, knorm=knorm, o=o, stream=stream)
 
 
+@functools.lru_cache(maxsize=256)
 def pdn_draft_verify_workspace_size(N: int, V: int) -> int:
     n = ctypes.c_size_t(0)
     st = _lib.pdn_draft_verify_workspace_size(N, V, ctypes.byref(n))
@@ -610,21 +624,25 @@ def pdn_draft_verify(p, ids, u, r, *, q=None, starts=None, accepted=None,
         raise ValueError("p must be [rows, V]")
     M, V = p.shape
     N, dev, f32, i32 = r.numel(), p.device, torch.float32, torch.int32
-    io = _io_of(p)
-    accepted = torch.empty(N, dtype=i32, device=dev) if accepted is None else accepted
-    token = torch.empty(N, dtype=i32, device=dev) if token is None else token
+    if dev.type != "cuda":
+        raise ValueError(f"p is on {dev}")
+    io = PDN_BF16 if _io_of(p) == "bf16" else PDN_F32
+    if accepted is None:
+        accepted = torch.empty(N, dtype=i32, device=dev)
+    if token is None:
+        token = torch.empty(N, dtype=i32, device=dev)
     if workspace is None:
-        workspace = torch.empty(max(pdn_draft_verify_workspace_size(N, V), 1),
+        workspace = torch.empty(pdn_draft_verify_workspace_size(N, V),
                                 dtype=torch.uint8, device=dev)
-    with torch.cuda.device(dev):
-        st = _lib.pdn_draft_verify(
-            N, M, V, PDN_BF16 if io == "bf16" else PDN_F32, _on("p", p, dev),
-            _on("q", q, dev, p.dtype, (M, V)), _on("ids", ids, dev, i32, (M,)),
-            _on("u", u, dev, f32, (M,)), _on("r", r, dev, f32, (N,)),
-            _on("starts", starts, dev, i32, (N + 1,)),
-            _on("accepted", accepted, dev, i32, (N,)),
-            _on("token", token, dev, i32, (N,)), _on("workspace", workspace, dev),
-            workspace.numel(), _stream(stream, dev))
+    rows, seqs = (M,), (N,)
+    st = _call_on(
+        dev, stream, _lib.pdn_draft_verify, N, M, V, io, _on("p", p, dev, p.dtype, p.shape),
+        _on("q", q, dev, p.dtype, p.shape), _on("ids", ids, dev, i32, rows),
+        _on("u", u, dev, f32, rows), _on("r", r, dev, f32, seqs),
+        _on("starts", starts, dev, i32, (N + 1,)),
+        _on("accepted", accepted, dev, i32, seqs), _on("token", token, dev, i32, seqs),
+        _on("workspace", workspace, dev, torch.uint8, workspace.shape),
+        workspace.numel())
     if st != PDN_OK:
         raise PdnError(st, "pdn_draft_verify")
     return accepted, token

@@ -41,8 +41,8 @@ constexpr int kBlk = 8;   // tokens of a block
 
 // TB: tokens of a block, 1 (one-token calls: the products on the vector unit)
 // or kBlk.
-template <typename T, int DK, int DV, bool CH, int TB>
-__global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
+template <typename T, int DK, int DV, bool CH, int TB, bool DRAFT>
+__global__ __launch_bounds__(DV * 2, TB == 1 && !DRAFT ? 4 : 1) void slot_tokens(SlotArgs a) {
   constexpr int NTHR = DV * 2, NW = DV / 32, MB = DK / 16, LD = DK + 4;
   __shared__ __attribute__((aligned(16))) float sKQ[2 * TB][LD], sKt[TB][LD], sKw[kBlk][LD];
   __shared__ __attribute__((aligned(16))) float sPart[NW][16][kBlk], sLP[16][kBlk + 4], sE[NW][kBlk][32];
@@ -88,7 +88,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
 
   // ---- drafts: the accepted tokens of the tape
   const int64_t R = DK + DV + (CH ? DK : 4) + (gram ? DK : 0);
-  if (a.tape) {
+  if constexpr (DRAFT) {
     int cnt = 0;
     if (a.accepted && !fresh) {
       const int pend = min(a.pending[src * a.H + h], a.tape_tokens);
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
         Gt[t] = G;
         lam[t] = CH ? fast_exp(G) : 1.f;
       }
-      float* rec = a.tape && key ? a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R : nullptr;
+      float* rec = DRAFT && key ? a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R : nullptr;
 #pragma unroll
       for (int t = 0; t < TB; ++t) {
         const float f = TB == 1 ? 1.f : lam[t];
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
       }
     }
     __syncthreads();
-    if (a.tape && !CH && tid < 4 * nt)
+    if (DRAFT && !CH && tid < 4 * nt)
       a.tape[((dst * a.tape_tokens + t0 + tid / 4) * a.H + h) * R + DK + DV + tid % 4] = sGp[tid / 4];
 
     if constexpr (TB == 1) {
@@ -308,7 +308,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
       }
       const floatx2 e = beta * (vv[0] - lam0 * y), o = a.scale * (lam0 * z + kq * e);
       if (lg == 0) st2<T>(ob + row0 * a.H * DV, o[0], o[1]);
-      if (a.tape) {
+      if (DRAFT) {
         if (lg == 0) *reinterpret_cast<floatx2*>(a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R + DK + v0) = e;
       } else {
 #pragma unroll
@@ -403,7 +403,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
           for (int i = 0; i < 4; ++i)
             if (tb + i < nt) st2<T>(ob + (row0 + tb + i) * a.H * DV, a.scale * o[0][i], a.scale * o[1][i]);
       }
-      if (a.tape) {
+      if (DRAFT) {
         if (lg < 2)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -412,7 +412,7 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
                   floatx2{e[0][i], e[1][i]};
       }
       // ---- the state after the block (drafts: only for the block after it)
-      if (!a.tape || t0 + TB < rows.n) {
+      if (!DRAFT || t0 + TB < rows.n) {
         if (lg < 2)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
@@ -441,20 +441,24 @@ __global__ __launch_bounds__(DV * 2) void slot_tokens(SlotArgs a) {
     }
     __syncthreads();
   }
-  if (!a.tape) store_state();
+  if (!DRAFT) store_state();
 }
 
-template <typename T, int DK, int DV, bool CH>
+template <typename T, int DK, int DV, bool CH, bool DRAFT>
 hipError_t launch_tb(const SlotArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(a.B * a.H));
-  if (a.T <= 1) hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, 1>), grid, dim3(DV * 2), 0, s, a);
-  else hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, kBlk>), grid, dim3(DV * 2), 0, s, a);
+  if (a.T <= 1) hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, 1, DRAFT>), grid, dim3(DV * 2), 0, s, a);
+  else hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, kBlk, DRAFT>), grid, dim3(DV * 2), 0, s, a);
   return hipGetLastError();
+}
+template <typename T, int DK, int DV, bool CH>
+hipError_t launch_draft(const SlotArgs& a, hipStream_t s) {
+  return a.tape ? launch_tb<T, DK, DV, CH, true>(a, s) : launch_tb<T, DK, DV, CH, false>(a, s);
 }
 
 template <typename T, int DK, int DV>
 hipError_t launch_gate(const SlotArgs& a, hipStream_t s) {
-  return a.gate == kGateChannel ? launch_tb<T, DK, DV, true>(a, s) : launch_tb<T, DK, DV, false>(a, s);
+  return a.gate == kGateChannel ? launch_draft<T, DK, DV, true>(a, s) : launch_draft<T, DK, DV, false>(a, s);
 }
 
 template <typename T>
