@@ -354,7 +354,8 @@ typedef struct {
   int64_t Hk;               /* query / key heads, a divisor of H; 0: H         */
   int64_t q_stride, k_stride, v_stride; /* elements from a token's row to the
                                next (q, k, v may be slices of one projection's
-                               rows; whole multiples of 16 bytes); 0: dense    */
+                               rows; whole multiples of 16 bytes, at most 2^25);
+                               0: dense                                        */
   const int32_t* starts;    /* [B + 1] first row of each sequence, and the end of
                                the last; NULL: B sequences of T rows           */
   const int32_t* slot;      /* [B] slot a sequence's state is read from; NULL: its

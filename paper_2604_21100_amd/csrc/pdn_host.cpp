@@ -197,7 +197,11 @@ pdn_status check_slots(const pdn_problem* p, const pdn_slots* s, bool draft, Slo
   z.qs = s->q_stride ? s->q_stride : wq;
   z.ks = s->k_stride ? s->k_stride : wq;
   z.vs = s->v_stride ? s->v_stride : wv;
-  if (z.qs < wq || z.ks < wq || z.vs < wv) return PDN_ERR_SHAPE;
+  // (a few rows are seen through a buffer of 32-bit offsets)
+  const int64_t far = (int64_t)1 << 25;
+  if (z.qs < wq || z.ks < wq || z.vs < wv || z.qs > far || z.ks > far || z.vs > far || wq > far || wv > far ||
+      p->H * (int64_t)p->dk > far)
+    return PDN_ERR_SHAPE;
   if (z.qs * esz % 16 || z.ks * esz % 16 || z.vs * esz % 16) return PDN_ERR_ALIGN;
   if (!span_ok(s->tokens, z.qs, wq, esz, &z.nq) || !span_ok(s->tokens, z.ks, wq, esz, &z.nk) ||
       !span_ok(s->tokens, z.vs, wv, esz, &z.nv) || !span_ok(s->tokens, wv, wv, esz, &z.no) ||

@@ -263,12 +263,9 @@ hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s);
 // More tokens than a block of pdn_slots.hip go in chunks of 32 on the bf16
 // matrix instructions (pdn_slot_chunks.hip), where queries and keys are bf16
 // numbers as they enter the products (no per-channel decay on them) and a write key
-// needs no sum over its channels.  (A chunk's rows are seen through a buffer of
-// 32-bit offsets.)
+// needs no sum over its channels.
 inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
-  const int64_t far = (int64_t)1 << 25;
-  return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.q_stride < far && a.k_stride < far && a.v_stride < far &&
-         a.Hk * a.dk < far && a.H * a.dv < far && a.knorm == kKnormNone &&
+  return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.knorm == kKnormNone &&
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
 }
 hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);

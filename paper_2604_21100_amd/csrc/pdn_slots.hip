@@ -1,17 +1,16 @@
 // The gated delta rule over packed sequences whose states live in slots of a
-// pool: decoding, prompts, and drafted tokens that are scored without moving
-// the state.  Per sequence and value head, with S^T the state and G the
-// inclusive prefix of the log-decay over a block of up to eight tokens
-// (lam = exp(G)):
+// pool: decoding, drafted tokens that are scored without moving the state, and
+// the prompts pdn_slot_chunks.hip does not take.  Per sequence and value head, with
+// S^T the state and G the inclusive prefix of the log-decay over a block of up
+// to eight tokens (lam = exp(G)):
 //   L[t][s] = beta_t k_t Lam_t/Lam_s . kt_s  (s < t)    P[t][s] = q_t Lam_t/Lam_s . kt_s  (s <= t)
 //   X = Diag(beta) (V - Diag(lam) K S^T)                E = (I + L)^{-1} X
 //   O = scale (Diag(lam) Q S^T + P E)                   S'^T = lam_C S^T + Kt^T Diag(lam_C / lam) E
 // All of it in fp32: states, operands and products (the fp32 matrix
 // instruction), so a state comes out as exact as a token-by-token one.
 //
-// A workgroup holds one head's state in registers: a wave 32 columns of it, a
-// lane the rows 16 m + 4 (l / 16) + i of the columns 2 (l % 16) and the next.
-// That is at once the accumulator layout of the update (16 x 16 tiles of S^T)
+// A workgroup holds one head's state in registers: a wave 16 or 32 columns of it,
+// a lane the rows 16 m + 4 (l / 16) + i of its one or two.  That is at once the accumulator layout of the update (16 x 16 tiles of S^T)
 // and, contracted in the order (m, i), the right operand of the products with
 // S^T, so the state goes from one block to the next without leaving its
 // registers.  The left operand of those products stacks the eight key rows
@@ -26,6 +25,7 @@
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 #include "pdn_slots.hpp"
+#include "pdn_tile.hpp"
 
 namespace pdn {
 
@@ -39,426 +39,640 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 constexpr int kBlk = 8;   // tokens of a block
 
-// TB: tokens of a block, 1 (one-token calls: the products on the vector unit)
-// or kBlk.
-template <typename T, int DK, int DV, bool CH, int TB, bool DRAFT>
-__global__ __launch_bounds__(DV * 2, TB == 1 && !DRAFT ? 4 : 1) void slot_tokens(SlotArgs a) {
-  constexpr int NTHR = DV * 2, NW = DV / 32, MB = DK / 16, LD = DK + 4;
-  __shared__ __attribute__((aligned(16))) float sKQ[2 * TB][LD], sKt[TB][LD], sKw[kBlk][LD];
-  __shared__ __attribute__((aligned(16))) float sPart[NW][16][kBlk], sLP[16][kBlk + 4], sE[NW][kBlk][32];
-  __shared__ __attribute__((aligned(16))) float sLam[DK], sSum[NW][TB];
+// A head's state, seen through a buffer: a lane's rows are then one offset and
+// constants, where pointers to them would take two registers each.
+template <int DK, int DV>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t state_head(const SlotArgs& a, int64_t slot, int64_t h) {
+  return buf_rsrc(reinterpret_cast<const char*>(a.S + (slot * a.H + h) * (DK * DV)), DK * DV * 4);
+}
+// a wave's 32 columns of it, two a lane (from element `at` of the head)
+template <int DK, int DV>
+struct Columns2 {
+  static constexpr int MB = DK / 16;
+  floatx4 t[MB][2];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int m = 0; m < MB; ++m) t[m][0] = t[m][1] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at) {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const floatx2 x =
+            __builtin_bit_cast(floatx2, __builtin_amdgcn_raw_buffer_load_b64(r, 4 * at, (16 * m + i) * DV * 4, 0));
+        t[m][0][i] = x[0];
+        t[m][1][i] = x[1];
+      }
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, int at) const {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, floatx2{t[m][0][i], t[m][1][i]}), r, 4 * at,
+                                              (16 * m + i) * DV * 4, 0);
+  }
+};
+// and 16 columns, one a lane
+template <int DK, int DV>
+struct Columns {
+  static constexpr int MB = DK / 16;
+  floatx4 t[MB];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int m = 0; m < MB; ++m) t[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at) {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        t[m][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, 4 * at, (16 * m + i) * DV * 4, 0));
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, int at) const {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = t[m][i];   // (the bits of t[m][i] itself would be those of t[m][0])
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), r, 4 * at, (16 * m + i) * DV * 4, 0);
+      }
+  }
+};
+
+// The write key of a token's channel, its query, and the factor its key row's sum
+// m = k . kt asks for.
+__device__ __forceinline__ float write_key(const SlotArgs& a, float k, float x, float A, float Ap, float mu) {
+  if (a.precond == kSquash) return squash_gain(A, mu, a.lnx) * k;
+  if (a.precond == kDiagSM) return k / (Ap + a.ridge);
+  return a.precond == kExternal ? x : k;
+}
+__device__ __forceinline__ bool needs_sum(const SlotArgs& a) { return a.precond == kDiagSM || a.knorm != kKnormNone; }
+__device__ __forceinline__ float sum_factor(const SlotArgs& a, float m, float beta, float g) {
+  if (a.precond == kDiagSM || a.knorm == kKnorm1pm) return 1.f / (1.f + m);
+  if (a.knorm == kKnormM) return 1.f / m;
+  return beta / ((a.gate == kGateScalar ? fast_exp(g) : 1.f) + beta * m);
+}
+
+// ---------------------------------------------------------------- one token
+//   S' = alpha S + e kt^T,  e = beta (v - (alpha S) k),  o = scale ((alpha S) q + (kt . q) e)
+// on the vector unit; what bounds it is reading and writing the state.
+template <typename T, int DK, int DV, bool CH>
+__global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
+  constexpr int NTHR = DV * 2, NW = DV / 32, MB = DK / 16;
+  __shared__ __attribute__((aligned(16))) float sK[DK], sQ[DK], sKt[DK], sLam[CH ? DK : 4];
+  __shared__ float sSum[NW];
+  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
+  if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
+  const SlotRows rows = slot_rows(a, seq);
+  const bool fresh = a.fresh && a.fresh[seq] != 0, gram = has_gram(a.precond);
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lg = l >> 4;
+  const int v0 = 32 * w + 2 * (l & 15), at = 4 * lg * DV + v0;
+  const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key, both = a.precond == kATQ;
+  const int c = tid % DK;
+  Columns2<DK, DV> S;
+  if (fresh) S.zero();
+  else S.load(state_head<DK, DV>(a, src, h), at);
+  float A = gram && key && !fresh ? a.A[(src * a.H + h) * DK + c] : 0.f;
+  if (rows.n > 0) {
+    const int64_t row = rows.lo, sc = row * a.H + h;
+    const float kv = key ? to_f(static_cast<const T*>(a.k)[row * a.k_stride + hk * DK + c]) : 0.f;
+    float qv = qry || (both && key) ? to_f(static_cast<const T*>(a.q)[row * a.q_stride + hk * DK + c]) : 0.f;
+    const float xv = a.precond == kExternal && key ? to_f(static_cast<const T*>(a.ktilde)[(row * a.Hk + hk) * DK + c]) : 0.f;
+    const floatx2 vv = ld2<T>(static_cast<const T*>(a.v) + row * a.v_stride + h * DV + v0);
+    const float beta = a.beta[sc], g = CH ? a.g[sc * DK + c] : a.gate == kGateScalar ? a.g[sc] : 0.f;
+    const float Ap = A;
+    if (gram) A = (a.g_p ? fast_exp(a.g_p[sc]) : 1.f) * A + a.beta_p[sc] * kv * kv;
+    float kt = write_key(a, kv, xv, A, Ap, a.precond == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f);
+    if (both) qv /= A + a.ridge;
+    if (needs_sum(a)) {
+      const float x = wave_sum(key ? kv * kt : 0.f);
+      if (l == 0) sSum[w] = x;
+      __syncthreads();
+      float m = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) m += sSum[i];
+      kt *= sum_factor(a, m, beta, g);
+    }
+    if (key) {
+      sK[c] = both ? 0.f : kv;   // (a linear-attention update has no correction by the state)
+      sKt[c] = kt;
+      if (CH) sLam[c] = fast_exp(g);
+    }
+    if (both ? key : qry) sQ[c] = qv;
+    __syncthreads();
+    const float lam0 = CH ? 1.f : fast_exp(g);
+    floatx2 y = {0.f, 0.f}, z = y;
+    float kq = 0.f;
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      const floatx4 k4 = *reinterpret_cast<const floatx4*>(&sK[16 * m + 4 * lg]);
+      const floatx4 q4 = *reinterpret_cast<const floatx4*>(&sQ[16 * m + 4 * lg]);
+      const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[16 * m + 4 * lg]);
+      if (CH) {
+        const floatx4 f = *reinterpret_cast<const floatx4*>(&sLam[16 * m + 4 * lg]);
+        S.t[m][0] *= f;
+        S.t[m][1] *= f;
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[0] += k4[i] * S.t[m][0][i];
+        y[1] += k4[i] * S.t[m][1][i];
+        z[0] += q4[i] * S.t[m][0][i];
+        z[1] += q4[i] * S.t[m][1][i];
+        kq += q4[i] * t4[i];
+      }
+    }
+#pragma unroll
+    for (int off = 16; off < 64; off <<= 1) {
+      y[0] += __shfl_xor(y[0], off, 64);
+      y[1] += __shfl_xor(y[1], off, 64);
+      z[0] += __shfl_xor(z[0], off, 64);
+      z[1] += __shfl_xor(z[1], off, 64);
+      kq += __shfl_xor(kq, off, 64);
+    }
+    const floatx2 e = beta * (vv - lam0 * y), o = a.scale * (lam0 * z + kq * e);
+    if (lg == 0) st2<T>(static_cast<T*>(a.o) + row * a.H * DV + h * DV + v0, o[0], o[1]);
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[16 * m + 4 * lg]);
+      S.t[m][0] = lam0 * S.t[m][0] + t4 * e[0];
+      S.t[m][1] = lam0 * S.t[m][1] + t4 * e[1];
+    }
+  }
+  S.store(state_head<DK, DV>(a, dst, h), at);
+  if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+}
+
+// ---------------------------------------------------------------- blocks of tokens
+// Everything that does not need the state is loaded first and worked on while
+// the state is on its way: a block's rows (16 bytes a thread), from them L and
+// P, and the accepted records.  A wave has 16 columns here, a lane one (with two,
+// the state and the rest of it take more registers than there are).
+template <typename T, int DK, int DV, bool CH, bool DRAFT>
+__global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  constexpr int NTHR = DV * 4, NW = DV / 16, MB = DK / 16, LD = DK + 4;
+  constexpr int RP = kBlk * DK * sizeof(T) / 16, NRP = (RP + NTHR - 1) / NTHR;   // 16-byte pieces of a block's key rows
+  constexpr int GP = kBlk * DK * 4 / 16, NGP = (GP + NTHR - 1) / NTHR;           // of a block's rows of fp32
+  __shared__ __attribute__((aligned(16))) T sRaw[3][kBlk][DK];   // keys, queries, the caller's write keys
+  __shared__ __attribute__((aligned(16))) float sKQ[2 * kBlk][LD], sKt[kBlk][LD];
+  // CH: g; the write keys with the decay to the block's end, and as they are.
+  // Drafts: the accepted records' write keys; A after each token.
+  __shared__ __attribute__((aligned(16))) float sG[CH ? kBlk : 1][LD], sKw[CH ? kBlk : 1][LD], sKr[CH && DRAFT ? kBlk : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kBlk : 1][LD], sAt[DRAFT ? kBlk : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sPart[NW][16][kBlk], sLP[16][kBlk + 4], sE[NW][kBlk][16];
+  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kBlk : 1][LD], sSum[NW][kBlk];
   // of each token: log-decay, its sum from the first token, the decay to and from
-  // the token within the block as factors (1 with a per-channel gate), write strength
-  __shared__ __attribute__((aligned(16))) float sG[TB], sGp[TB], sTo[TB], sOn[TB], sB[TB];
+  // the token within the block as factors (1 with a per-channel gate), write strength,
+  // preconditioner gain and decay
+  __shared__ __attribute__((aligned(16))) float sg[kBlk], sGp[kBlk], sTo[kBlk], sOn[kBlk], sB[kBlk], sBp[kBlk], sDp[kBlk];
   const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);
   const bool fresh = a.fresh && a.fresh[seq] != 0;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lr = l & 15, lg = l >> 4;
-  const int v0 = 32 * w + 2 * lr;
-  const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key;
-  const int c = tid % DK;
-  const int prec = a.precond;
-  const bool gram = has_gram(prec);
+  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lr = l & 15, lg = l >> 4, tb = 4 * (lg & 1);
+  const int v0 = 16 * w + lr;
+  const int prec = a.precond, c = tid % DK;
+  const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key, both = prec == kATQ, gram = has_gram(prec);
+  const int64_t R = DK + DV + (CH ? DK : 4) + (gram ? DK : 0), rs = a.H * R;   // a record; from one token's to the next
 
-  // ---- the state
-  floatx4 S[MB][2];
-  {
-    const float* sp = a.S + (src * a.H + h) * (DK * DV) + 4 * lg * DV + v0;
+  // ---- A block's rows, from memory into registers, then into LDS.  Rows are seen
+  // through a buffer that ends with the sequence (past it: zeros); what a call does
+  // not have is a buffer of no bytes.  (No branches: one would wait for its loads.)
+  u32x4 rk[NRP], rq[NRP], rx[NRP], rg[NGP];
+  float vn[4], vv[4];   // values: those under way, the block's
+  float s_b = 0.f, s_g = 0.f, s_bp = 0.f, s_gp = 0.f;
+  const bool scalar = a.gate == kGateScalar;
+  const float *const gb = scalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
+              *const gpb = gram && a.g_p ? a.g_p : a.beta;
+  auto load_rows = [&](int64_t t0) {
+    const int n = static_cast<int>(min<int64_t>(kBlk, rows.n - t0));
+    const int64_t row = rows.lo + t0;
+    auto view = [&](const void* p, int64_t stride, int64_t first, int width, int esz, bool there) {
+      return buf_rsrc(static_cast<const char*>(p) + (row * stride + first) * esz,
+                      there ? static_cast<uint32_t>(((n - 1) * stride + width) * esz) : 0);
+    };
+    auto piece = [&](__amdgpu_buffer_rsrc_t r, int64_t stride, int row_bytes, int esz, int x) {
+      const uint32_t at = x * NTHR + tid, t = at * 16 / row_bytes, o = at * 16 % row_bytes;
+      return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                           r, static_cast<int>(t * static_cast<uint32_t>(stride * esz) + o), 0, 0));
+    };
+    const __amdgpu_buffer_rsrc_t vk = view(a.k, a.k_stride, hk * DK, DK, sizeof(T), true),
+                                 vq = view(a.q, a.q_stride, hk * DK, DK, sizeof(T), true),
+                                 vx = view(a.ktilde, a.Hk * DK, hk * DK, DK, sizeof(T), prec == kExternal),
+                                 vw = view(a.v, a.v_stride, h * DV, DV, sizeof(T), true);
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
+    for (int x = 0; x < NRP; ++x) {
+      rk[x] = piece(vk, a.k_stride, DK * sizeof(T), sizeof(T), x);
+      rq[x] = piece(vq, a.q_stride, DK * sizeof(T), sizeof(T), x);
+      rx[x] = piece(vx, a.Hk * DK, DK * sizeof(T), sizeof(T), x);
+    }
+    if (CH) {
+      const __amdgpu_buffer_rsrc_t vg = view(a.g, a.H * DK, h * DK, DK, 4, true);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const floatx2 x = fresh ? floatx2{0.f, 0.f} : *reinterpret_cast<const floatx2*>(sp + (16 * m + i) * DV);
-        S[m][0][i] = x[0];
-        S[m][1][i] = x[1];
-      }
-  }
-  float A = gram && key && !fresh ? a.A[(src * a.H + h) * DK + c] : 0.f;
-  auto store_state = [&]() {
-    float* sp = a.S + (dst * a.H + h) * (DK * DV) + 4 * lg * DV + v0;
+      for (int x = 0; x < NGP; ++x) rg[x] = piece(vg, a.H * DK, DK * 4, 4, x);
+    }
 #pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<floatx2*>(sp + (16 * m + i) * DV) = floatx2{S[m][0][i], S[m][1][i]};
-    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+    for (int i = 0; i < 4; ++i) {
+      const int o = (tb + i) * static_cast<uint32_t>(a.v_stride * sizeof(T)) + v0 * sizeof(T);
+      if constexpr (sizeof(T) == 2)
+        vn[i] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(vw, o, 0, 0)) << 16);
+      else
+        vn[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(vw, o, 0, 0));
+    }
+    const int64_t sc = (row + min(tid & (kBlk - 1), n - 1)) * a.H + h;
+    const bool in = (tid & (kBlk - 1)) < n;
+    const float x_b = a.beta[sc], x_g = gb[sc], x_bp = bpb[sc], x_gp = gpb[sc];
+    s_b = in ? x_b : 0.f;
+    s_g = in && scalar ? x_g : 0.f;
+    s_bp = in && gram ? x_bp : 0.f;
+    s_gp = in && gram && a.g_p ? x_gp : 0.f;
   };
-
-  // ---- drafts: the accepted tokens of the tape
-  const int64_t R = DK + DV + (CH ? DK : 4) + (gram ? DK : 0);
-  if constexpr (DRAFT) {
-    int cnt = 0;
-    if (a.accepted && !fresh) {
-      const int pend = min(a.pending[src * a.H + h], a.tape_tokens);
-      cnt = max(min(a.accepted[seq], pend), 0);
+  float gacc = 0.f;   // log-decay summed over the blocks before (the scalar's; of a channel)
+  auto put_rows = [&]() {
+    auto put = [&](void* p, const u32x4& v, int x, int pieces, int row_bytes, int ld_bytes) {
+      const int at = x * NTHR + tid;
+      if (at < pieces)
+        *reinterpret_cast<u32x4*>(static_cast<char*>(p) + at * 16 / row_bytes * ld_bytes + at * 16 % row_bytes) = v;
+    };
+#pragma unroll
+    for (int x = 0; x < NRP; ++x) {
+      put(sRaw[0], rk[x], x, RP, DK * sizeof(T), DK * sizeof(T));
+      put(sRaw[1], rq[x], x, RP, DK * sizeof(T), DK * sizeof(T));
+      if (prec == kExternal) put(sRaw[2], rx[x], x, RP, DK * sizeof(T), DK * sizeof(T));
     }
-    if (cnt > 0) {
-      const float* rec = a.tape + (src * a.tape_tokens * a.H + h) * R;
-      const int64_t rs = a.H * R;   // to the next token's record
-      const float* last = rec + (cnt - 1) * rs;
-      const float Gn = CH ? 0.f : last[DK + DV];
-      if (gram && key) A = last[DK + DV + (CH ? DK : 4) + c];
+    if (CH)
 #pragma unroll
-      for (int m = 0; m < MB; ++m) {
-        floatx4 lam;
-        if (CH) {
-          const floatx4 g = *reinterpret_cast<const floatx4*>(last + DK + DV + 16 * m + 4 * lg);
+      for (int x = 0; x < NGP; ++x) put(sG, rg[x], x, GP, DK * 4, LD * 4);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) lam[i] = fast_exp(g[i]);
-        } else {
-          lam = fast_exp(Gn);
-        }
-        S[m][0] *= lam;
-        S[m][1] *= lam;
-      }
-      for (int b0 = 0; b0 < cnt; b0 += kBlk) {
-        for (int x = tid; x < kBlk * DK / 4; x += NTHR) {
-          const int t = x / (DK / 4), cc = 4 * (x % (DK / 4));
-          floatx4 kt = {0.f, 0.f, 0.f, 0.f};
-          if (b0 + t < cnt) {
-            const float* r = rec + (b0 + t) * rs;
-            kt = *reinterpret_cast<const floatx4*>(r + cc);
-            if (CH) {
-              const floatx4 g = *reinterpret_cast<const floatx4*>(r + DK + DV + cc);
-              const floatx4 gn = *reinterpret_cast<const floatx4*>(last + DK + DV + cc);
+    for (int i = 0; i < 4; ++i) vv[i] = vn[i];
+    if (tid < kBlk) {
+      const float nx = __shfl_down(s_g, 1, kBlk);
+      float to = s_g, on = tid + 1 < kBlk ? nx : 0.f;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) kt[i] *= fast_exp(gn[i] - g[i]);
-            } else {
-              kt *= fast_exp(Gn - r[DK + DV]);
-            }
-          }
-          *reinterpret_cast<floatx4*>(&sKw[t][cc]) = kt;
-        }
-        floatx2 e[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int t = b0 + 4 * j + lg;
-          e[j] = t < cnt ? *reinterpret_cast<const floatx2*>(rec + t * rs + DK + v0) : floatx2{0.f, 0.f};
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (b0 + 4 * j >= cnt) break;
-#pragma unroll
-          for (int m = 0; m < MB; ++m) {
-            const float x = sKw[4 * j + lg][16 * m + lr];
-            mma4(S[m][0], x, e[j][0]);
-            mma4(S[m][1], x, e[j][1]);
-          }
-        }
-        __syncthreads();
-      }
-    }
-    if (cnt > 0 || fresh || src != dst) store_state();
-    __syncthreads();   // (the count it overwrites may be the one just read)
-    if (tid == 0) a.pending[dst * a.H + h] = static_cast<int>(rows.n);
-  }
-
-  // ---- the tokens, in blocks
-  const T* qb = static_cast<const T*>(a.q) + hk * DK + c;
-  const T* kb = static_cast<const T*>(a.k) + hk * DK + c;
-  const T* xb = prec == kExternal ? static_cast<const T*>(a.ktilde) + hk * DK + c : nullptr;
-  const T* vb = static_cast<const T*>(a.v) + h * DV + v0;
-  T* ob = static_cast<T*>(a.o) + h * DV + v0;
-  const float mu = prec == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f;
-  float gacc = 0.f;   // log-decay summed over the blocks before (of the channel, or the scalar)
-  for (int64_t t0 = 0; t0 < rows.n; t0 += TB) {
-    const int nt = static_cast<int>(min<int64_t>(TB, rows.n - t0));
-    const int64_t row0 = rows.lo + t0;
-    // ---- key, query and write-key rows (a token past the end: zeros)
-    float kv[TB], qv[TB], kt[TB], gg[TB], bp[TB], gp[TB];
-    const bool both = prec == kATQ;   // the query depends on A: the key's thread forms it
-#pragma unroll
-    for (int t = 0; t < TB; ++t) {
-      const int64_t row = row0 + min(t, nt - 1), sc = row * a.H + h;
-      kv[t] = key ? to_f(kb[row * a.k_stride]) : 0.f;
-      qv[t] = qry || (both && key) ? to_f(qb[row * a.q_stride]) : 0.f;
-      kt[t] = prec == kExternal && key ? to_f(xb[row * a.Hk * DK]) : 0.f;
-      gg[t] = CH ? a.g[sc * DK + c] : 0.f;
-      bp[t] = gram ? a.beta_p[sc] : 0.f;
-      gp[t] = gram && a.g_p ? a.g_p[sc] : 0.f;
-      if (t >= nt) kv[t] = qv[t] = kt[t] = gg[t] = bp[t] = gp[t] = 0.f;
-    }
-    floatx2 vv[4];
-#pragma unroll
-    for (int i = 0; i < (TB == 1 ? 1 : 4); ++i) {
-      const int t = TB == 1 ? 0 : 4 * (lg & 1) + i;
-      vv[i] = ld2<T>(vb + (row0 + min(t, nt - 1)) * a.v_stride);
-    }
-    if (tid < TB) {
-      const int64_t sc = (row0 + min(tid, nt - 1)) * a.H + h;
-      sB[tid] = tid < nt ? a.beta[sc] : 0.f;
-      const float g = a.gate == kGateScalar && tid < nt ? a.g[sc] : 0.f;
-      const float nx = __shfl_down(g, 1, TB);
-      float to = g, on = tid + 1 < TB ? nx : 0.f;
-#pragma unroll
-      for (int off = 1; off < TB; off <<= 1) {
-        const float y = __shfl_up(to, off, TB), z = __shfl_down(on, off, TB);
+      for (int off = 1; off < kBlk; off <<= 1) {
+        const float y = __shfl_up(to, off, kBlk), z = __shfl_down(on, off, kBlk);
         if (tid >= off) to += y;
-        if (tid + off < TB) on += z;
+        if (tid + off < kBlk) on += z;
       }
-      sG[tid] = g;
-      sGp[tid] = gacc + to;
-      gacc += __shfl(to, TB - 1, TB);
+      sg[tid] = s_g;
       sTo[tid] = fast_exp(to);
       sOn[tid] = fast_exp(on);
-    }
-    float At[TB], rs[TB];
-#pragma unroll
-    for (int t = 0; t < TB; ++t) {
-      const float Ap = A;
-      if (gram && t < nt) A = fast_exp(gp[t]) * A + bp[t] * kv[t] * kv[t];
-      At[t] = A;
-      if (prec == kSquash) kt[t] = squash_gain(A, mu, a.lnx) * kv[t];
-      if (prec == kIdentity || prec == kATQ) kt[t] = kv[t];
-      if (prec == kDiagSM) kt[t] = kv[t] / (Ap + a.ridge);
-      if (prec == kATQ) qv[t] = qv[t] / (A + a.ridge);
-    }
-    if (prec == kDiagSM || a.knorm != kKnormNone) {   // the write key's row sums
-#pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        rs[t] = wave_sum(key ? kv[t] * kt[t] : 0.f);
-        if (l == 0) sSum[w][t] = rs[t];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        float m = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) m += sSum[i][t];
-        float f;
-        if (prec == kDiagSM) f = 1.f / (1.f + m);
-        else if (a.knorm == kKnormM) f = 1.f / m;
-        else if (a.knorm == kKnorm1pm) f = 1.f / (1.f + m);
-        else {
-          const float alpha = a.gate == kGateScalar ? fast_exp(sG[t]) : 1.f;
-          f = sB[t] / (alpha + sB[t] * m);
-        }
-        kt[t] = t < nt ? f * kt[t] : 0.f;
+      sB[tid] = s_b;
+      sBp[tid] = s_bp;
+      sDp[tid] = fast_exp(s_gp);
+      if (!CH) {
+        sGp[tid] = gacc + to;
+        gacc += __shfl(to, kBlk - 1, kBlk);
       }
     }
-    // a linear-attention update has no correction by the state: no key rows
-    const bool la = prec == kATQ;
+  };
+  if (rows.n > 0) load_rows(0);
+
+  // ---- drafts: the first accepted records
+  const float* const rec = DRAFT ? a.tape + (src * a.tape_tokens * a.H + h) * R : nullptr;
+  u32x4 ck[NGP], cg[NGP];
+  float ce[2];
+  auto load_records = [&](int b0) {   // (whether accepted or not; never past the tape)
+    const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kBlk));
+#pragma unroll
+    for (int x = 0; x < NGP; ++x) {
+      const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
+      ck[x] = cg[x] = u32x4{0, 0, 0, 0};
+      if (t < n) {
+        ck[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + cc);
+        if (CH) cg[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + DK + DV + cc);
+        else cg[x][0] = reinterpret_cast<const uint32_t*>(rec)[(b0 + t) * rs + DK + DV];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const int t = 4 * j + lg;
+      ce[j] = t < n ? rec[(b0 + t) * rs + DK + v0] : 0.f;
+    }
+  };
+  int cnt = 0;
+  if (DRAFT && a.accepted && !fresh) {
+    load_records(0);
+    const int64_t pend = min((int64_t)a.pending[src * a.H + h], a.tape_tokens);
+    cnt = static_cast<int>(max(min((int64_t)a.accepted[seq], pend), (int64_t)0));
+  }
+  const float* const last = DRAFT ? rec + max(cnt - 1, 0) * rs : nullptr;
+
+  // ---- the state
+  const int at = 4 * lg * DV + v0;
+  Columns<DK, DV> S;
+  if (fresh) S.zero();
+  else S.load(state_head<DK, DV>(a, src, h), at);
+  float A = 0.f;
+  if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
+  const float A0 = A;
+  const float mu = prec == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f;
+
+  // ---- a block's operands: key, query and write-key rows, L and P
+  auto operands = [&](int nt) {
     {
-      float G = 0.f, lam[TB], Gt[TB];
+      float kt[kBlk], kv[kBlk], G = 0.f, to[kBlk], At[kBlk];
+      const float Ab = A;   // before the block
 #pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        G += gg[t];
-        Gt[t] = G;
-        lam[t] = CH ? fast_exp(G) : 1.f;
+      for (int t = 0; t < kBlk; ++t) {
+        kv[t] = to_f(sRaw[0][t][c]);
+        if (CH) {
+          G += sG[t][c];
+          to[t] = G;
+        }
       }
-      float* rec = DRAFT && key ? a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R : nullptr;
+      if (gram) {   // (a token past the end leaves A: no gain, no decay)
 #pragma unroll
-      for (int t = 0; t < TB; ++t) {
-        const float f = TB == 1 ? 1.f : lam[t];
-        if (key) {
-          sKQ[t][c] = la ? 0.f : f * kv[t];
-          sKt[t][c] = CH && TB > 1 ? kt[t] * fast_exp(-Gt[t]) : kt[t];
-          if (CH && TB > 1) sKw[t][c] = kt[t] * fast_exp(G - Gt[t]);
-          if (rec && t < nt) {
-            float* r = rec + t * a.H * R;
-            r[c] = kt[t];
-            if (CH) r[DK + DV + c] = gacc + Gt[t];
-            if (gram) r[DK + DV + (CH ? DK : 4) + c] = At[t];
+        for (int t = 0; t < kBlk; ++t) {
+          A = sDp[t] * A + sBp[t] * kv[t] * kv[t];
+          At[t] = A;
+        }
+        if (DRAFT && key)
+#pragma unroll
+          for (int t = 0; t < kBlk; ++t) sAt[t][c] = At[t];
+      }
+      if (prec == kSquash) {
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) kt[t] = squash_gain(At[t], mu, a.lnx) * kv[t];
+      } else if (prec == kDiagSM) {
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) kt[t] = kv[t] / ((t ? At[t - 1] : Ab) + a.ridge);
+      } else {
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) kt[t] = prec == kExternal ? to_f(sRaw[2][t][c]) : kv[t];
+      }
+      if (both ? key : qry)
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) {
+          float q = to_f(sRaw[1][t][c]);
+          if (both) q /= At[t] + a.ridge;
+          sKQ[kBlk + t][c] = CH ? fast_exp(to[t]) * q : q;
+        }
+      if (needs_sum(a)) {   // the write key's row sums
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) {
+          const float x = wave_sum(key ? kv[t] * kt[t] : 0.f);
+          if (l == 0) sSum[w][t] = x;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) {
+          float m = 0.f;
+#pragma unroll
+          for (int i = 0; i < NW; ++i) m += sSum[i][t];
+          kt[t] = t < nt ? sum_factor(a, m, sB[t], sg[t]) * kt[t] : 0.f;
+        }
+      }
+      if (key)
+#pragma unroll
+        for (int t = 0; t < kBlk; ++t) {
+          // (a linear-attention update has no correction by the state: no key rows)
+          sKQ[t][c] = both ? 0.f : CH ? fast_exp(to[t]) * kv[t] : kv[t];
+          sKt[t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
+          if (CH) {
+            sKw[t][c] = kt[t] * fast_exp(G - to[t]);
+            if (DRAFT) {
+              sKr[t][c] = kt[t];
+              sGt[t][c] = gacc + to[t];
+            }
           }
         }
-        if (both ? key : qry) sKQ[TB + t][c] = f * qv[t];
-      }
       if (CH) {
-        if (key) sLam[c] = lam[TB - 1];
+        if (key) sLam[c] = fast_exp(G);
         gacc += G;
       }
     }
     __syncthreads();
-    if (DRAFT && !CH && tid < 4 * nt)
-      a.tape[((dst * a.tape_tokens + t0 + tid / 4) * a.H + h) * R + DK + DV + tid % 4] = sGp[tid / 4];
+    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave
+    floatx4 g4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m0 = 0; m0 < MB; m0 += NW) {
+      const int m = m0 + w;
+      if (MB < NW && m >= MB) break;
+      const floatx4 r4 = *reinterpret_cast<const floatx4*>(&sKQ[lr][16 * m + 4 * lg]);
+      const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[lr & 7][16 * m + 4 * lg]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
+    }
+    if (lr < kBlk)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sPart[w][4 * lg + i][lr] = g4[i];
+    __syncthreads();
+    if (tid < 16 * kBlk) {
+      const int r = tid / kBlk, s = tid % kBlk, t = r % kBlk;
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < NW; ++i) x += sPart[i][r][s];
+      if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
+        float g = 0.f;
+#pragma unroll
+        for (int j = 1; j < kBlk; ++j) g += j > s && j <= t ? sg[j] : 0.f;
+        x *= fast_exp(g);
+      }
+      sLP[r][s] = r < kBlk ? (s < t ? sB[t] * x : 0.f) : (s <= t ? x : 0.f);
+    }
+    __syncthreads();
+  };
 
-    if constexpr (TB == 1) {
-      const float lam0 = sTo[0], beta = sB[0];
-      floatx2 y = {0.f, 0.f}, z = y;
-      float kq = 0.f;
+  // ---- the accepted records' operand: write keys with their decay to the last
+  const float Gn = DRAFT && !CH && cnt > 0 ? last[DK + DV] : 0.f;
+  auto put_records = [&](int b0) {
+#pragma unroll
+    for (int x = 0; x < NGP; ++x) {
+      const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
+      if (at < GP) {
+        floatx4 kt = {0.f, 0.f, 0.f, 0.f};
+        if (b0 + t < cnt) {
+          kt = __builtin_bit_cast(floatx4, ck[x]);
+          const floatx4 g = __builtin_bit_cast(floatx4, cg[x]);
+          if (CH) {
+            const floatx4 gn = *reinterpret_cast<const floatx4*>(last + DK + DV + cc);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) kt[i] *= fast_exp(gn[i] - g[i]);
+          } else {
+            kt *= fast_exp(Gn - g[0]);
+          }
+        }
+        *reinterpret_cast<floatx4*>(&sC[t][cc]) = kt;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (b0 + 4 * j + lg >= cnt) ce[j] = 0.f;
+  };
+  auto apply_records = [&](int b0) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if (b0 + 4 * j >= cnt) break;
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
-        const floatx4 k4 = *reinterpret_cast<const floatx4*>(&sKQ[0][16 * m + 4 * lg]);
-        const floatx4 q4 = *reinterpret_cast<const floatx4*>(&sKQ[1][16 * m + 4 * lg]);
-        const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[0][16 * m + 4 * lg]);
-        if (CH) {
-          const floatx4 f = *reinterpret_cast<const floatx4*>(&sLam[16 * m + 4 * lg]);
-          S[m][0] *= f;
-          S[m][1] *= f;
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[0] += k4[i] * S[m][0][i];
-          y[1] += k4[i] * S[m][1][i];
-          z[0] += q4[i] * S[m][0][i];
-          z[1] += q4[i] * S[m][1][i];
-          kq += q4[i] * t4[i];
-        }
+        const float x = sC[4 * j + lg][16 * m + lr];
+        mma4(S.t[m], x, ce[j]);
       }
-#pragma unroll
-      for (int off = 16; off < 64; off <<= 1) {
-        y[0] += __shfl_xor(y[0], off, 64);
-        y[1] += __shfl_xor(y[1], off, 64);
-        z[0] += __shfl_xor(z[0], off, 64);
-        z[1] += __shfl_xor(z[1], off, 64);
-        kq += __shfl_xor(kq, off, 64);
-      }
-      const floatx2 e = beta * (vv[0] - lam0 * y), o = a.scale * (lam0 * z + kq * e);
-      if (lg == 0) st2<T>(ob + row0 * a.H * DV, o[0], o[1]);
-      if (DRAFT) {
-        if (lg == 0) *reinterpret_cast<floatx2*>(a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R + DK + v0) = e;
-      } else {
+    }
+  };
+
+  T* ob = static_cast<T*>(a.o) + h * DV + v0;
+  // (drafts come here without tokens too: their accepted records are applied in the first round)
+  for (int64_t t0 = 0; t0 < rows.n || (DRAFT && t0 == 0); t0 += kBlk) {
+    const int nt = static_cast<int>(max(min<int64_t>(kBlk, rows.n - t0), (int64_t)0));
+    const int64_t row0 = rows.lo + t0;
+    if (nt > 0) put_rows();
+    if (DRAFT && t0 == 0 && cnt > 0) put_records(0);
+    __syncthreads();
+    if (rows.n > t0 + kBlk) load_rows(t0 + kBlk);
+    if (nt > 0) operands(nt);
+    if (DRAFT && t0 == 0) {
+      if (cnt > 0) {
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
-          const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[0][16 * m + 4 * lg]);
-          S[m][0] = lam0 * S[m][0] + t4 * e[0];
-          S[m][1] = lam0 * S[m][1] + t4 * e[1];
+          floatx4 lam;
+          if (CH) {
+            const floatx4 g = *reinterpret_cast<const floatx4*>(last + DK + DV + 16 * m + 4 * lg);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lam[i] = fast_exp(g[i]);
+          } else {
+            lam = fast_exp(Gn);
+          }
+          S.t[m] *= lam;
+        }
+        apply_records(0);
+        for (int b0 = kBlk; b0 < cnt; b0 += kBlk) {
+          load_records(b0);
+          __syncthreads();
+          put_records(b0);
+          __syncthreads();
+          apply_records(b0);
         }
       }
-    } else {
-      // ---- (rows of K over rows of Q) times Kt^T, this wave's share of the channels, and times S^T
-      floatx4 g4 = {0.f, 0.f, 0.f, 0.f}, yz[2] = {g4, g4};
+      if (cnt > 0 || fresh || src != dst) {
+        S.store(state_head<DK, DV>(a, dst, h), at);
+        if (gram && key) a.A[(dst * a.H + h) * DK + c] = A0;
+      }
+      __syncthreads();   // (what is read of the tape has been read)
+      if (tid == 0) a.pending[dst * a.H + h] = static_cast<int>(rows.n);
+      if (nt == 0) break;
+    }
+    if (DRAFT) {   // the records, but for e
+      float* r0 = a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R;
+      for (int x = tid; x < nt * DK / 4; x += NTHR) {
+        const int t = x / (DK / 4), cc = 4 * (x % (DK / 4));
+        float* r = r0 + t * rs;
+        *reinterpret_cast<floatx4*>(r + cc) = *reinterpret_cast<const floatx4*>(CH ? &sKr[t][cc] : &sKt[t][cc]);
+        if (CH) *reinterpret_cast<floatx4*>(r + DK + DV + cc) = *reinterpret_cast<const floatx4*>(&sGt[t][cc]);
+        if (gram) *reinterpret_cast<floatx4*>(r + DK + DV + (CH ? DK : 4) + cc) = *reinterpret_cast<const floatx4*>(&sAt[t][cc]);
+      }
+      if (!CH && tid < 4 * nt) r0[tid / 4 * rs + DK + DV + tid % 4] = sGp[tid / 4];
+    }
+    // ---- (rows of K over rows of Q) times S^T
+    floatx4 yz = {0.f, 0.f, 0.f, 0.f}, yz1 = yz;   // (two sums: each product would wait for the one before)
+#pragma unroll
+    for (int m = 0; m < MB; ++m) {
+      const floatx4 r4 = *reinterpret_cast<const floatx4*>(&sKQ[lr][16 * m + 4 * lg]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma4(i & 1 ? yz1 : yz, r4[i], S.t[m][i]);
+    }
+    yz += yz1;
+    // ---- E: tokens 0-3 in the first 16 lanes, 4-7 in the next
+    floatx4 e;
+    {
+      floatx4 ld[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ld[i] = *reinterpret_cast<const floatx4*>(&sLP[tb + i][tb]);
+      const floatx4 be = *reinterpret_cast<const floatx4*>(&sB[tb]), lam = *reinterpret_cast<const floatx4*>(&sTo[tb]);
+      floatx4 x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = be[i] * (vv[i] - lam[i] * yz[i]);
+      yz *= lam;
+      auto solve = [&](floatx4 y) {
+        y[1] -= ld[1][0] * y[0];
+        y[2] -= ld[2][0] * y[0] + ld[2][1] * y[1];
+        y[3] -= ld[3][0] * y[0] + ld[3][1] * y[1] + ld[3][2] * y[2];
+        return y;
+      };
+      e = solve(x);
+      if (nt > 4) {
+        floatx4 f;   // e of tokens 0-3
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = __shfl(e[j], lr, 64);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const floatx4 lx = *reinterpret_cast<const floatx4*>(&sLP[4 + i][0]);
+          x[i] -= (lx[0] * f[0] + lx[1] * f[1]) + (lx[2] * f[2] + lx[3] * f[3]);
+        }
+        x = solve(x);
+        if (lg == 1) e = x;
+      }
+      if (lg >= 2) e = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    // ---- O: rows 8-15 of the products, plus P E
+    {
+      floatx4 p4 = *reinterpret_cast<const floatx4*>(&sLP[lr][tb]);
+      if (lr < kBlk || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+      if (lg >= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (tb + i < nt) ob[(row0 + tb + i) * a.H * DV] = from_f<T>(a.scale * yz[i]);
+    }
+    if (DRAFT && lg < 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (tb + i < nt)
+          a.tape[((dst * a.tape_tokens + t0 + tb + i) * a.H + h) * R + DK + v0] = e[i];
+    // ---- the state after the block (drafts: only for the block after it)
+    if (!DRAFT || t0 + kBlk < rows.n) {
+      const floatx4 wt = *reinterpret_cast<const floatx4*>(&sOn[tb]);
+      if (lg < 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sE[w][tb + i][lr] = wt[i] * e[i];
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      const float lc = sTo[kBlk - 1];
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
-        const floatx4 r4 = *reinterpret_cast<const floatx4*>(&sKQ[lr][16 * m + 4 * lg]);
-        if (m % NW == w) {
-          const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[lr & 7][16 * m + 4 * lg]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          mma4(yz[0], r4[i], S[m][0][i]);
-          mma4(yz[1], r4[i], S[m][1][i]);
-        }
+        floatx4 f = {lc, lc, lc, lc};
+        if (CH) f = *reinterpret_cast<const floatx4*>(&sLam[16 * m + 4 * lg]);
+        S.t[m] *= f;
       }
-      if (lr < kBlk)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sPart[w][4 * lg + i][lr] = g4[i];
-      __syncthreads();
-      if (tid < 16 * kBlk) {
-        const int r = tid / kBlk, s = tid % kBlk, t = r % kBlk;
-        float x = 0.f;
-#pragma unroll
-        for (int i = 0; i < NW; ++i) x += sPart[i][r][s];
-        if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
-          float g = 0.f;
-#pragma unroll
-          for (int j = 1; j < kBlk; ++j) g += j > s && j <= t ? sG[j] : 0.f;
-          x *= fast_exp(g);
-        }
-        sLP[r][s] = r < kBlk ? (s < t ? sB[t] * x : 0.f) : (s <= t ? x : 0.f);
-      }
-      __syncthreads();
-      // ---- E: tokens 0-3 in the first 16 lanes, 4-7 in the next
-      const int tb = 4 * (lg & 1);
-      floatx4 ld[4], lx[4], e[2];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        ld[i] = *reinterpret_cast<const floatx4*>(&sLP[tb + i][tb]);
-        lx[i] = *reinterpret_cast<const floatx4*>(&sLP[4 + i][0]);
-      }
-      const floatx4 be = *reinterpret_cast<const floatx4*>(&sB[tb]), lam = *reinterpret_cast<const floatx4*>(&sTo[tb]),
-                    wt = *reinterpret_cast<const floatx4*>(&sOn[tb]);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        floatx4 x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = be[i] * (vv[i][b] - lam[i] * yz[b][i]);
-        auto solve = [&](floatx4 y) {
-          y[1] -= ld[1][0] * y[0];
-          y[2] -= ld[2][0] * y[0] + ld[2][1] * y[1];
-          y[3] -= ld[3][0] * y[0] + ld[3][1] * y[1] + ld[3][2] * y[2];
-          return y;
-        };
-        floatx4 y = solve(x);
-        if (nt > 4) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float f = __shfl(y[j], lr, 64);   // e of token j
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] -= lx[i][j] * f;
-          }
-          const floatx4 y1 = solve(x);
-          if (lg == 1) y = y1;
-        }
-        e[b] = lg < 2 ? y : floatx4{0.f, 0.f, 0.f, 0.f};
-      }
-      // ---- O: rows 8-15 of the products, plus P E
-      {
-        floatx4 p4 = *reinterpret_cast<const floatx4*>(&sLP[lr][tb]);
-        if (lr < kBlk || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
-        floatx4 o[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          o[b] = lam * yz[b];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) mma4(o[b], p4[i], e[b][i]);
-        }
-        if (lg >= 2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tb + i < nt) st2<T>(ob + (row0 + tb + i) * a.H * DV, a.scale * o[0][i], a.scale * o[1][i]);
-      }
-      if (DRAFT) {
-        if (lg < 2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tb + i < nt)
-              *reinterpret_cast<floatx2*>(a.tape + ((dst * a.tape_tokens + t0 + tb + i) * a.H + h) * R + DK + v0) =
-                  floatx2{e[0][i], e[1][i]};
-      }
-      // ---- the state after the block (drafts: only for the block after it)
-      if (!DRAFT || t0 + TB < rows.n) {
-        if (lg < 2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<floatx2*>(&sE[w][tb + i][2 * lr]) = floatx2{wt[i] * e[0][i], wt[i] * e[1][i]};
-        __syncthreads();
-        const float lc = sTo[TB - 1];
+      for (int j = 0; j < 2; ++j) {
+        if (4 * j >= nt) break;
+        const float ej = sE[w][4 * j + lg][lr];
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
-          floatx4 f = {lc, lc, lc, lc};
-          if (CH) f = *reinterpret_cast<const floatx4*>(&sLam[16 * m + 4 * lg]);
-          S[m][0] *= f;
-          S[m][1] *= f;
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          if (4 * j >= nt) break;
-          const floatx2 ej = *reinterpret_cast<const floatx2*>(&sE[w][4 * j + lg][2 * lr]);
-#pragma unroll
-          for (int m = 0; m < MB; ++m) {
-            const float x = CH ? sKw[4 * j + lg][16 * m + lr] : sKt[4 * j + lg][16 * m + lr];
-            mma4(S[m][0], x, ej[0]);
-            mma4(S[m][1], x, ej[1]);
-          }
+          const float x = CH ? sKw[4 * j + lg][16 * m + lr] : sKt[4 * j + lg][16 * m + lr];
+          mma4(S.t[m], x, ej);
         }
       }
     }
     __syncthreads();
   }
-  if (!DRAFT) store_state();
+  if constexpr (!DRAFT) {
+    S.store(state_head<DK, DV>(a, dst, h), at);
+    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+  }
 }
 
-template <typename T, int DK, int DV, bool CH, bool DRAFT>
-hipError_t launch_tb(const SlotArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.B * a.H));
-  if (a.T <= 1) hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, 1, DRAFT>), grid, dim3(DV * 2), 0, s, a);
-  else hipLaunchKernelGGL((slot_tokens<T, DK, DV, CH, kBlk, DRAFT>), grid, dim3(DV * 2), 0, s, a);
-  return hipGetLastError();
-}
 template <typename T, int DK, int DV, bool CH>
-hipError_t launch_draft(const SlotArgs& a, hipStream_t s) {
-  return a.tape ? launch_tb<T, DK, DV, CH, true>(a, s) : launch_tb<T, DK, DV, CH, false>(a, s);
+hipError_t launch_form(const SlotArgs& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.B * a.H));
+  if (a.tape) hipLaunchKernelGGL((slot_blocks<T, DK, DV, CH, true>), grid, dim3(DV * 4), 0, s, a);
+  else if (a.T <= 1) hipLaunchKernelGGL((slot_step<T, DK, DV, CH>), grid, dim3(DV * 2), 0, s, a);
+  else hipLaunchKernelGGL((slot_blocks<T, DK, DV, CH, false>), grid, dim3(DV * 4), 0, s, a);
+  return hipGetLastError();
 }
 
 template <typename T, int DK, int DV>
 hipError_t launch_gate(const SlotArgs& a, hipStream_t s) {
-  return a.gate == kGateChannel ? launch_draft<T, DK, DV, true>(a, s) : launch_draft<T, DK, DV, false>(a, s);
+  return a.gate == kGateChannel ? launch_form<T, DK, DV, true>(a, s) : launch_form<T, DK, DV, false>(a, s);
 }
 
 template <typename T>

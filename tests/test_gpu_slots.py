@@ -276,19 +276,19 @@ def test_more_than_2_31_elements():
     rng = np.random.default_rng(7)
     H, d = 16, 128
     P = 2 ** 31 // (H * d * d) + 9   # the last slots start past 2^31 elements (8.6 GB)
-    M, gap = 6, 2 ** 29   # rows 2^29 elements apart: the last starts past 2^31
+    M, gap = 66, 2 ** 25   # rows 2^25 elements apart: the last starts past 2^31
     b = batch(rng, M, H, H, d, d, "bf16", "none", "identity")
     S, _ = pool(rng, 2, H, d, d, "identity")
-    o, S1, _, _ = want(b, S, None, [5, 1], "none", "identity")
+    o, S1, _, _ = want(b, S, None, [M - 1, 1], "none", "identity")
     big = torch.zeros(P, H, d, d, device="cuda")
     big[P - 1], big[3] = dev(S[0]), dev(S[1])
     pos, opt = dev_batch(b, "bf16", "identity")
     wide = torch.empty((M - 1) * gap + H * d, dtype=torch.bfloat16, device="cuda").as_strided((M, H, d), (gap, d, 1))
     wide.copy_(pos[2])
-    kw = dict(gate="none", precond="identity", starts=i32([0, 5, 6]), slots=i32([P - 1, 3]), max_tokens=5)
+    kw = dict(gate="none", precond="identity", starts=i32([0, M - 1, M]), slots=i32([P - 1, 3]), max_tokens=M)
     got = pdn.pdn_slot_fwd(pos[0], pos[1], wide, pos[3], big, **kw, **KW)
     torch.cuda.synchronize()
-    check((host(got), host(big[[P - 1, 3]]), None), (o, S1, None), "bf16", 5)
+    check((host(got), host(big[[P - 1, 3]]), None), (o, S1, None), "bf16", M)
 
 
 def test_refusals_of_the_binding():

@@ -50,6 +50,7 @@ def test_refusals(draft):
         (dict(s=S(q_stride=255)), pdn.PDN_ERR_SHAPE), (dict(s=S(q_stride=260)), pdn.PDN_ERR_ALIGN),
         (dict(s=S(k_stride=257)), pdn.PDN_ERR_ALIGN), (dict(s=S(v_stride=128)), pdn.PDN_ERR_SHAPE),
         (dict(s=S(q_stride=1 << 62)), pdn.PDN_ERR_SHAPE),
+        (dict(s=S(k_stride=(1 << 25) + 8)), pdn.PDN_ERR_SHAPE), (dict(p=prob(H=1 << 22), s=S(Hk=0)), pdn.PDN_ERR_SHAPE),
         (dict(i=inputs(q=None)), pdn.PDN_ERR_NULL), (dict(i=inputs(beta=None)), pdn.PDN_ERR_NULL), (dict(o=None), pdn.PDN_ERR_NULL),
         (dict(i=inputs(g=None)), pdn.PDN_ERR_NULL), (dict(i=inputs(beta_p=None)), pdn.PDN_ERR_NULL),
         (dict(i=inputs(log_a_scale=None)), pdn.PDN_ERR_NULL), (dict(s=S(S=None)), pdn.PDN_ERR_NULL),
