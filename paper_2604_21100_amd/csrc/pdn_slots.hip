@@ -235,10 +235,17 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);
   const bool fresh = a.fresh && a.fresh[seq] != 0;
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, lr = l & 15, lg = l >> 4, tb = 4 * (lg & 1);
-  const int v0 = 16 * w + lr;
-  const int prec = a.precond, c = tid % DK;
-  const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key, both = prec == kATQ, gram = has_gram(prec);
+  const int prec = a.precond, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const bool both = prec == kATQ, gram = has_gram(prec);
+  // The thread's number, made anew for each part: what is formed from it, addresses
+  // above all, is then formed where it is used (held throughout, all of them
+  // together take more registers than there are).
+  int tid = threadIdx.x;
+  auto anew = [&]() { asm volatile("" : "+v"(tid)); };
+#define IDS                                                                                                    \
+  [[maybe_unused]] const int l = tid & 63, lr = l & 15, lg = l >> 4, tb = 4 * (lg & 1), v0 = 16 * w + lr,       \
+                             c = tid % DK;                                                                     \
+  [[maybe_unused]] const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key
   const int64_t R = DK + DV + (CH ? DK : 4) + (gram ? DK : 0), rs = a.H * R;   // a record; from one token's to the next
 
   // ---- A block's rows, from memory into registers, then into LDS.  Rows are seen
@@ -251,6 +258,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   const float *const gb = scalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
               *const gpb = gram && a.g_p ? a.g_p : a.beta;
   auto load_rows = [&](int64_t t0) {
+    IDS;
     const int n = static_cast<int>(min<int64_t>(kBlk, rows.n - t0));
     const int64_t row = rows.lo + t0;
     auto view = [&](const void* p, int64_t stride, int64_t first, int width, int esz, bool there) {
@@ -339,6 +347,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   u32x4 ck[NGP], cg[NGP];
   float ce[2];
   auto load_records = [&](int b0) {   // (whether accepted or not; never past the tape)
+    IDS;
     const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kBlk));
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
@@ -365,17 +374,25 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   const float* const last = DRAFT ? rec + max(cnt - 1, 0) * rs : nullptr;
 
   // ---- the state
-  const int at = 4 * lg * DV + v0;
   Columns<DK, DV> S;
-  if (fresh) S.zero();
-  else S.load(state_head<DK, DV>(a, src, h), at);
   float A = 0.f;
-  if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
+  {
+    IDS;
+    if (fresh) S.zero();
+    else S.load(state_head<DK, DV>(a, src, h), 4 * lg * DV + v0);
+    if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
+  }
+  auto store_state = [&](float A) {
+    IDS;
+    S.store(state_head<DK, DV>(a, dst, h), 4 * lg * DV + v0);
+    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+  };
   const float A0 = A;
   const float mu = prec == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f;
 
   // ---- a block's operands: key, query and write-key rows, L and P
   auto operands = [&](int nt) {
+    IDS;
     {
       float kt[kBlk], kv[kBlk], G = 0.f, to[kBlk], At[kBlk];
       const float Ab = A;   // before the block
@@ -483,6 +500,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // ---- the accepted records' operand: write keys with their decay to the last
   const float Gn = DRAFT && !CH && cnt > 0 ? last[DK + DV] : 0.f;
   auto put_records = [&](int b0) {
+    IDS;
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
       const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
@@ -507,6 +525,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       if (b0 + 4 * j + lg >= cnt) ce[j] = 0.f;
   };
   auto apply_records = [&](int b0) {
+    IDS;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (b0 + 4 * j >= cnt) break;
@@ -518,18 +537,22 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     }
   };
 
-  T* ob = static_cast<T*>(a.o) + h * DV + v0;
   // (drafts come here without tokens too: their accepted records are applied in the first round)
   for (int64_t t0 = 0; t0 < rows.n || (DRAFT && t0 == 0); t0 += kBlk) {
     const int nt = static_cast<int>(max(min<int64_t>(kBlk, rows.n - t0), (int64_t)0));
     const int64_t row0 = rows.lo + t0;
+    anew();
     if (nt > 0) put_rows();
     if (DRAFT && t0 == 0 && cnt > 0) put_records(0);
     __syncthreads();
+    anew();
     if (rows.n > t0 + kBlk) load_rows(t0 + kBlk);
+    anew();
     if (nt > 0) operands(nt);
+    anew();
     if (DRAFT && t0 == 0) {
       if (cnt > 0) {
+        IDS;
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           floatx4 lam;
@@ -552,13 +575,15 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
         }
       }
       if (cnt > 0 || fresh || src != dst) {
-        S.store(state_head<DK, DV>(a, dst, h), at);
-        if (gram && key) a.A[(dst * a.H + h) * DK + c] = A0;
+        store_state(A0);
       }
       __syncthreads();   // (what is read of the tape has been read)
       if (tid == 0) a.pending[dst * a.H + h] = static_cast<int>(rows.n);
       if (nt == 0) break;
     }
+    anew();
+    IDS;
+    T* const ob = static_cast<T*>(a.o) + h * DV + v0;
     if (DRAFT) {   // the records, but for e
       float* r0 = a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R;
       for (int x = tid; x < nt * DK / 4; x += NTHR) {
@@ -656,10 +681,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     __syncthreads();
   }
   if constexpr (!DRAFT) {
-    S.store(state_head<DK, DV>(a, dst, h), at);
-    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+    store_state(A);
   }
 }
+#undef IDS
 
 template <typename T, int DK, int DV, bool CH>
 hipError_t launch_form(const SlotArgs& a, hipStream_t s) {
