@@ -136,39 +136,34 @@ __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
   if (tid < 2) a.sums[blockIdx.x * 2 + tid] = ((sW[tid][0] + sW[tid][1]) + sW[tid][2]) + sW[tid][3];
 }
 
-// inclusive sums over the workgroup's threads, in order; every thread also
-// gets the whole sum
-__device__ __forceinline__ double block_scan(double x, double* sW, double* all) {
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
+// inclusive sums over the wave's lanes, in order
+__device__ __forceinline__ double wave_scan(double x, int l) {
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
     const double y = __shfl_up(x, off, 64);
     if (l >= off) x += y;
   }
-  __syncthreads();
-  if (l == 63) sW[w] = x;
-  __syncthreads();
-  double before = 0.0, sum = 0.0;
-#pragma unroll
-  for (int i = 0; i < kThreads / kWave; ++i) {
-    if (i < w) before += sW[i];
-    sum += sW[i];
-  }
-  *all = sum;
-  return before + x;
+  return x;
 }
 
+// The first place of the wave's 64 (lane l's: its inclusive sum cum, its own share
+// x) whose sum is over the target: the lane, or -1; `last` keeps the last place
+// that has a share.
+__device__ __forceinline__ int first_over(double cum, double x, double target, int* last) {
+  const unsigned long long some = __ballot(x > 0.0), over = __ballot(x > 0.0 && cum > target);
+  *last = some ? 63 - __clzll(some) : -1;
+  return over ? __ffsll(over) - 1 : -1;
+}
+
+// A wave a sequence: the segment, 64 at a time, then in it the token, 32 a lane.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void verify_pick(VerifyArgs a) {
-  __shared__ double sW[kThreads / kWave];
-  __shared__ double sTot[2];
-  __shared__ unsigned long long sFirst, sLast;   // the first position over the target; the last with a weight, plus one
-  __shared__ double sBefore;
+__global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
+  constexpr int PER = kSeg / kWave;
   const int64_t segs = segments(a.V), seq = blockIdx.x;
   const Span s = seq_span(a, seq);
-  const int tid = threadIdx.x;
+  const int l = threadIdx.x;
   if (s.n == 0) {   // no rows
-    if (tid == 0) {
+    if (l == 0) {
       a.accepted[seq] = 0;
       a.token[seq] = -1;
     }
@@ -176,78 +171,82 @@ __global__ __launch_bounds__(kThreads) void verify_pick(VerifyArgs a) {
   }
   const double* sums = a.sums + seq * segs * 2;
   const int64_t n = a.accepted[seq] - 1;
-  double tot[2] = {0.0, 0.0};
-  for (int64_t b = 0; b < segs; b += kThreads)
+  const double r = a.r[seq];
+  // running sums of 64 segments, of both kinds
+  double x[2], cum[2];
+  auto sum_segments = [&](int64_t b, const double (&base)[2]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      double all;
-      block_scan(b + tid < segs ? sums[2 * (b + tid) + k] : 0.0, sW, &all);
-      tot[k] += all;
+      x[k] = b + l < segs ? sums[2 * (b + l) + k] : 0.0;
+      cum[k] = base[k] + wave_scan(x[k], l);
     }
+  };
+  double tot[2] = {0.0, 0.0};
+  for (int64_t b = 0; b < segs; b += kWave) {
+    sum_segments(b, tot);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) tot[k] = __shfl(cum[k], 63, 64);
+  }
   const int kind = tot[0] > 0.0 ? 0 : 1;   // nothing left over q: p itself
-  const double target = a.r[seq] * tot[kind];
-  // the segment, then the token in it: the first whose running sum is over the
-  // target, else the last that has a weight
-  if (tid == 0) {
-    sFirst = ~0ull;
-    sLast = 0ull;
-    sBefore = 0.0;
-  }
-  double base = 0.0;
-  for (int64_t b = 0; b < segs; b += kThreads) {
-    const double x = b + tid < segs ? sums[2 * (b + tid) + kind] : 0.0;
-    double all;
-    const double cum = base + block_scan(x, sW, &all);
-    if (b + tid < segs && x > 0.0) {
-      atomicMax(&sLast, static_cast<unsigned long long>(b + tid) + 1);
-      if (cum > target) atomicMin(&sFirst, static_cast<unsigned long long>(b + tid));
+  const double target = r * tot[kind];
+  // the first segment whose running sum is over the target, else the last that has a weight
+  int64_t seg = -1;
+  double base[2] = {0.0, 0.0}, before = 0.0;
+  bool found = false;
+  for (int64_t b = 0; b < segs && !found; b += kWave) {
+    if (segs > kWave) sum_segments(b, base);   // (else they are at hand)
+    const double c = kind ? cum[1] : cum[0], w = kind ? x[1] : x[0];
+    int last;
+    const int f = first_over(c, w, target, &last);
+    found = f >= 0;
+    const int at = found ? f : last;
+    if (at >= 0) {
+      seg = b + at;
+      before = __shfl(c - w, at, 64);
     }
-    __syncthreads();
-    const bool found = sFirst != ~0ull;
-    if (found && static_cast<unsigned long long>(b + tid) == sFirst) sBefore = cum - x;
-    __syncthreads();
-    if (found) break;
-    base += all;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) base[k] = __shfl(cum[k], 63, 64);
   }
-  const unsigned long long first = sFirst, last = sLast;
-  const double before = sBefore;
-  __syncthreads();
-  if (last == 0ull) {   // no token has a weight
-    if (tid == 0) a.token[seq] = -1;
+  if (seg < 0) {   // no token has a weight
+    if (l == 0) a.token[seq] = -1;
     return;
   }
-  const int64_t seg = static_cast<int64_t>(first != ~0ull ? first : last - 1);
-  if (tid == 0) {
-    sFirst = ~0ull;
-    sLast = 0ull;
-  }
-  double w0[kVec], w1[kVec], x = 0.0, all;
-  const int64_t j0 = seg * kSeg + tid * kVec;
-  weights(stop_row<T>(a, s, n), j0, a.V, w0, w1);
+  const Row<T> row = stop_row<T>(a, s, n);
+  const int64_t j0 = seg * kSeg + l * PER;
+  double v[PER / kVec][kVec], mine = 0.0;
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) x += kind ? w1[i] : w0[i];
-  double cum = before + (block_scan(x, sW, &all) - x);
-  unsigned long long f = ~0ull, g = 0ull;
+  for (int c = 0; c < PER / kVec; ++c) {
+    double w0[kVec], w1[kVec];
+    weights(row, j0 + c * kVec, a.V, w0, w1);
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    const double v = kind ? w1[i] : w0[i];
-    cum += v;
-    if (v > 0.0) {
-      g = static_cast<unsigned long long>(j0 + i) + 1;
-      if (f == ~0ull && first != ~0ull && cum > target) f = static_cast<unsigned long long>(j0 + i);
+    for (int i = 0; i < kVec; ++i) {
+      v[c][i] = kind ? w1[i] : w0[i];
+      mine += v[c][i];
     }
   }
-  if (f != ~0ull) atomicMin(&sFirst, f);
-  if (g) atomicMax(&sLast, g);
-  __syncthreads();
-  if (tid == 0) a.token[seq] = static_cast<int>(sFirst != ~0ull ? sFirst : sLast - 1);
+  const double upto = wave_scan(mine, l);
+  double sum = before + (upto - mine);
+  int last, f = first_over(before + upto, mine, target, &last);
+  if (f < 0 || !found) f = last;   // (rounding at a segment's very end, or no segment is over the target)
+  int first = -1, final = -1;
+#pragma unroll
+  for (int c = 0; c < PER / kVec; ++c)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      sum += v[c][i];
+      if (v[c][i] > 0.0) {
+        final = c * kVec + i;
+        if (first < 0 && found && sum > target) first = c * kVec + i;
+      }
+    }
+  if (l == f) a.token[seq] = static_cast<int>(j0 + (first >= 0 ? first : final));
 }
 
 template <typename T>
 hipError_t launch(const VerifyArgs& a, hipStream_t s) {
   if (a.rows > 0)
     hipLaunchKernelGGL((verify_sums<T>), dim3(static_cast<unsigned>(a.N * segments(a.V))), dim3(kThreads), 0, s, a);
-  hipLaunchKernelGGL((verify_pick<T>), dim3(static_cast<unsigned>(a.N)), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL((verify_pick<T>), dim3(static_cast<unsigned>(a.N)), dim3(kWave), 0, s, a);
   return hipGetLastError();
 }
 
