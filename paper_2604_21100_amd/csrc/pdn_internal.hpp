@@ -269,6 +269,8 @@ inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
 }
 hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);
+// Other runs of more than a block (pdn_slot_runs.hip).
+hipError_t launch_slot_runs(const SlotArgs& a, int io_bf16, hipStream_t s);
 
 // Verification of drafted tokens (pdn_verify.hip).
 struct VerifyArgs {

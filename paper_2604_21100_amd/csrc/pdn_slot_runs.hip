@@ -1,0 +1,368 @@
+// pdn_slot_fwd over more than a block of tokens in the modes whose operands are not
+// bf16 numbers (fp32 tensors, per-channel decays, write keys that need a sum over their
+// channels, preconditioned queries): the blocks of eight of pdn_slots.hip, one after
+// the other, in fp32 throughout, with the work split over two kinds of waves.
+//
+// Consumer waves hold the head's state, 16 columns each, and do what depends on it:
+//   X = Diag(beta) (V - Diag(lam) K S^T)   E = (I + L)^{-1} X   O = scale (Diag(lam) Q S^T + P E)
+//   S'^T = lam_C S^T + Kt^T Diag(lam_C / lam) E
+// Four producer waves form the operands of the blocks after it: key, query and write-
+// key rows, a channel a lane; their products, a share of the channels a wave.  A step
+// has two barriers; block n's operands are formed in one step, its L and P are
+// summed and it is consumed in the next.
+#include "pdn_device.hpp"
+#include "pdn_internal.hpp"
+#include "pdn_slots.hpp"
+#include "pdn_tile.hpp"
+
+namespace pdn {
+
+namespace {
+
+template <typename T, int DK, int DV, bool CH>
+struct Run {
+  static constexpr int LD = DK + 4, NW = DV / 16, LC = CH ? kSlotBlock : 1;
+  alignas(16) T raw[3][kSlotBlock][DK];              // keys, queries, the caller's write keys
+  alignas(16) float g[LC][LD];                       // CH: log-decays
+  // operands, of the block in use and the one after it: keys over queries; write
+  // keys, with CH decayed to the block's start, and to its end; CH: the decay over it
+  alignas(16) float KQ[2][2 * kSlotBlock][LD], Kt[2][kSlotBlock][LD], Kw[2][LC][LD], lam[2][CH ? DK : 4];
+  alignas(16) float part[4][16][kSlotBlock], LP[16][kSlotBlock + 4], E[NW][kSlotBlock][16], sum[4][kSlotBlock];
+  // of each token: log-decay, the decay to it and from it within the block, write
+  // strength, preconditioner gain and decay
+  alignas(16) float tok[4][6][kSlotBlock];
+};
+
+template <typename T, int DK, int DV, bool CH>
+__global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  using R = Run<T, DK, DV, CH>;
+  constexpr int B = kSlotBlock, NW = R::NW, MB = DK / 16;
+  __shared__ R s;
+  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
+  if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
+  const SlotRows rows = slot_rows(a, seq);
+  const bool fresh = a.fresh && a.fresh[seq] != 0;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
+  const int nb = static_cast<int>((rows.n + B - 1) / B);
+  const bool sums = slot_needs_sum(a);
+  // a block's rows as a buffer: past the sequence's end zeros, without rows no bytes
+  auto view = [&](int blk, const void* p, int64_t stride, int64_t first, int width, int esz, bool there) {
+    const int64_t t0 = static_cast<int64_t>(blk) * B, n = min(rows.n - t0, (int64_t)B);
+    return buf_rsrc(static_cast<const char*>(p) + ((rows.lo + t0) * stride + first) * esz,
+                    there && n > 0 ? static_cast<uint32_t>(((n - 1) * stride + width) * esz) : 0);
+  };
+
+  if (w < NW) {
+    // ------------------------------------------------------------ consumers
+    const int v0 = 16 * w + lr, tb = 4 * (lg & 1), at = 4 * lg * DV + v0;
+    SlotColumns<DK, DV> S;
+    if (fresh) S.zero();
+    else S.load(slot_head<DK, DV>(a, src, h), at);
+    float vn[4];
+    auto load_v = [&](int blk) {
+      const __amdgpu_buffer_rsrc_t r = view(blk, a.v, a.v_stride, h * DV, DV, sizeof(T), true);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vn[i] = buf_get<T>(r, (tb + i) * static_cast<uint32_t>(a.v_stride * sizeof(T)) + v0 * sizeof(T));
+    };
+    if (nb > 0) {
+      load_v(0);
+      lds_sync();
+    }
+    for (int it = 0; it <= nb && nb > 0; ++it) {
+      const int blk = it - 1, u = blk & 1;
+      if (sums) lds_sync();
+      floatx4 yz = {0.f, 0.f, 0.f, 0.f}, yz1 = yz;
+      if (blk >= 0) {
+        // ---- (rows of K over rows of Q) times S^T
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          const floatx4 r4 = *reinterpret_cast<const floatx4*>(&s.KQ[u][lr][16 * m + 4 * lg]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mma4(i & 1 ? yz1 : yz, r4[i], S.t[m][i]);
+        }
+        settled(yz, yz1);
+        yz += yz1;
+      }
+      lds_sync();   // A
+      if (blk >= 0) {
+        const int64_t t0 = static_cast<int64_t>(blk) * B;
+        const int nt = static_cast<int>(min<int64_t>(B, rows.n - t0));
+        const float(*tok)[B] = s.tok[blk & 3];
+        // ---- E: tokens 0-3 in the first 16 lanes, 4-7 in the next
+        floatx4 ld[4], lx[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          ld[i] = *reinterpret_cast<const floatx4*>(&s.LP[tb + i][tb]);
+          lx[i] = *reinterpret_cast<const floatx4*>(&s.LP[4 + i][0]);
+        }
+        const floatx4 be = *reinterpret_cast<const floatx4*>(&tok[3][tb]), lam = *reinterpret_cast<const floatx4*>(&tok[1][tb]),
+                      wt = *reinterpret_cast<const floatx4*>(&tok[2][tb]);
+        floatx4 p4 = *reinterpret_cast<const floatx4*>(&s.LP[lr][tb]);
+        const float lc = tok[1][B - 1];
+        reads_done();
+        floatx4 x;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = be[i] * (vn[i] - lam[i] * yz[i]);
+        yz *= lam;
+        load_v(it);
+        floatx4 e = slot_solve4(ld, x);
+        {
+          floatx4 f;   // e of tokens 0-3
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = __shfl(e[j], lr, 64);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] -= (lx[i][0] * f[0] + lx[i][1] * f[1]) + (lx[i][2] * f[2] + lx[i][3] * f[3]);
+          x = slot_solve4(ld, x);
+          if (lg == 1) e = x;
+        }
+        if (lg >= 2) e = floatx4{0.f, 0.f, 0.f, 0.f};
+        if (lg < 2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s.E[w][tb + i][lr] = wt[i] * e[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        // ---- the state after the block
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          floatx4 f = {lc, lc, lc, lc};
+          if (CH) f = *reinterpret_cast<const floatx4*>(&s.lam[u][16 * m + 4 * lg]);
+          S.t[m] *= f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const float ej = s.E[w][4 * j + lg][lr];
+#pragma unroll
+          for (int m = 0; m < MB; ++m) mma4(S.t[m], (CH ? s.Kw[u] : s.Kt[u])[4 * j + lg][16 * m + lr], ej);
+        }
+        settled(S.t);
+        // ---- O: rows 8-15 of the products, plus P E
+        if (lr < B || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+        settled(yz);
+        T* ob = static_cast<T*>(a.o) + (rows.lo + t0) * a.H * DV + h * DV + v0;
+        if (lg >= 2)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (tb + i < nt) ob[(tb + i) * a.H * DV] = from_f<T>(a.scale * yz[i]);
+      }
+      lds_sync();   // B
+    }
+    S.store(slot_head<DK, DV>(a, dst, h), at);
+  } else {
+    // ------------------------------------------------------------ producers
+    const int pw = w - NW, pt = pw * 64 + l, c = pt % DK;
+    const bool key = pt < DK, qry = !key && pt < 2 * DK;
+    const int prec = a.precond;
+    const bool gram = has_gram(prec), both = prec == kATQ, scalar = a.gate == kGateScalar;
+    const float mu = prec == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f;
+    const float *const gb = scalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
+                *const gpb = gram && a.g_p ? a.g_p : a.beta;
+    float A = gram && !fresh ? a.A[(src * a.H + h) * DK + c] : 0.f;   // (query threads follow it too)
+    constexpr int RP = B * DK * sizeof(T) / 16, NRP = (RP + 255) / 256, GP = B * DK * 4 / 16, NGP = (GP + 255) / 256;
+    u32x4 rk[NRP], rq[NRP], rx[NRP], rg[NGP];
+    float s_b, s_g, s_bp, s_gp;
+    auto load_rows = [&](int blk) {
+      const __amdgpu_buffer_rsrc_t vk = view(blk, a.k, a.k_stride, hk * DK, DK, sizeof(T), true),
+                                   vq = view(blk, a.q, a.q_stride, hk * DK, DK, sizeof(T), true),
+                                   vx = view(blk, a.ktilde, a.Hk * DK, hk * DK, DK, sizeof(T), prec == kExternal);
+      auto piece = [&](__amdgpu_buffer_rsrc_t r, int64_t stride, int row_bytes, int esz, int x) {
+        const uint32_t at = x * 256 + pt, t = at * 16 / row_bytes, o = at * 16 % row_bytes;
+        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                             r, static_cast<int>(t * static_cast<uint32_t>(stride * esz) + o), 0, 0));
+      };
+#pragma unroll
+      for (int x = 0; x < NRP; ++x) {
+        rk[x] = piece(vk, a.k_stride, DK * sizeof(T), sizeof(T), x);
+        rq[x] = piece(vq, a.q_stride, DK * sizeof(T), sizeof(T), x);
+        rx[x] = piece(vx, a.Hk * DK, DK * sizeof(T), sizeof(T), x);
+      }
+      if (CH) {
+        const __amdgpu_buffer_rsrc_t vg = view(blk, a.g, a.H * DK, h * DK, DK, 4, true);
+#pragma unroll
+        for (int x = 0; x < NGP; ++x) rg[x] = piece(vg, a.H * DK, DK * 4, 4, x);
+      }
+      // (each read whether it is used or not: a branch would wait for the loads)
+      const int64_t sc = (rows.lo + min(static_cast<int64_t>(blk) * B + (l & 7), rows.n - 1)) * a.H + h;
+      s_b = a.beta[sc];
+      s_g = gb[sc];
+      s_bp = bpb[sc];
+      s_gp = gpb[sc];
+    };
+    auto put_rows = [&](int blk) {
+      auto put = [&](void* p, const u32x4& v, int x, int pieces, int row_bytes, int ld_bytes) {
+        const int at = x * 256 + pt;
+        if (at < pieces)
+          *reinterpret_cast<u32x4*>(static_cast<char*>(p) + at * 16 / row_bytes * ld_bytes + at * 16 % row_bytes) = v;
+      };
+#pragma unroll
+      for (int x = 0; x < NRP; ++x) {
+        put(s.raw[0], rk[x], x, RP, DK * sizeof(T), DK * sizeof(T));
+        put(s.raw[1], rq[x], x, RP, DK * sizeof(T), DK * sizeof(T));
+        put(s.raw[2], rx[x], x, RP, DK * sizeof(T), DK * sizeof(T));
+      }
+      if (CH)
+#pragma unroll
+        for (int x = 0; x < NGP; ++x) put(s.g, rg[x], x, GP, DK * 4, R::LD * 4);
+      if (pw == 3) {
+        const int t = l & 7;
+        const bool in = static_cast<int64_t>(blk) * B + t < rows.n;
+        const float g = in && scalar ? s_g : 0.f, nx = __shfl_down(g, 1, B);
+        float to = g, on = t + 1 < B ? nx : 0.f;
+#pragma unroll
+        for (int off = 1; off < B; off <<= 1) {
+          const float y = __shfl_up(to, off, B), z = __shfl_down(on, off, B);
+          if (t >= off) to += y;
+          if (t + off < B) on += z;
+        }
+        if (l < B) {
+          float(*tok)[B] = s.tok[blk & 3];
+          tok[0][t] = g;
+          tok[1][t] = fast_exp(to);
+          tok[2][t] = fast_exp(on);
+          tok[3][t] = in ? s_b : 0.f;
+          tok[4][t] = in && gram ? s_bp : 0.f;
+          tok[5][t] = in && gram && a.g_p ? fast_exp(s_gp) : 1.f;
+        }
+      }
+    };
+    // key, query and write-key rows
+    auto put_operands = [&](int blk) {
+      const int u = blk & 1;
+      const float(*tok)[B] = s.tok[blk & 3];
+      const int nt = static_cast<int>(min<int64_t>(B, rows.n - static_cast<int64_t>(blk) * B));
+      float kt[B], kv[B], At[B], to[B], G = 0.f;
+      const float Ab = A;
+#pragma unroll
+      for (int t = 0; t < B; ++t) {
+        kv[t] = to_f(s.raw[0][t][c]);
+        if (CH) {
+          G += s.g[t][c];
+          to[t] = G;
+        }
+      }
+      if (gram)   // (a token past the end leaves A: no gain, no decay)
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          A = tok[5][t] * A + tok[4][t] * kv[t] * kv[t];
+          At[t] = A;
+        }
+      if (qry)
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          float q = to_f(s.raw[1][t][c]);
+          if (both) q /= At[t] + a.ridge;
+          s.KQ[u][B + t][c] = CH ? fast_exp(to[t]) * q : q;
+        }
+      if (key) {
+        if (prec == kSquash) {
+#pragma unroll
+          for (int t = 0; t < B; ++t) kt[t] = squash_gain(At[t], mu, a.lnx) * kv[t];
+        } else if (prec == kDiagSM) {
+#pragma unroll
+          for (int t = 0; t < B; ++t) kt[t] = kv[t] / ((t ? At[t - 1] : Ab) + a.ridge);
+        } else {
+#pragma unroll
+          for (int t = 0; t < B; ++t) kt[t] = prec == kExternal ? to_f(s.raw[2][t][c]) : kv[t];
+        }
+      }
+      if (sums) {   // the write key's row sums
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          float x = key ? kv[t] * kt[t] : 0.f;
+#pragma unroll
+          for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
+          if (l == 0) s.sum[pw][t] = x;
+        }
+        lds_sync();
+        if (key)
+#pragma unroll
+          for (int t = 0; t < B; ++t) {
+            float m = 0.f;
+#pragma unroll
+            for (int i = 0; i < DK / 64; ++i) m += s.sum[i][t];
+            kt[t] = t < nt ? slot_sum_factor(a, m, tok[3][t], tok[0][t]) * kt[t] : 0.f;
+          }
+      }
+      if (key)
+#pragma unroll
+        for (int t = 0; t < B; ++t) {
+          // (a linear-attention update has no correction by the state: no key rows)
+          s.KQ[u][t][c] = both ? 0.f : CH ? fast_exp(to[t]) * kv[t] : kv[t];
+          s.Kt[u][t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
+          if (CH) s.Kw[u][t][c] = kt[t] * fast_exp(G - to[t]);
+        }
+      if (CH && key) s.lam[u][c] = fast_exp(G);
+    };
+    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave
+    auto put_products = [&](int blk) {
+      const int u = blk & 1;
+      floatx4 g4 = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < MB / 4; ++x) {
+        const int m = 4 * x + pw;
+        const floatx4 r4 = *reinterpret_cast<const floatx4*>(&s.KQ[u][lr][16 * m + 4 * lg]);
+        const floatx4 t4 = *reinterpret_cast<const floatx4*>(&s.Kt[u][lr & 7][16 * m + 4 * lg]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
+      }
+      settled(g4);
+      if (lr < B)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s.part[pw][4 * lg + i][lr] = g4[i];
+    };
+    auto put_lp = [&](int blk) {   // (by the last two waves, which have no write keys to form)
+      const int r = (pt - 128) / B, x = pt % B, t = r % B;
+      const float(*tok)[B] = s.tok[blk & 3];
+      float v = (s.part[0][r][x] + s.part[1][r][x]) + (s.part[2][r][x] + s.part[3][r][x]);
+      if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
+        float g = 0.f;
+#pragma unroll
+        for (int j = 1; j < B; ++j) g += j > x && j <= t ? tok[0][j] : 0.f;
+        v *= fast_exp(g);
+      }
+      s.LP[r][x] = r < B ? (x < t ? tok[3][t] * v : 0.f) : (x <= t ? v : 0.f);
+    };
+    if (nb > 0) {
+      load_rows(0);
+      put_rows(0);
+      load_rows(1);
+      lds_sync();
+    }
+    for (int it = 0; it <= nb && nb > 0; ++it) {
+      if (it > 0 && pw >= 2) put_lp(it - 1);
+      if (it < nb) put_operands(it);
+      else if (sums) lds_sync();
+      lds_sync();   // A
+      if (it < nb) put_products(it);
+      put_rows(it + 1);
+      load_rows(it + 2);
+      lds_sync();   // B
+    }
+    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+  }
+}
+
+template <typename T, int DK, int DV>
+hipError_t launch_gate(const SlotArgs& a, hipStream_t s) {
+  const dim3 grid(static_cast<unsigned>(a.B * a.H)), threads(DV * 4 + 256);
+  if (a.gate == kGateChannel) hipLaunchKernelGGL((slot_runs<T, DK, DV, true>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((slot_runs<T, DK, DV, false>), grid, threads, 0, s, a);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_dims(const SlotArgs& a, hipStream_t s) {
+  if (a.dk == 64) return a.dv == 64 ? launch_gate<T, 64, 64>(a, s) : launch_gate<T, 64, 128>(a, s);
+  return a.dv == 64 ? launch_gate<T, 128, 64>(a, s) : launch_gate<T, 128, 128>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_slot_runs(const SlotArgs& a, int io_bf16, hipStream_t s) {
+  return io_bf16 ? launch_dims<bf16>(a, s) : launch_dims<float>(a, s);
+}
+
+}  // namespace pdn

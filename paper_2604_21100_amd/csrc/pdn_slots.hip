@@ -37,14 +37,6 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 
-constexpr int kBlk = 8;   // tokens of a block
-
-// A head's state, seen through a buffer: a lane's rows are then one offset and
-// constants, where pointers to them would take two registers each.
-template <int DK, int DV>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t state_head(const SlotArgs& a, int64_t slot, int64_t h) {
-  return buf_rsrc(reinterpret_cast<const char*>(a.S + (slot * a.H + h) * (DK * DV)), DK * DV * 4);
-}
 // a wave's 32 columns of it, two a lane (from element `at` of the head)
 template <int DK, int DV>
 struct Columns2 {
@@ -75,47 +67,12 @@ struct Columns2 {
                                               (16 * m + i) * DV * 4, 0);
   }
 };
-// and 16 columns, one a lane
-template <int DK, int DV>
-struct Columns {
-  static constexpr int MB = DK / 16;
-  floatx4 t[MB];
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int m = 0; m < MB; ++m) t[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at) {
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        t[m][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, 4 * at, (16 * m + i) * DV * 4, 0));
-  }
-  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, int at) const {
-#pragma unroll
-    for (int m = 0; m < MB; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float x = t[m][i];   // (the bits of t[m][i] itself would be those of t[m][0])
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), r, 4 * at, (16 * m + i) * DV * 4, 0);
-      }
-  }
-};
-
-// The write key of a token's channel, its query, and the factor its key row's sum
-// m = k . kt asks for.
+// the write key of a token's channel, but for the factor of slot_sum_factor
 __device__ __forceinline__ float write_key(const SlotArgs& a, float k, float x, float A, float Ap, float mu) {
   if (a.precond == kSquash) return squash_gain(A, mu, a.lnx) * k;
   if (a.precond == kDiagSM) return k / (Ap + a.ridge);
   return a.precond == kExternal ? x : k;
 }
-__device__ __forceinline__ bool needs_sum(const SlotArgs& a) { return a.precond == kDiagSM || a.knorm != kKnormNone; }
-__device__ __forceinline__ float sum_factor(const SlotArgs& a, float m, float beta, float g) {
-  if (a.precond == kDiagSM || a.knorm == kKnorm1pm) return 1.f / (1.f + m);
-  if (a.knorm == kKnormM) return 1.f / m;
-  return beta / ((a.gate == kGateScalar ? fast_exp(g) : 1.f) + beta * m);
-}
-
 // ---------------------------------------------------------------- one token
 //   S' = alpha S + e kt^T,  e = beta (v - (alpha S) k),  o = scale ((alpha S) q + (kt . q) e)
 // on the vector unit; what bounds it is reading and writing the state.
@@ -135,7 +92,7 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
   const int c = tid % DK;
   Columns2<DK, DV> S;
   if (fresh) S.zero();
-  else S.load(state_head<DK, DV>(a, src, h), at);
+  else S.load(slot_head<DK, DV>(a, src, h), at);
   float A = gram && key && !fresh ? a.A[(src * a.H + h) * DK + c] : 0.f;
   if (rows.n > 0) {
     const int64_t row = rows.lo, sc = row * a.H + h;
@@ -148,14 +105,14 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
     if (gram) A = (a.g_p ? fast_exp(a.g_p[sc]) : 1.f) * A + a.beta_p[sc] * kv * kv;
     float kt = write_key(a, kv, xv, A, Ap, a.precond == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f);
     if (both) qv /= A + a.ridge;
-    if (needs_sum(a)) {
+    if (slot_needs_sum(a)) {
       const float x = wave_sum(key ? kv * kt : 0.f);
       if (l == 0) sSum[w] = x;
       __syncthreads();
       float m = 0.f;
 #pragma unroll
       for (int i = 0; i < NW; ++i) m += sSum[i];
-      kt *= sum_factor(a, m, beta, g);
+      kt *= slot_sum_factor(a, m, beta, g);
     }
     if (key) {
       sK[c] = both ? 0.f : kv;   // (a linear-attention update has no correction by the state)
@@ -203,7 +160,7 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
       S.t[m][1] = lam0 * S.t[m][1] + t4 * e[1];
     }
   }
-  S.store(state_head<DK, DV>(a, dst, h), at);
+  S.store(slot_head<DK, DV>(a, dst, h), at);
   if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
 }
 
@@ -216,20 +173,20 @@ template <typename T, int DK, int DV, bool CH, bool DRAFT>
 __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
   constexpr int NTHR = DV * 4, NW = DV / 16, MB = DK / 16, LD = DK + 4;
-  constexpr int RP = kBlk * DK * sizeof(T) / 16, NRP = (RP + NTHR - 1) / NTHR;   // 16-byte pieces of a block's key rows
-  constexpr int GP = kBlk * DK * 4 / 16, NGP = (GP + NTHR - 1) / NTHR;           // of a block's rows of fp32
-  __shared__ __attribute__((aligned(16))) T sRaw[3][kBlk][DK];   // keys, queries, the caller's write keys
-  __shared__ __attribute__((aligned(16))) float sKQ[2 * kBlk][LD], sKt[kBlk][LD];
+  constexpr int RP = kSlotBlock * DK * sizeof(T) / 16, NRP = (RP + NTHR - 1) / NTHR;   // 16-byte pieces of a block's key rows
+  constexpr int GP = kSlotBlock * DK * 4 / 16, NGP = (GP + NTHR - 1) / NTHR;           // of a block's rows of fp32
+  __shared__ __attribute__((aligned(16))) T sRaw[3][kSlotBlock][DK];   // keys, queries, the caller's write keys
+  __shared__ __attribute__((aligned(16))) float sKQ[2 * kSlotBlock][LD], sKt[kSlotBlock][LD];
   // CH: g; the write keys with the decay to the block's end, and as they are.
   // Drafts: the accepted records' write keys; A after each token.
-  __shared__ __attribute__((aligned(16))) float sG[CH ? kBlk : 1][LD], sKw[CH ? kBlk : 1][LD], sKr[CH && DRAFT ? kBlk : 1][LD];
-  __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kBlk : 1][LD], sAt[DRAFT ? kBlk : 1][LD];
-  __shared__ __attribute__((aligned(16))) float sPart[NW][16][kBlk], sLP[16][kBlk + 4], sE[NW][kBlk][16];
-  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kBlk : 1][LD], sSum[NW][kBlk];
+  __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sKr[CH && DRAFT ? kSlotBlock : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kSlotBlock : 1][LD], sAt[DRAFT ? kSlotBlock : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sPart[NW][16][kSlotBlock], sLP[16][kSlotBlock + 4], sE[NW][kSlotBlock][16];
+  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kSlotBlock : 1][LD], sSum[NW][kSlotBlock];
   // of each token: log-decay, its sum from the first token, the decay to and from
   // the token within the block as factors (1 with a per-channel gate), write strength,
   // preconditioner gain and decay
-  __shared__ __attribute__((aligned(16))) float sg[kBlk], sGp[kBlk], sTo[kBlk], sOn[kBlk], sB[kBlk], sBp[kBlk], sDp[kBlk];
+  __shared__ __attribute__((aligned(16))) float sg[kSlotBlock], sGp[kSlotBlock], sTo[kSlotBlock], sOn[kSlotBlock], sB[kSlotBlock], sBp[kSlotBlock], sDp[kSlotBlock];
   const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
@@ -242,10 +199,15 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // together take more registers than there are).
   int tid = threadIdx.x;
   auto anew = [&]() { asm volatile("" : "+v"(tid)); };
-#define IDS                                                                                                    \
-  [[maybe_unused]] const int l = tid & 63, lr = l & 15, lg = l >> 4, tb = 4 * (lg & 1), v0 = 16 * w + lr,       \
-                             c = tid % DK;                                                                     \
-  [[maybe_unused]] const bool key = tid < DK, qry = NTHR >= 2 * DK ? tid / DK == 1 : key
+  struct Place {
+    int l, lr, lg, tb, v0, c;   // c: the channel whose rows a thread forms
+    bool key, qry;              // the key's and write key's, the query's
+  };
+  auto place = [&]() {
+    const int l = tid & 63, lg = l >> 4;
+    const bool key = tid < DK;
+    return Place{l, l & 15, lg, 4 * (lg & 1), 16 * w + (l & 15), tid % DK, key, NTHR >= 2 * DK ? tid / DK == 1 : key};
+  };
   const int64_t R = DK + DV + (CH ? DK : 4) + (gram ? DK : 0), rs = a.H * R;   // a record; from one token's to the next
 
   // ---- A block's rows, from memory into registers, then into LDS.  Rows are seen
@@ -258,8 +220,8 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   const float *const gb = scalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
               *const gpb = gram && a.g_p ? a.g_p : a.beta;
   auto load_rows = [&](int64_t t0) {
-    IDS;
-    const int n = static_cast<int>(min<int64_t>(kBlk, rows.n - t0));
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
+    const int n = static_cast<int>(min<int64_t>(kSlotBlock, rows.n - t0));
     const int64_t row = rows.lo + t0;
     auto view = [&](const void* p, int64_t stride, int64_t first, int width, int esz, bool there) {
       return buf_rsrc(static_cast<const char*>(p) + (row * stride + first) * esz,
@@ -288,13 +250,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int o = (tb + i) * static_cast<uint32_t>(a.v_stride * sizeof(T)) + v0 * sizeof(T);
-      if constexpr (sizeof(T) == 2)
-        vn[i] = __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(vw, o, 0, 0)) << 16);
-      else
-        vn[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(vw, o, 0, 0));
+      vn[i] = buf_get<T>(vw, o);
     }
-    const int64_t sc = (row + min(tid & (kBlk - 1), n - 1)) * a.H + h;
-    const bool in = (tid & (kBlk - 1)) < n;
+    const int64_t sc = (row + min(tid & (kSlotBlock - 1), n - 1)) * a.H + h;
+    const bool in = (tid & (kSlotBlock - 1)) < n;
     const float x_b = a.beta[sc], x_g = gb[sc], x_bp = bpb[sc], x_gp = gpb[sc];
     s_b = in ? x_b : 0.f;
     s_g = in && scalar ? x_g : 0.f;
@@ -319,14 +278,14 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       for (int x = 0; x < NGP; ++x) put(sG, rg[x], x, GP, DK * 4, LD * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) vv[i] = vn[i];
-    if (tid < kBlk) {
-      const float nx = __shfl_down(s_g, 1, kBlk);
-      float to = s_g, on = tid + 1 < kBlk ? nx : 0.f;
+    if (tid < kSlotBlock) {
+      const float nx = __shfl_down(s_g, 1, kSlotBlock);
+      float to = s_g, on = tid + 1 < kSlotBlock ? nx : 0.f;
 #pragma unroll
-      for (int off = 1; off < kBlk; off <<= 1) {
-        const float y = __shfl_up(to, off, kBlk), z = __shfl_down(on, off, kBlk);
+      for (int off = 1; off < kSlotBlock; off <<= 1) {
+        const float y = __shfl_up(to, off, kSlotBlock), z = __shfl_down(on, off, kSlotBlock);
         if (tid >= off) to += y;
-        if (tid + off < kBlk) on += z;
+        if (tid + off < kSlotBlock) on += z;
       }
       sg[tid] = s_g;
       sTo[tid] = fast_exp(to);
@@ -336,7 +295,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       sDp[tid] = fast_exp(s_gp);
       if (!CH) {
         sGp[tid] = gacc + to;
-        gacc += __shfl(to, kBlk - 1, kBlk);
+        gacc += __shfl(to, kSlotBlock - 1, kSlotBlock);
       }
     }
   };
@@ -347,8 +306,8 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   u32x4 ck[NGP], cg[NGP];
   float ce[2];
   auto load_records = [&](int b0) {   // (whether accepted or not; never past the tape)
-    IDS;
-    const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kBlk));
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
+    const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kSlotBlock));
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
       const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
@@ -374,17 +333,17 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   const float* const last = DRAFT ? rec + max(cnt - 1, 0) * rs : nullptr;
 
   // ---- the state
-  Columns<DK, DV> S;
+  SlotColumns<DK, DV> S;
   float A = 0.f;
   {
-    IDS;
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     if (fresh) S.zero();
-    else S.load(state_head<DK, DV>(a, src, h), 4 * lg * DV + v0);
+    else S.load(slot_head<DK, DV>(a, src, h), 4 * lg * DV + v0);
     if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
   }
   auto store_state = [&](float A) {
-    IDS;
-    S.store(state_head<DK, DV>(a, dst, h), 4 * lg * DV + v0);
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
+    S.store(slot_head<DK, DV>(a, dst, h), 4 * lg * DV + v0);
     if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
   };
   const float A0 = A;
@@ -392,12 +351,12 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 
   // ---- a block's operands: key, query and write-key rows, L and P
   auto operands = [&](int nt) {
-    IDS;
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     {
-      float kt[kBlk], kv[kBlk], G = 0.f, to[kBlk], At[kBlk];
+      float kt[kSlotBlock], kv[kSlotBlock], G = 0.f, to[kSlotBlock], At[kSlotBlock];
       const float Ab = A;   // before the block
 #pragma unroll
-      for (int t = 0; t < kBlk; ++t) {
+      for (int t = 0; t < kSlotBlock; ++t) {
         kv[t] = to_f(sRaw[0][t][c]);
         if (CH) {
           G += sG[t][c];
@@ -406,49 +365,49 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       }
       if (gram) {   // (a token past the end leaves A: no gain, no decay)
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) {
+        for (int t = 0; t < kSlotBlock; ++t) {
           A = sDp[t] * A + sBp[t] * kv[t] * kv[t];
           At[t] = A;
         }
         if (DRAFT && key)
 #pragma unroll
-          for (int t = 0; t < kBlk; ++t) sAt[t][c] = At[t];
+          for (int t = 0; t < kSlotBlock; ++t) sAt[t][c] = At[t];
       }
       if (prec == kSquash) {
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) kt[t] = squash_gain(At[t], mu, a.lnx) * kv[t];
+        for (int t = 0; t < kSlotBlock; ++t) kt[t] = squash_gain(At[t], mu, a.lnx) * kv[t];
       } else if (prec == kDiagSM) {
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) kt[t] = kv[t] / ((t ? At[t - 1] : Ab) + a.ridge);
+        for (int t = 0; t < kSlotBlock; ++t) kt[t] = kv[t] / ((t ? At[t - 1] : Ab) + a.ridge);
       } else {
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) kt[t] = prec == kExternal ? to_f(sRaw[2][t][c]) : kv[t];
+        for (int t = 0; t < kSlotBlock; ++t) kt[t] = prec == kExternal ? to_f(sRaw[2][t][c]) : kv[t];
       }
       if (both ? key : qry)
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) {
+        for (int t = 0; t < kSlotBlock; ++t) {
           float q = to_f(sRaw[1][t][c]);
           if (both) q /= At[t] + a.ridge;
-          sKQ[kBlk + t][c] = CH ? fast_exp(to[t]) * q : q;
+          sKQ[kSlotBlock + t][c] = CH ? fast_exp(to[t]) * q : q;
         }
-      if (needs_sum(a)) {   // the write key's row sums
+      if (slot_needs_sum(a)) {   // the write key's row sums
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) {
+        for (int t = 0; t < kSlotBlock; ++t) {
           const float x = wave_sum(key ? kv[t] * kt[t] : 0.f);
           if (l == 0) sSum[w][t] = x;
         }
         __syncthreads();
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) {
+        for (int t = 0; t < kSlotBlock; ++t) {
           float m = 0.f;
 #pragma unroll
           for (int i = 0; i < NW; ++i) m += sSum[i][t];
-          kt[t] = t < nt ? sum_factor(a, m, sB[t], sg[t]) * kt[t] : 0.f;
+          kt[t] = t < nt ? slot_sum_factor(a, m, sB[t], sg[t]) * kt[t] : 0.f;
         }
       }
       if (key)
 #pragma unroll
-        for (int t = 0; t < kBlk; ++t) {
+        for (int t = 0; t < kSlotBlock; ++t) {
           // (a linear-attention update has no correction by the state: no key rows)
           sKQ[t][c] = both ? 0.f : CH ? fast_exp(to[t]) * kv[t] : kv[t];
           sKt[t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
@@ -477,22 +436,23 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
     }
-    if (lr < kBlk)
+    settled(g4);
+    if (lr < kSlotBlock)
 #pragma unroll
       for (int i = 0; i < 4; ++i) sPart[w][4 * lg + i][lr] = g4[i];
     __syncthreads();
-    if (tid < 16 * kBlk) {
-      const int r = tid / kBlk, s = tid % kBlk, t = r % kBlk;
+    if (tid < 16 * kSlotBlock) {
+      const int r = tid / kSlotBlock, s = tid % kSlotBlock, t = r % kSlotBlock;
       float x = 0.f;
 #pragma unroll
       for (int i = 0; i < NW; ++i) x += sPart[i][r][s];
       if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
         float g = 0.f;
 #pragma unroll
-        for (int j = 1; j < kBlk; ++j) g += j > s && j <= t ? sg[j] : 0.f;
+        for (int j = 1; j < kSlotBlock; ++j) g += j > s && j <= t ? sg[j] : 0.f;
         x *= fast_exp(g);
       }
-      sLP[r][s] = r < kBlk ? (s < t ? sB[t] * x : 0.f) : (s <= t ? x : 0.f);
+      sLP[r][s] = r < kSlotBlock ? (s < t ? sB[t] * x : 0.f) : (s <= t ? x : 0.f);
     }
     __syncthreads();
   };
@@ -500,7 +460,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // ---- the accepted records' operand: write keys with their decay to the last
   const float Gn = DRAFT && !CH && cnt > 0 ? last[DK + DV] : 0.f;
   auto put_records = [&](int b0) {
-    IDS;
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
       const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
@@ -525,7 +485,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       if (b0 + 4 * j + lg >= cnt) ce[j] = 0.f;
   };
   auto apply_records = [&](int b0) {
-    IDS;
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (b0 + 4 * j >= cnt) break;
@@ -535,24 +495,25 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
         mma4(S.t[m], x, ce[j]);
       }
     }
+    settled(S.t);
   };
 
   // (drafts come here without tokens too: their accepted records are applied in the first round)
-  for (int64_t t0 = 0; t0 < rows.n || (DRAFT && t0 == 0); t0 += kBlk) {
-    const int nt = static_cast<int>(max(min<int64_t>(kBlk, rows.n - t0), (int64_t)0));
+  for (int64_t t0 = 0; t0 < rows.n || (DRAFT && t0 == 0); t0 += kSlotBlock) {
+    const int nt = static_cast<int>(max(min<int64_t>(kSlotBlock, rows.n - t0), (int64_t)0));
     const int64_t row0 = rows.lo + t0;
     anew();
     if (nt > 0) put_rows();
     if (DRAFT && t0 == 0 && cnt > 0) put_records(0);
     __syncthreads();
     anew();
-    if (rows.n > t0 + kBlk) load_rows(t0 + kBlk);
+    if (rows.n > t0 + kSlotBlock) load_rows(t0 + kSlotBlock);
     anew();
     if (nt > 0) operands(nt);
     anew();
     if (DRAFT && t0 == 0) {
       if (cnt > 0) {
-        IDS;
+        [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
           floatx4 lam;
@@ -566,7 +527,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           S.t[m] *= lam;
         }
         apply_records(0);
-        for (int b0 = kBlk; b0 < cnt; b0 += kBlk) {
+        for (int b0 = kSlotBlock; b0 < cnt; b0 += kSlotBlock) {
           load_records(b0);
           __syncthreads();
           put_records(b0);
@@ -582,7 +543,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       if (nt == 0) break;
     }
     anew();
-    IDS;
+    [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     T* const ob = static_cast<T*>(a.o) + h * DV + v0;
     if (DRAFT) {   // the records, but for e
       float* r0 = a.tape + ((dst * a.tape_tokens + t0) * a.H + h) * R;
@@ -603,6 +564,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma4(i & 1 ? yz1 : yz, r4[i], S.t[m][i]);
     }
+    settled(yz, yz1);
     yz += yz1;
     // ---- E: tokens 0-3 in the first 16 lanes, 4-7 in the next
     floatx4 e;
@@ -615,13 +577,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = be[i] * (vv[i] - lam[i] * yz[i]);
       yz *= lam;
-      auto solve = [&](floatx4 y) {
-        y[1] -= ld[1][0] * y[0];
-        y[2] -= ld[2][0] * y[0] + ld[2][1] * y[1];
-        y[3] -= ld[3][0] * y[0] + ld[3][1] * y[1] + ld[3][2] * y[2];
-        return y;
-      };
-      e = solve(x);
+      e = slot_solve4(ld, x);
       if (nt > 4) {
         floatx4 f;   // e of tokens 0-3
 #pragma unroll
@@ -631,7 +587,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           const floatx4 lx = *reinterpret_cast<const floatx4*>(&sLP[4 + i][0]);
           x[i] -= (lx[0] * f[0] + lx[1] * f[1]) + (lx[2] * f[2] + lx[3] * f[3]);
         }
-        x = solve(x);
+        x = slot_solve4(ld, x);
         if (lg == 1) e = x;
       }
       if (lg >= 2) e = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -639,9 +595,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     // ---- O: rows 8-15 of the products, plus P E
     {
       floatx4 p4 = *reinterpret_cast<const floatx4*>(&sLP[lr][tb]);
-      if (lr < kBlk || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
+      if (lr < kSlotBlock || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+      settled(yz);
       if (lg >= 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -653,14 +610,14 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
         if (tb + i < nt)
           a.tape[((dst * a.tape_tokens + t0 + tb + i) * a.H + h) * R + DK + v0] = e[i];
     // ---- the state after the block (drafts: only for the block after it)
-    if (!DRAFT || t0 + kBlk < rows.n) {
+    if (!DRAFT || t0 + kSlotBlock < rows.n) {
       const floatx4 wt = *reinterpret_cast<const floatx4*>(&sOn[tb]);
       if (lg < 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) sE[w][tb + i][lr] = wt[i] * e[i];
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      const float lc = sTo[kBlk - 1];
+      const float lc = sTo[kSlotBlock - 1];
 #pragma unroll
       for (int m = 0; m < MB; ++m) {
         floatx4 f = {lc, lc, lc, lc};
@@ -677,6 +634,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           mma4(S.t[m], x, ej);
         }
       }
+      settled(S.t);
     }
     __syncthreads();
   }
@@ -684,7 +642,6 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     store_state(A);
   }
 }
-#undef IDS
 
 template <typename T, int DK, int DV, bool CH>
 hipError_t launch_form(const SlotArgs& a, hipStream_t s) {
@@ -711,6 +668,7 @@ hipError_t launch_dims(const SlotArgs& a, hipStream_t s) {
 hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s) {
   if (a.B * a.H == 0) return hipSuccess;
   if (slot_chunk_form(a, io_bf16)) return launch_slot_chunks(a, s);
+  if (a.T > kSlotBlock && !a.tape) return launch_slot_runs(a, io_bf16, s);
   return io_bf16 ? launch_dims<bf16>(a, s) : launch_dims<float>(a, s);
 }
 

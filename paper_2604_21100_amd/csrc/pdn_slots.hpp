@@ -3,6 +3,7 @@
 
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
+#include "pdn_tile.hpp"
 
 namespace pdn {
 
@@ -37,6 +38,81 @@ __device__ __forceinline__ SlotRows slot_rows(const SlotArgs& a, int64_t seq) {
   lo = min(max(lo, (int64_t)0), a.tokens);
   hi = min(min(hi, a.tokens), lo + a.T);
   return SlotRows{lo, max(hi - lo, (int64_t)0)};
+}
+
+constexpr int kSlotBlock = 8;   // tokens of a block
+
+// A head's state, seen through a buffer: a lane's rows are then one offset and
+// constants, where pointers to them would take two registers each.
+template <int DK, int DV>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t slot_head(const SlotArgs& a, int64_t slot, int64_t h) {
+  return buf_rsrc(reinterpret_cast<const char*>(a.S + (slot * a.H + h) * (DK * DV)), DK * DV * 4);
+}
+// a wave's 16 columns of it, one a lane (from element `at` of the head)
+template <int DK, int DV>
+struct SlotColumns {
+  static constexpr int MB = DK / 16;
+  floatx4 t[MB];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int m = 0; m < MB; ++m) t[m] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, int at) {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        t[m][i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, 4 * at, (16 * m + i) * DV * 4, 0));
+  }
+  __device__ __forceinline__ void store(__amdgpu_buffer_rsrc_t r, int at) const {
+#pragma unroll
+    for (int m = 0; m < MB; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = t[m][i];   // (the bits of t[m][i] itself would be those of t[m][0])
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), r, 4 * at, (16 * m + i) * DV * 4, 0);
+      }
+  }
+};
+// A matrix product's result may be read ten or eleven issue slots after it at the
+// earliest.  The compiler counts them, but has been seen to count along one side of a
+// branch only and to read the last of a result's registers too early on the other.
+// Where code that branches follows a product, its results go through here.
+__device__ __forceinline__ void settled(floatx4& a) { asm volatile("s_nop 7\n\ts_nop 7" : "+v"(a)); }
+__device__ __forceinline__ void settled(floatx4& a, floatx4& b) {
+  asm volatile("s_nop 7\n\ts_nop 7" : "+v"(a), "+v"(b));
+}
+template <int N>
+__device__ __forceinline__ void settled(floatx4 (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += 4)
+    asm volatile("s_nop 7\n\ts_nop 7" : "+v"(t[i]), "+v"(t[i + 1]), "+v"(t[i + 2]), "+v"(t[i + 3]));
+}
+// one element of a buffer, as fp32
+template <typename T>
+__device__ __forceinline__ float buf_get(__amdgpu_buffer_rsrc_t r, int off) {
+  if constexpr (sizeof(T) == 2)
+    return __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0)) << 16);
+  else
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+}
+
+// whether a write key takes a factor that the sum m = k . kt gives, and that factor
+__device__ __forceinline__ bool slot_needs_sum(const SlotArgs& a) {
+  return a.precond == kDiagSM || a.knorm != kKnormNone;
+}
+__device__ __forceinline__ float slot_sum_factor(const SlotArgs& a, float m, float beta, float g) {
+  if (a.precond == kDiagSM || a.knorm == kKnorm1pm) return 1.f / (1.f + m);
+  if (a.knorm == kKnormM) return 1.f / m;
+  return beta / ((a.gate == kGateScalar ? fast_exp(g) : 1.f) + beta * m);
+}
+
+// (I + L)^{-1} y for four rows, L's rows in l
+__device__ __forceinline__ floatx4 slot_solve4(const floatx4 (&l)[4], floatx4 y) {
+  y[1] -= l[1][0] * y[0];
+  y[2] -= l[2][0] * y[0] + l[2][1] * y[1];
+  y[3] -= l[3][0] * y[0] + l[3][1] * y[1] + l[3][2] * y[2];
+  return y;
 }
 
 }  // namespace pdn

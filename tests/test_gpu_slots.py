@@ -105,6 +105,17 @@ CASES = [
     ("bf16", "scalar", "squash", "m", 2, 2, 64, 128, [66]),
     ("bf16", "channel", "identity", "none", 6, 2, 64, 64, [100, 7, 200]),
     ("bf16", "scalar", "external", "none", 4, 2, 64, 128, [100, 7, 200]),
+    # whole blocks of eight, and one token past them
+    ("f32", "scalar", "squash", "none", 2, 2, 128, 128, [16, 24, 32, 40]),
+    ("f32", "channel", "identity", "none", 2, 1, 128, 128, [17, 25, 8, 41]),
+    ("f32", "none", "atq", "none", 2, 2, 128, 128, [24, 9]),
+    ("f32", "channel", "atq", "none", 2, 2, 128, 128, [33, 16]),
+    ("f32", "scalar", "squash", "beta", 2, 1, 64, 128, [32, 15]),
+    ("f32", "channel", "diag_sm", "none", 2, 2, 128, 64, [48, 1, 0, 31]),
+    ("bf16", "channel", "squash", "none", 4, 2, 128, 128, [16, 24, 32, 40]),
+    # the split products' 32: whole chunks, one short, one past
+    ("bf16", "scalar", "squash", "none", 2, 2, 128, 128, [32, 64, 96]),
+    ("bf16", "scalar", "identity", "none", 2, 2, 64, 64, [95, 97, 31]),
 ]
 
 
