@@ -486,6 +486,15 @@ def _token_rows(name, t, device, dtype, shape):
     return t.data_ptr(), s0
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor, of `stream`'s memory where one is named: what is freed while
+    a call runs goes to that stream's next tensors, not to another's."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _call_on(device, stream, fn, *args):
     """fn(*args, stream) with `device` current."""
     if stream is None:
@@ -526,7 +535,7 @@ def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
     kp, ks = _token_rows("k", k, dev, dt, (M, Hk, dk))
     vp, vs = _token_rows("v", v, dev, dt, (M, H, dv))
     if o is None:
-        o = torch.empty((M, H, dv), dtype=dt, device=dev)
+        o = _empty((M, H, dv), dt, dev, stream)
     scalars, seqs = (M, H), (N,)
     inp = Inputs(qp, kp, vp, _on("beta", beta, dev, f32, scalars),
                  _on("g", g, dev, f32, (M, H, dk) if gate == "channel" else scalars),
@@ -628,12 +637,12 @@ def pdn_draft_verify(p, ids, u, r, *, q=None, starts=None, accepted=None,
         raise ValueError(f"p is on {dev}")
     io = PDN_BF16 if _io_of(p) == "bf16" else PDN_F32
     if accepted is None:
-        accepted = torch.empty(N, dtype=i32, device=dev)
+        accepted = _empty((N,), i32, dev, stream)
     if token is None:
-        token = torch.empty(N, dtype=i32, device=dev)
+        token = _empty((N,), i32, dev, stream)
     if workspace is None:
-        workspace = torch.empty(pdn_draft_verify_workspace_size(N, V),
-                                dtype=torch.uint8, device=dev)
+        workspace = _empty((pdn_draft_verify_workspace_size(N, V),),
+                           torch.uint8, dev, stream)
     rows, seqs = (M,), (N,)
     st = _call_on(
         dev, stream, _lib.pdn_draft_verify, N, M, V, io, _on("p", p, dev, p.dtype, p.shape),

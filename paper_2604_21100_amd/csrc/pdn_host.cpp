@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <array>
 #include <cmath>
 #include <cstdint>
 #include <vector>
@@ -96,7 +97,9 @@ struct Buf {
 
 // outputs must not overlap inputs, each other or the workspace; the workspace
 // must not overlap inputs
-pdn_status check_aliasing(const std::vector<Buf>& ins, const std::vector<Buf>& outs, Buf ws) {
+// (Bufs: a vector or an array)
+template <typename Ins, typename Outs>
+pdn_status check_aliasing(const Ins& ins, const Outs& outs, Buf ws) {
   for (size_t i = 0; i < outs.size(); ++i) {
     if (!outs[i].p || outs[i].bytes == 0) continue;
     const Range ro = rng(outs[i].p, outs[i].bytes);
@@ -183,8 +186,9 @@ pdn_status check_slots(const pdn_problem* p, const pdn_slots* s, bool draft, Slo
   if (s->tokens < 0 || s->slots < 0 || s->Hk < 0) return PDN_ERR_SHAPE;
   const int64_t Hk = s->Hk ? s->Hk : p->H;
   if (p->H > 0 && p->H % Hk != 0) return PDN_ERR_SHAPE;
-  // row numbers and slots are 32-bit on the device; one workgroup a head
-  if (s->tokens > INT32_MAX || s->slots > INT32_MAX || unused.BH >= (int64_t)1 << 24) return PDN_ERR_SHAPE;
+  // row numbers and slots are 32-bit on the device; one workgroup of at most 768
+  // work items a head, of which a launch holds fewer than 2^32
+  if (s->tokens > INT32_MAX || s->slots > INT32_MAX || unused.BH >= (int64_t)1 << 22) return PDN_ERR_SHAPE;
   int64_t even;
   if (!s->starts && (!mul_ok(p->B, p->T, &even) || even != s->tokens)) return PDN_ERR_SHAPE;
   if (!s->slot && p->B > s->slots) return PDN_ERR_SHAPE;
@@ -248,22 +252,20 @@ pdn_status slot_call(const pdn_problem* p, const pdn_inputs* in, const pdn_slots
   if (in->S0 || in->A0) return PDN_ERR_VALUE;
   if (!gram && s->A) return PDN_ERR_VALUE;
   if (!draft && (s->tape || s->pending || s->accepted)) return PDN_ERR_VALUE;
-  std::vector<Buf> ins = {{in->q, z.nq}, {in->k, z.nk}, {in->v, z.nv}, {in->beta, z.nscal}, {in->g, z.ngate}};
-  if (gram) {
-    ins.push_back({in->beta_p, z.nscal});
-    ins.push_back({in->g_p, z.nscal});
-  }
-  if (p->precond == PDN_PRECOND_SQUASH) ins.push_back({in->log_a_scale, p->H * 4});
-  if (p->precond == PDN_PRECOND_EXTERNAL) ins.push_back({in->ktilde, z.nx});
-  const std::vector<Buf> lists = {{s->starts, (p->B + 1) * 4}, {s->slot, z.nseq}, {s->slot_out, z.nseq},
-                                  {s->fresh, z.nseq}, {s->accepted, z.nseq}};
-  const std::vector<Buf> outs = {{o, z.no}, {s->S, z.nS}, {s->A, z.nA}, {s->tape, z.ntape}, {s->pending, z.npend}};
-  for (const std::vector<Buf>& v : {ins, outs})
-    for (const Buf& x : v)
-      if (x.p && !aligned16(x.p)) return PDN_ERR_ALIGN;
-  for (const Buf& x : lists)
-    if (x.p && (reinterpret_cast<uintptr_t>(x.p) & 3u)) return PDN_ERR_ALIGN;
-  ins.insert(ins.end(), lists.begin(), lists.end());
+  const Buf none{nullptr, 0};   // (what a mode does not read is not looked at)
+  constexpr size_t kTensors = 9;
+  const std::array<Buf, kTensors + 5> ins = {{
+      {in->q, z.nq}, {in->k, z.nk}, {in->v, z.nv}, {in->beta, z.nscal}, {in->g, z.ngate},
+      gram ? Buf{in->beta_p, z.nscal} : none, gram ? Buf{in->g_p, z.nscal} : none,
+      p->precond == PDN_PRECOND_SQUASH ? Buf{in->log_a_scale, p->H * 4} : none,
+      p->precond == PDN_PRECOND_EXTERNAL ? Buf{in->ktilde, z.nx} : none,
+      // lists
+      {s->starts, (p->B + 1) * 4}, {s->slot, z.nseq}, {s->slot_out, z.nseq}, {s->fresh, z.nseq}, {s->accepted, z.nseq}}};
+  const std::array<Buf, 5> outs = {{{o, z.no}, {s->S, z.nS}, {s->A, z.nA}, {s->tape, z.ntape}, {s->pending, z.npend}}};
+  for (size_t i = 0; i < ins.size(); ++i)
+    if (ins[i].p && (reinterpret_cast<uintptr_t>(ins[i].p) & (i < kTensors ? 15u : 3u))) return PDN_ERR_ALIGN;
+  for (const Buf& x : outs)
+    if (x.p && !aligned16(x.p)) return PDN_ERR_ALIGN;
   if ((st = check_aliasing(ins, outs, Buf{nullptr, 0})) != PDN_OK) return st;
   if (!work) return PDN_OK;
 
@@ -612,7 +614,8 @@ static pdn_status check_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dty
   // ids and row numbers are 32-bit; a workgroup a segment and sequence
   int64_t blocks, bytes;
   if (N > INT32_MAX || rows > INT32_MAX || V > INT32_MAX || (V == 0 && rows > 0)) return PDN_ERR_SHAPE;
-  if (!mul_ok(N, pdn::verify_blocks(V), &blocks) || blocks >= (int64_t)1 << 24) return PDN_ERR_SHAPE;
+  if (!mul_ok(N, pdn::verify_blocks(V), &blocks) || blocks >= (int64_t)1 << 24 || N >= (int64_t)1 << 24)
+    return PDN_ERR_SHAPE;
   if (!mul_ok(rows, V, &bytes) || !mul_ok(bytes, 4, &bytes)) return PDN_ERR_SHAPE;
   if (even && N > 0 && rows % N != 0) return PDN_ERR_SHAPE;
   *row_bytes = rows * V * (dtype == PDN_BF16 ? 2 : 4);
@@ -636,12 +639,13 @@ pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype,
   if (st != PDN_OK) return st;
   if (N > 0 && (!accepted || !token)) return PDN_ERR_NULL;
   if (N > 0 && rows > 0 && (!p || !ids || !u || !r)) return PDN_ERR_NULL;
-  const std::vector<Buf> ins = {{p, rb}, {q, rb}, {ids, rows * 4}, {u, rows * 4}, {r, N * 4}, {starts, (N + 1) * 4}};
-  const std::vector<Buf> outs = {{accepted, N * 4}, {token, N * 4}};
-  for (const std::vector<Buf>& v : {ins, outs})   // (probabilities: to an element, as a row of an odd V is)
-    for (const Buf& x : v)
-      if (x.p && (reinterpret_cast<uintptr_t>(x.p) & (dtype == PDN_BF16 && (x.p == p || x.p == q) ? 1u : 3u)))
-        return PDN_ERR_ALIGN;
+  const std::array<Buf, 6> ins = {
+      {{p, rb}, {q, rb}, {ids, rows * 4}, {u, rows * 4}, {r, N * 4}, {starts, (N + 1) * 4}}};
+  const std::array<Buf, 2> outs = {{{accepted, N * 4}, {token, N * 4}}};
+  for (size_t i = 0; i < ins.size(); ++i)   // (probabilities: to an element, as a row of an odd V is)
+    if (reinterpret_cast<uintptr_t>(ins[i].p) & (dtype == PDN_BF16 && i < 2 ? 1u : 3u)) return PDN_ERR_ALIGN;
+  for (const Buf& x : outs)
+    if (reinterpret_cast<uintptr_t>(x.p) & 3u) return PDN_ERR_ALIGN;
   if ((st = check_aliasing(ins, outs, Buf{ws, N > 0 ? static_cast<int64_t>(ws_bytes) : 0})) != PDN_OK) return st;
   if (N == 0) return PDN_OK;
   if (wb > 0 && (!ws || ws_bytes < static_cast<size_t>(wb) || (reinterpret_cast<uintptr_t>(ws) & 255u) != 0))

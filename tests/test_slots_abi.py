@@ -44,7 +44,7 @@ def test_refusals(draft):
         (dict(s=S(tokens=-1)), pdn.PDN_ERR_SHAPE), (dict(s=S(slots=-1)), pdn.PDN_ERR_SHAPE),
         (dict(s=S(Hk=3)), pdn.PDN_ERR_SHAPE), (dict(s=S(Hk=8)), pdn.PDN_ERR_SHAPE), (dict(s=S(Hk=-2)), pdn.PDN_ERR_SHAPE),
         (dict(s=S(tokens=1 << 31)), pdn.PDN_ERR_SHAPE), (dict(s=S(slots=1 << 31)), pdn.PDN_ERR_SHAPE),
-        (dict(p=prob(B=1 << 23)), pdn.PDN_ERR_SHAPE),
+        (dict(p=prob(B=1 << 23)), pdn.PDN_ERR_SHAPE), (dict(p=prob(B=1 << 20)), pdn.PDN_ERR_SHAPE),   # B H of 2^22
         (dict(s=S(starts=None)), pdn.PDN_ERR_SHAPE),                  # 3 x 8 rows are not 20
         (dict(s=S(slot=None, slots=2)), pdn.PDN_ERR_SHAPE),           # three sequences, two slots
         (dict(s=S(q_stride=255)), pdn.PDN_ERR_SHAPE), (dict(s=S(q_stride=260)), pdn.PDN_ERR_ALIGN),
@@ -99,7 +99,7 @@ def test_verify_refusals():
     for kw, status in [
             (dict(N=-1), pdn.PDN_ERR_SHAPE), (dict(rows=-1), pdn.PDN_ERR_SHAPE), (dict(V=-1), pdn.PDN_ERR_SHAPE),
             (dict(V=0), pdn.PDN_ERR_SHAPE), (dict(rows=10, starts=None), pdn.PDN_ERR_SHAPE),
-            (dict(N=1 << 24), pdn.PDN_ERR_SHAPE), (dict(V=1 << 31), pdn.PDN_ERR_SHAPE), (dict(rows=1 << 31), pdn.PDN_ERR_SHAPE),
+            (dict(N=1 << 24), pdn.PDN_ERR_SHAPE), (dict(N=1 << 24, V=0, rows=0), pdn.PDN_ERR_SHAPE), (dict(V=1 << 31), pdn.PDN_ERR_SHAPE), (dict(rows=1 << 31), pdn.PDN_ERR_SHAPE),
             (dict(dtype=7), pdn.PDN_ERR_DTYPE), (dict(p=None), pdn.PDN_ERR_NULL), (dict(ids=None), pdn.PDN_ERR_NULL),
             (dict(u=None), pdn.PDN_ERR_NULL), (dict(r=None), pdn.PDN_ERR_NULL), (dict(accepted=None), pdn.PDN_ERR_NULL),
             (dict(token=None), pdn.PDN_ERR_NULL), (dict(p=A + 2), pdn.PDN_ERR_ALIGN),
