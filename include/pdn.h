@@ -335,8 +335,13 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* problem, const pdn_inputs* in,
  * most tokens one of them has (a longer one is cut there), chunk is unused.
  * The recurrence, its modes and the meaning of the other members are those of
  * pdn_chunk_fwd; states and products are fp32 for both io types.
+ * Log-decays without the per-channel gate, and g_p, may be as low as the type
+ * goes, and -inf (the state is forgotten: e.g. a document's first token).
  * Per-channel gate: of each eight tokens of a sequence (T > 1: counted from
  * its first in the call) the log-decays of a channel must sum to more than -87.
+ * A NaN or Inf in a token shows in that sequence and slot only; within the
+ * sequence it may also show in o of tokens up to 31 before it (T > 1).
+ * B H must be below 2^22.
  *
  * `starts`, `slot`, `slot_out`, `fresh`, `accepted` are device arrays, read by
  * the kernels and not checked on the host; whatever they hold, accesses stay
@@ -368,9 +373,8 @@ typedef struct {
   /* pdn_slot_draft only (NULL and 0 in pdn_slot_fwd): */
   float* tape;              /* [slots, tape_tokens, H, R] records of pending tokens,
                                R = dk + dv + (per-channel gate: dk, else 4) + (A: dk):
-                               write key, correction e_t, log-decay summed from the first
-                               pending token (without the per-channel gate four
-                               times the same), A_t                            */
+                               write key, correction e_t, log-decay (without
+                               the per-channel gate four times the same), A_t  */
   int64_t tape_tokens;      /* >= T                                            */
   int32_t* pending;         /* [slots, H] records a slot has (of every head the
                                same); zero at first                            */
@@ -405,7 +409,8 @@ pdn_status pdn_slot_draft(const pdn_problem* problem, const pdn_inputs* in,
  * where that is zero everywhere), or from p after the last draft; -1 where no
  * token has a positive weight.  A sequence without rows: 0 and -1.
  * u: [rows] (a sequence's last is unused), r: [N], in [0, 1).  p and q need
- * not be normalised; NaN counts as zero weight.  `starts` as in pdn_slots
+ * not be normalised; NaN counts as zero weight (an infinite sum: the last token
+ * with a weight is taken).  `starts` as in pdn_slots
  * (NULL: rows / N rows each).  Sums are taken in 64 bits.
  * `ws` must be 256-byte aligned, of pdn_draft_verify_workspace_size bytes. */
 pdn_status pdn_draft_verify_workspace_size(int64_t N, int64_t V, size_t* bytes);

@@ -318,7 +318,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
       const int t = ll & 31;
       const bool in = static_cast<int64_t>(ch) * kC + t < rows.n;
       const float be = in ? s_be : 0.f, bp = in ? s_bp : 0.f, gp = in && a.g_p ? s_gp : 0.f;
-      double to = in && a.gate == kGateScalar ? s_g : 0.f;
+      double to = in && a.gate == kGateScalar ? sum_decay(s_g) : 0.f;
 #pragma unroll
       for (int off = 1; off < kC; off <<= 1) {
         const double x = __shfl_up(to, off, kC);

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       if (pw == 3) {
         const int t = l & 7;
         const bool in = static_cast<int64_t>(blk) * B + t < rows.n;
-        const float g = in && scalar ? s_g : 0.f, nx = __shfl_down(g, 1, B);
+        const float g = in && scalar ? sum_decay(s_g) : 0.f, nx = __shfl_down(g, 1, B);
         float to = g, on = t + 1 < B ? nx : 0.f;
 #pragma unroll
         for (int off = 1; off < B; off <<= 1) {

@@ -1,4 +1,5 @@
-// What the kernels on a pool of states share (pdn_slots.hip, pdn_slot_chunks.hip).
+// What the kernels on a pool of states share (pdn_slots.hip, pdn_slot_chunks.hip,
+// pdn_slot_runs.hip).
 #pragma once
 
 #include "pdn_device.hpp"
@@ -41,6 +42,11 @@ __device__ __forceinline__ SlotRows slot_rows(const SlotArgs& a, int64_t seq) {
 }
 
 constexpr int kSlotBlock = 8;   // tokens of a block
+
+// A token's log-decay where those of several tokens are added up.  e^-128 is zero
+// in fp32, and so is every decay over such a token; a sum that held a value far
+// below, an infinity above all, would have lost the tokens after it.  (NaN stays.)
+__device__ __forceinline__ float sum_decay(float g) { return g < -128.f ? -128.f : g; }
 
 // A head's state, seen through a buffer: a lane's rows are then one offset and
 // constants, where pointers to them would take two registers each.

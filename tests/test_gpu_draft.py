@@ -125,6 +125,35 @@ def test_forked_drafts(gate):
     assert pending.cpu().tolist() == [[2, 2], [0, 0], [6, 6], [3, 3]]
 
 
+@pytest.mark.parametrize("T", [4, 8, 20])
+@pytest.mark.parametrize("gate", ["scalar", "channel"])
+def test_strong_decay_of_drafts(T, gate):
+    """Accepted tokens whose log-decays add up to hundreds, or hold -inf without the
+    per-channel gate: those after keep their small ones."""
+    import paper_2604_21100_amd as pdn
+    rng = np.random.default_rng(31 + T)
+    H, d, P = 2, 128, 3
+    S, A = pool(rng, P, H, d, d, "squash")
+    Sd, Ad = dev(S), dev(A)
+    tape, pending = tape_of(P, T, H, d, d, gate, "squash")
+    b = batch(rng, P * T, H, H, d, d, "f32", gate, "squash")
+    for n in range(P):
+        for t in range(0, T, 3):
+            b["g"][n * T + t] = [-np.inf, -400.0, -90.0][n] if gate == "scalar" else -25.0
+    pos, opt = dev_batch(b, "f32", "squash")
+    kw = dict(A=Ad, gate=gate, max_tokens=T, **KW)
+    starts = [n * T for n in range(P + 1)]
+    o = host(pdn.pdn_slot_draft(*pos, Sd, tape, pending, starts=i32(starts), **opt, **kw))
+    acc = [T, T - 1, 2]
+    pdn.pdn_slot_draft(*pos, Sd, tape, pending, accepted=i32(acc), starts=i32([0] * (P + 1)), **opt, **kw)
+    for n in range(P):
+        rows = np.arange(n * T, (n + 1) * T)
+        ro = tokens(b, rows, S[n], A[n], gate, "squash")[0]
+        _, s, a = tokens(b, rows[:acc[n]], S[n], A[n], gate, "squash")
+        # (bars of the rule; of each sequence by itself)
+        assert rel_err(o[rows], ro) <= 1e-5 and rel_err(host(Sd)[n], s) <= 1e-5 and rel_err(host(Ad)[n], a) <= 1e-5
+
+
 # ------------------------------------------------------------- verification
 def ref_verify(p, q, ids, u, r, starts):
     acc, tok = [], []

@@ -223,6 +223,49 @@ def test_strong_decay_and_zero_keys(T):
         check(run(b, S, A, "f32", gate, "squash", starts=i32(starts), max_tokens=T), (o, S1, A1), "f32", T, gate)
 
 
+@pytest.mark.parametrize("T", [1, 8, 60])
+@pytest.mark.parametrize("io", ["bf16", "f32"])
+def test_state_forgotten(T, io):
+    """Log-decays of -inf, of the lowest value and of -1e5 (a document's first
+    token): nothing comes through, and the tokens after keep their small decays."""
+    rng = np.random.default_rng(85 + T)
+    low = [-np.inf, float(np.finfo(np.float32).min), -1e5]
+    b = batch(rng, 3 * T, 2, 2, 128, 128, io, "scalar", "squash")
+    for n in range(3):
+        for t in {0, T // 3, T // 2, T - 1}:
+            b["g"][n * T + t, n % 2] = low[(n + t) % 3]
+            b["g_p"][n * T + t, 1] = low[n]
+    S, A = pool(rng, 3, 2, 128, 128, "squash")
+    o, S1, A1, starts = want(b, S, A, [T] * 3, "scalar", "squash")
+    assert np.isfinite(S1).all()
+    check(run(b, S, A, io, "scalar", "squash", starts=i32(starts), max_tokens=T), (o, S1, A1), io, T)
+
+
+@pytest.mark.parametrize("T", [1, 6, 70])
+def test_two_streams_at_once(T):
+    """Calls on two streams, each with its own half of a pool, their outputs and
+    workspaces allocated by the calls; and the same pool's halves in one call."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    rng = np.random.default_rng(95 + T)
+    N, H, d = 4, 4, 128
+    b = batch(rng, N * T, H, H, d, d, "bf16", "scalar", "squash")
+    S, A = pool(rng, N, H, d, d, "squash")
+    ref = want(b, S, A, [T] * N, "scalar", "squash")
+    pos, opt = dev_batch(b, "bf16", "squash")
+    Sd, Ad = dev(S), dev(A)
+    cut = lambda x, lo: x if x is None or x.dim() == 1 else x[lo * T:(lo + 2) * T]   # noqa: E731
+    lists = [i32([0, 1]), i32([2, 3])]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    outs = [pdn.pdn_slot_fwd(*[cut(x, 2 * i) for x in pos], Sd, A=Ad, gate="scalar", slots=lists[i], max_tokens=T,
+                             starts=None, stream=streams[i], **{n: cut(x, 2 * i) for n, x in opt.items()}, **KW)
+            for i in range(2)]
+    torch.cuda.synchronize()
+    check((np.concatenate([host(x) for x in outs]), host(Sd), host(Ad)), ref[:3], "bf16", T)
+    check(run(b, S, A, "bf16", "scalar", "squash", max_tokens=T), ref[:3], "bf16", T)
+
+
 @pytest.mark.parametrize("T", [1, 8, 100])
 def test_nan_stays_in_its_sequence(T):
     """A sequence with NaN values does not reach its neighbours or other slots."""
