@@ -373,8 +373,10 @@ typedef struct {
   /* pdn_slot_draft only (NULL and 0 in pdn_slot_fwd): */
   float* tape;              /* [slots, tape_tokens, H, R] records of pending tokens,
                                R = dk + dv + (per-channel gate: dk, else 4) + (A: dk):
-                               write key, correction e_t, log-decay (without
-                               the per-channel gate four times the same), A_t  */
+                               write key, correction e_t, log-decay summed from the first
+                               pending token (without the per-channel gate four
+                               times the same; the decay between two records
+                               is as exact as fp32 has their sums), A_t        */
   int64_t tape_tokens;      /* >= T                                            */
   int32_t* pending;         /* [slots, H] records a slot has (of every head the
                                same); zero at first                            */

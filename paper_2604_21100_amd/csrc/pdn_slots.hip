@@ -16,9 +16,9 @@
 // registers.  The left operand of those products stacks the eight key rows
 // on the eight query rows: 16, a whole tile.
 //
-// Drafted tokens: a record of each (write key, correction e, log-decay,
-// preconditioner state) stays on the tape; the next call's first pass over the
-// state applies the accepted ones, eight by eight,
+// Drafted tokens: a record of each (write key, correction e, prefix of the
+// log-decay, preconditioner state) stays on the tape; the next call's first
+// pass over the state applies the accepted ones,
 //   S'^T = lam_n S^T + sum_{s <= n} (lam_n / lam_s) kt_s e_s.
 // One workgroup holds a whole head, so a slot's tape and states may be read
 // and written by the same call.
@@ -178,15 +178,15 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   __shared__ __attribute__((aligned(16))) T sRaw[3][kSlotBlock][DK];   // keys, queries, the caller's write keys
   __shared__ __attribute__((aligned(16))) float sKQ[2 * kSlotBlock][LD], sKt[kSlotBlock][LD];
   // CH: g; the write keys with the decay to the block's end, and as they are.
-  // Drafts: the accepted records' write keys and, with CH, their log-decays, and the
-  // decay over them; A after each token.
+  // Drafts: the accepted records' write keys; A after each token.
   __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sKr[CH && DRAFT ? kSlotBlock : 1][LD];
   __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kSlotBlock : 1][LD], sAt[DRAFT ? kSlotBlock : 1][LD];
   __shared__ __attribute__((aligned(16))) float sPart[NW][16][kSlotBlock], sLP[16][kSlotBlock + 4], sE[NW][kSlotBlock][16];
-  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGr[CH && DRAFT ? kSlotBlock : 1][LD], sLr[CH && DRAFT ? DK : 4], sSum[NW][kSlotBlock];
-  // of each token: log-decay, the decay to and from the token within the block as
-  // factors (1 with a per-channel gate), write strength, preconditioner gain and decay
-  __shared__ __attribute__((aligned(16))) float sg[kSlotBlock], sTo[kSlotBlock], sOn[kSlotBlock], sB[kSlotBlock], sBp[kSlotBlock], sDp[kSlotBlock];
+  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kSlotBlock : 1][LD], sSum[NW][kSlotBlock];
+  // of each token: log-decay, its sum from the first token, the decay to and from
+  // the token within the block as factors (1 with a per-channel gate), write strength,
+  // preconditioner gain and decay
+  __shared__ __attribute__((aligned(16))) float sg[kSlotBlock], sGp[kSlotBlock], sTo[kSlotBlock], sOn[kSlotBlock], sB[kSlotBlock], sBp[kSlotBlock], sDp[kSlotBlock];
   const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
@@ -260,6 +260,9 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     s_bp = in && gram ? x_bp : 0.f;
     s_gp = in && gram && a.g_p ? x_gp : 0.f;
   };
+  // Drafts: log-decay summed over the blocks before (the scalar's; of a channel), in
+  // 64 bits, so that a record's sum is rounded once.
+  double gacc = 0.0;
   auto put_rows = [&]() {
     auto put = [&](void* p, const u32x4& v, int x, int pieces, int row_bytes, int ld_bytes) {
       const int at = x * NTHR + tid;
@@ -292,6 +295,16 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       sB[tid] = s_b;
       sBp[tid] = s_bp;
       sDp[tid] = fast_exp(s_gp);
+      if (DRAFT && !CH) {
+        double sum = s_g;
+#pragma unroll
+        for (int off = 1; off < kSlotBlock; off <<= 1) {
+          const double y = __shfl_up(sum, off, kSlotBlock);
+          if (tid >= off) sum += y;
+        }
+        sGp[tid] = static_cast<float>(gacc + sum);
+        gacc += __shfl(sum, kSlotBlock - 1, kSlotBlock);
+      }
     }
   };
   if (rows.n > 0) load_rows(0);
@@ -299,7 +312,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // ---- drafts: the first accepted records
   const float* const rec = DRAFT ? a.tape + (src * a.tape_tokens * a.H + h) * R : nullptr;
   u32x4 ck[NGP], cg[NGP];
-  float ce[2], cs;
+  float ce[2];
   auto load_records = [&](int b0) {   // (whether accepted or not; never past the tape)
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kSlotBlock));
@@ -310,9 +323,9 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       if (t < n) {
         ck[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + cc);
         if (CH) cg[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + DK + DV + cc);
+        else cg[x][0] = reinterpret_cast<const uint32_t*>(rec)[(b0 + t) * rs + DK + DV];
       }
     }
-    cs = !CH && (l & 7) < n ? rec[(b0 + (l & 7)) * rs + DK + DV] : 0.f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int t = 4 * j + lg;
@@ -408,10 +421,16 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           sKt[t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
           if (CH) {
             sKw[t][c] = kt[t] * fast_exp(G - to[t]);
-            if (DRAFT) sKr[t][c] = kt[t];
+            if (DRAFT) {
+              sKr[t][c] = kt[t];
+              sGt[t][c] = static_cast<float>(gacc + to[t]);
+            }
           }
         }
-      if (CH && key) sLam[c] = fast_exp(G);
+      if (CH) {
+        if (key) sLam[c] = fast_exp(G);
+        if (DRAFT) gacc += G;
+      }
     }
     __syncthreads();
     // (rows of K over rows of Q) times Kt^T, a share of the channels a wave
@@ -446,70 +465,35 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     __syncthreads();
   };
 
-  // ---- eight accepted records and the state after them: write keys or, without the
-  // per-channel gate, corrections with the decay to the last of them.  Decays are
-  // summed from record to record, so a record holds its own: a difference of two
-  // long sums would lose a short one.
-  float lam_r = 1.f;   // the decay over them (CH: sLr)
-  auto put_records = [&](int b0) {   // into LDS; what was not accepted as zeros
+  // ---- the accepted records' operand: write keys with their decay to the last
+  const float Gn = DRAFT && !CH && cnt > 0 ? last[DK + DV] : 0.f;
+  auto put_records = [&](int b0) {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
       const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
       if (at < GP) {
-        const bool in = b0 + t < cnt;
-        *reinterpret_cast<u32x4*>(&sC[t][cc]) = in ? ck[x] : u32x4{0, 0, 0, 0};
-        if (CH) *reinterpret_cast<u32x4*>(&sGr[t][cc]) = in ? cg[x] : u32x4{0, 0, 0, 0};
-      }
-    }
-    if (!CH) {
-      float on = b0 + (l & 7) < cnt ? cs : 0.f;   // summed from a record to the last: its own included
+        floatx4 kt = {0.f, 0.f, 0.f, 0.f};
+        if (b0 + t < cnt) {
+          kt = __builtin_bit_cast(floatx4, ck[x]);
+          const floatx4 g = __builtin_bit_cast(floatx4, cg[x]);
+          if (CH) {
+            const floatx4 gn = *reinterpret_cast<const floatx4*>(last + DK + DV + cc);
 #pragma unroll
-      for (int off = 1; off < kSlotBlock; off <<= 1) {
-        const float z = __shfl_down(on, off, kSlotBlock);
-        if ((l & 7) + off < kSlotBlock) on += z;
+            for (int i = 0; i < 4; ++i) kt[i] *= fast_exp(gn[i] - g[i]);
+          } else {
+            kt *= fast_exp(Gn - g[0]);
+          }
+        }
+        *reinterpret_cast<floatx4*>(&sC[t][cc]) = kt;
       }
-      lam_r = fast_exp(__shfl(on, 0, 64));
-      const float after = __shfl_down(on, 1, kSlotBlock);
-      on = fast_exp((l & 7) + 1 < kSlotBlock ? after : 0.f);
-#pragma unroll
-      for (int j = 0; j < 2; ++j) ce[j] *= __shfl(on, 4 * j + lg, 64);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j)
       if (b0 + 4 * j + lg >= cnt) ce[j] = 0.f;
   };
-  auto decay_records = [&]() {   // (CH; after a barrier)
-#pragma unroll
-    for (int x = 0; x < NGP; ++x) {
-      const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
-      if (at < GP) {
-        floatx4 on = {0.f, 0.f, 0.f, 0.f}, own = on;
-#pragma unroll
-        for (int j = kSlotBlock - 1; j >= 0; --j) {
-          const floatx4 g = *reinterpret_cast<const floatx4*>(&sGr[j][cc]);
-          if (j > t) on += g;
-          if (j == t) own = g;
-        }
-        floatx4 kt = *reinterpret_cast<const floatx4*>(&sC[t][cc]), f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          kt[i] *= fast_exp(on[i]);
-          f[i] = fast_exp(on[i] + own[i]);
-        }
-        *reinterpret_cast<floatx4*>(&sC[t][cc]) = kt;
-        if (t == 0) *reinterpret_cast<floatx4*>(&sLr[cc]) = f;
-      }
-    }
-  };
   auto apply_records = [&](int b0) {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
-#pragma unroll
-    for (int m = 0; m < MB; ++m) {
-      floatx4 f = {lam_r, lam_r, lam_r, lam_r};
-      if (CH) f = *reinterpret_cast<const floatx4*>(&sLr[16 * m + 4 * lg]);
-      S.t[m] *= f;
-    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if (b0 + 4 * j >= cnt) break;
@@ -534,23 +518,29 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     anew();
     if (DRAFT && rows.n > t0 + kSlotBlock) load_rows(t0 + kSlotBlock);
     anew();
-    if (CH && DRAFT && t0 == 0 && cnt > 0) decay_records();
-    anew();
     if (nt > 0) operands(nt);
     anew();
     if (DRAFT && t0 == 0) {
       if (cnt > 0) {
-        if (nt == 0) __syncthreads();
+        [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
+#pragma unroll
+        for (int m = 0; m < MB; ++m) {
+          floatx4 lam;
+          if (CH) {
+            const floatx4 g = *reinterpret_cast<const floatx4*>(last + DK + DV + 16 * m + 4 * lg);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lam[i] = fast_exp(g[i]);
+          } else {
+            lam = fast_exp(Gn);
+          }
+          S.t[m] *= lam;
+        }
         apply_records(0);
         for (int b0 = kSlotBlock; b0 < cnt; b0 += kSlotBlock) {
           load_records(b0);
           __syncthreads();
           put_records(b0);
           __syncthreads();
-          if (CH) {
-            decay_records();
-            __syncthreads();
-          }
           apply_records(b0);
         }
       }
@@ -570,10 +560,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
         const int t = x / (DK / 4), cc = 4 * (x % (DK / 4));
         float* r = r0 + t * rs;
         *reinterpret_cast<floatx4*>(r + cc) = *reinterpret_cast<const floatx4*>(CH ? &sKr[t][cc] : &sKt[t][cc]);
-        if (CH) *reinterpret_cast<floatx4*>(r + DK + DV + cc) = *reinterpret_cast<const floatx4*>(&sG[t][cc]);
+        if (CH) *reinterpret_cast<floatx4*>(r + DK + DV + cc) = *reinterpret_cast<const floatx4*>(&sGt[t][cc]);
         if (gram) *reinterpret_cast<floatx4*>(r + DK + DV + (CH ? DK : 4) + cc) = *reinterpret_cast<const floatx4*>(&sAt[t][cc]);
       }
-      if (!CH && tid < 4 * nt) r0[tid / 4 * rs + DK + DV + tid % 4] = sg[tid / 4];
+      if (!CH && tid < 4 * nt) r0[tid / 4 * rs + DK + DV + tid % 4] = sGp[tid / 4];
     }
     // ---- (rows of K over rows of Q) times S^T
     floatx4 yz = {0.f, 0.f, 0.f, 0.f}, yz1 = yz;   // (two sums: each product would wait for the one before)
