@@ -178,11 +178,12 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   __shared__ __attribute__((aligned(16))) T sRaw[3][kSlotBlock][DK];   // keys, queries, the caller's write keys
   __shared__ __attribute__((aligned(16))) float sKQ[2 * kSlotBlock][LD], sKt[kSlotBlock][LD];
   // CH: g; the write keys with the decay to the block's end, and as they are.
-  // Drafts: the accepted records' write keys; A after each token.
-  __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sKr[CH && DRAFT ? kSlotBlock : 1][LD];
+  // Drafts: the accepted records' write keys and, with CH, their log-decays and the
+  // decay over them; A after each token.
+  __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sKr[CH && DRAFT ? kSlotBlock : 1][LD], sGr[CH && DRAFT ? kSlotBlock : 1][LD];
   __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kSlotBlock : 1][LD], sAt[DRAFT ? kSlotBlock : 1][LD];
   __shared__ __attribute__((aligned(16))) float sPart[NW][16][kSlotBlock], sLP[16][kSlotBlock + 4], sE[NW][kSlotBlock][16];
-  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kSlotBlock : 1][LD], sSum[NW][kSlotBlock];
+  __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kSlotBlock : 1][LD], sSum[NW][kSlotBlock], sLr[CH && DRAFT ? DK : 4];
   // of each token: log-decay, its sum from the first token, the decay to and from
   // the token within the block as factors (1 with a per-channel gate), write strength,
   // preconditioner gain and decay
@@ -312,7 +313,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // ---- drafts: the first accepted records
   const float* const rec = DRAFT ? a.tape + (src * a.tape_tokens * a.H + h) * R : nullptr;
   u32x4 ck[NGP], cg[NGP];
-  float ce[2];
+  float ce[2], cs = 0.f;
   auto load_records = [&](int b0) {   // (whether accepted or not; never past the tape)
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     const int n = static_cast<int>(min(a.tape_tokens - b0, (int64_t)kSlotBlock));
@@ -323,9 +324,9 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       if (t < n) {
         ck[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + cc);
         if (CH) cg[x] = *reinterpret_cast<const u32x4*>(rec + (b0 + t) * rs + DK + DV + cc);
-        else cg[x][0] = reinterpret_cast<const uint32_t*>(rec)[(b0 + t) * rs + DK + DV];
       }
     }
+    cs = !CH && (l & 7) < n ? rec[(b0 + (l & 7)) * rs + DK + DV] : 0.f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int t = 4 * j + lg;
@@ -340,14 +341,14 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   }
   const float* const last = DRAFT ? rec + max(cnt - 1, 0) * rs : nullptr;
 
-  // ---- the state
+  // ---- the state (A first: what is loaded after the state is there after it)
   SlotColumns<DK, DV> S;
   float A = 0.f;
   {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
+    if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
     if (fresh) S.zero();
     else S.load(slot_head<DK, DV>(a, src, h), 4 * lg * DV + v0);
-    if (gram && key && !fresh) A = cnt > 0 ? last[DK + DV + (CH ? DK : 4) + c] : a.A[(src * a.H + h) * DK + c];
   }
   auto store_state = [&](float A) {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
@@ -465,32 +466,51 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     __syncthreads();
   };
 
-  // ---- the accepted records' operand: write keys with their decay to the last
-  const float Gn = DRAFT && !CH && cnt > 0 ? last[DK + DV] : 0.f;
-  auto put_records = [&](int b0) {
+  // ---- eight accepted records: write keys or, without the per-channel gate, corrections
+  // with their decay to the last accepted token (one of the first eight, as a rule:
+  // its sum is then at hand, where a load would wait for the state's)
+  float lam_r = 1.f;   // the decay over all of them (CH: sLr)
+  auto put_records = [&](int b0) {   // into LDS; what was not accepted as zeros
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
     for (int x = 0; x < NGP; ++x) {
       const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
       if (at < GP) {
-        floatx4 kt = {0.f, 0.f, 0.f, 0.f};
-        if (b0 + t < cnt) {
-          kt = __builtin_bit_cast(floatx4, ck[x]);
-          const floatx4 g = __builtin_bit_cast(floatx4, cg[x]);
-          if (CH) {
-            const floatx4 gn = *reinterpret_cast<const floatx4*>(last + DK + DV + cc);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) kt[i] *= fast_exp(gn[i] - g[i]);
-          } else {
-            kt *= fast_exp(Gn - g[0]);
-          }
-        }
-        *reinterpret_cast<floatx4*>(&sC[t][cc]) = kt;
+        *reinterpret_cast<u32x4*>(&sC[t][cc]) = b0 + t < cnt ? ck[x] : u32x4{0, 0, 0, 0};
+        if (CH) *reinterpret_cast<u32x4*>(&sGr[t][cc]) = cg[x];
       }
     }
+    float f = 0.f;
+    if (!CH) {
+      const float Gn = cnt > kSlotBlock ? last[DK + DV] : __shfl(cs, max(cnt - 1, 0), 64);
+      lam_r = fast_exp(Gn);
+      f = fast_exp(Gn - cs);
+    }
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < 2; ++j) {
+      if (!CH) ce[j] *= __shfl(f, 4 * j + lg, 64);
       if (b0 + 4 * j + lg >= cnt) ce[j] = 0.f;
+    }
+  };
+  auto decay_records = [&](int b0) {   // (CH; after a barrier)
+#pragma unroll
+    for (int x = 0; x < NGP; ++x) {
+      const int at = x * NTHR + tid, t = at / (DK / 4), cc = 4 * (at % (DK / 4));
+      if (at < GP) {
+        floatx4 gn;
+        if (cnt > kSlotBlock) gn = *reinterpret_cast<const floatx4*>(last + DK + DV + cc);
+        else gn = *reinterpret_cast<const floatx4*>(&sGr[cnt - 1][cc]);
+        const floatx4 g = *reinterpret_cast<const floatx4*>(&sGr[t][cc]);
+        floatx4 kt = *reinterpret_cast<const floatx4*>(&sC[t][cc]), f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (b0 + t < cnt) kt[i] *= fast_exp(gn[i] - g[i]);
+          f[i] = fast_exp(gn[i]);
+        }
+        *reinterpret_cast<floatx4*>(&sC[t][cc]) = kt;
+        if (t == 0) *reinterpret_cast<floatx4*>(&sLr[cc]) = f;
+      }
+    }
   };
   auto apply_records = [&](int b0) {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
@@ -518,21 +538,18 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     anew();
     if (DRAFT && rows.n > t0 + kSlotBlock) load_rows(t0 + kSlotBlock);
     anew();
+    if (CH && DRAFT && t0 == 0 && cnt > 0) decay_records(0);
+    anew();
     if (nt > 0) operands(nt);
     anew();
     if (DRAFT && t0 == 0) {
       if (cnt > 0) {
+        if (CH && nt == 0) __syncthreads();
         [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
 #pragma unroll
         for (int m = 0; m < MB; ++m) {
-          floatx4 lam;
-          if (CH) {
-            const floatx4 g = *reinterpret_cast<const floatx4*>(last + DK + DV + 16 * m + 4 * lg);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) lam[i] = fast_exp(g[i]);
-          } else {
-            lam = fast_exp(Gn);
-          }
+          floatx4 lam = {lam_r, lam_r, lam_r, lam_r};
+          if (CH) lam = *reinterpret_cast<const floatx4*>(&sLr[16 * m + 4 * lg]);
           S.t[m] *= lam;
         }
         apply_records(0);
@@ -541,6 +558,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           __syncthreads();
           put_records(b0);
           __syncthreads();
+          if (CH) {
+            decay_records(b0);
+            __syncthreads();
+          }
           apply_records(b0);
         }
       }
