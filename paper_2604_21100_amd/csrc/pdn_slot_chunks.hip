@@ -77,11 +77,10 @@ __device__ __forceinline__ void mma_parts(floatx4& acc, const bf16x8 (&a)[NA], c
 // use, and those one, two and three after it), what is formed from them twice.
 template <int DK, int DV, int NP>
 struct Lay {
-  static constexpr int kTile = kC * DK * 2, kVal = kC * DV * 2, kMat = kC * kC * 2;
+  static constexpr int kTile = kC * DK * 2, kMat = kC * kC * 2;
   static constexpr int oK = 0, oQ = oK + 4 * kTile, oX = oQ + 4 * kTile;            // oX: external write keys
   static constexpr int oT = oX + (NP == 0 ? 4 * kTile : 0);                         // write keys' parts
-  static constexpr int oV = oT + (NP == 3 ? 2 * 3 * kTile : 0);
-  static constexpr int oO = oV + kVal, oM = oO + kVal, oP = oM + 3 * kMat;
+  static constexpr int oM = oT + (NP == 3 ? 2 * 3 * kTile : 0), oP = oM + 3 * kMat;
   static constexpr int oL = oP + 2 * 2 * kMat, kL = kC * (kC + 4) * 4, oF = oL + kL;   // L, M in fp32
   static constexpr int oA = oF + kL;                                                // per segment and channel, sums of bp k^2
   static constexpr int oS = oA + (NP == 3 ? 512 * 4 : 0), kS = 8 * kC * 4;          // see load_scalars
@@ -110,8 +109,6 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
   auto mat_p = [&](int it, int p) { return sm + L::oP + ((it & 1) * 2 + p) * L::kMat; };
   auto scal = [&](int it, int x) { return sm + L::oS + (it & 3) * L::kS + x * kC * 4; };
 
-  typedef __attribute__((address_space(3))) bf16 lds_bf16;
-
   if (w < NC) {
     // ------------------------------------------------------------ consumers
     const int v0 = 16 * w + m;
@@ -123,6 +120,22 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
 #pragma unroll
         for (int r = 0; r < 8; ++r) S[kk][r / 4][r % 4] = fresh ? 0.f : sp[(32 * kk + r) * DV];
     }
+    // A chunk's rows of v and o, this lane's eight of a column (two bytes a lane: 32
+    // adjacent ones a row and wave, and the waves of a row run together).  Past the
+    // sequence's end nothing is read, or written.
+    auto view = [&](const void* p, int64_t stride, int ch) {
+      const int64_t t0 = static_cast<int64_t>(ch) * kC, n = min<int64_t>(kC, rows.n - t0);
+      return buf_rsrc(static_cast<const char*>(p) + ((rows.lo + t0) * stride + h * DV) * 2,
+                      n > 0 ? static_cast<uint32_t>(((n - 1) * stride + DV) * 2) : 0);
+    };
+    float vn[8];
+    auto load_v = [&](int ch) {
+      const __amdgpu_buffer_rsrc_t r = view(a.v, a.v_stride, ch);
+      const uint32_t step = static_cast<uint32_t>(a.v_stride * 2), at = 8 * g * step + v0 * 2;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) vn[i] = buf_get<bf16>(r, static_cast<int>(at + i * step));
+    };
+    load_v(0);
     lds_sync();
     lds_sync();
     lds_sync();   // (the first chunk is being formed)
@@ -140,8 +153,6 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
         }
       };
       load_kq(0);
-      const bf16x8 v8 = lds_frag_t(sm + L::oV + tile_off<DV / 8>(8 * g + (m >> 2), 2 * w + ((m & 3) >> 1)) + (m & 1) * 8,
-                                   4 * DV * 2);
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         y[u] = z[u] = e[u] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -176,9 +187,10 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
           for (int i = 0; i < 4; ++i)   // (a row past the end has no strength, and no value that could spoil that)
-            x[u][i] = be[u][i] * (static_cast<float>(v8[4 * u + i]) - lam[u][i] * y[u][i]);
+            x[u][i] = be[u][i] * (vn[4 * u + i] - lam[u][i] * y[u][i]);
           z[u] *= lam[u];
         }
+        load_v(ch + 1);
         parts8<3>(x[0], x[1], xp);
       }
       lds_sync();   // A
@@ -211,14 +223,16 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
         mma_parts(t, tp[x & 1], wp, 2);
       }
       parts8<2>(e[0], e[1], ep);
-      // ---- O, which the producers store
+      // ---- O
+      const __amdgpu_buffer_rsrc_t ro = view(a.o, a.H * DV, ch);
+      const uint32_t step = static_cast<uint32_t>(a.H * DV * 2), at = 8 * g * step + v0 * 2;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         mma_parts(z[u], pp[u], ep, 1);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<lds_bf16*>(sm + L::oO + tile_off<DV / 8>(8 * g + 4 * u + i, v0 >> 3) + (v0 & 7) * 2) =
-              static_cast<bf16>(a.scale * z[u][i]);
+          __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, static_cast<bf16>(a.scale * z[u][i])), ro,
+                                                static_cast<int>(at + (4 * u + i) * step), 0, 0);
       }
       lds_sync();   // B
     }
@@ -271,23 +285,8 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
         lds_put(sm + o + tile_off<N>(at / N, at % N), __builtin_bit_cast(bf16x8, from[x]));
       }
     };
-    // a chunk's outputs (rows past the end are past the buffer's range)
-    auto store_o = [&](int ch) {
-      constexpr int N = DV / 8;
-      const int64_t HV = a.H * DV;
-      const int n = static_cast<int>(min<int64_t>(kC, rows.n - static_cast<int64_t>(ch) * kC));
-      const __amdgpu_buffer_rsrc_t r =
-          buf_rsrc(static_cast<const char*>(a.o) + ((rows.lo + static_cast<int64_t>(ch) * kC) * HV + h * DV) * 2,
-                   static_cast<uint32_t>(((n - 1) * HV + DV) * 2));
-#pragma unroll
-      for (int x = 0; x < kC * N / 256; ++x) {
-        const uint32_t at = pw * 64 + ll + 256 * x;
-        buf_put16(r, at / N * static_cast<uint32_t>(HV * 2) + at % N * 16, lds_frag(sm + L::oO + tile_off<N>(at / N, at % N)));
-      }
-    };
     constexpr std::integral_constant<int, DK> wk;
-    constexpr std::integral_constant<int, DV> wv;
-    u32x4 rk[DK / 64], rq[DK / 64], rx[DK / 64], rv[DV / 64];
+    u32x4 rk[DK / 64], rq[DK / 64], rx[DK / 64];
     auto load_keys = [&](int ch) {
       load_tile(ch, a.k, a.k_stride, hk * DK, wk, rk);
       load_tile(ch, a.q, a.q_stride, hk * DK, wk, rq);
@@ -528,13 +527,11 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
       anew();
       if (it > 0 && pw < 2) put_inverse();
       anew();
-      if (live) load_tile(it, a.v, a.v_stride, h * DV, wv, rv);
       if (it > 0 && it + 1 < nch && pw == 3) put_scalars(it + 1);
       if (it + 2 < nch) {
         load_keys(it + 2);
         if (pw == 3) load_scalars(it + 2);
       }
-      if (it > 1) store_o(it - 2);
       anew();
       if (gram && live) put_write_keys(it);
       lds_sync();   // A
@@ -543,7 +540,6 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
       anew();
       if (gram && it + 1 < nch) put_sums(it + 1);
       anew();
-      if (live) put_tile(wv, rv, L::oV);   // (the consumers have used theirs)
       if (it + 2 < nch) put_keys(it + 2);
       // No load is under way any more.  Said outright (vmcnt 0), or the compiler,
       // which does not see that a load's branch and its use's go together, waits
@@ -551,7 +547,6 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
       __builtin_amdgcn_s_waitcnt(0x0f70);
       lds_sync();   // B
     }
-    if (nch > 0) store_o(nch - 1);
     if (gram && pt0 < PAIRS) *reinterpret_cast<floatx2*>(ap + dst * a.H * DK) = A;
   }
 }
