@@ -94,7 +94,8 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
   constexpr int NC = DV / 16, KK = DK / 32, NCH = DK / 8, RK = DK * 2, NT = NP == 3 ? 3 : 1;
   __shared__ __attribute__((aligned(1024))) char smem[L::total];
   lds_char* const sm = (lds_char*)smem;
-  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const SlotWhere where = slot_where(a);
+  const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);

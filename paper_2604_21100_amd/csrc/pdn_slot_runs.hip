@@ -39,7 +39,8 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
   using R = Run<T, DK, DV, CH>;
   constexpr int B = kSlotBlock, NW = R::NW, MB = DK / 16;
   __shared__ R s;
-  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const SlotWhere where = slot_where(a);
+  const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);
@@ -47,11 +48,21 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, lr = l & 15, lg = l >> 4;
   const int nb = static_cast<int>((rows.n + B - 1) / B);
   const bool sums = slot_needs_sum(a);
-  // a block's rows as a buffer: past the sequence's end zeros, without rows no bytes
-  auto view = [&](int blk, const void* p, int64_t stride, int64_t first, int width, int esz, bool there) {
-    const int64_t t0 = static_cast<int64_t>(blk) * B, n = min(rows.n - t0, (int64_t)B);
-    return buf_rsrc(static_cast<const char*>(p) + ((rows.lo + t0) * stride + first) * esz,
-                    there && n > 0 ? static_cast<uint32_t>(((n - 1) * stride + width) * esz) : 0);
+  // A tensor's rows block by block: a buffer that ends with the sequence (past it reads
+  // are zeros and writes are dropped; of a tensor that is not there, all), moved on by
+  // a block each time (its place as a product would take tens of instructions).
+  struct Rows {
+    const char* base;
+    uint32_t step, width;   // bytes
+  };
+  auto rows_of = [&](const void* p, int64_t stride, int64_t first, int width, int esz) {
+    return Rows{static_cast<const char*>(p) + (rows.lo * stride + first) * esz, p ? static_cast<uint32_t>(stride * esz) : 0,
+                p ? static_cast<uint32_t>(width * esz) : 0};
+  };
+  auto next = [&](Rows& r, int n) {   // n: rows left
+    const __amdgpu_buffer_rsrc_t v = buf_rsrc(r.base, n > 0 ? (min(n, B) - 1) * r.step + r.width : 0);
+    r.base += static_cast<uint64_t>(r.step) * B;
+    return v;
   };
 
   if (w < NW) {
@@ -61,13 +72,16 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
     if (fresh) S.zero();
     else S.load(slot_head<DK, DV>(a, src, h), at);
     float vn[4];
-    auto load_v = [&](int blk) {
-      const __amdgpu_buffer_rsrc_t r = view(blk, a.v, a.v_stride, h * DV, DV, sizeof(T), true);
+    Rows rv = rows_of(a.v, a.v_stride, h * DV, DV, sizeof(T)), ro = rows_of(a.o, a.H * DV, h * DV, DV, sizeof(T));
+    int left = static_cast<int>(rows.n), left_v = left;   // rows from the block in use, and from the next values
+    auto load_v = [&]() {
+      const __amdgpu_buffer_rsrc_t r = next(rv, left_v);
+      left_v -= B;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vn[i] = buf_get<T>(r, (tb + i) * static_cast<uint32_t>(a.v_stride * sizeof(T)) + v0 * sizeof(T));
+      for (int i = 0; i < 4; ++i) vn[i] = buf_get<T>(r, static_cast<int>((tb + i) * rv.step + v0 * sizeof(T)));
     };
     if (nb > 0) {
-      load_v(0);
+      load_v();
       lds_sync();
     }
     for (int it = 0; it <= nb && nb > 0; ++it) {
@@ -87,8 +101,6 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       }
       lds_sync();   // A
       if (blk >= 0) {
-        const int64_t t0 = static_cast<int64_t>(blk) * B;
-        const int nt = static_cast<int>(min<int64_t>(B, rows.n - t0));
         const float(*tok)[B] = s.tok[blk & 3];
         // ---- E: tokens 0-3 in the first 16 lanes, 4-7 in the next
         floatx4 ld[4], lx[4];
@@ -106,7 +118,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = be[i] * (vn[i] - lam[i] * yz[i]);
         yz *= lam;
-        load_v(it);
+        load_v();
         floatx4 e = slot_solve4(ld, x);
         {
           floatx4 f;   // e of tokens 0-3
@@ -142,11 +154,11 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
         settled(yz);
-        T* ob = static_cast<T*>(a.o) + (rows.lo + t0) * a.H * DV + h * DV + v0;
+        const __amdgpu_buffer_rsrc_t r = next(ro, left);
+        left -= B;
         if (lg >= 2)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (tb + i < nt) ob[(tb + i) * a.H * DV] = from_f<T>(a.scale * yz[i]);
+          for (int i = 0; i < 4; ++i) buf_put<T>(r, static_cast<int>((tb + i) * ro.step + v0 * sizeof(T)), a.scale * yz[i]);
       }
       lds_sync();   // B
     }
@@ -158,38 +170,37 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
     const int prec = a.precond;
     const bool gram = has_gram(prec), both = prec == kATQ, scalar = a.gate == kGateScalar;
     const float mu = prec == kSquash ? fast_exp(a.log_a_scale[h]) : 0.f;
-    const float *const gb = scalar ? a.g : a.beta, *const bpb = gram ? a.beta_p : a.beta,
-                *const gpb = gram && a.g_p ? a.g_p : a.beta;
     float A = gram && !fresh ? a.A[(src * a.H + h) * DK + c] : 0.f;   // (query threads follow it too)
     constexpr int RP = B * DK * sizeof(T) / 16, NRP = (RP + 255) / 256, GP = B * DK * 4 / 16, NGP = (GP + 255) / 256;
     u32x4 rk[NRP], rq[NRP], rx[NRP], rg[NGP];
     float s_b, s_g, s_bp, s_gp;
-    auto load_rows = [&](int blk) {
-      const __amdgpu_buffer_rsrc_t vk = view(blk, a.k, a.k_stride, hk * DK, DK, sizeof(T), true),
-                                   vq = view(blk, a.q, a.q_stride, hk * DK, DK, sizeof(T), true),
-                                   vx = view(blk, a.ktilde, a.Hk * DK, hk * DK, DK, sizeof(T), prec == kExternal);
-      auto piece = [&](__amdgpu_buffer_rsrc_t r, int64_t stride, int row_bytes, int esz, int x) {
+    // (each read whether it is used or not: a branch would wait for the loads)
+    Rows vk = rows_of(a.k, a.k_stride, hk * DK, DK, sizeof(T)), vq = rows_of(a.q, a.q_stride, hk * DK, DK, sizeof(T)),
+         vx = rows_of(prec == kExternal ? a.ktilde : nullptr, a.Hk * DK, hk * DK, DK, sizeof(T)),
+         vg = rows_of(CH ? a.g : nullptr, a.H * DK, h * DK, DK, 4),
+         nbe = rows_of(a.beta, a.H, h, 1, 4), ng = rows_of(scalar ? a.g : nullptr, a.H, h, 1, 4),
+         nbp = rows_of(gram ? a.beta_p : nullptr, a.H, h, 1, 4), ngp = rows_of(gram ? a.g_p : nullptr, a.H, h, 1, 4);
+    int left = static_cast<int>(rows.n);
+    auto load_rows = [&]() {
+      auto piece = [&](__amdgpu_buffer_rsrc_t r, uint32_t step, int row_bytes, int x) {
         const uint32_t at = x * 256 + pt, t = at * 16 / row_bytes, o = at * 16 % row_bytes;
-        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                             r, static_cast<int>(t * static_cast<uint32_t>(stride * esz) + o), 0, 0));
+        return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(t * step + o), 0, 0));
       };
+      auto rows_in = [&](Rows& v, auto& to, int row_bytes) {
+        const __amdgpu_buffer_rsrc_t r = next(v, left);
 #pragma unroll
-      for (int x = 0; x < NRP; ++x) {
-        rk[x] = piece(vk, a.k_stride, DK * sizeof(T), sizeof(T), x);
-        rq[x] = piece(vq, a.q_stride, DK * sizeof(T), sizeof(T), x);
-        rx[x] = piece(vx, a.Hk * DK, DK * sizeof(T), sizeof(T), x);
-      }
-      if (CH) {
-        const __amdgpu_buffer_rsrc_t vg = view(blk, a.g, a.H * DK, h * DK, DK, 4, true);
-#pragma unroll
-        for (int x = 0; x < NGP; ++x) rg[x] = piece(vg, a.H * DK, DK * 4, 4, x);
-      }
-      // (each read whether it is used or not: a branch would wait for the loads)
-      const int64_t sc = (rows.lo + min(static_cast<int64_t>(blk) * B + (l & 7), rows.n - 1)) * a.H + h;
-      s_b = a.beta[sc];
-      s_g = gb[sc];
-      s_bp = bpb[sc];
-      s_gp = gpb[sc];
+        for (int x = 0; x < static_cast<int>(sizeof(to) / 16); ++x) to[x] = piece(r, v.step, row_bytes, x);
+      };
+      rows_in(vk, rk, DK * sizeof(T));
+      rows_in(vq, rq, DK * sizeof(T));
+      rows_in(vx, rx, DK * sizeof(T));
+      if (CH) rows_in(vg, rg, DK * 4);
+      auto number = [&](Rows& v) { return buf_get<float>(next(v, left), static_cast<int>((l & 7) * v.step)); };
+      s_b = number(nbe);
+      s_g = number(ng);
+      s_bp = number(nbp);
+      s_gp = number(ngp);
+      left -= B;
     };
     auto put_rows = [&](int blk) {
       auto put = [&](void* p, const u32x4& v, int x, int pieces, int row_bytes, int ld_bytes) {
@@ -208,23 +219,17 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
         for (int x = 0; x < NGP; ++x) put(s.g, rg[x], x, GP, DK * 4, R::LD * 4);
       if (pw == 3) {
         const int t = l & 7;
-        const bool in = static_cast<int64_t>(blk) * B + t < rows.n;
-        const float g = in && scalar ? sum_decay(s_g) : 0.f, nx = __shfl_down(g, 1, B);
-        float to = g, on = t + 1 < B ? nx : 0.f;
-#pragma unroll
-        for (int off = 1; off < B; off <<= 1) {
-          const float y = __shfl_up(to, off, B), z = __shfl_down(on, off, B);
-          if (t >= off) to += y;
-          if (t + off < B) on += z;
-        }
+        const float g = sum_decay(s_g);   // (zero where there is none)
+        float to, on;
+        block_sums(g, l, &to, &on);
         if (l < B) {
           float(*tok)[B] = s.tok[blk & 3];
           tok[0][t] = g;
           tok[1][t] = fast_exp(to);
           tok[2][t] = fast_exp(on);
-          tok[3][t] = in ? s_b : 0.f;
-          tok[4][t] = in && gram ? s_bp : 0.f;
-          tok[5][t] = in && gram && a.g_p ? fast_exp(s_gp) : 1.f;
+          tok[3][t] = s_b;
+          tok[4][t] = s_bp;
+          tok[5][t] = fast_exp(s_gp);
         }
       }
     };
@@ -326,9 +331,12 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       s.LP[r][x] = r < B ? (x < t ? tok[3][t] * v : 0.f) : (x <= t ? v : 0.f);
     };
     if (nb > 0) {
-      load_rows(0);
+      load_rows();
       put_rows(0);
-      load_rows(1);
+      // A has been loaded too.  Said outright (vmcnt 0), or the compiler waits for it, and
+      // with it for the loads just issued, each time round the loop.
+      __builtin_amdgcn_s_waitcnt(0x0f70);
+      load_rows();
       lds_sync();
     }
     for (int it = 0; it <= nb && nb > 0; ++it) {
@@ -338,7 +346,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       lds_sync();   // A
       if (it < nb) put_products(it);
       put_rows(it + 1);
-      load_rows(it + 2);
+      load_rows();
       lds_sync();   // B
     }
     if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;

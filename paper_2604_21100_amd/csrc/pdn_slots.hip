@@ -81,7 +81,8 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
   constexpr int NTHR = DV * 2, NW = DV / 32, MB = DK / 16;
   __shared__ __attribute__((aligned(16))) float sK[DK], sQ[DK], sKt[DK], sLam[CH ? DK : 4];
   __shared__ float sSum[NW];
-  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const SlotWhere where = slot_where(a);
+  const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);
@@ -188,7 +189,8 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   // the token within the block as factors (1 with a per-channel gate), write strength,
   // preconditioner gain and decay
   __shared__ __attribute__((aligned(16))) float sg[kSlotBlock], sGp[kSlotBlock], sTo[kSlotBlock], sOn[kSlotBlock], sB[kSlotBlock], sBp[kSlotBlock], sDp[kSlotBlock];
-  const int64_t seq = blockIdx.x / a.H, h = blockIdx.x % a.H, hk = h / (a.H / a.Hk);
+  const SlotWhere where = slot_where(a);
+  const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
   const SlotRows rows = slot_rows(a, seq);
@@ -281,15 +283,9 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       for (int x = 0; x < NGP; ++x) put(sG, rg[x], x, GP, DK * 4, LD * 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) vv[i] = vn[i];
+    float to, on;
+    block_sums(s_g, tid, &to, &on);
     if (tid < kSlotBlock) {
-      const float nx = __shfl_down(s_g, 1, kSlotBlock);
-      float to = s_g, on = tid + 1 < kSlotBlock ? nx : 0.f;
-#pragma unroll
-      for (int off = 1; off < kSlotBlock; off <<= 1) {
-        const float y = __shfl_up(to, off, kSlotBlock), z = __shfl_down(on, off, kSlotBlock);
-        if (tid >= off) to += y;
-        if (tid + off < kSlotBlock) on += z;
-      }
       sg[tid] = s_g;
       sTo[tid] = fast_exp(to);
       sOn[tid] = fast_exp(on);

@@ -2,6 +2,8 @@
 // pdn_slot_runs.hip).
 #pragma once
 
+#include <type_traits>
+
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 #include "pdn_tile.hpp"
@@ -23,6 +25,16 @@ __device__ __forceinline__ void st2(T* p, float x, float y) {
   v[0] = from_f<T>(x);
   v[1] = from_f<T>(y);
   *reinterpret_cast<typename Vec2<T>::type*>(p) = v;
+}
+
+// A workgroup's sequence, value head and key head (B H is below 2^22; divided in 32
+// bits, as 64 take hundreds of instructions).
+struct SlotWhere {
+  int64_t seq, h, hk;
+};
+__device__ __forceinline__ SlotWhere slot_where(const SlotArgs& a) {
+  const uint32_t H = static_cast<uint32_t>(a.H), seq = blockIdx.x / H, h = blockIdx.x - seq * H;
+  return SlotWhere{seq, h, h / (H / static_cast<uint32_t>(a.Hk))};
 }
 
 // The rows of a sequence: n of the packed tensors, from lo.  What `starts`
@@ -47,6 +59,27 @@ constexpr int kSlotBlock = 8;   // tokens of a block
 // in fp32, and so is every decay over such a token; a sum that held a value far
 // below, an infinity above all, would have lost the tokens after it.  (NaN stays.)
 __device__ __forceinline__ float sum_decay(float g) { return g < -128.f ? -128.f : g; }
+
+// Of a block's log-decays, one in each of the first eight lanes: the sum up to a lane's
+// own, and of those after it.
+__device__ __forceinline__ void block_sums(float g, int l, float* to, float* on) {
+  auto moved = [](float x, auto ctrl) {   // from another of 16 lanes, past their ends zero
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  auto down = [&](float x, auto n) { return moved(x, std::integral_constant<int, 0x100 + decltype(n)::value>{}); };   // lane + n
+  auto up = [&](float x, auto n) { return moved(x, std::integral_constant<int, 0x110 + decltype(n)::value>{}); };     // lane - n
+  constexpr std::integral_constant<int, 1> one;
+  constexpr std::integral_constant<int, 2> two;
+  constexpr std::integral_constant<int, 4> four;
+  const float x = l < kSlotBlock ? g : 0.f;
+  float p = x, s = down(x, one);
+  p += up(p, one);
+  s += down(s, one);
+  p += up(p, two);
+  s += down(s, two);
+  *to = p + up(p, four);
+  *on = s + down(s, four);
+}
 
 // A head's state, seen through a buffer: a lane's rows are then one offset and
 // constants, where pointers to them would take two registers each.
@@ -101,6 +134,14 @@ __device__ __forceinline__ float buf_get(__amdgpu_buffer_rsrc_t r, int off) {
     return __builtin_bit_cast(float, static_cast<uint32_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0)) << 16);
   else
     return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+}
+
+template <typename T>
+__device__ __forceinline__ void buf_put(__amdgpu_buffer_rsrc_t r, int off, float x) {
+  if constexpr (sizeof(T) == 2)
+    __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, from_f<T>(x)), r, off, 0, 0);
+  else
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, x), r, off, 0, 0);
 }
 
 // whether a write key takes a factor that the sum m = k . kt gives, and that factor
