@@ -148,11 +148,13 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
 #pragma unroll
           for (int m = 0; m < MB; ++m) mma4(S.t[m], (CH ? s.Kw[u] : s.Kt[u])[4 * j + lg][16 * m + lr], ej);
         }
-        settled(S.t);
         // ---- O: rows 8-15 of the products, plus P E
         if (lr < B || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+        // (the state's products are behind it too: its next use is a step away)
+#pragma unroll
+        for (int m = 0; m < MB; ++m) asm volatile("" : "+v"(S.t[m]));
         settled(yz);
         const __amdgpu_buffer_rsrc_t r = next(ro, left);
         left -= B;
@@ -330,16 +332,21 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       }
       s.LP[r][x] = r < B ? (x < t ? tok[3][t] * v : 0.f) : (x <= t ? v : 0.f);
     };
-    if (nb > 0) {
-      load_rows();
-      put_rows(0);
-      // A has been loaded too.  Said outright (vmcnt 0), or the compiler waits for it, and
-      // with it for the loads just issued, each time round the loop.
-      __builtin_amdgcn_s_waitcnt(0x0f70);
-      load_rows();
-      lds_sync();
+    auto store_A = [&]() {
+      if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+    };
+    if (nb == 0) {   // (by itself: see below)
+      store_A();
+      return;
     }
-    for (int it = 0; it <= nb && nb > 0; ++it) {
+    load_rows();
+    put_rows(0);
+    // A has been loaded too.  Said outright (vmcnt 0), and on every way into the loop, or
+    // the compiler waits for it, and with it for the loads just issued, each time round.
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    load_rows();
+    lds_sync();
+    for (int it = 0; it <= nb; ++it) {
       if (it > 0 && pw >= 2) put_lp(it - 1);
       if (it < nb) put_operands(it);
       else if (sums) lds_sync();
@@ -349,7 +356,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
       load_rows();
       lds_sync();   // B
     }
-    if (gram && key) a.A[(dst * a.H + h) * DK + c] = A;
+    store_A();
   }
 }
 
