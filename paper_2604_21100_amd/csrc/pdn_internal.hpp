@@ -263,13 +263,18 @@ hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s);
 // More tokens than a block of pdn_slots.hip go in chunks of 32 on the bf16
 // matrix instructions (pdn_slot_chunks.hip), where queries and keys are bf16
 // numbers as they enter the products (no per-channel decay on them) and a write key
-// needs no sum over its channels.
+// needs no sum over its channels.  Heads of 128 x 128, us, a block of at most eight |
+// these chunks | runs of blocks (pdn_slot_runs.hip):
+//            SQUASH  16 heads       256 heads      1024 heads     k~ = k, 1024 heads
+//   8 tokens    9.1  11.0   9.7   12.2 14.6 12.5   34  56  50     33 47 46
+//   9 tokens    -    10.6  13.0   -    14.0 16.0   -   54  63     -  46 59
+//   32 tokens   -    10.7  19.8   -    15.1 23.8   -   58  91     -  49 87
 inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
   return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.knorm == kKnormNone &&
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
 }
 hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);
-// Other runs of more than a block (pdn_slot_runs.hip).
+// Other runs of more than a block (pdn_slot_runs.hip; blocks: the table above).
 hipError_t launch_slot_runs(const SlotArgs& a, int io_bf16, hipStream_t s);
 
 // Verification of drafted tokens (pdn_verify.hip).

@@ -1,16 +1,17 @@
-// The gated delta rule over packed sequences whose states live in slots of a
-// pool: decoding, drafted tokens that are scored without moving the state, and
-// the prompts pdn_slot_chunks.hip does not take.  Per sequence and value head, with
-// S^T the state and G the inclusive prefix of the log-decay over a block of up
-// to eight tokens (lam = exp(G)):
+// The gated delta rule over packed sequences whose states live in slots of a pool:
+// single tokens (slot_step), two to eight tokens and drafted ones, which are scored
+// without moving the state (slot_blocks).  Longer runs are pdn_slot_chunks.hip's and
+// pdn_slot_runs.hip's.  Per sequence and value head, with S^T the state and G the
+// inclusive prefix of the log-decay over a block of up to eight tokens (lam = exp(G)):
 //   L[t][s] = beta_t k_t Lam_t/Lam_s . kt_s  (s < t)    P[t][s] = q_t Lam_t/Lam_s . kt_s  (s <= t)
 //   X = Diag(beta) (V - Diag(lam) K S^T)                E = (I + L)^{-1} X
 //   O = scale (Diag(lam) Q S^T + P E)                   S'^T = lam_C S^T + Kt^T Diag(lam_C / lam) E
 // All of it in fp32: states, operands and products (the fp32 matrix
 // instruction), so a state comes out as exact as a token-by-token one.
 //
-// A workgroup holds one head's state in registers: a wave 16 or 32 columns of it,
-// a lane the rows 16 m + 4 (l / 16) + i of its one or two.  That is at once the accumulator layout of the update (16 x 16 tiles of S^T)
+// A workgroup holds one head's state in registers: a wave 16 or 32 columns of it, a
+// lane the rows 16 m + 4 (l / 16) + i of its one or two.  That is at once the
+// accumulator layout of the update (16 x 16 tiles of S^T)
 // and, contracted in the order (m, i), the right operand of the products with
 // S^T, so the state goes from one block to the next without leaving its
 // registers.  The left operand of those products stacks the eight key rows
@@ -75,7 +76,12 @@ __device__ __forceinline__ float write_key(const SlotArgs& a, float k, float x, 
 }
 // ---------------------------------------------------------------- one token
 //   S' = alpha S + e kt^T,  e = beta (v - (alpha S) k),  o = scale ((alpha S) q + (kt . q) e)
-// on the vector unit; what bounds it is reading and writing the state.
+// on the vector unit: six operations a state element, which no matrix instruction
+// would make fewer.  What bounds it is reading and writing the state, so the rest is
+// kept small: 104 registers and 2 KB of LDS, four workgroups a compute unit, the
+// loads of some in flight beside the work of others (64 sequences x 16 heads of 128 x
+// 128: 26 us, 5.2 TB/s; 256 x 32: 214 us, 5.0 TB/s; a 1 GiB copy makes 5.1).  One
+// sequence of 16 heads: 6 us, a launch and four dependent memory latencies.
 template <typename T, int DK, int DV, bool CH>
 __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
   constexpr int NTHR = DV * 2, NW = DV / 32, MB = DK / 16;
@@ -170,6 +176,14 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
 // the state is on its way: a block's rows (16 bytes a thread), from them L and
 // P, and the accepted records.  A wave has 16 columns here, a lane one (with two,
 // the state and the rest of it take more registers than there are).
+//
+// What bounds it is the chain of a workgroup, of which a compute unit holds two: rows,
+// L and P (two barriers), the state's arrival, records, products, solve.  Drafts of
+// 64 sequences x 16 heads: 44 us for 152 MB, 3.5 TB/s; 96 x 16 of four tokens with
+// per-channel decays 62 us, 3.5 TB/s; five tokens of one sequence 10 us.  Eight
+// tokens of 64 x 16 heads without a tape 34 us.  (With pending counts read ahead of
+// the rows drafts took 45 and 64 us; with a register budget for three workgroups
+// the state spills.)
 template <typename T, int DK, int DV, bool CH, bool DRAFT>
 __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -14,6 +14,12 @@
 // then one workgroup a sequence finds the segment, and in it the token.
 // Segment sums are added in one order, so the token does not depend on which
 // workgroup was first.
+//
+// What bounds it: the row's (or two rows') reading in the first launch, 14 us for 64
+// sequences of 131072 (56 MB, 4 TB/s), and two launches' latency: the second is one
+// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.5 us, 64 of
+// 131072: 20 us.  A whole workgroup a sequence in the second, with barriers between
+// its levels, took 16 and 30 us in all.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 
