@@ -12,6 +12,7 @@ from __future__ import annotations
 import ctypes
 import functools
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpdn.so")
@@ -144,8 +145,7 @@ _lib.pdn_chunk_fwd_noalloc.argtypes = [
     _vp]
 _lib.pdn_chunk_fwd_noalloc.restype = ctypes.c_int
 for _f in (_lib.pdn_slot_fwd, _lib.pdn_slot_draft):
-    _f.argtypes = [ctypes.POINTER(Problem), ctypes.POINTER(Inputs),
-                   ctypes.POINTER(Slots), _vp, _vp]
+    _f.argtypes = [_vp] * 5   # (the structures by reference, or their bytes)
     _f.restype = ctypes.c_int
 _lib.pdn_draft_verify.argtypes = [ctypes.c_int64, ctypes.c_int64,
                                   ctypes.c_int64, ctypes.c_int, *[_vp] * 9,
@@ -454,30 +454,44 @@ def pdn_chunk_bwd(q, k, v, beta, dO, *, g=None, gate="none", precond="squash",
 
 
 # ------------------------------------------------------- states in a pool
+# These calls run once a token, so the binding's own time counts: a structure's
+# bytes are packed in one step, and a tensor that is as it has to be is looked
+# at once (a decode call takes 14 us of the host, 3.4 of them the library's).
+def _packer(cls):
+    codes = {ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f", _vp: "P"}
+    s = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
+    assert s.size == ctypes.sizeof(cls)
+    return s.pack
+
+
+_pack_problem, _pack_inputs, _pack_slots = _packer(Problem), _packer(Inputs), _packer(Slots)
+
+
 def _on(name, t, device, dtype, shape):
-    """Pointer of a dense tensor of this dtype and shape on `device` (None: NULL)."""
+    """Address of a dense tensor of this dtype and shape on `device` (None: 0)."""
     if t is None:
-        return None
+        return 0
+    if (t.dtype is dtype and t.shape == shape and t.device == device
+            and t.is_contiguous()):
+        return t.data_ptr()
+    _check_on(name, t, device, dtype, shape)
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _check_on(name, t, device, dtype, shape):
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, not on {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
 
 
 def _token_rows(name, t, device, dtype, shape):
-    """A [tokens, heads, d] tensor with dense rows: its pointer and the elements
+    """A [tokens, heads, d] tensor with dense rows: its address and the elements
     from one token to the next (0: dense)."""
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {shape}, got {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
+    if not (t.dtype is dtype and t.shape == shape and t.device == device):
+        _check_on(name, t, device, dtype, shape)
     if t.is_contiguous():
         return t.data_ptr(), 0
     s0, s1, s2 = t.stride()
@@ -501,7 +515,7 @@ def _call_on(device, stream, fn, *args):
         raw = torch._C._cuda_getCurrentRawStream(device.index)
     else:
         raw = stream.cuda_stream
-    if torch.cuda.current_device() == device.index:
+    if torch._C._cuda_getDevice() == device.index:
         return fn(*args, raw)
     with torch.cuda.device(device):
         return fn(*args, raw)
@@ -529,31 +543,31 @@ def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
     T = max_tokens
     if T is None:   # without starts: rows shared out evenly
         T = M if starts is not None else M // N if N else 0
-    prob = Problem(N, T, H, dk, dv, 64, PDN_BF16 if _io_of(q) == "bf16" else PDN_F32,
-                   GATES[gate], PRECONDS[precond], x, scale, ridge, KNORMS[knorm])
     qp, qs = _token_rows("q", q, dev, dt, (M, Hk, dk))
     kp, ks = _token_rows("k", k, dev, dt, (M, Hk, dk))
     vp, vs = _token_rows("v", v, dev, dt, (M, H, dv))
     if o is None:
         o = _empty((M, H, dv), dt, dev, stream)
     scalars, seqs = (M, H), (N,)
-    inp = Inputs(qp, kp, vp, _on("beta", beta, dev, f32, scalars),
-                 _on("g", g, dev, f32, (M, H, dk) if gate == "channel" else scalars),
-                 _on("beta_p", beta_p, dev, f32, scalars),
-                 _on("g_p", g_p, dev, f32, scalars),
-                 _on("log_a_scale", log_a_scale, dev, f32, (H,)),
-                 None, None, _on("ktilde", ktilde, dev, dt, (M, Hk, dk)))
-    sl = Slots(M, P, Hk, qs, ks, vs, _on("starts", starts, dev, i32, (N + 1,)),
-               _on("slots", slots, dev, i32, seqs),
-               _on("slots_out", slots_out, dev, i32, seqs),
-               _on("fresh", fresh, dev, i32, seqs), _on("S", S, dev, f32, S.shape),
-               _on("A", A, dev, f32, (P, H, dk)))
+    prob = _pack_problem(N, T, H, dk, dv, 64, PDN_BF16 if _io_of(q) == "bf16" else PDN_F32,
+                         GATES[gate], PRECONDS[precond], x, scale, ridge, KNORMS[knorm])
+    inp = _pack_inputs(qp, kp, vp, _on("beta", beta, dev, f32, scalars),
+                       _on("g", g, dev, f32, (M, H, dk) if gate == "channel" else scalars),
+                       _on("beta_p", beta_p, dev, f32, scalars),
+                       _on("g_p", g_p, dev, f32, scalars),
+                       _on("log_a_scale", log_a_scale, dev, f32, (H,)),
+                       0, 0, _on("ktilde", ktilde, dev, dt, (M, Hk, dk)))
+    records = 0
     if tape is not None:
-        sl.tape = _on("tape", tape, dev, f32,
-                      (P, tape.shape[1], H, pdn_tape_record(dk, dv, gate, precond)))
-        sl.tape_tokens = tape.shape[1]
-        sl.pending = _on("pending", pending, dev, i32, (P, H))
-        sl.accepted = _on("accepted", accepted, dev, i32, seqs)
+        records = tape.shape[1]
+        tape = _on("tape", tape, dev, f32, (P, records, H, pdn_tape_record(dk, dv, gate, precond)))
+        pending = _on("pending", pending, dev, i32, (P, H))
+        accepted = _on("accepted", accepted, dev, i32, seqs)
+    sl = _pack_slots(M, P, Hk, qs, ks, vs, _on("starts", starts, dev, i32, (N + 1,)),
+                     _on("slots", slots, dev, i32, seqs),
+                     _on("slots_out", slots_out, dev, i32, seqs),
+                     _on("fresh", fresh, dev, i32, seqs), _on("S", S, dev, f32, S.shape),
+                     _on("A", A, dev, f32, (P, H, dk)), tape or 0, records, pending or 0, accepted or 0)
     st = _call_on(dev, stream, fn, prob, inp, sl, _on("o", o, dev, dt, (M, H, dv)))
     if st != PDN_OK:
         raise PdnError(st, where)
