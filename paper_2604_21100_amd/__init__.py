@@ -10,9 +10,7 @@ fails loudly if the library has not been built.
 from __future__ import annotations
 
 import ctypes
-import functools
 import os
-import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpdn.so")
@@ -34,6 +32,12 @@ try:
 except ImportError:   # no torch: the C ABI alone, nothing else maps HIP
     torch = None
 _lib = ctypes.CDLL(LIB_PATH)
+if torch is not None:
+    try:
+        from . import _pdn_torch
+    except ImportError as e:
+        raise ImportError(f"_pdn_torch is missing or was built for another "
+                          f"torch ({e}): build it with the library") from e
 
 
 def loaded_hip_runtimes():
@@ -454,124 +458,35 @@ def pdn_chunk_bwd(q, k, v, beta, dO, *, g=None, gate="none", precond="squash",
 
 
 # ------------------------------------------------------- states in a pool
-# These calls run once a token, so the binding's own time counts: a structure's
-# bytes are packed in one step, and a tensor that is as it has to be is looked
-# at once (a decode call takes 14 us of the host, 3.4 of them the library's).
-def _packer(cls):
-    codes = {ctypes.c_int64: "q", ctypes.c_int32: "i", ctypes.c_float: "f", _vp: "P"}
-    s = struct.Struct("@" + "".join(codes[t] for _, t in cls._fields_) + "0q")
-    assert s.size == ctypes.sizeof(cls)
-    return s.pack
+# These calls run once a token, so checks and marshalling are compiled
+# (csrc/pdn_torch.cpp): a decode call takes the host 7 us, the launch included.
+def _address(fn):
+    return ctypes.cast(fn, _vp).value
 
 
-_pack_problem, _pack_inputs, _pack_slots = _packer(Problem), _packer(Inputs), _packer(Slots)
+_SLOT_FWD, _SLOT_DRAFT, _VERIFY, _VERIFY_SIZE = map(_address, (
+    _lib.pdn_slot_fwd, _lib.pdn_slot_draft, _lib.pdn_draft_verify,
+    _lib.pdn_draft_verify_workspace_size))
 
 
-def _on(name, t, device, dtype, shape):
-    """Address of a dense tensor of this dtype and shape on `device` (None: 0)."""
-    if t is None:
-        return 0
-    if (t.dtype is dtype and t.shape == shape and t.device == device
-            and t.is_contiguous()):
-        return t.data_ptr()
-    _check_on(name, t, device, dtype, shape)
-    raise ValueError(f"{name} must be contiguous")
-
-
-def _check_on(name, t, device, dtype, shape):
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not on {device}")
-
-
-def _token_rows(name, t, device, dtype, shape):
-    """A [tokens, heads, d] tensor with dense rows: its address and the elements
-    from one token to the next (0: dense)."""
-    if not (t.dtype is dtype and t.shape == shape and t.device == device):
-        _check_on(name, t, device, dtype, shape)
-    if t.is_contiguous():
-        return t.data_ptr(), 0
-    s0, s1, s2 = t.stride()
-    if s2 != 1 or s1 != shape[2] and shape[1] > 1:
-        raise ValueError(f"a token's row of {name} must be dense")
-    return t.data_ptr(), s0
-
-
-def _empty(shape, dtype, device, stream):
-    """A new tensor, of `stream`'s memory where one is named: what is freed while
-    a call runs goes to that stream's next tensors, not to another's."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
-
-
-def _call_on(device, stream, fn, *args):
-    """fn(*args, stream) with `device` current."""
-    if stream is None:
-        raw = torch._C._cuda_getCurrentRawStream(device.index)
+def _call_on(where, device, stream, fn, *args):
+    """fn(*args, stream) with `device` current, and `stream` too where one is
+    named: what the call allocates is then that stream's memory, and what is
+    freed while it runs goes to that stream's next tensors, not to another's."""
+    if stream is not None:
+        if stream.device != device:
+            raise ValueError(f"the stream is on {stream.device}, not on {device}")
+        with torch.cuda.stream(stream):
+            out = fn(*args, stream.cuda_stream)
+    elif device.type != "cuda" or torch._C._cuda_getDevice() == device.index:
+        out = fn(*args, torch._C._cuda_getCurrentRawStream(device.index or 0)
+                 if device.type == "cuda" else 0)
     else:
-        raw = stream.cuda_stream
-    if torch._C._cuda_getDevice() == device.index:
-        return fn(*args, raw)
-    with torch.cuda.device(device):
-        return fn(*args, raw)
-
-
-def _slot_call(fn, where, q, k, v, beta, S, tape, pending, accepted, *, starts,
-               slots, slots_out, fresh, max_tokens, g, gate, precond, beta_p,
-               g_p, log_a_scale, A, ktilde, x, scale, ridge, knorm, o, stream):
-    if S.dim() != 4 or q.dim() != 3 or v.dim() != 3:
-        raise ValueError("S must be [slots, H, dk, dv], q, k [tokens, Hk, dk] "
-                         "and v [tokens, H, dv]")
-    P, H, dk, dv = S.shape
-    M, Hk, _ = q.shape
-    dev, f32, i32, dt = S.device, torch.float32, torch.int32, q.dtype
-    if dev.type != "cuda":
-        raise ValueError(f"S is on {dev}")
-    if starts is not None:
-        N = starts.numel() - 1
-        if N < 0:
-            raise ValueError("starts must hold one entry more than sequences")
-    elif slots is not None:
-        N = slots.numel()
-    else:
-        N = M // max_tokens if max_tokens else M
-    T = max_tokens
-    if T is None:   # without starts: rows shared out evenly
-        T = M if starts is not None else M // N if N else 0
-    qp, qs = _token_rows("q", q, dev, dt, (M, Hk, dk))
-    kp, ks = _token_rows("k", k, dev, dt, (M, Hk, dk))
-    vp, vs = _token_rows("v", v, dev, dt, (M, H, dv))
-    if o is None:
-        o = _empty((M, H, dv), dt, dev, stream)
-    scalars, seqs = (M, H), (N,)
-    prob = _pack_problem(N, T, H, dk, dv, 64, PDN_BF16 if _io_of(q) == "bf16" else PDN_F32,
-                         GATES[gate], PRECONDS[precond], x, scale, ridge, KNORMS[knorm])
-    inp = _pack_inputs(qp, kp, vp, _on("beta", beta, dev, f32, scalars),
-                       _on("g", g, dev, f32, (M, H, dk) if gate == "channel" else scalars),
-                       _on("beta_p", beta_p, dev, f32, scalars),
-                       _on("g_p", g_p, dev, f32, scalars),
-                       _on("log_a_scale", log_a_scale, dev, f32, (H,)),
-                       0, 0, _on("ktilde", ktilde, dev, dt, (M, Hk, dk)))
-    records = 0
-    if tape is not None:
-        records = tape.shape[1]
-        tape = _on("tape", tape, dev, f32, (P, records, H, pdn_tape_record(dk, dv, gate, precond)))
-        pending = _on("pending", pending, dev, i32, (P, H))
-        accepted = _on("accepted", accepted, dev, i32, seqs)
-    sl = _pack_slots(M, P, Hk, qs, ks, vs, _on("starts", starts, dev, i32, (N + 1,)),
-                     _on("slots", slots, dev, i32, seqs),
-                     _on("slots_out", slots_out, dev, i32, seqs),
-                     _on("fresh", fresh, dev, i32, seqs), _on("S", S, dev, f32, S.shape),
-                     _on("A", A, dev, f32, (P, H, dk)), tape or 0, records, pending or 0, accepted or 0)
-    st = _call_on(dev, stream, fn, prob, inp, sl, _on("o", o, dev, dt, (M, H, dv)))
-    if st != PDN_OK:
-        raise PdnError(st, where)
-    return o
+        with torch.cuda.device(device):
+            out = fn(*args, torch._C._cuda_getCurrentRawStream(device.index))
+    if type(out) is int:
+        raise PdnError(out, where)
+    return out
 
 
 def pdn_tape_record(dk, dv, gate="none", precond="squash") -> int:
@@ -593,12 +508,11 @@ def pdn_slot_fwd(q, k, v, beta, S, *, starts=None, slots=None, slots_out=None,
     int32 on the device.  Without starts the rows are shared evenly
     by the sequences (one row each without slots too).  max_tokens: the most
     rows a sequence has (default: unknown, at most all).  Returns o."""
-    return _slot_call(
-        _lib.pdn_slot_fwd, "pdn_slot_fwd", q, k, v, beta, S, None, None, None,
-        starts=starts, slots=slots, slots_out=slots_out, fresh=fresh,
-        max_tokens=max_tokens, g=g, gate=gate, precond=precond, beta_p=beta_p,
-        g_p=g_p, log_a_scale=log_a_scale, A=A, ktilde=ktilde, x=x, scale=scale,
-        ridge=ridge, knorm=knorm, o=o, stream=stream)
+    return _call_on(
+        "pdn_slot_fwd", S.device, stream, _pdn_torch.slot, _SLOT_FWD, q, k, v,
+        beta, S, None, None, None, 0, starts, slots, slots_out, fresh,
+        max_tokens, g, GATES[gate], PRECONDS[precond], beta_p, g_p,
+        log_a_scale, A, ktilde, x, scale, ridge, KNORMS[knorm], o)
 
 
 def pdn_slot_draft(q, k, v, beta, S, tape, pending, *, accepted=None,
@@ -618,15 +532,14 @@ def pdn_slot_draft(q, k, v, beta, S, tape, pending, *, accepted=None,
         raise ValueError("tape must be [slots, tokens, H, record]")
     if max_tokens is None and starts is not None:
         max_tokens = tape.shape[1]
-    return _slot_call(
-        _lib.pdn_slot_draft, "pdn_slot_draft", q, k, v, beta, S, tape, pending,
-        accepted, starts=starts, slots=slots, slots_out=slots_out, fresh=fresh,
-        max_tokens=max_tokens, g=g, gate=gate, precond=precond, beta_p=beta_p,
-        g_p=g_p, log_a_scale=log_a_scale, A=A, ktilde=ktilde, x=x, scale=scale,
-        ridge=ridge, knorm=knorm, o=o, stream=stream)
+    return _call_on(
+        "pdn_slot_draft", S.device, stream, _pdn_torch.slot, _SLOT_DRAFT, q, k,
+        v, beta, S, tape, pending, accepted,
+        pdn_tape_record(*S.shape[-2:], gate, precond), starts, slots,
+        slots_out, fresh, max_tokens, g, GATES[gate], PRECONDS[precond],
+        beta_p, g_p, log_a_scale, A, ktilde, x, scale, ridge, KNORMS[knorm], o)
 
 
-@functools.lru_cache(maxsize=256)
 def pdn_draft_verify_workspace_size(N: int, V: int) -> int:
     n = ctypes.c_size_t(0)
     st = _lib.pdn_draft_verify_workspace_size(N, V, ctypes.byref(n))
@@ -643,29 +556,6 @@ def pdn_draft_verify(p, ids, u, r, *, q=None, starts=None, accepted=None,
     p, q: [rows, V], fp32 or bf16; ids [rows] int32, the tokens fed; u [rows],
     r [N] fp32 in [0, 1).  Returns (accepted, token), int32 [N]: the rows that hold
     (what pdn_slot_draft applies) and the token after them."""
-    if p.dim() != 2:
-        raise ValueError("p must be [rows, V]")
-    M, V = p.shape
-    N, dev, f32, i32 = r.numel(), p.device, torch.float32, torch.int32
-    if dev.type != "cuda":
-        raise ValueError(f"p is on {dev}")
-    io = PDN_BF16 if _io_of(p) == "bf16" else PDN_F32
-    if accepted is None:
-        accepted = _empty((N,), i32, dev, stream)
-    if token is None:
-        token = _empty((N,), i32, dev, stream)
-    if workspace is None:
-        workspace = _empty((pdn_draft_verify_workspace_size(N, V),),
-                           torch.uint8, dev, stream)
-    rows, seqs = (M,), (N,)
-    st = _call_on(
-        dev, stream, _lib.pdn_draft_verify, N, M, V, io, _on("p", p, dev, p.dtype, p.shape),
-        _on("q", q, dev, p.dtype, p.shape), _on("ids", ids, dev, i32, rows),
-        _on("u", u, dev, f32, rows), _on("r", r, dev, f32, seqs),
-        _on("starts", starts, dev, i32, (N + 1,)),
-        _on("accepted", accepted, dev, i32, seqs), _on("token", token, dev, i32, seqs),
-        _on("workspace", workspace, dev, torch.uint8, workspace.shape),
-        workspace.numel())
-    if st != PDN_OK:
-        raise PdnError(st, "pdn_draft_verify")
-    return accepted, token
+    return _call_on(
+        "pdn_draft_verify", p.device, stream, _pdn_torch.verify, _VERIFY,
+        _VERIFY_SIZE, p, q, ids, u, r, starts, accepted, token, workspace)
