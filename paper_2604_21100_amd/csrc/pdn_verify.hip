@@ -17,8 +17,8 @@
 //
 // What bounds it: the row's (or two rows') reading in the first launch, 14 us for 64
 // sequences of 131072 (56 MB, 4 TB/s), and two launches' latency: the second is one
-// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.5 us, 64 of
-// 131072: 20 us.  A whole workgroup a sequence in the second, with barriers between
+// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.1 us, 64 of
+// 131072: 19.8 us.  A whole workgroup a sequence in the second, with barriers between
 // its levels, took 16 and 30 us in all.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
@@ -166,8 +166,22 @@ template <typename T>
 __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
   constexpr int PER = kSeg / kWave;
   const int64_t segs = segments(a.V), seq = blockIdx.x;
-  const Span s = seq_span(a, seq);
   const int l = threadIdx.x;
+  // Everything that can be read at once is, before the first of it is waited for (a
+  // sequence without rows has no sums, and does not use what is read here).
+  const double* const sums = a.sums + seq * segs * 2;
+  int64_t n = 0;
+  double r = 0.0, x[2], cum[2];
+  auto load_sums = [&](int64_t b) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) x[k] = b + l < segs ? sums[2 * (b + l) + k] : 0.0;
+  };
+  if (a.rows > 0) {
+    n = a.accepted[seq] - 1;
+    r = a.r[seq];
+    load_sums(0);
+  }
+  const Span s = seq_span(a, seq);
   if (s.n == 0) {   // no rows
     if (l == 0) {
       a.accepted[seq] = 0;
@@ -175,17 +189,11 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
     }
     return;
   }
-  const double* sums = a.sums + seq * segs * 2;
-  const int64_t n = a.accepted[seq] - 1;
-  const double r = a.r[seq];
   // running sums of 64 segments, of both kinds
-  double x[2], cum[2];
   auto sum_segments = [&](int64_t b, const double (&base)[2]) {
+    if (segs > kWave) load_sums(b);   // (else they are at hand)
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      x[k] = b + l < segs ? sums[2 * (b + l) + k] : 0.0;
-      cum[k] = base[k] + wave_scan(x[k], l);
-    }
+    for (int k = 0; k < 2; ++k) cum[k] = base[k] + wave_scan(x[k], l);
   };
   double tot[2] = {0.0, 0.0};
   for (int64_t b = 0; b < segs; b += kWave) {

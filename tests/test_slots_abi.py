@@ -118,3 +118,26 @@ def test_verify_refusals():
 def test_record_size():
     assert pdn.pdn_tape_record(128, 64, "scalar", "identity") == 128 + 64 + 4
     assert pdn.pdn_tape_record(128, 64, "channel", "squash") == 3 * 128 + 64
+
+
+def test_host_tensors_are_refused():
+    """The compiled part of the binding, without a GPU: what it says of tensors on the
+    host, of wrong kinds and dimensions."""
+    torch = pytest.importorskip("torch")
+    z = torch.zeros
+    rows, S = z(4, 2, 64), z(4, 2, 64, 64)
+    good = dict(q=rows, k=rows, v=rows, beta=z(4, 2), S=S)
+    for bad, err in ((dict(), ValueError), (dict(S=S[0]), ValueError), (dict(q=rows[0]), ValueError),
+                     (dict(q=None), TypeError), (dict(v=[1.0]), TypeError)):
+        a = dict(good, **bad)
+        with pytest.raises(err):
+            pdn.pdn_slot_fwd(a["q"], a["k"], a["v"], a["beta"], a["S"], precond="identity")
+        with pytest.raises(err):
+            pdn.pdn_slot_draft(a["q"], a["k"], a["v"], a["beta"], a["S"], z(4, 1, 2, 132), z(4, 2, dtype=torch.int32),
+                               precond="identity")
+    with pytest.raises(KeyError):
+        pdn.pdn_slot_fwd(rows, rows, rows, z(4, 2), S, precond="none of them")
+    i = z(4, dtype=torch.int32)
+    for p, err in ((z(4, 9), ValueError), (z(4), ValueError), (None, (TypeError, AttributeError))):
+        with pytest.raises(err):
+            pdn.pdn_draft_verify(p, i, z(4), z(2))
