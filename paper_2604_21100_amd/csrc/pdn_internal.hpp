@@ -274,6 +274,17 @@ inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
 }
 hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);
+// Heads of 128 columns in two workgroups, half the columns each, where there is a
+// compute unit for every one of them (a workgroup has one to itself) and no
+// preconditioner state (read and written in place it has to be one workgroup's).
+// 512 tokens, k~ = k, us, whole | halves:
+//   heads                     16       128       160       256
+//   chunks, scalar gate     60 46     67  56    69 100    76 109
+//   runs, per-channel      210 155   217 165   220 235   231 252
+//   runs, fp32             201 147   211 158   215 228   218 237
+inline bool slot_halves(const SlotArgs& a) {
+  return a.dv == 128 && !has_gram(a.precond) && a.B * a.H <= 128;
+}
 // Other runs of more than a block (pdn_slot_runs.hip; blocks: the table above).
 hipError_t launch_slot_runs(const SlotArgs& a, int io_bf16, hipStream_t s);
 

@@ -30,8 +30,6 @@
 // Measured and not kept: 32 columns a wave (217 against 178 us: too few waves hide
 // the chain), tokens shared unevenly among the producers to even out their time (171
 // to 172 us), the remainders x - p[0] by the bf16 dot product (no faster).
-#include <type_traits>
-
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 #include "pdn_slots.hpp"
@@ -85,7 +83,7 @@ __device__ __forceinline__ void mma_parts(floatx4& acc, const bf16x8 (&a)[NA], c
 
 // LDS, byte offsets.  K and Q tiles and per-token numbers four times (the chunk in
 // use, and those one, two and three after it), what is formed from them twice.
-template <int DK, int DV, int NP>
+template <int DK, int NP>
 struct Lay {
   static constexpr int kTile = kC * DK * 2, kMat = kC * kC * 2;
   static constexpr int oK = 0, oQ = oK + 4 * kTile, oX = oQ + 4 * kTile;            // oX: external write keys
@@ -97,14 +95,16 @@ struct Lay {
   static constexpr int total = oS + 4 * kS;
 };
 
-// NP: the write keys' parts, 3 (SQUASH); 1: they are the keys; 0: the caller's
-template <int DK, int DV, int NP>
-__global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
-  using L = Lay<DK, DV, NP>;
-  constexpr int NC = DV / 16, KK = DK / 32, NCH = DK / 8, RK = DK * 2, NT = NP == 3 ? 3 : 1;
+// NP: the write keys' parts, 3 (SQUASH); 1: they are the keys; 0: the caller's.
+// W: the head's columns that a workgroup holds.
+template <int DK, int DV, int NP, int W>
+__global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
+  using L = Lay<DK, NP>;
+  static_assert(W == DV || NP != 3, "a preconditioner state in place is one workgroup's to read and write");
+  constexpr int NC = W / 16, KK = DK / 32, NCH = DK / 8, RK = DK * 2, NT = NP == 3 ? 3 : 1;
   __shared__ __attribute__((aligned(1024))) char smem[L::total];
   lds_char* const sm = (lds_char*)smem;
-  const SlotWhere where = slot_where(a);
+  const SlotWhere where = slot_where(a, DV / W);
   const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
 
   if (w < NC) {
     // ------------------------------------------------------------ consumers
-    const int v0 = 16 * w + m;
+    const int v0 = where.part * W + 16 * w + m;
     floatx4 S[KK][2];
     {
       const float* sp = a.S + (src * a.H + h) * (DK * DV) + 8 * g * DV + v0;
@@ -276,38 +276,35 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
     // A chunk's rows, through registers (16 bytes a lane and piece of a tile) into
     // LDS; those past the sequence's end read as zeros.
     typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-    auto load_tile = [&](int ch, const void* p, int64_t stride, int64_t first, auto width, u32x4* to) {
-      constexpr int W = decltype(width)::value, N = W / 8;
+    auto load_tile = [&](int ch, const void* p, int64_t stride, int64_t first, u32x4* to) {
       const int64_t row = rows.lo + static_cast<int64_t>(ch) * kC;
       const int n = static_cast<int>(min<int64_t>(kC, rows.n - static_cast<int64_t>(ch) * kC));
       const __amdgpu_buffer_rsrc_t r = buf_rsrc(static_cast<const char*>(p) + (row * stride + first) * 2,
-                                                static_cast<uint32_t>(((n - 1) * stride + W) * 2));
+                                                static_cast<uint32_t>(((n - 1) * stride + DK) * 2));
 #pragma unroll
-      for (int x = 0; x < kC * N / 256; ++x) {
+      for (int x = 0; x < kC * NCH / 256; ++x) {
         const uint32_t at = pw * 64 + ll + 256 * x;
-        to[x] = __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(at / N * static_cast<uint32_t>(stride * 2) + at % N * 16), 0, 0);
+        to[x] = __builtin_amdgcn_raw_buffer_load_b128(r, static_cast<int>(at / NCH * static_cast<uint32_t>(stride * 2) + at % NCH * 16), 0, 0);
       }
     };
-    auto put_tile = [&](auto width, const u32x4* from, int o) {
-      constexpr int N = decltype(width)::value / 8;
+    auto put_tile = [&](const u32x4* from, int o) {
 #pragma unroll
-      for (int x = 0; x < kC * N / 256; ++x) {
+      for (int x = 0; x < kC * NCH / 256; ++x) {
         const uint32_t at = pw * 64 + ll + 256 * x;
-        lds_put(sm + o + tile_off<N>(at / N, at % N), __builtin_bit_cast(bf16x8, from[x]));
+        lds_put(sm + o + tile_off<NCH>(at / NCH, at % NCH), __builtin_bit_cast(bf16x8, from[x]));
       }
     };
-    constexpr std::integral_constant<int, DK> wk;
     u32x4 rk[DK / 64], rq[DK / 64], rx[DK / 64];
     auto load_keys = [&](int ch) {
-      load_tile(ch, a.k, a.k_stride, hk * DK, wk, rk);
-      load_tile(ch, a.q, a.q_stride, hk * DK, wk, rq);
-      if (NP == 0) load_tile(ch, a.ktilde, a.Hk * DK, hk * DK, wk, rx);
+      load_tile(ch, a.k, a.k_stride, hk * DK, rk);
+      load_tile(ch, a.q, a.q_stride, hk * DK, rq);
+      if (NP == 0) load_tile(ch, a.ktilde, a.Hk * DK, hk * DK, rx);
     };
     auto put_keys = [&](int ch) {
       const int buf = (ch & 3) * L::kTile;
-      put_tile(wk, rk, L::oK + buf);
-      put_tile(wk, rq, L::oQ + buf);
-      if (NP == 0) put_tile(wk, rx, L::oX + buf);
+      put_tile(rk, L::oK + buf);
+      put_tile(rq, L::oQ + buf);
+      if (NP == 0) put_tile(rx, L::oX + buf);
     };
     // Its per-token numbers, a lane a token: 0 write strength, 1 lam, 2 w, 3 gain
     // and 4 decay of the preconditioner, 5 that decay over a segment, 6 log-decay
@@ -562,11 +559,18 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_chunks(SlotArgs a) {
   }
 }
 
+template <int DK, int DV, int NP, int W>
+hipError_t launch_parts(const SlotArgs& a, hipStream_t st) {
+  static_assert(Lay<DK, NP>::total <= 160 * 1024, "a chunk's operands must fit the LDS of a compute unit");
+  hipLaunchKernelGGL((slot_chunks<DK, DV, NP, W>), dim3(static_cast<unsigned>(a.B * a.H * (DV / W))), dim3(W * 4 + 256), 0, st, a);
+  return hipGetLastError();
+}
+
 template <int DK, int DV, int NP>
 hipError_t launch(const SlotArgs& a, hipStream_t st) {
-  static_assert(Lay<DK, DV, NP>::total <= 160 * 1024, "a chunk's operands must fit the LDS of a compute unit");
-  hipLaunchKernelGGL((slot_chunks<DK, DV, NP>), dim3(static_cast<unsigned>(a.B * a.H)), dim3(DV * 4 + 256), 0, st, a);
-  return hipGetLastError();
+  if constexpr (DV == 128 && NP != 3)
+    if (slot_halves(a)) return launch_parts<DK, DV, NP, 64>(a, st);
+  return launch_parts<DK, DV, NP, DV>(a, st);
 }
 
 template <int NP>

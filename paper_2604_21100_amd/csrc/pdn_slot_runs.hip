@@ -27,9 +27,9 @@ namespace pdn {
 
 namespace {
 
-template <typename T, int DK, int DV, bool CH>
+template <typename T, int DK, int W, bool CH>
 struct Run {
-  static constexpr int LD = DK + 4, NW = DV / 16, LC = CH ? kSlotBlock : 1;
+  static constexpr int LD = DK + 4, NW = W / 16, LC = CH ? kSlotBlock : 1;
   alignas(16) T raw[3][kSlotBlock][DK];              // keys, queries, the caller's write keys
   alignas(16) float g[LC][LD];                       // CH: log-decays
   // operands, of the block in use and the one after it: keys over queries; write
@@ -41,13 +41,15 @@ struct Run {
   alignas(16) float tok[4][6][kSlotBlock];
 };
 
-template <typename T, int DK, int DV, bool CH>
-__global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
+// W: the head's columns that a workgroup holds (half of them: without a preconditioner
+// state, which in place is one workgroup's to read and write)
+template <typename T, int DK, int DV, bool CH, int W>
+__global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-  using R = Run<T, DK, DV, CH>;
+  using R = Run<T, DK, W, CH>;
   constexpr int B = kSlotBlock, NW = R::NW, MB = DK / 16;
   __shared__ R s;
-  const SlotWhere where = slot_where(a);
+  const SlotWhere where = slot_where(a, DV / W);
   const int64_t seq = where.seq, h = where.h, hk = where.hk;
   const int64_t src = a.slot ? a.slot[seq] : seq, dst = a.slot_out ? a.slot_out[seq] : src;
   if (src < 0 || src >= a.slots || dst < 0 || dst >= a.slots) return;
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
 
   if (w < NW) {
     // ------------------------------------------------------------ consumers
-    const int v0 = 16 * w + lr, tb = 4 * (lg & 1), at = 4 * lg * DV + v0;
+    const int v0 = where.part * W + 16 * w + lr, tb = 4 * (lg & 1), at = 4 * lg * DV + v0;
     SlotColumns<DK, DV> S;
     if (fresh) S.zero();
     else S.load(slot_head<DK, DV>(a, src, h), at);
@@ -368,12 +370,22 @@ __global__ __launch_bounds__(DV * 4 + 256) void slot_runs(SlotArgs a) {
   }
 }
 
+template <typename T, int DK, int DV, bool CH>
+hipError_t launch(const SlotArgs& a, hipStream_t s) {
+  const unsigned heads = static_cast<unsigned>(a.B * a.H);
+  if constexpr (DV == 128) {
+    if (slot_halves(a)) {
+      hipLaunchKernelGGL((slot_runs<T, DK, DV, CH, 64>), dim3(2 * heads), dim3(64 * 4 + 256), 0, s, a);
+      return hipGetLastError();
+    }
+  }
+  hipLaunchKernelGGL((slot_runs<T, DK, DV, CH, DV>), dim3(heads), dim3(DV * 4 + 256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int DK, int DV>
 hipError_t launch_gate(const SlotArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.B * a.H)), threads(DV * 4 + 256);
-  if (a.gate == kGateChannel) hipLaunchKernelGGL((slot_runs<T, DK, DV, true>), grid, threads, 0, s, a);
-  else hipLaunchKernelGGL((slot_runs<T, DK, DV, false>), grid, threads, 0, s, a);
-  return hipGetLastError();
+  return a.gate == kGateChannel ? launch<T, DK, DV, true>(a, s) : launch<T, DK, DV, false>(a, s);
 }
 
 template <typename T>

@@ -27,14 +27,16 @@ __device__ __forceinline__ void st2(T* p, float x, float y) {
   *reinterpret_cast<typename Vec2<T>::type*>(p) = v;
 }
 
-// A workgroup's sequence, value head and key head (B H is below 2^22; divided in 32
-// bits, as 64 take hundreds of instructions).
+// A workgroup's sequence, value head, key head and which of the head's `parts` of
+// the columns (B H is below 2^22; divided in 32 bits, as 64 take hundreds of
+// instructions).
 struct SlotWhere {
   int64_t seq, h, hk;
+  int part;
 };
-__device__ __forceinline__ SlotWhere slot_where(const SlotArgs& a) {
-  const uint32_t H = static_cast<uint32_t>(a.H), seq = blockIdx.x / H, h = blockIdx.x - seq * H;
-  return SlotWhere{seq, h, h / (H / static_cast<uint32_t>(a.Hk))};
+__device__ __forceinline__ SlotWhere slot_where(const SlotArgs& a, uint32_t parts = 1) {
+  const uint32_t at = blockIdx.x / parts, H = static_cast<uint32_t>(a.H), seq = at / H, h = at - seq * H;
+  return SlotWhere{seq, h, h / (H / static_cast<uint32_t>(a.Hk)), static_cast<int>(blockIdx.x - at * parts)};
 }
 
 // The rows of a sequence: n of the packed tensors, from lo.  What `starts`

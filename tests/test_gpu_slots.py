@@ -137,6 +137,29 @@ def test_rule(io, gate, precond, knorm, H, Hk, dk, dv, lens):
         assert np.array_equal(got[2][rest], A[rest])
 
 
+@pytest.mark.parametrize("io,gate,precond", [("bf16", "scalar", "identity"), ("bf16", "none", "external"),
+                                              ("bf16", "channel", "identity"), ("f32", "scalar", "external")])
+def test_heads_whole_and_in_halves(io, gate, precond):
+    """129 heads are a workgroup each, 128 two of half the columns: the same values,
+    in place, and with a fork and a new sequence among them."""
+    rng = np.random.default_rng(129)
+    N, H, d, lens = 43, 3, 128, [11 + n % 24 for n in range(43)]
+    b = batch(rng, sum(lens), H, H, d, d, io, gate, precond)
+    S, A = pool(rng, N + 1, H, d, d, precond)
+    src, fresh = list(range(N)), [int(n == 5) for n in range(N)]
+    dst = [N if n == 7 else n for n in range(N)]
+    o, S1, A1, starts = want(b, S, A, lens, gate, precond, src, dst, fresh)
+    whole = run(b, S, A, io, gate, precond, starts=i32(starts), slots=i32(src), slots_out=i32(dst), fresh=i32(fresh),
+                max_tokens=max(lens))
+    check(whole, (o, S1, A1), io, max(lens))
+    n = 42   # 126 heads
+    part = run(b, S, A, io, gate, precond, starts=i32(starts[:n + 1]), slots=i32(src[:n]), slots_out=i32(dst[:n]),
+               fresh=i32(fresh[:n]), max_tokens=max(lens))
+    o[starts[n]:] = np.nan
+    S1[n - N - 1] = S[n - N - 1]
+    check(part, (o, S1, A1), io, max(lens))
+
+
 @pytest.mark.parametrize("T", [1, 6, 50])
 def test_forks_fresh_padding(T):
     """Two sequences read one slot and write others; one is new; one has no
