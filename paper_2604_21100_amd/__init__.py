@@ -507,7 +507,8 @@ def pdn_slot_fwd(q, k, v, beta, S, *, starts=None, slots=None, slots_out=None,
     read and written in place.  starts [N + 1], slots, slots_out, fresh [N]:
     int32 on the device.  Without starts the rows are shared evenly
     by the sequences (one row each without slots too).  max_tokens: the most
-    rows a sequence has (default: unknown, at most all).  Returns o."""
+    rows a sequence has (default: unknown, at most all; worth giving, as one
+    row or a few take leaner kernels).  Returns o."""
     return _call_on(
         "pdn_slot_fwd", S.device, stream, _pdn_torch.slot, _SLOT_FWD, q, k, v,
         beta, S, None, None, None, 0, starts, slots, slots_out, fresh,

@@ -182,8 +182,8 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
 // 64 sequences x 16 heads: 44 us for 152 MB, 3.5 TB/s; 96 x 16 of four tokens with
 // per-channel decays 62 us, 3.5 TB/s; five tokens of one sequence 10 us.  Eight
 // tokens of 64 x 16 heads without a tape 34 us.  (With pending counts read ahead of
-// the rows drafts took 45 and 64 us; with a register budget for three workgroups
-// the state spills.)
+// the rows drafts took 45 and 64 us, with the state first 46 and 66; a third workgroup
+// would leave a lane 80 of the 127 registers that it takes.)
 template <typename T, int DK, int DV, bool CH, bool DRAFT>
 __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
