@@ -9,9 +9,9 @@
 // numbers is exact, and a running sum over a large vocabulary has to be finer
 // than the steps between its tokens, which 32 bits are not.
 //
-// Two launches: the row the sequence stops at is summed in segments of 2048
-// tokens, a workgroup each (every one finds the row for itself: a few reads),
-// then one workgroup a sequence finds the segment, and in it the token.
+// Two launches (one up to 24576 tokens: verify_one): the row the sequence stops at is
+// summed in segments of 2048 tokens, a workgroup each (every one finds the row for
+// itself: a few reads), then one wave a sequence finds the segment, and in it the token.
 // Segment sums are added in one order, so the token does not depend on which
 // workgroup was first.
 //
@@ -161,37 +161,16 @@ __device__ __forceinline__ int first_over(double cum, double x, double target, i
   return over ? __ffsll(over) - 1 : -1;
 }
 
-// A wave a sequence: the segment, 64 at a time, then in it the token, 32 a lane.
-template <typename T>
-__global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
-  constexpr int PER = kSeg / kWave;
-  const int64_t segs = segments(a.V), seq = blockIdx.x;
-  const int l = threadIdx.x;
-  // Everything that can be read at once is, before the first of it is waited for (a
-  // sequence without rows has no sums, and does not use what is read here).
-  const double* const sums = a.sums + seq * segs * 2;
-  int64_t n = 0;
-  double r = 0.0, x[2], cum[2];
-  auto load_sums = [&](int64_t b) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) x[k] = b + l < segs ? sums[2 * (b + l) + k] : 0.0;
-  };
-  if (a.rows > 0) {
-    n = a.accepted[seq] - 1;
-    r = a.r[seq];
-    load_sums(0);
-  }
-  const Span s = seq_span(a, seq);
-  if (s.n == 0) {   // no rows
-    if (l == 0) {
-      a.accepted[seq] = 0;
-      a.token[seq] = -1;
-    }
-    return;
-  }
+// The token, by one wave: the segment (of PER tokens a lane), 64 at a time, then in it
+// the token.  load_sums(b, x): the sums of segment b + l, of both kinds; x holds
+// those of the first 64.
+template <typename T, int PER, typename Load>
+__device__ __forceinline__ void pick(const VerifyArgs& a, int64_t seq, const Span& s, int64_t n, double r, int64_t segs,
+                                     int l, const Load& load_sums, double (&x)[2]) {
+  double cum[2];
   // running sums of 64 segments, of both kinds
   auto sum_segments = [&](int64_t b, const double (&base)[2]) {
-    if (segs > kWave) load_sums(b);   // (else they are at hand)
+    if (segs > kWave) load_sums(b, x);   // (else they are at hand)
 #pragma unroll
     for (int k = 0; k < 2; ++k) cum[k] = base[k] + wave_scan(x[k], l);
   };
@@ -226,7 +205,7 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
     return;
   }
   const Row<T> row = stop_row<T>(a, s, n);
-  const int64_t j0 = seg * kSeg + l * PER;
+  const int64_t j0 = (seg * kWave + l) * PER;
   double v[PER / kVec][kVec], mine = 0.0;
 #pragma unroll
   for (int c = 0; c < PER / kVec; ++c) {
@@ -257,7 +236,94 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
 }
 
 template <typename T>
+__global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
+  const int64_t segs = segments(a.V), seq = blockIdx.x;
+  const int l = threadIdx.x;
+  // Everything that can be read at once is, before the first of it is waited for (a
+  // sequence without rows has no sums, and does not use what is read here).
+  const double* const sums = a.sums + seq * segs * 2;
+  int64_t n = 0;
+  double r = 0.0, x[2];
+  auto load_sums = [&](int64_t b, double (&x)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) x[k] = b + l < segs ? sums[2 * (b + l) + k] : 0.0;
+  };
+  if (a.rows > 0) {
+    n = a.accepted[seq] - 1;
+    r = a.r[seq];
+    load_sums(0, x);
+  }
+  const Span s = seq_span(a, seq);
+  if (s.n == 0) {   // no rows
+    if (l == 0) {
+      a.accepted[seq] = 0;
+      a.token[seq] = -1;
+    }
+    return;
+  }
+  pick<T, kSeg / kWave>(a, seq, s, n, r, segs, l, load_sums, x);
+}
+
+// Vocabularies of up to three steps of it in one launch: a workgroup a sequence, a wave
+// a segment of 512 tokens in turn; sums in LDS, the token by the first wave.  A step of 8192
+// tokens takes 1.5 us of one compute unit, where the other form's first launch has them
+// all and its second costs 4 to 5 us (fp32 with q, us, two launches | one):
+//               1000       8000       16000      24000      32000
+//   1 sequence  10.2  5.4   9.3  6.1   9.2  7.6   9.4  9.0   9.3 10.3
+//   64          11.6  6.0  11.4  6.7  11.6  8.1  12.1  9.5  12.7 11.1
+//   256         12.0  6.3  13.4  7.2  15.8 10.2  19.7 12.1  20.0 14.2
+// (A wave's segments all loaded first: 8.3 us at 1000 tokens, 10.2 at 32000.)
+constexpr int kOneWaves = 16, kOneSeg = kWave * kVec, kOneMost = 3 * kOneWaves * kOneSeg;
+template <typename T>
+__global__ __launch_bounds__(kOneWaves * kWave) void verify_one(VerifyArgs a) {
+  __shared__ double sums[kOneMost / kOneSeg][2];
+  const int64_t seq = blockIdx.x;
+  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, segs = static_cast<int>((a.V + kOneSeg - 1) / kOneSeg);
+  const Span s = a.rows > 0 ? seq_span(a, seq) : Span{0, 0};
+  if (s.n == 0) {   // no rows
+    if (threadIdx.x == 0) {
+      a.accepted[seq] = 0;
+      a.token[seq] = -1;
+    }
+    return;
+  }
+  const double r = a.r[seq];
+  const int64_t n = held<T>(a, s, l);
+  if (threadIdx.x == 0) a.accepted[seq] = static_cast<int>(n + 1);
+  const Row<T> row = stop_row<T>(a, s, n);
+#pragma unroll 2
+  for (int seg = w; seg < segs; seg += kOneWaves) {
+    double w0[kVec], w1[kVec], x0 = 0.0, x1 = 0.0;
+    weights(row, seg * static_cast<int64_t>(kOneSeg) + l * kVec, a.V, w0, w1);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      x0 += w0[i];
+      x1 += w1[i];
+    }
+    x0 = wave_add(x0);
+    x1 = wave_add(x1);
+    if (l == 0) {
+      sums[seg][0] = x0;
+      sums[seg][1] = x1;
+    }
+  }
+  __syncthreads();
+  if (w > 0) return;
+  double x[2];
+  auto load_sums = [&](int64_t b, double (&x)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) x[k] = b + l < segs ? sums[b + l][k] : 0.0;
+  };
+  load_sums(0, x);
+  pick<T, kVec>(a, seq, s, n, r, segs, l, load_sums, x);
+}
+
+template <typename T>
 hipError_t launch(const VerifyArgs& a, hipStream_t s) {
+  if (a.V <= kOneMost && a.N < 1 << 22) {   // (a launch holds fewer than 2^32 work items)
+    hipLaunchKernelGGL((verify_one<T>), dim3(static_cast<unsigned>(a.N)), dim3(kOneWaves * kWave), 0, s, a);
+    return hipGetLastError();
+  }
   if (a.rows > 0)
     hipLaunchKernelGGL((verify_sums<T>), dim3(static_cast<unsigned>(a.N * segments(a.V))), dim3(kThreads), 0, s, a);
   hipLaunchKernelGGL((verify_pick<T>), dim3(static_cast<unsigned>(a.N)), dim3(kWave), 0, s, a);

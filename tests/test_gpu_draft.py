@@ -201,7 +201,7 @@ def probs(rng, rows, V, dtype):
     return t, t.double().cpu().numpy()
 
 
-@pytest.mark.parametrize("V", [1, 7, 2048, 2049, 50257, 300_000])
+@pytest.mark.parametrize("V", [1, 7, 512, 2048, 2049, 8193, 24576, 24577, 50257, 300_000])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("given", [True, False])
 def test_verify(V, dtype, given):
@@ -250,15 +250,18 @@ def test_verify_long_drafts_and_edges():
     rows[6] = [0.25, np.nan, 0.25, 0, 0.5, 0]
     rows[7] = [0, 0.5, np.inf, 0.5, 0, 0]
     r = np.array([0.0, 0.5, 1.0 - 2.0 ** -24, 1.0, 0.3, 0.3, 0.5, 0.3], dtype=np.float32)
-    acc, tok = pdn.pdn_draft_verify(dev(rows), i32([0] * 8), dev(np.zeros(8)), dev(r), starts=i32(range(9)))
-    assert acc.cpu().tolist() == [1] * 8
-    # (an infinite whole: nothing is over the target, so the last token with a weight)
-    assert tok.cpu().tolist() == [2, 3, 3, 3, -1, -1, 4, 3]
-    # p under q everywhere: the draft may be refused, the next token is drawn from p
     half = np.full((2, 4), 0.25, dtype=np.float32)
-    acc, tok = pdn.pdn_draft_verify(dev(half), i32([0, 1]), dev(np.array([1.0, 0.0])), dev(np.array([0.6])),
-                                    q=dev(half), starts=i32([0, 2]))
-    assert acc.cpu().tolist() == [1] and tok.cpu().tolist() == [2]
+    for zeros in (0, 9000, 30_000):   # tokens without a weight around them: every form and segment
+        for before in (0, zeros // 2):
+            wide = lambda z: dev(np.pad(z, ((0, 0), (before, zeros - before))))   # noqa: E731
+            acc, tok = pdn.pdn_draft_verify(wide(rows), i32([0] * 8), dev(np.zeros(8)), dev(r), starts=i32(range(9)))
+            assert acc.cpu().tolist() == [1] * 8
+            # (an infinite whole: nothing is over the target, so the last token with a weight)
+            assert tok.cpu().tolist() == [x if x < 0 else before + x for x in (2, 3, 3, 3, -1, -1, 4, 3)]
+            # p under q everywhere: the draft may be refused, the next token is drawn from p
+            acc, tok = pdn.pdn_draft_verify(wide(half), i32([0, before + 1]), dev(np.array([1.0, 0.0])),
+                                            dev(np.array([0.6])), q=wide(half), starts=i32([0, 2]))
+            assert acc.cpu().tolist() == [1] and tok.cpu().tolist() == [before + 2]
     # even rows without starts; starts that leave the tensors
     acc, tok = pdn.pdn_draft_verify(dev(rows), i32([0] * 8), dev(np.ones(8)), dev(r[:4]))
     assert acc.cpu().tolist() == [1] * 4
