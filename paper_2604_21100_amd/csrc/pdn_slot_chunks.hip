@@ -9,8 +9,9 @@
 // three bf16 numbers, which hold all its 24 bits, and of a product of two such
 // sums the six terms down to 2^-16 are taken: what is dropped is 2^-24 of the
 // product.  Queries and keys in bf16 are exact as they are.  The instruction adds
-// in fp32, and the state stays fp32 in its accumulators.  What only goes into o,
-// which is rounded to bf16, is taken as two numbers (2^-16).
+// in fp32, and the state stays fp32 in its accumulators.  That goes for o as well: its
+// terms may cancel, and two parts (2^-16) would show in it after its own rounding (they
+// took 158 and 220 us where three take 164 and 238).
 //
 // A workgroup holds one head's state for all of its sequence.  Its consumer waves
 // own 16 columns each: a lane has rows 32 kk + 8 g + 4 u + i (g = lane / 16) of
@@ -25,7 +26,7 @@
 // (its LDS), 5.2 us with SQUASH and 3.5 without.  The vector unit issues in about two
 // thirds of the cycles (splitting operands, a third of it; write keys and their
 // logarithms), the matrix unit in a third.  16 ragged prompts of up to 1000 tokens x 16
-// heads, SQUASH: 172 us; 8 of up to 2048 x 32 heads, k~ = k: 225 us; on the fp32 matrix
+// heads, SQUASH: 164 us; 8 of up to 2048 x 32 heads, k~ = k: 238 us; on the fp32 matrix
 // instruction the operations alone would be 100 and 171 us, were lengths equal.
 // Measured and not kept: 32 columns a wave (217 against 178 us: too few waves hide
 // the chain), tokens shared unevenly among the producers to even out their time (171
@@ -89,7 +90,7 @@ struct Lay {
   static constexpr int oK = 0, oQ = oK + 4 * kTile, oX = oQ + 4 * kTile;            // oX: external write keys
   static constexpr int oT = oX + (NP == 0 ? 4 * kTile : 0);                         // write keys' parts
   static constexpr int oM = oT + (NP == 3 ? 2 * 3 * kTile : 0), oP = oM + 3 * kMat;
-  static constexpr int oL = oP + 2 * 2 * kMat, kL = kC * (kC + 4) * 4, oF = oL + kL;   // L, M in fp32
+  static constexpr int oL = oP + 2 * 3 * kMat, kL = kC * (kC + 4) * 4, oF = oL + kL;   // L, M in fp32
   static constexpr int oA = oF + kL;                                                // per segment and channel, sums of bp k^2
   static constexpr int oS = oA + (NP == 3 ? 512 * 4 : 0), kS = 8 * kC * 4;          // see load_scalars
   static constexpr int total = oS + 4 * kS;
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
     return sm + (NP == 3 ? L::oT + ((it & 1) * 3 + p) * L::kTile : (NP == 1 ? L::oK : L::oX) + (it & 3) * L::kTile);
   };
   auto mat_m = [&](int p) { return sm + L::oM + p * L::kMat; };
-  auto mat_p = [&](int it, int p) { return sm + L::oP + ((it & 1) * 2 + p) * L::kMat; };
+  auto mat_p = [&](int it, int p) { return sm + L::oP + ((it & 1) * 3 + p) * L::kMat; };
   auto scal = [&](int it, int x) { return sm + L::oS + (it & 3) * L::kS + x * kC * 4; };
 
   if (w < NC) {
@@ -179,7 +180,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           mma_parts(y[u], kq[kk & 1][0][u], sp, 2);
-          mma_parts(z[u], kq[kk & 1][1][u], sp, 1);
+          mma_parts(z[u], kq[kk & 1][1][u], sp, 2);
         }
       }
       // ---- X
@@ -206,7 +207,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
       }
       lds_sync();   // A
       // ---- E = M X, the state after the chunk
-      bf16x8 ep[2], wp[3], mp[2][3];
+      bf16x8 ep[3], wp[3], mp[2][3];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -217,7 +218,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) mma_parts(e[u], mp[u], xp, 2);
       parts8<3>(w0 * e[0], w1 * e[1], wp);
-      bf16x8 pp[2][2];
+      bf16x8 pp[2][3];
 #pragma unroll
       for (int x = 0; x < 2 * KK; ++x) {
         if (x + 1 < 2 * KK) {
@@ -226,20 +227,20 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int p = 0; p < 2; ++p) pp[u][p] = lds_frag(mat_p(ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
+            for (int p = 0; p < 3; ++p) pp[u][p] = lds_frag(mat_p(ch, p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
         }
         reads_done();
         floatx4& t = S[x >> 1][x & 1];
         t *= lc;
         mma_parts(t, tp[x & 1], wp, 2);
       }
-      parts8<2>(e[0], e[1], ep);
+      parts8<3>(e[0], e[1], ep);
       // ---- O
       const __amdgpu_buffer_rsrc_t ro = view(a.o, a.H * DV, ch);
       const uint32_t step = static_cast<uint32_t>(a.H * DV * 2), at = 8 * g * step + v0 * 2;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        mma_parts(z[u], pp[u], ep, 1);
+        mma_parts(z[u], pp[u], ep, 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, static_cast<bf16>(a.scale * z[u][i])), ro,
@@ -432,7 +433,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           mma_parts(kk4, k1[x], tp[x], 2);
-          mma_parts(qk4, q1[x], tp[x], 1);
+          mma_parts(qk4, q1[x], tp[x], 2);
         }
       }
 #pragma unroll
@@ -445,10 +446,10 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
           *fl(L::oL, t, s) = s < t ? be[i + b] * d * kk4[i + b] : 0.f;
           pr[b] = s <= t ? d * qk4[i + b] : 0.f;
         }
-        uint32_t p[2];
-        parts<2>(pr, p);
+        uint32_t p[3];
+        parts<3>(pr, p);
 #pragma unroll
-        for (int q = 0; q < 2; ++q)
+        for (int q = 0; q < 3; ++q)
 #pragma unroll
           for (int b = 0; b < 2; ++b)
             *reinterpret_cast<lds_u16*>(mat_p(ch, q) + tile_off<4>(8 * g + 4 * u + i + b, s >> 3) + (s & 7) * 2) =
