@@ -503,7 +503,7 @@ def pdn_slot_fwd(q, k, v, beta, S, *, starts=None, slots=None, slots_out=None,
     """Advance states of a pool over packed sequences (pdn_slot_fwd of pdn.h).
 
     q, k [tokens, Hk, dk] and v [tokens, H, dv], rows of any token stride
-    (slices of one projection); S [slots, H, dk, dv] and A [slots, H, dk] are
+    that keeps them apart (slices of one projection); S [slots, H, dk, dv] and A [slots, H, dk] are
     read and written in place.  starts [N + 1], slots, slots_out, fresh [N]:
     int32 on the device.  Without starts the rows are shared evenly
     by the sequences (one row each without slots too).  max_tokens: the most

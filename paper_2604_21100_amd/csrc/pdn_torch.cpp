@@ -59,7 +59,8 @@ T* on(const char* name, PyObject* o, at::Device device, at::ScalarType dtype, at
   return static_cast<T*>(t->data_ptr());
 }
 
-// a [tokens, heads, d] tensor with dense rows; stride: from one token to the next (0: dense)
+// a [tokens, heads, d] tensor with dense rows; stride: from one token to the next (0: dense,
+// so a row that is expanded over the tokens must not get there as it is)
 const void* token_rows(const char* name, PyObject* o, at::Device device, at::ScalarType dtype, at::IntArrayRef shape,
                        int64_t* stride) {
   const at::Tensor& t = given(o, name);
@@ -68,6 +69,9 @@ const void* token_rows(const char* name, PyObject* o, at::Device device, at::Sca
   if (!t.is_contiguous()) {
     if (t.stride(2) != 1 || (t.stride(1) != shape[2] && shape[1] > 1))
       refuse(PyExc_ValueError, std::string("a token's row of ") + name + " must be dense");
+    if (shape[0] > 1 && t.stride(0) < shape[1] * shape[2])
+      refuse(PyExc_ValueError, std::string("a token's row of ") + name + " must not overlap another's (stride " +
+                                   std::to_string(t.stride(0)) + ")");
     *stride = t.stride(0);
   }
   return t.data_ptr();
@@ -107,7 +111,6 @@ PyObject* slot(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (S.dim() != 4 || q.dim() != 3 || v.dim() != 3)
       refuse(PyExc_ValueError, "S must be [slots, H, dk, dv], q, k [tokens, Hk, dk] and v [tokens, H, dv]");
     const at::Device dev = S.device();
-    if (!dev.is_cuda()) refuse(PyExc_ValueError, "S is on " + dev.str());
     const int64_t P = S.size(0), H = S.size(1), dk = S.size(2), dv = S.size(3), M = q.size(0), Hk = q.size(1);
     const at::ScalarType dt = q.scalar_type(), f32 = at::kFloat, i32 = at::kInt;
     const at::Tensor *starts = tensor(a[kStarts], "starts"), *slots = tensor(a[kSlots], "slots");
@@ -162,6 +165,7 @@ PyObject* slot(PyObject*, PyObject* const* a, Py_ssize_t n) {
       s.pending = on<int32_t>("pending", a[kPending], dev, i32, counts);
       s.accepted = on<int32_t>("accepted", a[kAccepted], dev, i32, seqs);
     }
+    if (!dev.is_cuda()) refuse(PyExc_ValueError, "S is on " + dev.str());
     at::Tensor made;
     void* o;
     if (a[kO] == Py_None) {
