@@ -32,12 +32,26 @@ try:
 except ImportError:   # no torch: the C ABI alone, nothing else maps HIP
     torch = None
 _lib = ctypes.CDLL(LIB_PATH)
-if torch is not None:
-    try:
-        from . import _pdn_torch
-    except ImportError as e:
+
+
+class _NotBuilt:
+    """In the compiled binding's place: the calls that need it (those on a pool of
+    states) say what is wrong, everything else goes without it."""
+
+    def __init__(self, why):
+        self._why = why
+
+    def __getattr__(self, name):
         raise ImportError(f"_pdn_torch is missing or was built for another "
-                          f"torch ({e}): build it with the library") from e
+                          f"torch ({self._why}): build it with the library")
+
+
+try:
+    if torch is None:
+        raise ImportError("no torch")
+    from . import _pdn_torch
+except ImportError as _e:
+    _pdn_torch = _NotBuilt(_e)
 
 
 def loaded_hip_runtimes():

@@ -79,7 +79,6 @@ def build(verbose: bool = False) -> str:
     """Compile every source for gfx950, link libpdn.so and build _pdn_torch;
     returns libpdn.so's path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
-    build_torch(verbose)
     with ThreadPoolExecutor(max_workers=min(4, len(SOURCES))) as ex:
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
     tmp = LIB + ".tmp"
@@ -90,6 +89,7 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    build_torch(verbose)   # (after the library, which does without it)
     return LIB
 
 
