@@ -39,12 +39,13 @@ struct Sizes {
   int esz;
 };
 
-pdn_status check_problem(const pdn_problem* p, Sizes* sz) {
+// types, head sizes, modes and their numbers; `chunked`: the chunk too
+pdn_status check_mode(const pdn_problem* p, bool chunked) {
   if (!p) return PDN_ERR_NULL;
   if (p->B < 0 || p->T < 0 || p->H < 0) return PDN_ERR_SHAPE;
   if (p->io != PDN_F32 && p->io != PDN_BF16) return PDN_ERR_DTYPE;
   if ((p->dk != 64 && p->dk != 128) || (p->dv != 64 && p->dv != 128)) return PDN_ERR_UNSUPPORTED;
-  if (!pdn::chunk_supported(p->chunk)) return PDN_ERR_UNSUPPORTED;
+  if (chunked && !pdn::chunk_supported(p->chunk)) return PDN_ERR_UNSUPPORTED;
   if (p->gate != PDN_GATE_NONE && p->gate != PDN_GATE_SCALAR && p->gate != PDN_GATE_CHANNEL)
     return PDN_ERR_VALUE;
   if (p->precond != PDN_PRECOND_SQUASH && p->precond != PDN_PRECOND_IDENTITY &&
@@ -58,6 +59,12 @@ pdn_status check_problem(const pdn_problem* p, Sizes* sz) {
   if (p->knorm < PDN_KNORM_NONE || p->knorm > PDN_KNORM_BETA) return PDN_ERR_VALUE;
   if (p->knorm != PDN_KNORM_NONE && p->precond != PDN_PRECOND_SQUASH) return PDN_ERR_VALUE;
   if (p->knorm == PDN_KNORM_BETA && p->gate == PDN_GATE_CHANNEL) return PDN_ERR_UNSUPPORTED;
+  return PDN_OK;
+}
+
+pdn_status check_problem(const pdn_problem* p, Sizes* sz) {
+  const pdn_status st = check_mode(p, true);
+  if (st != PDN_OK) return st;
   Sizes s{};
   int64_t bt;
   if (!mul_ok(p->B, p->H, &s.BH) || !mul_ok(p->B, p->T, &bt) || !mul_ok(bt, p->H, &s.tok))
@@ -176,19 +183,19 @@ bool span_ok(int64_t rows, int64_t stride, int64_t width, int esz, int64_t* out)
 }
 
 pdn_status check_slots(const pdn_problem* p, const pdn_slots* s, bool draft, SlotSizes* out) {
-  Sizes unused;
-  if (!p) return PDN_ERR_NULL;
-  pdn_problem one = *p;   // (the chunk is not used by these calls)
-  one.chunk = 64;
-  pdn_status st = check_problem(&one, &unused);
+  const pdn_status st = check_mode(p, false);
   if (st != PDN_OK) return st;
   if (!s) return PDN_ERR_NULL;
   if (s->tokens < 0 || s->slots < 0 || s->Hk < 0) return PDN_ERR_SHAPE;
   const int64_t Hk = s->Hk ? s->Hk : p->H;
   if (p->H > 0 && p->H % Hk != 0) return PDN_ERR_SHAPE;
   // row numbers and slots are 32-bit on the device; one workgroup of at most 768
-  // work items a head, of which a launch holds fewer than 2^32
-  if (s->tokens > INT32_MAX || s->slots > INT32_MAX || unused.BH >= (int64_t)1 << 22) return PDN_ERR_SHAPE;
+  // work items a head, of which a launch holds fewer than 2^32.  (T is only where a
+  // sequence is cut: any number.)
+  int64_t heads;
+  if (s->tokens > INT32_MAX || s->slots > INT32_MAX || p->B > INT32_MAX || !mul_ok(p->B, p->H, &heads) ||
+      heads >= (int64_t)1 << 22)
+    return PDN_ERR_SHAPE;
   int64_t even;
   if (!s->starts && (!mul_ok(p->B, p->T, &even) || even != s->tokens)) return PDN_ERR_SHAPE;
   if (!s->slot && p->B > s->slots) return PDN_ERR_SHAPE;
@@ -270,7 +277,7 @@ pdn_status slot_call(const pdn_problem* p, const pdn_inputs* in, const pdn_slots
   if (!work) return PDN_OK;
 
   pdn::SlotArgs a{};
-  a.B = p->B; a.T = p->T; a.H = p->H; a.Hk = s->Hk ? s->Hk : p->H;
+  a.B = p->B; a.T = p->T < INT32_MAX ? p->T : INT32_MAX; a.H = p->H; a.Hk = s->Hk ? s->Hk : p->H;
   a.tokens = s->tokens; a.slots = s->slots;
   a.q_stride = z.qs; a.k_stride = z.ks; a.v_stride = z.vs;
   a.dk = p->dk; a.dv = p->dv;

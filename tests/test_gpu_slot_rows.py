@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from slot_util import KW, batch, dev, dev_batch, host, i32, pool
-from test_gpu_slots import check, want
+from test_gpu_slots import check, run, want
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,15 @@ def test_a_row_for_all_tokens(T, io):
     o = pdn.pdn_slot_fwd(*one, Sd, gate="none", precond="identity", **KW)
     ro, rS, _, _ = want({n: None if x is None else x[:1] for n, x in b.items()}, S[:1], None, [1], "none", "identity")
     check((host(o), host(Sd), None), (ro, rS, None), io, 1)
+
+
+@pytest.mark.parametrize("gate", ["scalar", "channel"])
+def test_no_limit_on_a_sequence(gate):
+    """max_tokens past any length, or not given: nothing is cut."""
+    rng = np.random.default_rng(3)
+    lens, H, d = [5, 0, 70, 1], 2, 128
+    b = batch(rng, sum(lens), H, H, d, d, "bf16", gate, "squash")
+    S, A = pool(rng, 4, H, d, d, "squash")
+    o, S1, A1, starts = want(b, S, A, lens, gate, "squash")
+    for most in (None, 2 ** 40, 2 ** 63 - 1):
+        check(run(b, S, A, "bf16", gate, "squash", starts=i32(starts), max_tokens=most), (o, S1, A1), "bf16", 70)
