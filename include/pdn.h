@@ -335,10 +335,8 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* problem, const pdn_inputs* in,
  * most tokens one of them has (a longer one is cut there), chunk is unused.
  * The recurrence, its modes and the meaning of the other members are those of
  * pdn_chunk_fwd; states and products are fp32 for both io types.
- * Log-decays without the per-channel gate, and g_p, may be as low as the type
- * goes, and -inf (the state is forgotten: e.g. a document's first token).
- * Per-channel gate: of each eight tokens of a sequence (T > 1: counted from
- * its first in the call) the log-decays of a channel must sum to more than -87.
+ * Log-decays, a channel's too, and g_p may be as low as the type goes, and -inf
+ * (the state, or a channel of it, is forgotten: e.g. a document's first token).
  * A NaN or Inf in a token shows in that sequence and slot only; within the
  * sequence it may also show in o of tokens up to 31 before it (T > 1).
  * B H must be below 2^22.

@@ -11,13 +11,13 @@
 // has two barriers; block n's operands are formed in one step, its L and P are
 // summed and it is consumed in the next.
 //
-// What bounds it: the step's chain, 1.8 us at 64 x 64 and 3.4 at 128 x 128, of which the
+// What bounds it: the step's chain, 1.8 us at 64 x 64 and 3.7 at 128 x 128, of which the
 // fp32 matrix instructions are a sixth and two fifths (the products with the state fill
 // the matrix unit while nothing else gets on; then the producers' write keys, decays
 // and rows; then solve, update and output).  3 fp32 prompts of up to 333 tokens x 4
-// heads of 64: 75 us; 12 per-channel ones of up to 700 x 16 heads of 128: 298 us (one
-// after the other, without producers: 135 and 479).  Producers at a higher priority
-// make it slower (79 and 309 us).
+// heads of 64: 74 us; 12 per-channel ones of up to 700 x 16 heads of 128: 324 us (one
+// after the other, without producers, 135 and, with products a quarter cheaper, 479).
+// Producers at a higher priority made it 5 and 4 % slower.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
 #include "pdn_slots.hpp"
@@ -33,8 +33,10 @@ struct Run {
   alignas(16) T raw[3][kSlotBlock][DK];              // keys, queries, the caller's write keys
   alignas(16) float g[LC][LD];                       // CH: log-decays
   // operands, of the block in use and the one after it: keys over queries; write
-  // keys, with CH decayed to the block's start, and to its end; CH: the decay over it
+  // keys, with CH as they are and decayed to the block's end; CH: the decay over it
   alignas(16) float KQ[2][2 * kSlotBlock][LD], Kt[2][kSlotBlock][LD], Kw[2][LC][LD], lam[2][CH ? DK : 4];
+  // CH: operands of the products of channel_rows (the columns of the second are Kt)
+  alignas(16) float R1[CH ? 16 : 1][LD], R2[CH ? 16 : 1][LD], C1[CH ? kPairCols : 1][LD];
   alignas(16) float part[4][16][kSlotBlock], LP[16][kSlotBlock + 4], E[NW][kSlotBlock][16], sum[4][kSlotBlock];
   // of each token: log-decay, the decay to it and from it within the block, write
   // strength, preconditioner gain and decay
@@ -250,14 +252,16 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
       const int u = blk & 1;
       const float(*tok)[B] = s.tok[blk & 3];
       const int nt = static_cast<int>(min<int64_t>(B, rows.n - static_cast<int64_t>(blk) * B));
-      float kt[B], kv[B], At[B], to[B], G = 0.f;
+      float kt[B], kv[B], At[B];
+      float ex[B], up[B], lam = 1.f;   // CH: a token's decay, that from the block's start
       const float Ab = A;
 #pragma unroll
       for (int t = 0; t < B; ++t) {
         kv[t] = to_f(s.raw[0][t][c]);
         if (CH) {
-          G += s.g[t][c];
-          to[t] = G;
+          ex[t] = fast_exp(s.g[t][c]);
+          lam *= ex[t];
+          up[t] = lam;
         }
       }
       if (gram)   // (a token past the end leaves A: no gain, no decay)
@@ -266,13 +270,16 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
           A = tok[5][t] * A + tok[4][t] * kv[t] * kv[t];
           At[t] = A;
         }
-      if (qry)
+      if (qry) {
+        float q[B];
 #pragma unroll
         for (int t = 0; t < B; ++t) {
-          float q = to_f(s.raw[1][t][c]);
-          if (both) q /= At[t] + a.ridge;
-          s.KQ[u][B + t][c] = CH ? fast_exp(to[t]) * q : q;
+          q[t] = to_f(s.raw[1][t][c]);
+          if (both) q[t] /= At[t] + a.ridge;
+          if (!CH) s.KQ[u][B + t][c] = q[t];
         }
+        if constexpr (CH) channel_rows(q, ex, up, 1, c, s.KQ[u], s.R1, s.R2);
+      }
       if (key) {
         if (prec == kSquash) {
 #pragma unroll
@@ -303,25 +310,37 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
             kt[t] = t < nt ? slot_sum_factor(a, m, tok[3][t], tok[0][t]) * kt[t] : 0.f;
           }
       }
-      if (key)
+      if (key) {
+        // (a linear-attention update has no correction by the state: no key rows)
+        if (both)
 #pragma unroll
-        for (int t = 0; t < B; ++t) {
-          // (a linear-attention update has no correction by the state: no key rows)
-          s.KQ[u][t][c] = both ? 0.f : CH ? fast_exp(to[t]) * kv[t] : kv[t];
-          s.Kt[u][t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
-          if (CH) s.Kw[u][t][c] = kt[t] * fast_exp(G - to[t]);
+          for (int t = 0; t < B; ++t) kv[t] = 0.f;
+        if constexpr (CH) {
+          channel_rows(kv, ex, up, 0, c, s.KQ[u], s.R1, s.R2);
+          channel_cols(kt, ex, c, s.C1, s.Kt[u], s.Kw[u]);
+          s.lam[u][c] = lam;
+        } else {
+#pragma unroll
+          for (int t = 0; t < B; ++t) {
+            s.KQ[u][t][c] = kv[t];
+            s.Kt[u][t][c] = kt[t];
+          }
         }
-      if (CH && key) s.lam[u][c] = fast_exp(G);
+      }
     };
-    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave
+    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave; CH: two waves
+    // each of the two products
+    constexpr int NP = CH ? 2 : 4;
     auto put_products = [&](int blk) {
-      const int u = blk & 1;
+      const int u = blk & 1, pass = pw / NP;
+      const float(*const rows16)[R::LD] = !CH ? s.KQ[u] : pass ? s.R2 : s.R1;
+      const float(*const cols8)[R::LD] = !CH || pass ? s.Kt[u] : s.C1;
       floatx4 g4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 0; x < MB / 4; ++x) {
-        const int m = 4 * x + pw;
-        const floatx4 r4 = *reinterpret_cast<const floatx4*>(&s.KQ[u][lr][16 * m + 4 * lg]);
-        const floatx4 t4 = *reinterpret_cast<const floatx4*>(&s.Kt[u][lr & 7][16 * m + 4 * lg]);
+      for (int x = 0; x < MB / NP; ++x) {
+        const int m = NP * x + pw % NP;
+        const floatx4 r4 = *reinterpret_cast<const floatx4*>(&rows16[lr][16 * m + 4 * lg]);
+        const floatx4 t4 = *reinterpret_cast<const floatx4*>(&cols8[lr & 7][16 * m + 4 * lg]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
       }
@@ -333,7 +352,14 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
     auto put_lp = [&](int blk) {   // (by the last two waves, which have no write keys to form)
       const int r = (pt - 128) / B, x = pt % B, t = r % B;
       const float(*tok)[B] = s.tok[blk & 3];
-      float v = (s.part[0][r][x] + s.part[1][r][x]) + (s.part[2][r][x] + s.part[3][r][x]);
+      float v;
+      if (CH) {
+        int col;
+        const int row = channel_pair(r, x, &col), p = row / 16 * NP;
+        v = s.part[p][row % 16][col] + s.part[p + 1][row % 16][col];
+      } else {
+        v = (s.part[0][r][x] + s.part[1][r][x]) + (s.part[2][r][x] + s.part[3][r][x]);
+      }
       if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
         float g = 0.f;
 #pragma unroll

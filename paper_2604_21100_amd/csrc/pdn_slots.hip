@@ -179,8 +179,8 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
 //
 // What bounds it is the chain of a workgroup, of which a compute unit holds two: rows,
 // L and P (two barriers), the state's arrival, records, products, solve.  Drafts of
-// 64 sequences x 16 heads: 44 us for 152 MB, 3.5 TB/s; 96 x 16 of four tokens with
-// per-channel decays 62 us, 3.5 TB/s; five tokens of one sequence 10 us.  Eight
+// 64 sequences x 16 heads: 45 us for 152 MB, 3.4 TB/s; 96 x 16 of four tokens with
+// per-channel decays 65 us, 3.3 TB/s; five tokens of one sequence 10 us.  Eight
 // tokens of 64 x 16 heads without a tape 34 us.  (With pending counts read ahead of
 // the rows drafts took 45 and 64 us, with the state first 46 and 66; a third workgroup
 // would leave a lane 80 of the 127 registers that it takes.)
@@ -192,10 +192,12 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   constexpr int GP = kSlotBlock * DK * 4 / 16, NGP = (GP + NTHR - 1) / NTHR;           // of a block's rows of fp32
   __shared__ __attribute__((aligned(16))) T sRaw[3][kSlotBlock][DK];   // keys, queries, the caller's write keys
   __shared__ __attribute__((aligned(16))) float sKQ[2 * kSlotBlock][LD], sKt[kSlotBlock][LD];
-  // CH: g; the write keys with the decay to the block's end, and as they are.
+  // CH: g; the write keys with the decay to the block's end; operands of the products
+  // of channel_rows (the columns of the second are the write keys).
   // Drafts: the accepted records' write keys and, with CH, their log-decays and the
   // decay over them; A after each token.
-  __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sKr[CH && DRAFT ? kSlotBlock : 1][LD], sGr[CH && DRAFT ? kSlotBlock : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sG[CH ? kSlotBlock : 1][LD], sKw[CH ? kSlotBlock : 1][LD], sGr[CH && DRAFT ? kSlotBlock : 1][LD];
+  __shared__ __attribute__((aligned(16))) float sR1[CH ? 16 : 1][LD], sR2[CH ? 16 : 1][LD], sC1[CH ? kPairCols : 1][LD];
   __shared__ __attribute__((aligned(16))) float sC[DRAFT ? kSlotBlock : 1][LD], sAt[DRAFT ? kSlotBlock : 1][LD];
   __shared__ __attribute__((aligned(16))) float sPart[NW][16][kSlotBlock], sLP[16][kSlotBlock + 4], sE[NW][kSlotBlock][16];
   __shared__ __attribute__((aligned(16))) float sLam[CH ? DK : 4], sGt[CH && DRAFT ? kSlotBlock : 1][LD], sSum[NW][kSlotBlock], sLr[CH && DRAFT ? DK : 4];
@@ -372,14 +374,16 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   auto operands = [&](int nt) {
     [[maybe_unused]] const auto [l, lr, lg, tb, v0, c, key, qry] = place();
     {
-      float kt[kSlotBlock], kv[kSlotBlock], G = 0.f, to[kSlotBlock], At[kSlotBlock];
+      float kt[kSlotBlock], kv[kSlotBlock], At[kSlotBlock];
+      float ex[kSlotBlock], up[kSlotBlock], lam = 1.f;   // CH: a token's decay, that from the block's start
       const float Ab = A;   // before the block
 #pragma unroll
       for (int t = 0; t < kSlotBlock; ++t) {
         kv[t] = to_f(sRaw[0][t][c]);
         if (CH) {
-          G += sG[t][c];
-          to[t] = G;
+          ex[t] = fast_exp(sG[t][c]);
+          lam *= ex[t];
+          up[t] = lam;
         }
       }
       if (gram) {   // (a token past the end leaves A: no gain, no decay)
@@ -402,13 +406,16 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
 #pragma unroll
         for (int t = 0; t < kSlotBlock; ++t) kt[t] = prec == kExternal ? to_f(sRaw[2][t][c]) : kv[t];
       }
-      if (both ? key : qry)
+      if (both ? key : qry) {
+        float q[kSlotBlock];
 #pragma unroll
         for (int t = 0; t < kSlotBlock; ++t) {
-          float q = to_f(sRaw[1][t][c]);
-          if (both) q /= At[t] + a.ridge;
-          sKQ[kSlotBlock + t][c] = CH ? fast_exp(to[t]) * q : q;
+          q[t] = to_f(sRaw[1][t][c]);
+          if (both) q[t] /= At[t] + a.ridge;
+          if (!CH) sKQ[kSlotBlock + t][c] = q[t];
         }
+        if constexpr (CH) channel_rows(q, ex, up, 1, c, sKQ, sR1, sR2);
+      }
       if (slot_needs_sum(a)) {   // the write key's row sums
 #pragma unroll
         for (int t = 0; t < kSlotBlock; ++t) {
@@ -424,34 +431,47 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
           kt[t] = t < nt ? slot_sum_factor(a, m, sB[t], sg[t]) * kt[t] : 0.f;
         }
       }
-      if (key)
+      if (key) {
+        // (a linear-attention update has no correction by the state: no key rows)
+        if (both)
 #pragma unroll
-        for (int t = 0; t < kSlotBlock; ++t) {
-          // (a linear-attention update has no correction by the state: no key rows)
-          sKQ[t][c] = both ? 0.f : CH ? fast_exp(to[t]) * kv[t] : kv[t];
-          sKt[t][c] = CH ? kt[t] * fast_exp(-to[t]) : kt[t];
-          if (CH) {
-            sKw[t][c] = kt[t] * fast_exp(G - to[t]);
-            if (DRAFT) {
-              sKr[t][c] = kt[t];
-              sGt[t][c] = static_cast<float>(gacc + to[t]);
-            }
+          for (int t = 0; t < kSlotBlock; ++t) kv[t] = 0.f;
+        if constexpr (CH) {
+          channel_rows(kv, ex, up, 0, c, sKQ, sR1, sR2);
+          channel_cols(kt, ex, c, sC1, sKt, sKw);
+          sLam[c] = lam;
+        } else {
+#pragma unroll
+          for (int t = 0; t < kSlotBlock; ++t) {
+            sKQ[t][c] = kv[t];
+            sKt[t][c] = kt[t];
           }
         }
-      if (CH) {
-        if (key) sLam[c] = fast_exp(G);
-        if (DRAFT) gacc += G;
+      }
+      if (CH && DRAFT) {   // (a token's log-decay as where a scalar gate's are summed)
+        float G = 0.f;
+#pragma unroll
+        for (int t = 0; t < kSlotBlock; ++t) {
+          G += sum_decay(sG[t][c]);
+          if (key) sGt[t][c] = static_cast<float>(gacc + G);
+        }
+        gacc += G;
       }
     }
     __syncthreads();
-    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave
+    // (rows of K over rows of Q) times Kt^T, a share of the channels a wave; CH: half
+    // the waves each of the two products
+    constexpr int NP = CH ? NW / 2 : NW;
+    const int pass = w / NP, m1 = w % NP;
+    const float(*const rows16)[LD] = !CH ? sKQ : pass ? sR2 : sR1;
+    const float(*const cols8)[LD] = !CH || pass ? sKt : sC1;
     floatx4 g4 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int m0 = 0; m0 < MB; m0 += NW) {
-      const int m = m0 + w;
-      if (MB < NW && m >= MB) break;
-      const floatx4 r4 = *reinterpret_cast<const floatx4*>(&sKQ[lr][16 * m + 4 * lg]);
-      const floatx4 t4 = *reinterpret_cast<const floatx4*>(&sKt[lr & 7][16 * m + 4 * lg]);
+    for (int m0 = 0; m0 < MB; m0 += NP) {
+      const int m = m0 + m1;
+      if (MB < NP && m >= MB) break;
+      const floatx4 r4 = *reinterpret_cast<const floatx4*>(&rows16[lr][16 * m + 4 * lg]);
+      const floatx4 t4 = *reinterpret_cast<const floatx4*>(&cols8[lr & 7][16 * m + 4 * lg]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) mma4(g4, r4[i], t4[i]);
     }
@@ -463,8 +483,10 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     if (tid < 16 * kSlotBlock) {
       const int r = tid / kSlotBlock, s = tid % kSlotBlock, t = r % kSlotBlock;
       float x = 0.f;
+      int row = r, col = s;
+      if (CH) row = channel_pair(r, s, &col);
 #pragma unroll
-      for (int i = 0; i < NW; ++i) x += sPart[i][r][s];
+      for (int i = 0; i < NP; ++i) x += sPart[i + (CH ? row / 16 * NP : 0)][row % 16][col];
       if (!CH) {   // (summed token by token: a difference of two long sums would lose a short one)
         float g = 0.f;
 #pragma unroll
@@ -590,7 +612,7 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
       for (int x = tid; x < nt * DK / 4; x += NTHR) {
         const int t = x / (DK / 4), cc = 4 * (x % (DK / 4));
         float* r = r0 + t * rs;
-        *reinterpret_cast<floatx4*>(r + cc) = *reinterpret_cast<const floatx4*>(CH ? &sKr[t][cc] : &sKt[t][cc]);
+        *reinterpret_cast<floatx4*>(r + cc) = *reinterpret_cast<const floatx4*>(&sKt[t][cc]);
         if (CH) *reinterpret_cast<floatx4*>(r + DK + DV + cc) = *reinterpret_cast<const floatx4*>(&sGt[t][cc]);
         if (gram) *reinterpret_cast<floatx4*>(r + DK + DV + (CH ? DK : 4) + cc) = *reinterpret_cast<const floatx4*>(&sAt[t][cc]);
       }

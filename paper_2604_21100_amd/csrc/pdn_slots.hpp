@@ -83,6 +83,70 @@ __device__ __forceinline__ void block_sums(float g, int l, float* to, float* on)
   *on = s + down(s, four);
 }
 
+// With a per-channel gate the products of a block's eight tokens,
+//   sum over c of x_t[c] (e_s+1 .. e_t)[c] kt_s[c],   x a key or query, e_t = exp(g_t),
+// take the decays between two tokens apart at a token r between them, s <= r < t, so that
+// both factors, x_t e_r+1 .. e_t and kt_s e_s+1 .. e_r, are of decays that a channel goes through and
+// none is ever divided by, however little a channel keeps.  With r the last
+// token of the half, pair or token of the block that s is in and t is not, each
+// pair of tokens is in one of two products of sixteen rows:
+//   the first     rows  keys 4-7, queries 4-7 (r = 3), keys and queries 2, 3 (r = 1) and 6, 7 (r = 5)
+//                 columns  write keys 0-3 (r = 3), 0, 1 (r = 1), 4, 5 (r = 5)
+//   the second    rows  keys 1, 3, 5, 7 and queries 1, 3, 5, 7 (r = t - 1), queries as they are
+//                 columns  write keys as they are
+// (One product, of rows with the decay from the block's start and write keys
+// divided by it, overflows where a block's log-decays add up to less than -87 and
+// its write keys are not small; it took 299 and 61 us where the two take 324 and 65: 12 per-
+// channel prompts of up to 700 tokens x 16 heads, 96 x 16 drafts of four.)
+constexpr int kPairCols = 8;   // columns of either
+// a channel's keys (q 0) or queries (q 1), x: rows for the products with the state
+// (decayed from the block's start: up[t]), and of both products
+template <int LD>
+__device__ __forceinline__ void channel_rows(const float (&x)[kSlotBlock], const float (&e)[kSlotBlock],
+                                             const float (&up)[kSlotBlock], int q, int c, float (*kq)[LD], float (*r1)[LD],
+                                             float (*r2)[LD]) {
+  float d = 1.f;
+#pragma unroll
+  for (int t = 0; t < kSlotBlock; ++t) {
+    kq[kSlotBlock * q + t][c] = up[t] * x[t];
+    if (t >= 4) {
+      d *= e[t];
+      r1[4 * q + t - 4][c] = d * x[t];
+    }
+    if (t & 2) r1[8 + 4 * q + (t >> 2) * 2 + (t & 1)][c] = (t & 1 ? e[t - 1] * e[t] : e[t]) * x[t];
+    if (t & 1) r2[4 * q + t / 2][c] = e[t] * x[t];
+    if (q) r2[8 + t][c] = x[t];
+  }
+}
+// its write keys: columns of both, and decayed to the block's end
+template <int LD>
+__device__ __forceinline__ void channel_cols(const float (&kt)[kSlotBlock], const float (&e)[kSlotBlock], int c,
+                                             float (*c1)[LD], float (*c2)[LD], float (*to_end)[LD]) {
+  float on = 1.f, d = 1.f;
+#pragma unroll
+  for (int s = kSlotBlock - 1; s >= 0; --s) {
+    c2[s][c] = kt[s];
+    to_end[s][c] = on * kt[s];
+    on *= e[s];
+    if (s < 4) {
+      c1[s][c] = d * kt[s];
+      d *= e[s];
+    }
+    if (!(s & 2)) c1[4 + (s >> 2) * 2 + (s & 1)][c] = (s & 1 ? 1.f : e[s + 1]) * kt[s];
+  }
+}
+// where of the two products (32 rows) row r of K over Q with token s <= t is
+__device__ __forceinline__ int channel_pair(int r, int s, int* col) {
+  const int t = r % kSlotBlock, q = r / kSlotBlock, x = t ^ s;
+  *col = s;
+  if (x >= 4) return 4 * q + (t & 3);
+  if (x >= 2) {
+    *col = 4 + (t >> 2) * 2 + (s & 1);
+    return 8 + 4 * q + (t >> 2) * 2 + (t & 1);
+  }
+  return 16 + (x ? 4 * q + t / 2 : 8 + t);
+}
+
 // A head's state, seen through a buffer: a lane's rows are then one offset and
 // constants, where pointers to them would take two registers each.
 template <int DK, int DV>
