@@ -279,8 +279,8 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     s_bp = in && gram ? x_bp : 0.f;
     s_gp = in && gram && a.g_p ? x_gp : 0.f;
   };
-  // Drafts: log-decay summed over the blocks before (the scalar's; of a channel), in
-  // 64 bits, so that a record's sum is rounded once.
+  // Drafts: log-decay summed over the tokens before (the scalar's over the blocks before;
+  // a channel's) in 64 bits, so that a record's sum is rounded once.
   double gacc = 0.0;
   auto put_rows = [&]() {
     auto put = [&](void* p, const u32x4& v, int x, int pieces, int row_bytes, int ld_bytes) {
@@ -449,13 +449,11 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
         }
       }
       if (CH && DRAFT) {   // (a token's log-decay as where a scalar gate's are summed)
-        float G = 0.f;
 #pragma unroll
         for (int t = 0; t < kSlotBlock; ++t) {
-          G += sum_decay(sG[t][c]);
-          if (key) sGt[t][c] = static_cast<float>(gacc + G);
+          gacc += sum_decay(sG[t][c]);
+          if (key) sGt[t][c] = static_cast<float>(gacc);
         }
-        gacc += G;
       }
     }
     __syncthreads();

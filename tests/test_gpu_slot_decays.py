@@ -77,3 +77,25 @@ def test_any_decay_of_drafts(T, precond):
         e = rel_err(o[rows], ro), rel_err(host(Sd)[n], s)
         print(precond, T, n, e, G)
         assert e[0] <= bo and e[1] <= 1e-5 + T * 2.0 ** -23 * G
+
+
+@pytest.mark.parametrize("T", [3, 8, 21])
+@pytest.mark.parametrize("gate", ["scalar", "channel"])
+def test_a_record_rounds_its_sum_once(gate, T):
+    """The summed log-decay of a pending token is within half a step, 2^-24 of it, of the
+    exact sum (a little more where that itself is taken in 64 bits)."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    rng = np.random.default_rng(T)
+    P, H, d = 2, 2, 128
+    b = batch(rng, P * T, H, H, d, d, "f32", gate, "identity", strength=1.0)
+    b["g"][::4] = (30.0 * b["g"][::4]).astype(np.float32).astype(np.float64)
+    b["g"] = np.maximum(b["g"], -128.0)
+    tape = torch.full((P, T, H, pdn.pdn_tape_record(d, d, gate, "identity")), float("nan"), device="cuda")
+    pos, opt = dev_batch(b, "f32", "identity")
+    pdn.pdn_slot_draft(*pos, torch.zeros(P, H, d, d, device="cuda"), tape, torch.zeros(P, H, dtype=torch.int32, device="cuda"),
+                       gate=gate, precond="identity", max_tokens=T, **opt, **KW)
+    G = np.cumsum(b["g"].reshape(P, T, H, -1), 1)
+    off = np.abs(host(tape)[..., 2 * d:2 * d + (d if gate == "channel" else 4)] - G) / np.abs(G)
+    print(gate, T, "%.3f half steps" % (off.max() * 2 ** 24))
+    assert off.max() <= 2.0 ** -24 * (1 + 2.0 ** -20)
