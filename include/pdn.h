@@ -337,8 +337,8 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* problem, const pdn_inputs* in,
  * pdn_chunk_fwd; states and products are fp32 for both io types.
  * Log-decays, a channel's too, and g_p may be as low as the type goes, and -inf
  * (the state, or a channel of it, is forgotten: e.g. a document's first token).
- * A NaN or Inf in a token shows in that sequence and slot only; within the
- * sequence it may also show in o of tokens up to 31 before it (T > 1).
+ * A NaN or Inf in a token shows in that sequence and slot only, from that token
+ * on (one of a query in that token's o, one of a value in its column).
  * B H must be below 2^22.
  *
  * `starts`, `slot`, `slot_out`, `fresh`, `accepted` are device arrays, read by

@@ -23,10 +23,10 @@
 // 16 x 16 inverses by substitution and M21 = -M22 L21 M11.
 //
 // What bounds it: a chunk's chain on one compute unit, which a workgroup has to itself
-// (its LDS), 5.2 us with SQUASH and 3.5 without.  The vector unit issues in about two
+// (its LDS), 5.3 us with SQUASH and 3.8 without.  The vector unit issues in about two
 // thirds of the cycles (splitting operands, a third of it; write keys and their
 // logarithms), the matrix unit in a third.  16 ragged prompts of up to 1000 tokens x 16
-// heads, SQUASH: 164 us; 8 of up to 2048 x 32 heads, k~ = k: 238 us; on the fp32 matrix
+// heads, SQUASH: 168 us; 8 of up to 2048 x 32 heads, k~ = k: 242 us; on the fp32 matrix
 // instruction the operations alone would be 100 and 171 us, were lengths equal.
 // Measured and not kept: 32 columns a wave (217 against 178 us: too few waves hide
 // the chain), tokens shared unevenly among the producers to even out their time (171
@@ -120,6 +120,10 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
   auto mat_m = [&](int p) { return sm + L::oM + p * L::kMat; };
   auto mat_p = [&](int it, int p) { return sm + L::oP + ((it & 1) * 3 + p) * L::kMat; };
   auto scal = [&](int it, int x) { return sm + L::oS + (it & 3) * L::kS + x * kC * 4; };
+  // the first row of chunk it's L that is not all numbers (the inverse is formed without
+  // what is none, and its rows from that one on are made NaN)
+  typedef __attribute__((address_space(3))) int lds_int;
+  auto first_row = [&](int it) { return reinterpret_cast<lds_int*>(scal(it, 5) + 8 * 4); };
 
   if (w < NC) {
     // ------------------------------------------------------------ consumers
@@ -193,8 +197,8 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
       load_t(0);
       reads_done();
       bf16x8 xp[3];
+      floatx4 x[2];
       {
-        floatx4 x[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -238,9 +242,39 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
       // ---- O
       const __amdgpu_buffer_rsrc_t ro = view(a.o, a.H * DV, ch);
       const uint32_t step = static_cast<uint32_t>(a.H * DV * 2), at = 8 * g * step + v0 * 2;
+      floatx4 pe[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        mma_parts(z[u], pp[u], ep, 2);
+        pe[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+        mma_parts(pe[u], pp[u], ep, 2);
+      }
+      if (__any(!all_numbers(e[0]) || !all_numbers(e[1]))) {   // (both once more, without them)
+        const int first = min(first_of(take_out(x[0], 8 * g, take_out(x[1], 8 * g + 4, kC))), *first_row(ch));
+        parts8<3>(x[0], x[1], xp);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          bf16x8 m3[3];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) m3[p] = lds_frag(mat_m(p) + tile_off<4>(r0, g) + 4 * u * (kC * 2));
+          e[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+          mma_parts(e[u], m3, xp, 2);
+        }
+        settled(e[0], e[1]);
+        put_from(e[0], 8 * g, first, 0.f);
+        put_from(e[1], 8 * g + 4, first, 0.f);
+        parts8<3>(e[0], e[1], ep);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          pe[u] = floatx4{0.f, 0.f, 0.f, 0.f};
+          mma_parts(pe[u], pp[u], ep, 2);
+        }
+        settled(pe[0], pe[1]);
+        put_from(pe[0], 8 * g, first, __builtin_nanf(""));
+        put_from(pe[1], 8 * g + 4, first, __builtin_nanf(""));
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        z[u] += pe[u];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, static_cast<bf16>(a.scale * z[u][i])), ro,
@@ -344,7 +378,8 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
         put(2, fast_exp(static_cast<float>(end - to)));
         put(3, bp);
         put(4, dp);
-        if (t % TOK == 0) *reinterpret_cast<lds_float*>(scal(ch, 5) + t / TOK * 4) = ds;
+        if (t % TOK == 0) *reinterpret_cast<lds_float*>(scal(ch, 5) + t / TOK * 4) = ds;   // (eight at most)
+        if (t == 0) *first_row(ch) = kC;
         *reinterpret_cast<lds_double*>(scal(ch, 6) + t * 8) = to;
       }
     };
@@ -437,15 +472,17 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; i += 2) {
-        floatx2 pr;
+      for (int i = 0; i < 4; ++i) {
+        const int t = 8 * g + 4 * u + i;
+        const float d = fast_exp(static_cast<float>(Gt[i] - Gs));
+        kk4[i] = s < t ? be[i] * d * kk4[i] : 0.f;
+        qk4[i] = s <= t ? d * qk4[i] : 0.f;
+      }
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const int t = 8 * g + 4 * u + i + b;
-          const float d = fast_exp(static_cast<float>(Gt[i + b] - Gs));
-          *fl(L::oL, t, s) = s < t ? be[i + b] * d * kk4[i + b] : 0.f;
-          pr[b] = s <= t ? d * qk4[i + b] : 0.f;
-        }
+      for (int i = 0; i < 4; i += 2) {
+        const floatx2 pr = {qk4[i], qk4[i + 1]};
+#pragma unroll
+        for (int b = 0; b < 2; ++b) *fl(L::oL, 8 * g + 4 * u + i + b, s) = kk4[i + b];
         uint32_t p[3];
         parts<3>(pr, p);
 #pragma unroll
@@ -455,11 +492,17 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
             *reinterpret_cast<lds_u16*>(mat_p(ch, q) + tile_off<4>(8 * g + 4 * u + i + b, s >> 3) + (s & 7) * 2) =
                 static_cast<uint16_t>(b ? p[q] >> 16 : p[q]);
       }
+      if (__any(!all_numbers(kk4))) {
+        const int t = take_out(kk4, 8 * g + 4 * u, kC);
+        if (t < kC) __hip_atomic_fetch_min(first_row(ch), t, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *fl(L::oL, 8 * g + 4 * u + i, s) = kk4[i];
+      }
     };
     // M, by two waves: a lane a row of a 16 x 16 block, from M (I + L) = I, column
     // after column from the last, in both; then one puts the blocks into place, the
     // other forms M21.
-    auto put_inverse = [&]() {
+    auto put_inverse = [&](int ch) {
       const int m = ll & 15, g = ll >> 4, b0 = ll & 16;   // lanes 0-15 the first block, 16-31 the second
       float x[16];
 #pragma unroll
@@ -484,6 +527,10 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
           for (int c = 0; c < j; ++c) x[c] -= x[j] * lt[j2][j & 1][c / 4][c % 4];
       }
       if (pw == 0) {
+        const int first = *first_row(ch);
+        if (__any(first < kC))
+#pragma unroll
+          for (int c = 0; c < 16; ++c) x[c] = b0 + m >= first ? __builtin_nanf("") : x[c];
         if (ll < 32)
 #pragma unroll
           for (int c = 0; c < 16; c += 8) {
@@ -534,7 +581,7 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_chunks(SlotArgs a) {
     for (int it = 0; it <= nch; ++it) {
       const bool live = it < nch;
       anew();
-      if (it > 0 && pw < 2) put_inverse();
+      if (it > 0 && pw < 2) put_inverse(it - 1);
       anew();
       if (it > 0 && it + 1 < nch && pw == 3) put_scalars(it + 1);
       if (it + 2 < nch) {

@@ -15,7 +15,7 @@
 // fp32 matrix instructions are a sixth and two fifths (the products with the state fill
 // the matrix unit while nothing else gets on; then the producers' write keys, decays
 // and rows; then solve, update and output).  3 fp32 prompts of up to 333 tokens x 4
-// heads of 64: 74 us; 12 per-channel ones of up to 700 x 16 heads of 128: 324 us (one
+// heads of 64: 76 us; 12 per-channel ones of up to 700 x 16 heads of 128: 327 us (one
 // after the other, without producers, 135 and, with products a quarter cheaper, 479).
 // Producers at a higher priority made it 5 and 4 % slower.
 #include "pdn_device.hpp"
@@ -162,12 +162,22 @@ __global__ __launch_bounds__(W * 4 + 256) void slot_runs(SlotArgs a) {
         }
         // ---- O: rows 8-15 of the products, plus P E
         if (lr < B || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
+        floatx4 pe = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+        for (int i = 0; i < 4; ++i) mma4(pe, p4[i], e[i]);
         // (the state's products are behind it too: its next use is a step away)
 #pragma unroll
         for (int m = 0; m < MB; ++m) asm volatile("" : "+v"(S.t[m]));
-        settled(yz);
+        settled(pe);
+        if (__any(!all_numbers(e))) {   // (once more, without them)
+          const int first = first_of(take_out(e, tb, B));
+          pe = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mma4(pe, p4[i], e[i]);
+          settled(pe);
+          put_from(pe, tb, first, __builtin_nanf(""));
+        }
+        yz += pe;
         const __amdgpu_buffer_rsrc_t r = next(ro, left);
         left -= B;
         if (lg >= 2)

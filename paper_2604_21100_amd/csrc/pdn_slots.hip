@@ -656,9 +656,14 @@ __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
     {
       floatx4 p4 = *reinterpret_cast<const floatx4*>(&sLP[lr][tb]);
       if (lr < kSlotBlock || lg >= 2) p4 = floatx4{0.f, 0.f, 0.f, 0.f};
+      const bool hurt = __any(!all_numbers(e));
+      floatx4 en = e;
+      int first = kSlotBlock;
+      if (hurt) first = first_of(take_out(en, tb, kSlotBlock));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) mma4(yz, p4[i], e[i]);
+      for (int i = 0; i < 4; ++i) mma4(yz, p4[i], en[i]);
       settled(yz);
+      if (hurt) put_from(yz, tb, first, __builtin_nanf(""));
       if (lg >= 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
