@@ -9,7 +9,7 @@
 // numbers is exact, and a running sum over a large vocabulary has to be finer
 // than the steps between its tokens, which 32 bits are not.
 //
-// Two launches (one up to 24576 tokens: verify_one): the row the sequence stops at is
+// Two launches (one for smaller vocabularies: verify_one): the row the sequence stops at is
 // summed in segments of 2048 tokens, a workgroup each (every one finds the row for
 // itself: a few reads), then one wave a sequence finds the segment, and in it the token.
 // Segment sums are added in one order, so the token does not depend on which
@@ -17,8 +17,8 @@
 //
 // What bounds it: the row's (or two rows') reading in the first launch, 14 us for 64
 // sequences of 131072 (56 MB, 4 TB/s), and two launches' latency: the second is one
-// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.1 us, 64 of
-// 131072: 19.8 us.  A whole workgroup a sequence in the second, with barriers between
+// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.2 us in a graph
+// (9.8 to 10.4 called one by one, the host's time), 64 of 131072: 18.3 us.  A whole workgroup a sequence in the second, with barriers between
 // its levels, took 16 and 30 us in all.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
@@ -264,16 +264,25 @@ __global__ __launch_bounds__(kWave) void verify_pick(VerifyArgs a) {
   pick<T, kSeg / kWave>(a, seq, s, n, r, segs, l, load_sums, x);
 }
 
-// Vocabularies of up to three steps of it in one launch: a workgroup a sequence, a wave
-// a segment of 512 tokens in turn; sums in LDS, the token by the first wave.  A step of 8192
+// Smaller vocabularies in one launch: a workgroup a sequence, a wave a segment of 512
+// tokens in turn; sums in LDS, the token by the first wave.  A step of 8192
 // tokens takes 1.5 us of one compute unit, where the other form's first launch has them
-// all and its second costs 4 to 5 us (fp32 with q, us, two launches | one):
-//               1000       8000       16000      24000      32000
-//   1 sequence  10.2  5.4   9.3  6.1   9.2  7.6   9.4  9.0   9.3 10.3
-//   64          11.6  6.0  11.4  6.7  11.6  8.1  12.1  9.5  12.7 11.1
-//   256         12.0  6.3  13.4  7.2  15.8 10.2  19.7 12.1  20.0 14.2
+// all and its second costs 4 to 5 us.  The more sequences there are the fewer compute units
+// that leaves idle (fp32 with q, us, two launches | one; less with bf16 or without q, the
+// line between them the same within 1 us):
+//               1000       8000       16000      24576      32000      40000      50257      65536
+//   1 sequence  10.2  5.4   9.3  6.1   9.3  7.6   9.1  8.8   9.3 10.4   9.1 12.1   9.2 13.7   9.2 16.4
+//   16                               10.2  8.0   9.9  9.2  10.2 10.8  10.7 12.8  10.4 14.5  10.1 17.1
+//   64          11.6  6.0  11.4  6.7  11.6  8.1  10.8  9.4  12.6 11.1  12.6 14.3  14.1 16.2  14.1 19.8
+//   128                              13.1  8.5  12.8 10.7  15.0 12.9  17.2 15.5  18.0 17.0  18.9 20.2
+//   256         12.0  6.3  13.4  7.2  15.9  9.8  17.3 11.9  20.0 14.4  21.9 16.9  24.5 18.6  26.8 21.9
+//   512                              20.6 14.5  22.8 17.7  28.2 20.9  31.9 24.9  37.7 29.2  47.8 38.3
 // (A wave's segments all loaded first: 8.3 us at 1000 tokens, 10.2 at 32000.)
-constexpr int kOneWaves = 16, kOneSeg = kWave * kVec, kOneMost = 3 * kOneWaves * kOneSeg;
+constexpr int kOneWaves = 16, kOneSeg = kWave * kVec, kOneMost = 8 * kOneWaves * kOneSeg;
+bool one_launch(int64_t N, int64_t V) {
+  if (N >= 1 << 22) return false;   // (a launch holds fewer than 2^32 work items)
+  return V <= 24576 || (V <= kOneMost && V <= 24576 + 192 * N);
+}
 template <typename T>
 __global__ __launch_bounds__(kOneWaves * kWave) void verify_one(VerifyArgs a) {
   __shared__ double sums[kOneMost / kOneSeg][2];
@@ -320,7 +329,7 @@ __global__ __launch_bounds__(kOneWaves * kWave) void verify_one(VerifyArgs a) {
 
 template <typename T>
 hipError_t launch(const VerifyArgs& a, hipStream_t s) {
-  if (a.V <= kOneMost && a.N < 1 << 22) {   // (a launch holds fewer than 2^32 work items)
+  if (one_launch(a.N, a.V)) {
     hipLaunchKernelGGL((verify_one<T>), dim3(static_cast<unsigned>(a.N)), dim3(kOneWaves * kWave), 0, s, a);
     return hipGetLastError();
   }
