@@ -266,9 +266,9 @@ hipError_t launch_slots(const SlotArgs& a, int io_bf16, hipStream_t s);
 // needs no sum over its channels.  Heads of 128 x 128, us, a block of at most eight |
 // these chunks | runs of blocks (pdn_slot_runs.hip):
 //            SQUASH  16 heads       256 heads      1024 heads     k~ = k, 1024 heads
-//   8 tokens    9.1  11.0   9.7   12.2 14.6 12.5   34  56  50     33 47 46
-//   9 tokens    -    10.6  13.0   -    14.0 16.0   -   54  63     -  46 59
-//   32 tokens   -    10.7  19.8   -    15.1 23.8   -   58  91     -  49 87
+//   8 tokens    9.1  11.0   9.8   12.2 14.4 12.6   35  58  50     34 49 47
+//   9 tokens    -    11.0  13.0   -    14.3 16.2   -   58  63     -  48 60
+//   32 tokens   -    11.0  19.8   -    15.6 24.0   -   62  92     -  51 87
 inline bool slot_chunk_form(const SlotArgs& a, bool io_bf16) {
   return a.T > 8 && !a.tape && io_bf16 && a.gate != kGateChannel && a.knorm == kKnormNone &&
          (a.precond == kSquash || a.precond == kIdentity || a.precond == kExternal);
@@ -279,9 +279,9 @@ hipError_t launch_slot_chunks(const SlotArgs& a, hipStream_t s);
 // preconditioner state (read and written in place it has to be one workgroup's).
 // 512 tokens, k~ = k, us, whole | halves:
 //   heads                     16       128       160       256
-//   chunks, scalar gate     60 46     67  56    69 100    76 109
-//   runs, per-channel      210 155   217 165   220 235   231 252
-//   runs, fp32             201 147   211 158   215 228   218 237
+//   chunks, scalar gate     65 51     73  60    74 107    82 115
+//   runs, per-channel      226 168   230 183   235 260   240 267
+//   runs, fp32             202 150   213 161   211 227   222 233
 inline bool slot_halves(const SlotArgs& a) {
   return a.dv == 128 && !has_gram(a.precond) && a.B * a.H <= 128;
 }
