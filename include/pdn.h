@@ -385,7 +385,10 @@ typedef struct {
 /* Advances each sequence's state over its tokens: reads it from `slot`, writes
  * the state after the last token (S, A) to `slot_out`, and o.  in->S0 and in->A0
  * must be NULL (PDN_ERR_VALUE).  One launch, no workspace.  Tokens pending
- * on a tape are not looked at: apply or drop them first (pdn_slot_draft). */
+ * on a tape are not looked at: apply or drop them first (pdn_slot_draft).
+ * A head's tokens run on one compute unit, one chunk after the other: one long
+ * prompt of few heads is faster through pdn_chunk_fwd (16 heads x 2048 tokens in
+ * bf16: 71 us against 319), whose bf16 states are less exact. */
 pdn_status pdn_slot_fwd(const pdn_problem* problem, const pdn_inputs* in,
                         const pdn_slots* slots, void* o, void* hip_stream);
 

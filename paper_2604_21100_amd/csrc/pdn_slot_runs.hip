@@ -12,7 +12,7 @@
 // summed and it is consumed in the next.
 //
 // What bounds it: the step's chain, 1.8 us at 64 x 64 and 3.7 at 128 x 128, of which the
-// fp32 matrix instructions are a sixth and two fifths (the products with the state fill
+// fp32 matrix instructions are a fifth and two fifths (the products with the state fill
 // the matrix unit while nothing else gets on; then the producers' write keys, decays
 // and rows; then solve, update and output).  3 fp32 prompts of up to 333 tokens x 4
 // heads of 64: 76 us; 12 per-channel ones of up to 700 x 16 heads of 128: 327 us (one

@@ -78,7 +78,7 @@ __device__ __forceinline__ float write_key(const SlotArgs& a, float k, float x, 
 //   S' = alpha S + e kt^T,  e = beta (v - (alpha S) k),  o = scale ((alpha S) q + (kt . q) e)
 // on the vector unit: six operations a state element, which no matrix instruction
 // would make fewer.  What bounds it is reading and writing the state, so the rest is
-// kept small: 104 registers and 2 KB of LDS, four workgroups a compute unit, the
+// kept small: at most 108 registers and 2 KB of LDS, four workgroups a compute unit, the
 // loads of some in flight beside the work of others (64 sequences x 16 heads of 128 x
 // 128: 26 us, 5.2 TB/s; 256 x 32: 214 us, 5.0 TB/s; a 1 GiB copy makes 5.1).  One
 // sequence of 16 heads: 6 us, a launch and four dependent memory latencies.
@@ -179,11 +179,11 @@ __global__ __launch_bounds__(DV * 2, 4) void slot_step(SlotArgs a) {
 //
 // What bounds it is the chain of a workgroup, of which a compute unit holds two: rows,
 // L and P (two barriers), the state's arrival, records, products, solve.  Drafts of
-// 64 sequences x 16 heads: 45 us for 152 MB, 3.4 TB/s; 96 x 16 of four tokens with
-// per-channel decays 65 us, 3.3 TB/s; five tokens of one sequence 10 us.  Eight
-// tokens of 64 x 16 heads without a tape 34 us.  (With pending counts read ahead of
+// 64 sequences x 16 heads: 44 us for 152 MB, 3.5 TB/s; 96 x 16 of four tokens with
+// per-channel decays 63 us, 3.4 TB/s; five tokens of one sequence 10 us.  Eight
+// tokens of 64 x 16 heads without a tape 35 us.  (With pending counts read ahead of
 // the rows drafts took 45 and 64 us, with the state first 46 and 66; a third workgroup
-// would leave a lane 80 of the 127 registers that it takes.)
+// would leave a lane 80 of the 128 registers that it takes.)
 template <typename T, int DK, int DV, bool CH, bool DRAFT>
 __global__ __launch_bounds__(DV * 4, 4) void slot_blocks(SlotArgs a) {
   typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -15,10 +15,10 @@
 // Segment sums are added in one order, so the token does not depend on which
 // workgroup was first.
 //
-// What bounds it: the row's (or two rows') reading in the first launch, 14 us for 64
-// sequences of 131072 (56 MB, 4 TB/s), and two launches' latency: the second is one
-// wave's chain of dependent reads, 6 to 7 us.  One sequence of 50257: 9.2 us in a graph
-// (9.8 to 10.4 called one by one, the host's time), 64 of 131072: 18.3 us.  A whole workgroup a sequence in the second, with barriers between
+// What bounds it: the row's (or two rows') reading in the first launch, 12 us for 64
+// sequences of 131072 (56 MB, 4.5 TB/s), and two launches' latency: the second is one
+// wave's chain of dependent reads, 5 to 8 us.  One sequence of 50257: 9.2 us in a graph
+// (9.8 to 10.4 called one by one, the host's time), 64 of 131072: 18.1 us.  A whole workgroup a sequence in the second, with barriers between
 // its levels, took 16 and 30 us in all.
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
