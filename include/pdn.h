@@ -338,7 +338,8 @@ pdn_status pdn_chunk_bwd_train(const pdn_problem* problem, const pdn_inputs* in,
  * Log-decays, a channel's too, and g_p may be as low as the type goes, and -inf
  * (the state, or a channel of it, is forgotten: e.g. a document's first token).
  * A NaN or Inf in a token shows in that sequence and slot only, from that token
- * on (one of a query in that token's o, one of a value in its column).
+ * on (one of a query in that token's o, one of a value in its column; a NaN of
+ * beta_p or g_p with SQUASH in A only, which then gives the write keys' gain x).
  * B H must be below 2^22.
  *
  * `starts`, `slot`, `slot_out`, `fresh`, `accepted` are device arrays, read by
