@@ -58,7 +58,7 @@
 extern "C" {
 #endif
 
-#define PDN_ABI_VERSION 6
+#define PDN_ABI_VERSION 7
 
 typedef enum {
   PDN_OK = 0,
@@ -423,6 +423,165 @@ pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype,
                             const float* u, const float* r, const int32_t* starts,
                             int32_t* accepted, int32_t* token, void* ws,
                             size_t ws_bytes, void* hip_stream);
+
+/* ------------------------------------------------- around the rule in a block
+ * What a block does between its matrix products and the rule: the residual sum
+ * with the norms on both sides of it, and the norms over each head's channels.
+ * Forward and backward, for training batches and for a server's few rows alike.
+ *
+ * Weights, the scale and their gradients are fp32, sums and factors too; the
+ * tensors of rows are fp32 or bf16, rounded once when they are written.  They
+ * need to be aligned to an element only (16 bytes are faster).  Rows do not
+ * depend on each other: a NaN or Inf shows in its own row, and in the gradients of the
+ * vectors in its channel.  A row's squares are summed in fp32: a row with a sum past
+ * 3.4e38 gives zeros.  Gradients of vectors are summed in one order, so a
+ * call's results are the same each time.  No call allocates. */
+
+typedef struct {
+  int64_t rows, D;      /* rows of D channels; D from 1 to 16384               */
+  pdn_dtype io;         /* y, u, du, dy                                        */
+  pdn_dtype stream;     /* residual, h, dh, dresidual                          */
+  int32_t post_norm;    /* non-zero: y is normed itself                        */
+  float alpha;          /* the branch's factor; finite                         */
+  float eps;            /* > 0, finite                                         */
+} pdn_rnorm;
+
+/* A block's output joins the residual stream; the next block's input is its norm:
+ *   a = y, or with post_norm  y / sqrt(mean(y^2) + eps) * post_weight
+ *   h = residual + alpha * scale * a
+ *   u = h / sqrt(mean(h^2) + eps) * weight
+ * (u of h before its rounding.)  residual [rows, D] or NULL (= 0); weight,
+ * post_weight, scale [D] or NULL (= 1; post_weight without post_norm is
+ * PDN_ERR_VALUE); h NULL: not written.  h may be residual itself (updated in
+ * place, stream dtype); nothing else may overlap. */
+pdn_status pdn_residual_norm(const pdn_rnorm* problem, const void* y, const void* residual,
+                             const float* weight, const float* post_weight, const float* scale,
+                             void* u, void* h, void* hip_stream);
+
+/* Gradients of <du, u> + <dh, h>, from the h that the forward wrote (or, where
+ * none was, its like).  dh: NULL (= 0).  y is needed with post_norm and for dscale.
+ * dresidual and the vectors' gradients may be NULL to skip them; a vector that is
+ * not given has none (PDN_ERR_VALUE).  dresidual may be dh itself.  `ws`: 256-byte
+ * aligned, of at least pdn_residual_norm_bwd_workspace_size bytes. */
+pdn_status pdn_residual_norm_bwd_workspace_size(const pdn_rnorm* problem, size_t* bytes);
+pdn_status pdn_residual_norm_bwd(const pdn_rnorm* problem, const void* du, const void* dh,
+                                 const void* h, const void* y, const float* weight,
+                                 const float* post_weight, const float* scale, void* dy,
+                                 void* dresidual, float* dweight, float* dpost_weight,
+                                 float* dscale, void* ws, size_t ws_bytes, void* hip_stream);
+
+typedef enum {
+  PDN_NORM_RMS = 0,     /* x / sqrt(mean(x^2) + eps): a recurrence's output    */
+  PDN_NORM_L2 = 1       /* x / sqrt(sum(x^2) + eps): queries and keys          */
+} pdn_norm;
+typedef enum {
+  PDN_ACT_NONE = 0,     /* no gate                                             */
+  PDN_ACT_SILU = 1,     /* z / (1 + exp(-z))                                   */
+  PDN_ACT_SIGMOID = 2   /* 1 / (1 + exp(-z))                                   */
+} pdn_act;
+
+typedef struct {
+  int64_t tokens, H;    /* tensors [tokens, H, d], a token's row dense         */
+  int32_t d;            /* channels of a head; from 1 to 512                   */
+  pdn_dtype io;         /* every tensor of rows                                */
+  pdn_norm norm;
+  pdn_act act;
+  int32_t head_weight;  /* weight and dweight are 0: [d], else: [H, d]         */
+  float eps;            /* > 0, finite                                         */
+  int64_t x_stride, z_stride, y_stride, dy_stride, dx_stride, dz_stride;
+                        /* elements from a token's row to the next, at least
+                           H d (rows may be slices of wider ones); 0: dense    */
+} pdn_hnorm;
+
+/* y = norm(x) * weight * act(z), over each head's channels.  weight: NULL (= 1); z:
+ * NULL iff PDN_ACT_NONE.  y may be x itself (same stride); nothing else may
+ * overlap, but rows of one stride may interleave. */
+pdn_status pdn_head_norm(const pdn_hnorm* problem, const void* x, const void* z,
+                         const float* weight, void* y, void* hip_stream);
+
+/* Gradients of <dy, y>.  dz: NULL iff PDN_ACT_NONE; dweight: NULL to skip it, or
+ * without a weight.  dx may be dy itself (same stride).  `ws` as above. */
+pdn_status pdn_head_norm_bwd_workspace_size(const pdn_hnorm* problem, size_t* bytes);
+pdn_status pdn_head_norm_bwd(const pdn_hnorm* problem, const void* dy, const void* x,
+                             const void* z, const float* weight, void* dx, void* dz,
+                             float* dweight, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* ------------------------------------------------------ from logits to tokens
+ * pdn_logits makes of logits the probabilities that pdn_draft_verify reads;
+ * pdn_token_counts keeps the table of tokens that a sequence has had, in the same
+ * slots as its state.  A round: pdn_slot_draft .. logits -> pdn_logits ->
+ * pdn_draft_verify -> pdn_token_counts with its `accepted`, and pdn_slot_draft again.
+ *
+ * A count is 32 bits: the lower 31 how often the sequence generated the token, the
+ * sign bit set if the prompt has it.
+ *
+ * Rows are packed as in pdn_draft_verify: `starts` [N + 1], NULL for rows / N rows
+ * each.  Lists on the device are not checked: row numbers are clamped to [0, rows],
+ * a sequence whose slot is outside [0, slots) is left out (its rows of `out`, and
+ * the table, stay as they were), tokens outside [0, V) count for nothing.  Rows that
+ * belong to no sequence stay as they were. */
+
+typedef struct {
+  int64_t rows, V, N;        /* N sequences                                     */
+  pdn_dtype dtype;           /* logits                                          */
+  pdn_dtype out_dtype;
+  int32_t probs;             /* 0: the changed logits, else probabilities       */
+  int64_t stride;            /* elements from a row of logits to the next, at
+                                least V; 0: V.  Rows of out are dense           */
+  const void* logits;        /* [rows, V]                                       */
+  const int32_t* starts;
+  const float* temperature;  /* [N], or NULL (= 1)                              */
+  const float* repetition;   /* [N] or NULL (= 1)                               */
+  const float* presence;     /* [N] or NULL (= 0)                               */
+  const float* frequency;    /* [N] or NULL (= 0)                               */
+  const int32_t* counts;     /* [slots, V] or NULL (= 0)                        */
+  int64_t slots;             /* rows of counts                                  */
+  const int32_t* slot;       /* [N] or NULL (the sequence's own number); with
+                                counts only                                     */
+  const int32_t* ids;        /* [rows] tokens fed (as for pdn_draft_verify), not
+                                in the table yet: row t of a sequence counts
+                                those of its rows up to t.  NULL: none          */
+  const int32_t* bias_starts;/* [N + 1] a sequence's entries of the next two, or
+                                NULL                                            */
+  const int32_t* bias_ids;   /* [biases]; of a token listed twice in a sequence
+                                the last entry holds                            */
+  const float* bias_values;  /* [biases]                                        */
+  int64_t biases;
+  const int32_t* mask;       /* [masks, (V + 31) / 32]: token j is allowed where
+                                bit j % 32 of word j / 32 is set; or NULL       */
+  int64_t masks;
+  const int32_t* mask_rows;  /* [rows] a row's mask, outside [0, masks): none.
+                                NULL: its own number (masks >= rows)            */
+} pdn_logits_args;
+
+/* Token j of a row, c its count (table and ids), l its logit:
+ *   l = l > 0 ? l / repetition : l * repetition    if c > 0 or the prompt has it
+ *   l = (l - frequency * c) - presence             if c > 0
+ *   l = l + bias
+ *   l = -inf                                       if the mask does not allow it
+ * each step rounded to fp32.  out: l, or p = softmax(l / temperature); with a
+ * temperature that is not above 0 (or NaN) one at the largest l (the lowest token of
+ * several), else zero.  A row in which nothing is left (every l -inf) is zeros:
+ * pdn_draft_verify then gives token -1.  Tokens at +inf share the probability.
+ * A NaN in a place that the mask forbids is not seen; any other makes its row NaN.
+ * out [rows, V] may be the logits themselves (same dtype, dense); nothing else may
+ * overlap.  All row tensors need to be aligned to an element only.  `ws`: 256-byte
+ * aligned, of pdn_logits_workspace_size bytes (none without probs). */
+pdn_status pdn_logits_workspace_size(int64_t rows, int64_t V, size_t* bytes);
+pdn_status pdn_logits(const pdn_logits_args* args, void* out, void* ws, size_t ws_bytes,
+                      void* hip_stream);
+
+/* Adds tokens to the table: of each sequence's ids the first accepted[n] (NULL: all),
+ * as generated ones, or with `prompt` as the prompt's.  The counts are read from
+ * slot[n] (NULL: n; `fresh` non-zero: zero, nothing is read) and written to slot_out[n]
+ * (NULL: slot; another one: a fork).  Without slot_out and fresh only the tokens'
+ * own entries are touched.  A slot written by one sequence must not be read or written
+ * by another of the same call, but sequences may add to one slot without slot_out and
+ * fresh.  accepted is pdn_draft_verify's: the tokens fed that hold. */
+pdn_status pdn_token_counts(int64_t N, int64_t rows, int64_t V, int64_t slots, int32_t prompt,
+                            const int32_t* ids, const int32_t* starts, const int32_t* slot,
+                            const int32_t* slot_out, const int32_t* fresh,
+                            const int32_t* accepted, int32_t* counts, void* hip_stream);
 
 /* Static, NUL-terminated description of a status code. */
 const char* pdn_status_string(pdn_status status);

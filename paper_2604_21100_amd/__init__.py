@@ -91,6 +91,10 @@ GRAM_PRECONDS = ("squash", "diag_sm", "atq")
 # write-key normalisation of the squash mode (pdn_knorm)
 KNORMS = {"none": 0, "m": 1, "1pm": 2, "beta": 3}
 
+# what a head norm divides by, and the activation of its gate (pdn_norm, pdn_act)
+NORMS = {"rms": 0, "l2": 1}
+ACTS = {"none": 0, "silu": 1, "sigmoid": 2}
+
 _vp = ctypes.c_void_p
 
 
@@ -127,6 +131,37 @@ class Slots(ctypes.Structure):
                                       "S", "A", "tape")]
                 + [("tape_tokens", ctypes.c_int64), ("pending", _vp),
                    ("accepted", _vp)])
+
+
+class Rnorm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("D", ctypes.c_int64),
+                ("io", ctypes.c_int), ("stream", ctypes.c_int),
+                ("post_norm", ctypes.c_int32), ("alpha", ctypes.c_float),
+                ("eps", ctypes.c_float)]
+
+
+class Hnorm(ctypes.Structure):
+    _fields_ = ([("tokens", ctypes.c_int64), ("H", ctypes.c_int64),
+                 ("d", ctypes.c_int32), ("io", ctypes.c_int),
+                 ("norm", ctypes.c_int), ("act", ctypes.c_int),
+                 ("head_weight", ctypes.c_int32), ("eps", ctypes.c_float)]
+                + [(n, ctypes.c_int64) for n in (
+                    "x_stride", "z_stride", "y_stride", "dy_stride",
+                    "dx_stride", "dz_stride")])
+
+
+class LogitsArgs(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int64) for n in ("rows", "V", "N")]
+                + [("dtype", ctypes.c_int), ("out_dtype", ctypes.c_int),
+                   ("probs", ctypes.c_int32), ("stride", ctypes.c_int64)]
+                + [(n, _vp) for n in ("logits", "starts", "temperature",
+                                      "repetition", "presence", "frequency",
+                                      "counts")]
+                + [("slots", ctypes.c_int64)]
+                + [(n, _vp) for n in ("slot", "ids", "bias_starts",
+                                      "bias_ids", "bias_values")]
+                + [("biases", ctypes.c_int64), ("mask", _vp),
+                   ("masks", ctypes.c_int64), ("mask_rows", _vp)])
 
 
 _lib.pdn_workspace_size.argtypes = [ctypes.POINTER(Problem), ctypes.c_int,
@@ -172,6 +207,29 @@ _lib.pdn_draft_verify.restype = ctypes.c_int
 _lib.pdn_draft_verify_workspace_size.argtypes = [
     ctypes.c_int64, ctypes.c_int64, ctypes.POINTER(ctypes.c_size_t)]
 _lib.pdn_draft_verify_workspace_size.restype = ctypes.c_int
+_size_p = ctypes.POINTER(ctypes.c_size_t)
+_lib.pdn_residual_norm.argtypes = [ctypes.POINTER(Rnorm), *[_vp] * 8]
+_lib.pdn_residual_norm_bwd.argtypes = [ctypes.POINTER(Rnorm), *[_vp] * 13,
+                                       ctypes.c_size_t, _vp]
+_lib.pdn_residual_norm_bwd_workspace_size.argtypes = [ctypes.POINTER(Rnorm),
+                                                      _size_p]
+_lib.pdn_head_norm.argtypes = [ctypes.POINTER(Hnorm), *[_vp] * 5]
+_lib.pdn_head_norm_bwd.argtypes = [ctypes.POINTER(Hnorm), *[_vp] * 8,
+                                   ctypes.c_size_t, _vp]
+_lib.pdn_head_norm_bwd_workspace_size.argtypes = [ctypes.POINTER(Hnorm),
+                                                  _size_p]
+_lib.pdn_logits.argtypes = [ctypes.POINTER(LogitsArgs), _vp, _vp,
+                            ctypes.c_size_t, _vp]
+_lib.pdn_logits_workspace_size.argtypes = [ctypes.c_int64, ctypes.c_int64,
+                                           _size_p]
+_lib.pdn_token_counts.argtypes = [*[ctypes.c_int64] * 4, ctypes.c_int32,
+                                  *[_vp] * 8]
+for _f in (_lib.pdn_residual_norm, _lib.pdn_residual_norm_bwd,
+           _lib.pdn_residual_norm_bwd_workspace_size, _lib.pdn_head_norm,
+           _lib.pdn_head_norm_bwd, _lib.pdn_head_norm_bwd_workspace_size,
+           _lib.pdn_logits, _lib.pdn_logits_workspace_size,
+           _lib.pdn_token_counts):
+    _f.restype = ctypes.c_int
 _lib.pdn_noalloc_scratch_bytes.argtypes = []
 _lib.pdn_noalloc_scratch_bytes.restype = ctypes.c_size_t
 _lib.pdn_status_string.argtypes = [ctypes.c_int]
@@ -182,7 +240,7 @@ _lib.pdn_scan_segments.argtypes = [ctypes.POINTER(Problem),
                                    ctypes.POINTER(ctypes.c_int)]
 _lib.pdn_scan_segments.restype = ctypes.c_int
 
-ABI_VERSION = 6   # PDN_ABI_VERSION: the struct layouts mirrored above
+ABI_VERSION = 7   # PDN_ABI_VERSION: the struct layouts mirrored above
 if _lib.pdn_abi_version() != ABI_VERSION:
     raise ImportError(f"{LIB_PATH} implements ABI version "
                       f"{_lib.pdn_abi_version()}, this binding mirrors "
@@ -194,7 +252,11 @@ EXPORTED = ("pdn_workspace_size", "pdn_chunk_fwd", "pdn_chunk_fwd_events",
             "pdn_noalloc_scratch_bytes", "pdn_status_string",
             "pdn_abi_version", "pdn_scan_segments", "pdn_slot_fwd",
             "pdn_slot_draft", "pdn_draft_verify",
-            "pdn_draft_verify_workspace_size")
+            "pdn_draft_verify_workspace_size", "pdn_residual_norm",
+            "pdn_residual_norm_bwd", "pdn_residual_norm_bwd_workspace_size",
+            "pdn_head_norm", "pdn_head_norm_bwd",
+            "pdn_head_norm_bwd_workspace_size", "pdn_logits",
+            "pdn_logits_workspace_size", "pdn_token_counts")
 FWD_STAGE_EVENTS = 4   # PDN_FWD_STAGE_EVENTS
 BWD_STAGE_EVENTS = 7   # PDN_BWD_STAGE_EVENTS
 FWD_STAGES = ("precond", "chunk_prep", "chunk_scan")
@@ -574,3 +636,140 @@ def pdn_draft_verify(p, ids, u, r, *, q=None, starts=None, accepted=None,
     return _call_on(
         "pdn_draft_verify", p.device, stream, _pdn_torch.verify, _VERIFY,
         _VERIFY_SIZE, p, q, ids, u, r, starts, accepted, token, workspace)
+
+
+# ------------------------------------------------- around the rule in a block
+(_RNORM, _RNORM_BWD, _RNORM_SIZE, _HNORM, _HNORM_BWD, _HNORM_SIZE, _LOGITS,
+ _LOGITS_SIZE, _COUNTS) = map(_address, (
+     _lib.pdn_residual_norm, _lib.pdn_residual_norm_bwd,
+     _lib.pdn_residual_norm_bwd_workspace_size, _lib.pdn_head_norm,
+     _lib.pdn_head_norm_bwd, _lib.pdn_head_norm_bwd_workspace_size,
+     _lib.pdn_logits, _lib.pdn_logits_workspace_size, _lib.pdn_token_counts))
+
+
+def _dtype_number(dtype):
+    if dtype is None:
+        return -1
+    if dtype == torch.float32:
+        return PDN_F32
+    if dtype == torch.bfloat16:
+        return PDN_BF16
+    raise TypeError(f"tensors must be float32 or bfloat16, got {dtype}")
+
+
+def _act(act, z):
+    return ACTS[act if act is not None else "none" if z is None else "silu"]
+
+
+def pdn_residual_norm(y, residual=None, *, weight=None, post_norm=False,
+                      post_weight=None, scale=None, alpha=1.0, eps=1e-6,
+                      h_dtype=None, want_h=True, u=None, h=None, stream=None):
+    """A block's output y joins the residual stream, and the next block's input
+    is the norm of the sum (pdn_residual_norm of pdn.h):
+
+      h = residual + alpha * scale * (y, or RMSNorm(y) * post_weight)
+      u = RMSNorm(h) * weight
+
+    y, u: [..., D]; residual, h of their own dtype (an fp32 stream, say);
+    weight, post_weight, scale: [D] fp32 or None (= 1).  Without a residual
+    h_dtype (default: y's) names h's.  h may be residual itself.  Returns
+    (u, h); h is None with want_h=False."""
+    return _call_on(
+        "pdn_residual_norm", y.device, stream, _pdn_torch.residual_norm,
+        _RNORM, y, residual, weight, post_weight, scale, post_norm, alpha, eps,
+        _dtype_number(h_dtype), want_h, u, h)
+
+
+def pdn_residual_norm_bwd(du, h, y=None, *, dh=None, weight=None,
+                          post_norm=False, post_weight=None, scale=None,
+                          alpha=1.0, eps=1e-6, outputs=None,
+                          want_residual=True, want_vectors=True,
+                          workspace=None, stream=None):
+    """Gradients of <du, u> + <dh, h> of pdn_residual_norm, from the h that
+    it returned; y where it was normed or scaled.  Returns a dict of dy,
+    dresidual and, of the vectors given, dweight, dpost_weight, dscale.
+    ``outputs``: dict of preallocated tensors (dresidual may be dh)."""
+    out = outputs or {}
+    return _call_on(
+        "pdn_residual_norm_bwd", du.device, stream,
+        _pdn_torch.residual_norm_bwd, _RNORM_BWD, _RNORM_SIZE, du, h, y, dh,
+        weight, post_weight, scale, post_norm, alpha, eps, want_residual,
+        want_vectors, out.get("dy"), out.get("dresidual"), out.get("dweight"),
+        out.get("dpost_weight"), out.get("dscale"), workspace)
+
+
+def pdn_head_norm(x, *, norm="rms", weight=None, z=None, act=None, eps=1e-6,
+                  y=None, stream=None):
+    """Norm over each head's channels, with a weight and an output gate
+    (pdn_head_norm of pdn.h): norm(x) * weight * act(z).
+
+    x, z, y: [..., H, d], tokens' rows of any even spacing (slices of one
+    projection); norm "rms", or "l2" for unit queries and keys; weight [d] or
+    [H, d] fp32; act "silu" (default where z is given) or "sigmoid".  y may be
+    x itself.  Returns y."""
+    return _call_on(
+        "pdn_head_norm", x.device, stream, _pdn_torch.head_norm, _HNORM, x,
+        NORMS[norm], weight, z, _act(act, z), eps, y)
+
+
+def pdn_head_norm_bwd(dy, x, *, norm="rms", weight=None, z=None, act=None,
+                      eps=1e-6, outputs=None, want_vectors=True,
+                      workspace=None, stream=None):
+    """Gradients of <dy, y> of pdn_head_norm.  Returns a dict of dx and, where
+    there is a gate and a weight, dz and dweight.  ``outputs``: dict of
+    preallocated tensors, rows spaced like x's may be (dx may be dy)."""
+    out = outputs or {}
+    return _call_on(
+        "pdn_head_norm_bwd", x.device, stream, _pdn_torch.head_norm_bwd,
+        _HNORM_BWD, _HNORM_SIZE, dy, x, NORMS[norm], weight, z, _act(act, z),
+        eps, want_vectors, out.get("dx"), out.get("dz"), out.get("dweight"),
+        workspace)
+
+
+def pdn_logits_workspace_size(rows: int, V: int) -> int:
+    n = ctypes.c_size_t(0)
+    st = _lib.pdn_logits_workspace_size(rows, V, ctypes.byref(n))
+    if st != PDN_OK:
+        raise PdnError(st, "pdn_logits_workspace_size")
+    return n.value
+
+
+def pdn_logits(logits, *, probs=True, temperature=None, repetition=None,
+               presence=None, frequency=None, counts=None, slots=None,
+               ids=None, starts=None, bias=None, mask=None, mask_rows=None,
+               dtype=None, out=None, workspace=None, stream=None):
+    """Logits to the probabilities that pdn_draft_verify reads (pdn_logits of
+    pdn.h): penalties for repeated tokens, biases, grammar masks, softmax.
+
+    logits: [rows, V], rows of any spacing; starts [N + 1], slots [N]: the
+    packed sequences and their rows of counts [slots, V] (int32, see
+    pdn_token_counts); ids [rows]: the tokens fed, not counted yet;
+    temperature (0: the largest logit), repetition, presence, frequency: [N]
+    fp32; bias: (starts [N + 1], ids, values), lists of tokens and what is added
+    to their logits; mask: [masks, (V + 31) // 32] int32, a bit a token that is
+    allowed, mask_rows [rows] the mask of each row (-1: none).  Without starts
+    the rows are shared evenly by the sequences.  probs=False: the changed logits
+    themselves.  dtype: of the result (default fp32, of logits theirs); out may be
+    the logits.  Returns [rows, V]."""
+    bias = bias if bias is not None else (None, None, None)
+    if len(bias) != 3:
+        raise ValueError("bias must be (starts, ids, values)")
+    return _call_on(
+        "pdn_logits", logits.device, stream, _pdn_torch.logits, _LOGITS,
+        _LOGITS_SIZE, logits, probs, temperature, repetition, presence,
+        frequency, counts, slots, ids, starts, *bias, mask, mask_rows, out,
+        _dtype_number(dtype), workspace)
+
+
+def pdn_token_counts(ids, counts, *, starts=None, slots=None, slots_out=None,
+                     fresh=None, accepted=None, prompt=False, stream=None):
+    """Add tokens to the table of counts that pdn_logits reads
+    (pdn_token_counts of pdn.h): counts [slots, V] int32, zero at first.
+
+    ids: packed tokens; of each sequence the first accepted[n] (None: all) are
+    added to its row slots[n], as generated, or with prompt=True as the
+    prompt's.  fresh[n] non-zero: the row is cleared first; slots_out: the rows are
+    written there (a fork).  Returns counts."""
+    return _call_on(
+        "pdn_token_counts", counts.device, stream, _pdn_torch.token_counts,
+        _COUNTS, ids, counts, starts, slots, slots_out, fresh, accepted, prompt)

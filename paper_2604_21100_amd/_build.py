@@ -19,7 +19,8 @@ BUILD_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["pdn_host.cpp", "pdn_fwd.hip", "pdn_bwd.hip", "pdn_scan.hip",
            "pdn_rscan.hip", "pdn_step.hip", "pdn_slots.hip",
-           "pdn_slot_chunks.hip", "pdn_slot_runs.hip", "pdn_verify.hip"]
+           "pdn_slot_chunks.hip", "pdn_slot_runs.hip", "pdn_verify.hip",
+           "pdn_block_host.cpp", "pdn_block.hip", "pdn_logits.hip"]
 
 # Packed-fp32 VALU ops are disabled for all device code (they have produced
 # silent wrong results on this hardware generation); hipcc's host pass warns

@@ -304,6 +304,95 @@ struct VerifyArgs {
 int64_t verify_blocks(int64_t V);   // segments a row is summed in
 hipError_t launch_verify(const VerifyArgs& a, int io_bf16, hipStream_t s);
 
+// Norms around the rule in a block (pdn_block.hip): see pdn_rnorm and pdn_hnorm in pdn.h.
+struct RnormArgs {
+  int64_t rows, D;
+  float alpha, eps;
+  const void* y;
+  const void* residual;   // (forward)
+  const float* weight;
+  const float* post_weight;
+  const float* scale;
+  void* u;
+  void* h;
+  // backward
+  const void* du;
+  const void* dh;
+  const void* h_in;
+  void* dy;
+  void* dresidual;
+  float* dweight;
+  float* dpost_weight;
+  float* dscale;
+  float* part;            // [3][rnorm_parts][D] sums of some rows each
+  bool post_norm;
+};
+int64_t rnorm_parts(int64_t rows, int64_t D);
+hipError_t launch_rnorm_fwd(const RnormArgs& a, int io_bf16, int stream_bf16, hipStream_t s);
+hipError_t launch_rnorm_bwd(const RnormArgs& a, int io_bf16, int stream_bf16, hipStream_t s);
+constexpr int64_t kRnormMaxD = 16384;
+
+enum HeadAct { kActNone = 0, kActSilu = 1, kActSigmoid = 2 };
+struct HnormArgs {
+  int64_t M, H;           // tokens, heads
+  int d, act;
+  bool l2, head_weight;
+  float eps;
+  int64_t sx, sz, sy, sdy, sdx, sdz;   // elements from a token to the next
+  const void* x;
+  const void* z;
+  const float* weight;
+  void* y;
+  // backward
+  const void* dy;
+  void* dx;
+  void* dz;
+  float* dweight;
+  float* part;            // [hnorm_parts / H][H][d] sums of some tokens each
+};
+int64_t hnorm_parts(int64_t M, int64_t H, int d);
+hipError_t launch_hnorm_fwd(const HnormArgs& a, int io_bf16, hipStream_t s);
+hipError_t launch_hnorm_bwd(const HnormArgs& a, int io_bf16, hipStream_t s);
+constexpr int kHnormMaxD = 512;
+
+// From logits to tokens (pdn_logits.hip): see pdn_logits_args in pdn.h.
+struct LogitsArgs {
+  int64_t rows, V, N, stride, slots, biases, masks;
+  bool probs;
+  const void* logits;
+  void* out;
+  const int32_t* starts;
+  const float* temperature;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const int32_t* counts;
+  const int32_t* slot;
+  const int32_t* ids;
+  const int32_t* bias_starts;
+  const int32_t* bias_ids;
+  const float* bias_values;
+  const int32_t* mask;
+  const int32_t* mask_rows;
+  void* parts;            // [rows, logits_segments(V)] of 16 bytes
+};
+__host__ __device__ int64_t logits_segments(int64_t V);
+hipError_t launch_logits(const LogitsArgs& a, int in_bf16, int out_bf16, hipStream_t s);
+
+struct CountArgs {
+  int64_t N, rows, V, slots;
+  bool prompt;
+  const int32_t* ids;
+  const int32_t* starts;
+  const int32_t* slot;
+  const int32_t* slot_out;
+  const int32_t* fresh;
+  const int32_t* accepted;
+  int32_t* counts;
+};
+__host__ __device__ int64_t count_segments(int64_t V);
+hipError_t launch_counts(const CountArgs& a, hipStream_t s);
+
 struct WsLayout {
   size_t sumL, sumD, Abound, KtG, Tm, Pm, G, Qt, QL, KL, seg_end, seg_phi, seg_start, total;
   ScanSplit split;
