@@ -17,6 +17,7 @@
 
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
+#include "pdn_lanes.hpp"
 
 namespace pdn {
 
@@ -24,37 +25,84 @@ namespace {
 
 constexpr int kVec = 8;
 
-// Eight elements from column c of a row of n (aligned to an element only; past the
-// row: zero), or back.
-template <typename T>
-__device__ __forceinline__ void ld_row(const T* p, int c, int n, float (&v)[kVec]) {
-  T raw[kVec];
-  if (c + kVec <= n) {
-    __builtin_memcpy(raw, p + c, sizeof raw);
-  } else {
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) raw[i] = c + i < n ? p[c + i] : from_f<T>(0.f);
+// The eight columns of a thread: from `col` on in a row of n.  Loads must not branch (a wait for
+// each would follow it), so every thread loads eight columns of the row that are there,
+// and `keep` says which of them are its own: a last thread with fewer than eight takes the row's
+// last eight, one without any the first.  By the row: a multiple of eight columns, more than
+// eight, or fewer (its only thread then loads element by element).
+enum RowKind { kEights, kMore, kFewer };
+inline RowKind row_kind(int64_t n) { return n % 8 == 0 ? kEights : n > 8 ? kMore : kFewer; }
+template <RowKind KIND>
+struct Cols {
+  int at, n;
+  uint32_t keep;   // bit i: column at + i
+  __device__ __forceinline__ Cols(int col, int n) : n(n) {
+    const bool on = col < n;
+    if constexpr (KIND == kEights) {
+      at = on ? col : 0;
+      keep = on ? 0xff : 0;
+    } else if constexpr (KIND == kMore) {
+      at = on ? min(col, n - kVec) : 0;
+      keep = on ? (0xffu << (col - at)) & 0xff : 0;
+    } else {
+      at = 0;
+      keep = on ? (1u << n) - 1 : 0;
+    }
   }
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) v[i] = to_f(raw[i]);
-}
+};
+
+// Eight elements as they are in memory (aligned to an element only).
 template <typename T>
-__device__ __forceinline__ void st_row(T* p, int c, int n, const float (&v)[kVec]) {
-  T raw[kVec];
+struct Raw {
+  static constexpr int kWords = kVec * sizeof(T) / 4;
+  uint32_t w[kWords];
+  template <RowKind KIND>
+  __device__ __forceinline__ void load(const T* p, const Cols<KIND>& c) {
+    if constexpr (KIND != kFewer) {
+      __builtin_memcpy(w, p + c.at, sizeof w);
+    } else {
+      T x[kVec];
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) raw[i] = from_f<T>(v[i]);
-  if (c + kVec <= n) {
-    __builtin_memcpy(p + c, raw, sizeof raw);
-  } else {
+      for (int i = 0; i < kVec; ++i) x[i] = p[min(i, c.n - 1)];
+      __builtin_memcpy(w, x, sizeof w);
+    }
+  }
+  // zero in the columns that are not its own (apart from the load, as it waits for it)
+  template <RowKind KIND>
+  __device__ __forceinline__ void settle(const Cols<KIND>& c) {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (KIND == kEights) w[i] = c.keep ? w[i] : 0;
+      else if constexpr (sizeof(T) == 4) w[i] = c.keep >> i & 1 ? w[i] : 0;
+      else w[i] &= (c.keep >> (2 * i) & 1 ? 0xffffu : 0) | (c.keep >> (2 * i + 1) & 1 ? 0xffff0000u : 0);
+    }
+  }
+  __device__ __forceinline__ float operator[](int i) const {
+    if constexpr (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+    else return __builtin_bit_cast(float, i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+template <typename T, RowKind KIND>
+__device__ __forceinline__ void store(T* p, const Cols<KIND>& c, const float (&v)[kVec]) {
+  T x[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) x[i] = from_f<T>(v[i]);
+  if (c.keep == 0xff) {
+    __builtin_memcpy(p + c.at, x, sizeof x);
+  } else if constexpr (KIND != kEights) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
-      if (c + i < n) p[c + i] = raw[i];
+      if (c.keep >> i & 1) p[c.at + i] = x[i];
   }
 }
 // of a vector that may be NULL (= 1)
-__device__ __forceinline__ void ld_weight(const float* p, int c, int n, float (&v)[kVec]) {
+template <RowKind KIND>
+__device__ __forceinline__ void ld_weight(const float* p, const Cols<KIND>& c, float (&v)[kVec]) {
   if (p) {
-    ld_row(p, c, n, v);
+    Raw<float> r;
+    r.load(p, c);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) v[i] = r[i];
   } else {
 #pragma unroll
     for (int i = 0; i < kVec; ++i) v[i] = 1.f;
@@ -67,9 +115,7 @@ __device__ __forceinline__ float factor(float squares, float c, float eps) { ret
 template <int N>
 __device__ __forceinline__ void block_sum(float (&x)[N], float (*buf)[16][4], int& turn) {
 #pragma unroll
-  for (int k = 0; k < N; ++k)
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) x[k] += __shfl_xor(x[k], off, 64);
+  for (int k = 0; k < N; ++k) x[k] = wave_sum(x[k]);
   const int waves = blockDim.x >> 6;
   if (waves == 1) return;
   float(*const b)[4] = buf[turn & 1];
@@ -85,50 +131,63 @@ __device__ __forceinline__ void block_sum(float (&x)[N], float (*buf)[16][4], in
     for (int k = 0; k < N; ++k) x[k] += b[w][k];
 }
 
-template <typename TI, typename TS, int CH, bool POST>
-__global__ void rnorm_fwd(RnormArgs a) {
+template <int CH, RowKind KIND>
+__device__ __forceinline__ Cols<KIND> cols(int k, int D) {
+  return Cols<KIND>((k * blockDim.x + threadIdx.x) * kVec, D);
+}
+
+template <typename TI, typename TS, int CH, bool POST, RowKind KIND>
+__global__ __launch_bounds__(1024) void rnorm_fwd(RnormArgs a) {
   __shared__ float buf[2][16][4];
   int turn = 0;
   const int D = static_cast<int>(a.D);
   const float c = 1.f / a.D;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float h[CH][kVec], q[1];
-    const TI* const y = static_cast<const TI*>(a.y) + row * D;
-    float ry = 1.f;
+    const int64_t at = row * a.D;
+    Raw<TI> y[CH];
+    Raw<TS> x[CH];
 #pragma unroll
-    for (int k = 0; k < CH; ++k) ld_row(y, (k * blockDim.x + threadIdx.x) * kVec, D, h[k]);
+    for (int k = 0; k < CH; ++k) {
+      const auto o = cols<CH, KIND>(k, D);
+      y[k].load(static_cast<const TI*>(a.y) + at, o);
+      if (a.residual) x[k].load(static_cast<const TS*>(a.residual) + at, o);
+    }
+#pragma unroll
+    for (int k = 0; k < CH; ++k) y[k].settle(cols<CH, KIND>(k, D));
+    float h[CH][kVec], q[1] = {0.f}, ry = 1.f;
     if constexpr (POST) {
-      q[0] = 0.f;
 #pragma unroll
       for (int k = 0; k < CH; ++k)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) q[0] += h[k][i] * h[k][i];
+        for (int i = 0; i < kVec; ++i) q[0] += y[k][i] * y[k][i];
       block_sum(q, buf, turn);
       ry = factor(q[0], c, a.eps);
+      q[0] = 0.f;
     }
-    q[0] = 0.f;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * kVec;
+      const auto o = cols<CH, KIND>(k, D);
       float v[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) h[k][i] = y[k][i];
       if constexpr (POST) {
-        ld_weight(a.post_weight, col, D, v);
+        ld_weight(a.post_weight, o, v);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) h[k][i] *= ry * v[i];
       }
       if (a.scale) {
-        ld_row(a.scale, col, D, v);
+        ld_weight(a.scale, o, v);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) h[k][i] *= v[i];
       }
 #pragma unroll
       for (int i = 0; i < kVec; ++i) h[k][i] *= a.alpha;
       if (a.residual) {
-        ld_row(static_cast<const TS*>(a.residual) + row * D, col, D, v);
+        x[k].settle(o);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) h[k][i] += v[i];
+        for (int i = 0; i < kVec; ++i) h[k][i] += x[k][i];
       }
-      if (a.h) st_row(static_cast<TS*>(a.h) + row * D, col, D, h[k]);
+      if (a.h) store(static_cast<TS*>(a.h) + at, o, h[k]);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) q[0] += h[k][i] * h[k][i];
     }
@@ -136,88 +195,123 @@ __global__ void rnorm_fwd(RnormArgs a) {
     const float rh = factor(q[0], c, a.eps);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * kVec;
+      const auto o = cols<CH, KIND>(k, D);
       float v[kVec];
-      ld_weight(a.weight, col, D, v);
+      ld_weight(a.weight, o, v);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) v[i] *= h[k][i] * rh;
-      st_row(static_cast<TI*>(a.u) + row * D, col, D, v);
+      store(static_cast<TI*>(a.u) + at, o, v);
     }
   }
 }
 
-// A workgroup takes every gridDim-th row and keeps the vectors' gradients of its columns in
-// registers; rnorm_parts of them are summed by sum_parts.
-template <typename TI, typename TS, int CH, bool POST, bool SCALE>
-__global__ void rnorm_bwd(RnormArgs a) {
+// The backward: a workgroup takes every gridDim-th row and keeps the vectors' gradients of its
+// columns in registers; rnorm_parts of them are summed by sum_parts.  AHEAD: rows of
+// few threads, with the next row loaded while this one waits for its sums, and the vectors
+// in registers.
+constexpr int kAheadThreads = 256;
+template <typename TI, typename TS, int CH, bool Y, RowKind KIND>
+struct BackRows {   // what a row's step reads
+  Raw<TI> du[CH], y[Y ? CH : 1];
+  Raw<TS> h[CH], dh[CH];
+  __device__ __forceinline__ void load(const RnormArgs& a, int64_t row) {
+    const int64_t at = row * a.D;
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
+      du[k].load(static_cast<const TI*>(a.du) + at, o);
+      h[k].load(static_cast<const TS*>(a.h_in) + at, o);
+      if constexpr (Y) {
+        if (a.y) y[k].load(static_cast<const TI*>(a.y) + at, o);
+      }
+      if (a.dh) dh[k].load(static_cast<const TS*>(a.dh) + at, o);
+    }
+  }
+  __device__ __forceinline__ void settle(const RnormArgs& a) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
+      du[k].settle(o);
+      h[k].settle(o);
+      if constexpr (Y) y[k].settle(o);
+      dh[k].settle(o);
+    }
+  }
+};
+// the vectors at this thread's columns
+template <int CH, bool POST, bool SCALE, RowKind KIND>
+struct Vectors {
+  float w[CH][kVec], wp[POST ? CH : 1][kVec], sc[SCALE ? CH : 1][kVec];
+  __device__ __forceinline__ void load(const RnormArgs& a) {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
+      ld_weight(a.weight, o, w[k]);
+      if constexpr (POST) ld_weight(a.post_weight, o, wp[k]);
+      if constexpr (SCALE) ld_weight(a.scale, o, sc[k]);
+    }
+  }
+};
+template <typename TI, typename TS, int CH, bool POST, bool SCALE, bool AHEAD, RowKind KIND>
+__global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024, AHEAD ? 3 : 4) void rnorm_bwd(RnormArgs a) {
   __shared__ float buf[2][16][4];
   int turn = 0;
   const int D = static_cast<int>(a.D);
   const float c = 1.f / a.D;
   float dw[CH][kVec] = {}, dp[POST ? CH : 1][kVec] = {}, ds[SCALE ? CH : 1][kVec] = {};
+  Vectors<CH, POST, SCALE, KIND> v;
+  if constexpr (AHEAD) v.load(a);
+  BackRows<TI, TS, CH, POST || SCALE, KIND> r;
+  r.load(a, blockIdx.x);
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    float du[CH][kVec], h[CH][kVec], y[POST || SCALE ? CH : 1][kVec], q[POST ? 3 : 2] = {};
-    const int64_t at = row * D;
+    BackRows<TI, TS, CH, POST || SCALE, KIND> next;
+    if constexpr (AHEAD) {
+      r.settle(a);
+      if (row + gridDim.x < a.rows) next.load(a, row + gridDim.x);
+    } else {
+      if (row != blockIdx.x) r.load(a, row);
+      v.load(a);
+      r.settle(a);
+    }
+    const int64_t at = row * a.D;
+    float e[POST ? CH : 1][kVec], q[POST ? 3 : 2] = {};
 #pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * kVec;
-      float w[kVec];
-      ld_row(static_cast<const TI*>(a.du) + at, col, D, du[k]);
-      ld_row(static_cast<const TS*>(a.h_in) + at, col, D, h[k]);
-      if constexpr (POST || SCALE) {
-        if (a.y) ld_row(static_cast<const TI*>(a.y) + at, col, D, y[k]);
-      }
-      ld_weight(a.weight, col, D, w);
+    for (int k = 0; k < CH; ++k)
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        q[0] += h[k][i] * h[k][i];
-        q[1] += du[k][i] * w[i] * h[k][i];
-        if constexpr (POST) q[2] += y[k][i] * y[k][i];
+        q[0] += r.h[k][i] * r.h[k][i];
+        q[1] += r.du[k][i] * v.w[k][i] * r.h[k][i];
+        if constexpr (POST) q[2] += r.y[k][i] * r.y[k][i];
       }
-    }
     block_sum(q, buf, turn);
     const float rh = factor(q[0], c, a.eps), mh = (rh * q[1] * c) * rh * rh;
     const float ry = POST ? factor(q[POST ? 2 : 0], c, a.eps) : 1.f;
     float p[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const int col = (k * blockDim.x + threadIdx.x) * kVec;
-      float t[kVec], v[kVec];
-      ld_weight(a.weight, col, D, v);
+      const auto o = cols<CH, KIND>(k, D);
+      float t[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        t[i] = rh * (du[k][i] * v[i]) - h[k][i] * mh;
-        dw[k][i] += du[k][i] * (h[k][i] * rh);
+        t[i] = rh * (r.du[k][i] * v.w[k][i]) - r.h[k][i] * mh;
+        dw[k][i] += r.du[k][i] * (r.h[k][i] * rh);
+        if (a.dh) t[i] += r.dh[k][i];
       }
-      if (a.dh) {
-        ld_row(static_cast<const TS*>(a.dh) + at, col, D, v);
+      if (a.dresidual) store(static_cast<TS*>(a.dresidual) + at, o, t);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) t[i] += v[i];
-      }
-      if (a.dresidual) st_row(static_cast<TS*>(a.dresidual) + at, col, D, t);
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) t[i] *= a.alpha;
-      float wp[kVec];
-      if constexpr (POST) ld_weight(a.post_weight, col, D, wp);
-      if constexpr (SCALE) {
-        ld_weight(a.scale, col, D, v);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          if (a.y) ds[k][i] += t[i] * (POST ? y[k][i] * ry * wp[i] : y[k][i]);
-          t[i] *= v[i];
+      for (int i = 0; i < kVec; ++i) {
+        t[i] *= a.alpha;
+        if constexpr (SCALE) {
+          if (a.y) ds[k][i] += t[i] * (POST ? r.y[k][i] * ry * v.wp[POST ? k : 0][i] : r.y[k][i]);
+          t[i] *= v.sc[k][i];
+        }
+        if constexpr (POST) {
+          dp[k][i] += t[i] * (r.y[k][i] * ry);
+          e[k][i] = t[i] * v.wp[k][i];
+          p[0] += e[k][i] * r.y[k][i];
         }
       }
-      if constexpr (POST) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          dp[k][i] += t[i] * (y[k][i] * ry);
-          t[i] *= wp[i];
-          p[0] += t[i] * y[k][i];
-          du[k][i] = t[i];
-        }
-      } else {
-        st_row(static_cast<TI*>(a.dy) + at, col, D, t);
-      }
+      if constexpr (!POST) store(static_cast<TI*>(a.dy) + at, o, t);
     }
     if constexpr (POST) {
       block_sum(p, buf, turn);
@@ -225,51 +319,64 @@ __global__ void rnorm_bwd(RnormArgs a) {
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) du[k][i] = ry * du[k][i] - y[k][i] * my;
-        st_row(static_cast<TI*>(a.dy) + at, (k * blockDim.x + threadIdx.x) * kVec, D, du[k]);
+        for (int i = 0; i < kVec; ++i) e[k][i] = ry * e[k][i] - r.y[k][i] * my;
+        store(static_cast<TI*>(a.dy) + at, cols<CH, KIND>(k, D), e[k]);
       }
     }
+    if constexpr (AHEAD) r = next;
   }
 #pragma unroll
   for (int k = 0; k < CH; ++k) {
-    const int col = (k * blockDim.x + threadIdx.x) * kVec;
+    const auto o = cols<CH, KIND>(k, D);
     float* const part = a.part + blockIdx.x * a.D;
     const int64_t each = gridDim.x * a.D;
-    if (a.dweight) st_row(part, col, D, dw[k]);
+    if (a.dweight) store(part, o, dw[k]);
     if constexpr (POST) {
-      if (a.dpost_weight) st_row(part + each, col, D, dp[k]);
+      if (a.dpost_weight) store(part + each, o, dp[k]);
     }
     if constexpr (SCALE) {
-      if (a.dscale) st_row(part + 2 * each, col, D, ds[k]);
+      if (a.dscale) store(part + 2 * each, o, ds[k]);
     }
   }
 }
 
-// out[j] = sum over p of part[p][j], for up to three vectors: 64 columns a workgroup, a
-// sixteenth of the parts a wave, in 64 bits and always in the same order.
+// out[j] = sum over p of part[p][j], for up to three vectors: 16 columns a workgroup, every
+// 64th part a thread, in 64 bits and always in the same order.  What bounds it is
+// latency: sixteen parts are loaded at a time.
 struct SumArgs {
   const float* part[3];
   float* out[3];
   int64_t parts, width;
 };
+constexpr int kSumCols = 16, kSumRows = 64, kSumDeep = 8;
 __global__ __launch_bounds__(1024) void sum_parts(SumArgs a) {
-  __shared__ double sum[16][kWave];
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63;
-  const int64_t j = blockIdx.x * static_cast<int64_t>(kWave) + l;
-  const float* const part = a.part[blockIdx.y];
+  __shared__ double sum[kSumRows][kSumCols + 1];
+  const int c = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
+  const int64_t j = blockIdx.x * static_cast<int64_t>(kSumCols) + c;
+  const float* const part = a.part[blockIdx.y] + min(j, a.width - 1);
   double x = 0.0;
-  if (j < a.width)
-    for (int64_t p = w; p < a.parts; p += 16) x += part[p * a.width + j];
-  sum[w][l] = x;
+  for (int64_t p = g; p < a.parts; p += kSumRows * kSumDeep) {
+    float v[kSumDeep];
+#pragma unroll
+    for (int k = 0; k < kSumDeep; ++k) v[k] = part[min(p + k * kSumRows, a.parts - 1) * a.width];   // (no branch, so no wait)
+#pragma unroll
+    for (int k = 0; k < kSumDeep; ++k) x += p + k * kSumRows < a.parts ? v[k] : 0.f;
+  }
+  sum[g][c] = x;
   __syncthreads();
-  if (w == 0 && j < a.width) {
-    for (int k = 1; k < 16; ++k) x += sum[k][l];
+  if (g < 8) {
+    for (int k = 8; k < kSumRows; k += 8) x += sum[g + k][c];
+    sum[g][c] = x;   // (rows past the eighth are read above, these below)
+  }
+  __syncthreads();
+  if (g == 0 && j < a.width) {
+    for (int k = 1; k < 8; ++k) x += sum[k][c];
     a.out[blockIdx.y][j] = static_cast<float>(x);
   }
 }
 hipError_t launch_sums(const SumArgs& a, int vectors, hipStream_t s) {
   if (vectors == 0) return hipSuccess;
-  const unsigned blocks = static_cast<unsigned>((a.width + kWave - 1) / kWave);
+  const unsigned blocks = static_cast<unsigned>((a.width + kSumCols - 1) / kSumCols);
   hipLaunchKernelGGL(sum_parts, dim3(blocks, vectors), dim3(1024), 0, s, a);
   return hipGetLastError();
 }
@@ -281,31 +388,50 @@ int row_threads(int64_t D) {
   return t;
 }
 
-template <typename TI, typename TS, int CH>
+template <typename TI, typename TS, int CH, RowKind KIND>
 hipError_t rnorm_fwd_ch(const RnormArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20))), block(row_threads(a.D));
-  if (a.post_norm) hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, false>), grid, block, 0, s, a);
+  if (a.post_norm) hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, true, KIND>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, false, KIND>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+template <typename TI, typename TS, RowKind KIND>
+hipError_t rnorm_fwd_at(const RnormArgs& a, hipStream_t s) {
+  if constexpr (KIND != kFewer) {
+    if (a.D > 1024 * kVec) return rnorm_fwd_ch<TI, TS, 2, KIND>(a, s);
+  }
+  return rnorm_fwd_ch<TI, TS, 1, KIND>(a, s);
 }
 template <typename TI, typename TS>
 hipError_t rnorm_fwd_of(const RnormArgs& a, hipStream_t s) {
-  return a.D > 1024 * kVec ? rnorm_fwd_ch<TI, TS, 2>(a, s) : rnorm_fwd_ch<TI, TS, 1>(a, s);
+  const RowKind kind = row_kind(a.D);
+  return kind == kEights ? rnorm_fwd_at<TI, TS, kEights>(a, s) : kind == kMore ? rnorm_fwd_at<TI, TS, kMore>(a, s)
+                                                                              : rnorm_fwd_at<TI, TS, kFewer>(a, s);
 }
 
-template <typename TI, typename TS, int CH>
+template <typename TI, typename TS, int CH, bool AHEAD, RowKind KIND>
 hipError_t rnorm_bwd_ch(const RnormArgs& a, hipStream_t s) {
   const dim3 grid(static_cast<unsigned>(rnorm_parts(a.rows, a.D))), block(row_threads(a.D));
   const bool scale = a.scale || a.dscale;
-  if (a.post_norm && scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, true>), grid, block, 0, s, a);
-  else if (a.post_norm) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, false>), grid, block, 0, s, a);
-  else if (scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, false>), grid, block, 0, s, a);
+  if (a.post_norm && scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, true, AHEAD, KIND>), grid, block, 0, s, a);
+  else if (a.post_norm) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, false, AHEAD, KIND>), grid, block, 0, s, a);
+  else if (scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, true, AHEAD, KIND>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, false, AHEAD, KIND>), grid, block, 0, s, a);
   return hipGetLastError();
+}
+template <typename TI, typename TS, RowKind KIND>
+hipError_t rnorm_bwd_at(const RnormArgs& a, hipStream_t s) {
+  if constexpr (KIND != kFewer) {
+    if (row_threads(a.D) > kAheadThreads)
+      return a.D > 1024 * kVec ? rnorm_bwd_ch<TI, TS, 2, false, KIND>(a, s) : rnorm_bwd_ch<TI, TS, 1, false, KIND>(a, s);
+  }
+  return rnorm_bwd_ch<TI, TS, 1, true, KIND>(a, s);
 }
 template <typename TI, typename TS>
 hipError_t rnorm_bwd_of(const RnormArgs& a, hipStream_t s) {
-  return a.D > 1024 * kVec ? rnorm_bwd_ch<TI, TS, 2>(a, s) : rnorm_bwd_ch<TI, TS, 1>(a, s);
+  const RowKind kind = row_kind(a.D);
+  return kind == kEights ? rnorm_bwd_at<TI, TS, kEights>(a, s) : kind == kMore ? rnorm_bwd_at<TI, TS, kMore>(a, s)
+                                                                              : rnorm_bwd_at<TI, TS, kFewer>(a, s);
 }
 
 // act(z) and its derivative, from e = exp(-|z|) (no overflow at either end)
@@ -340,21 +466,21 @@ int head_lanes(int d) {
   while (L * kVec < d) L *= 2;
   return L;
 }
-__device__ __forceinline__ float lanes_sum(float x, int L) {
-  for (int off = L >> 1; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
-}
-
-template <typename T, int ACT>
+template <typename T, int ACT, RowKind KIND>
 __global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L) {
-  const int col = (threadIdx.x & (L - 1)) * kVec, group = threadIdx.x / L, groups = kThreads / L;
+  const Cols<KIND> o((threadIdx.x & (L - 1)) * kVec, a.d);
+  const int group = threadIdx.x / L, groups = kThreads / L;
   const int64_t head = blockIdx.x % a.H, first = blockIdx.x / a.H, each = gridDim.x / a.H;
+  const T* const px = static_cast<const T*>(a.x) + head * a.d;
+  const T* const pz = static_cast<const T*>(a.z) + head * a.d;
   float w[kVec];
-  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, col, a.d, w);
+  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, o, w);
   for (int64_t t = first * groups + group; t < a.M; t += each * groups) {
-    float x[kVec], z[kVec], q = 0.f;
-    ld_row(static_cast<const T*>(a.x) + t * a.sx + head * a.d, col, a.d, x);
-    if constexpr (ACT != kActNone) ld_row(static_cast<const T*>(a.z) + t * a.sz + head * a.d, col, a.d, z);
+    Raw<T> x, z;
+    x.load(px + t * a.sx, o);
+    if constexpr (ACT != kActNone) z.load(pz + t * a.sz, o);
+    x.settle(o);
+    float v[kVec], q = 0.f;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) q += x[i] * x[i];
     const float r = factor(lanes_sum(q, L), a.l2 ? 1.f : 1.f / a.d, a.eps);
@@ -362,82 +488,109 @@ __global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L) {
     for (int i = 0; i < kVec; ++i) {
       float act, slope;
       gate<T, ACT>(ACT == kActNone ? 0.f : z[i], act, slope);
-      x[i] = x[i] * r * w[i];
-      if constexpr (ACT != kActNone) x[i] *= act;
+      v[i] = x[i] * r * w[i];
+      if constexpr (ACT != kActNone) v[i] *= act;
     }
-    st_row(static_cast<T*>(a.y) + t * a.sy + head * a.d, col, a.d, x);
+    store(static_cast<T*>(a.y) + t * a.sy + head * a.d, o, v);
   }
 }
 
-template <typename T, int ACT>
+template <typename T, int ACT, RowKind KIND>
 __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L) {
   __shared__ float sum[kThreads / kWave][kWave * kVec];
   const int col = (threadIdx.x & (L - 1)) * kVec, group = threadIdx.x / L, groups = kThreads / L;
+  const Cols<KIND> o(col, a.d);
   const int64_t head = blockIdx.x % a.H, first = blockIdx.x / a.H, each = gridDim.x / a.H;
   const float c = a.l2 ? 1.f : 1.f / a.d;
+  const T* const px = static_cast<const T*>(a.x) + head * a.d;
+  const T* const pz = static_cast<const T*>(a.z) + head * a.d;
+  const T* const pdy = static_cast<const T*>(a.dy) + head * a.d;
   float w[kVec], dw[kVec] = {};
-  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, col, a.d, w);
+  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, o, w);
   for (int64_t t = first * groups + group; t < a.M; t += each * groups) {
-    float x[kVec], z[kVec], dy[kVec], slope[kVec], q = 0.f, p = 0.f;
-    ld_row(static_cast<const T*>(a.x) + t * a.sx + head * a.d, col, a.d, x);
-    ld_row(static_cast<const T*>(a.dy) + t * a.sdy + head * a.d, col, a.d, dy);
-    if constexpr (ACT != kActNone) ld_row(static_cast<const T*>(a.z) + t * a.sz + head * a.d, col, a.d, z);
+    Raw<T> x, z, dy;
+    x.load(px + t * a.sx, o);
+    dy.load(pdy + t * a.sdy, o);
+    if constexpr (ACT != kActNone) z.load(pz + t * a.sz, o);
+    x.settle(o);
+    dy.settle(o);
+    if constexpr (ACT != kActNone) z.settle(o);
+    float g[kVec], v[kVec], slope[kVec], q = 0.f, p = 0.f;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
-      q += x[i] * x[i];
       float act;
+      q += x[i] * x[i];
       gate<T, ACT>(ACT == kActNone ? 0.f : z[i], act, slope[i]);
       slope[i] *= dy[i] * w[i];
-      if constexpr (ACT != kActNone) dy[i] *= act;
-      p += dy[i] * w[i] * x[i];
+      g[i] = ACT == kActNone ? dy[i] : dy[i] * act;
+      p += g[i] * w[i] * x[i];
     }
     const float r = factor(lanes_sum(q, L), c, a.eps), m = (r * lanes_sum(p, L) * c) * r * r;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       slope[i] *= x[i] * r;
-      dw[i] += dy[i] * (x[i] * r);
-      x[i] = r * (dy[i] * w[i]) - x[i] * m;
+      dw[i] += g[i] * (x[i] * r);
+      v[i] = r * (g[i] * w[i]) - x[i] * m;
     }
-    st_row(static_cast<T*>(a.dx) + t * a.sdx + head * a.d, col, a.d, x);
-    if constexpr (ACT != kActNone) st_row(static_cast<T*>(a.dz) + t * a.sdz + head * a.d, col, a.d, slope);
+    store(static_cast<T*>(a.dx) + t * a.sdx + head * a.d, o, v);
+    if constexpr (ACT != kActNone) store(static_cast<T*>(a.dz) + t * a.sdz + head * a.d, o, slope);
   }
   if (!a.dweight) return;
-  // the groups' sums: over a wave's by shuffles, then over the waves
+  // the groups' sums: over a wave's by shuffles, then over the waves (a window's columns that are
+  // another lane's are zero, and that lane's place is further down)
 #pragma unroll
   for (int i = 0; i < kVec; ++i)
     for (int off = L; off < kWave; off <<= 1) dw[i] += __shfl_xor(dw[i], off, 64);
   const int wave = threadIdx.x / kWave, l = threadIdx.x & 63;
   if (l < L)
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) sum[wave][l * kVec + i] = dw[i];
+    for (int i = 0; i < kVec; ++i)
+      if (o.keep >> i & 1) sum[wave][o.at + i] = dw[i];
   __syncthreads();
   for (int j = threadIdx.x; j < a.d; j += kThreads)
     a.part[blockIdx.x * static_cast<int64_t>(a.d) + j] = (sum[0][j] + sum[1][j]) + (sum[2][j] + sum[3][j]);
 }
 
-template <typename T>
-hipError_t hnorm_fwd_of(const HnormArgs& a, hipStream_t s) {
+template <typename T, RowKind KIND>
+hipError_t hnorm_fwd_at(const HnormArgs& a, hipStream_t s) {
   const int L = head_lanes(a.d), groups = kThreads / L;
   const int64_t each = std::max<int64_t>(std::min<int64_t>((a.M + groups - 1) / groups, (1 << 20) / a.H), 1);
   const dim3 grid(static_cast<unsigned>(each * a.H)), block(kThreads);
-  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_fwd<T, kActSilu>), grid, block, 0, s, a, L);
-  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_fwd<T, kActSigmoid>), grid, block, 0, s, a, L);
-  else hipLaunchKernelGGL((hnorm_fwd<T, kActNone>), grid, block, 0, s, a, L);
+  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_fwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
+  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_fwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L);
+  else hipLaunchKernelGGL((hnorm_fwd<T, kActNone, KIND>), grid, block, 0, s, a, L);
   return hipGetLastError();
+}
+template <typename T, RowKind KIND>
+hipError_t hnorm_bwd_at(const HnormArgs& a, hipStream_t s) {
+  const int L = head_lanes(a.d);
+  const dim3 grid(static_cast<unsigned>(hnorm_parts(a.M, a.H, a.d))), block(kThreads);
+  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_bwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
+  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_bwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L);
+  else hipLaunchKernelGGL((hnorm_bwd<T, kActNone, KIND>), grid, block, 0, s, a, L);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t hnorm_fwd_of(const HnormArgs& a, hipStream_t s) {
+  const RowKind kind = row_kind(a.d);
+  return kind == kEights ? hnorm_fwd_at<T, kEights>(a, s) : kind == kMore ? hnorm_fwd_at<T, kMore>(a, s) : hnorm_fwd_at<T, kFewer>(a, s);
 }
 template <typename T>
 hipError_t hnorm_bwd_of(const HnormArgs& a, hipStream_t s) {
-  const int L = head_lanes(a.d);
-  const dim3 grid(static_cast<unsigned>(hnorm_parts(a.M, a.H, a.d))), block(kThreads);
-  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_bwd<T, kActSilu>), grid, block, 0, s, a, L);
-  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_bwd<T, kActSigmoid>), grid, block, 0, s, a, L);
-  else hipLaunchKernelGGL((hnorm_bwd<T, kActNone>), grid, block, 0, s, a, L);
-  return hipGetLastError();
+  const RowKind kind = row_kind(a.d);
+  return kind == kEights ? hnorm_bwd_at<T, kEights>(a, s) : kind == kMore ? hnorm_bwd_at<T, kMore>(a, s) : hnorm_bwd_at<T, kFewer>(a, s);
+}
+
+// at most so many parts, of as nearly the same number of rows as can be
+int64_t balanced_parts(int64_t rows, int64_t most) {
+  const int64_t each = (rows + most - 1) / most;
+  return each > 0 ? (rows + each - 1) / each : 0;
 }
 
 }  // namespace
 
-int64_t rnorm_parts(int64_t rows, int64_t) { return std::min<int64_t>(rows, 1024); }
+int64_t rnorm_parts(int64_t rows, int64_t) { return balanced_parts(rows, 768); }
 
 hipError_t launch_rnorm_fwd(const RnormArgs& a, int io_bf16, int stream_bf16, hipStream_t s) {
   if (io_bf16) return stream_bf16 ? rnorm_fwd_of<bf16, bf16>(a, s) : rnorm_fwd_of<bf16, float>(a, s);
@@ -467,7 +620,7 @@ hipError_t launch_rnorm_bwd(const RnormArgs& a, int io_bf16, int stream_bf16, hi
 int64_t hnorm_parts(int64_t M, int64_t H, int d) {
   if (M == 0 || H == 0) return 0;
   const int groups = kThreads / head_lanes(d);
-  return H * std::max<int64_t>(std::min<int64_t>((M + groups - 1) / groups, 2048 / H), 1);
+  return H * std::max<int64_t>(std::min<int64_t>((M + groups - 1) / groups, 1024 / H), 1);
 }
 
 hipError_t launch_hnorm_fwd(const HnormArgs& a, int io_bf16, hipStream_t s) {

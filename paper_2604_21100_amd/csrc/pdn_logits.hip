@@ -8,8 +8,7 @@
 // Two launches: of every segment of a row the largest l, the sum of e under it, and where
 // the temperature is zero its first place; then each segment again with those of all.
 // A row's counts come from the table (read along with the logits) and from the few tokens
-// of its own sequence's rows, which the segment's workgroup counts in shared memory, as it
-// marks there which entry of the bias list a token has.
+// of its own sequence's rows.
 //
 // What bounds it: reading the logits twice and writing p.
 #include <algorithm>
@@ -17,12 +16,13 @@
 
 #include "pdn_device.hpp"
 #include "pdn_internal.hpp"
+#include "pdn_lanes.hpp"
 
 namespace pdn {
 
 namespace {
 
-constexpr int kThreads = 256, kVec = 8, kSeg = kThreads * kVec;
+constexpr int kThreads = 256, kVec = 8, kWaveSpan = kWave * kVec, kSeg = kThreads * kVec;
 constexpr float kInf = __builtin_inff();
 
 struct Part {
@@ -32,138 +32,207 @@ struct Part {
 };
 
 __device__ __forceinline__ int64_t clamp_row(int64_t x, int64_t rows) { return min(max(x, (int64_t)0), rows); }
+__device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 
 // a row's sequence and what it has of it
 struct RowOf {
-  int64_t seq, first;   // its first row; seq < 0: left out
+  bool out;             // left out
+  int64_t first;        // its sequence's first row
   const int32_t* counts;
-  float temperature, repetition, presence, frequency;
   const uint8_t* mask;
+  float temperature, repetition, presence, frequency;
   int64_t bias_lo, bias_hi;
 };
 __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row) {
   RowOf r{};
   const int l = threadIdx.x & 63;
-  if (a.starts) {   // the last sequence that starts at the row or before: 64 of them at a time
-    int64_t upto = 0;
-    for (int64_t n0 = 0; n0 < a.N; n0 += kWave) {
-      const bool before = n0 + l < a.N && clamp_row(a.starts[n0 + l], a.rows) <= row;
-      const unsigned long long m = __ballot(before);
-      if (m) upto = n0 + 64 - __clzll(m);
-    }
-    r.seq = upto - 1;
-    if (r.seq < 0 || clamp_row(a.starts[r.seq + 1], a.rows) <= row) {
-      r.seq = -1;
-      return r;
-    }
-    r.first = clamp_row(a.starts[r.seq], a.rows);
+  int64_t n, slot = 0;
+  const int64_t m = a.mask ? a.mask_rows ? a.mask_rows[row] : row : -1;
+  const bool told = a.starts && a.N < kWave;   // a lane a sequence: all there is of each is read at once
+  if (told) {
+    const int at = min(l, static_cast<int>(a.N)), of = max(min(l, static_cast<int>(a.N) - 1), 0);
+    const int32_t start = a.starts[at], from = a.counts && a.slot ? a.slot[of] : of, bias = a.bias_starts ? a.bias_starts[at] : 0;
+    const float t = a.temperature ? a.temperature[of] : 1.f, p = a.repetition ? a.repetition[of] : 1.f;
+    const float q = a.presence ? a.presence[of] : 0.f, f = a.frequency ? a.frequency[of] : 0.f;
+    const unsigned long long before = __ballot(l < a.N && clamp_row(start, a.rows) <= row);
+    const int s = before ? 63 - __clzll(before) : -1;
+    r.out = s < 0 || clamp_row(lane_int(start, max(s, 0) + 1), a.rows) <= row;
+    n = max(s, 0);
+    r.first = clamp_row(lane_int(start, static_cast<int>(n)), a.rows);
+    slot = lane_int(from, static_cast<int>(n));
+    r.temperature = read_lane(t, static_cast<int>(n));
+    r.repetition = read_lane(p, static_cast<int>(n));
+    r.presence = read_lane(q, static_cast<int>(n));
+    r.frequency = read_lane(f, static_cast<int>(n));
+    r.bias_lo = clamp_row(lane_int(bias, static_cast<int>(n)), a.biases);
+    r.bias_hi = clamp_row(lane_int(bias, static_cast<int>(n) + 1), a.biases);
   } else {
-    const int64_t each = a.rows / a.N;
-    r.seq = row / each;
-    r.first = r.seq * each;
-  }
-  const int64_t n = r.seq;
-  if (a.counts) {
-    const int64_t slot = a.slot ? a.slot[n] : n;
-    if (slot < 0 || slot >= a.slots) {
-      r.seq = -1;
-      return r;
+    if (a.starts) {   // the last sequence that starts at the row or before: 64 of them at a time
+      int64_t upto = 0;
+      for (int64_t n0 = 0; n0 < a.N; n0 += kWave) {
+        const unsigned long long before = __ballot(n0 + l < a.N && clamp_row(a.starts[min(n0 + l, a.N)], a.rows) <= row);
+        if (before) upto = n0 + 64 - __clzll(before);
+      }
+      n = max(upto - 1, (int64_t)0);
+      r.first = clamp_row(a.starts[n], a.rows);
+      r.out = upto == 0 || clamp_row(a.starts[n + 1], a.rows) <= row;
+    } else {
+      const uint32_t each = static_cast<uint32_t>(a.rows) / static_cast<uint32_t>(a.N);
+      n = static_cast<uint32_t>(row) / each;
+      r.first = n * each;
+      r.out = false;
     }
-    r.counts = a.counts + slot * a.V;
+    if (a.counts) slot = a.slot ? a.slot[n] : n;
+    r.temperature = a.temperature ? a.temperature[n] : 1.f;
+    r.repetition = a.repetition ? a.repetition[n] : 1.f;
+    r.presence = a.presence ? a.presence[n] : 0.f;
+    r.frequency = a.frequency ? a.frequency[n] : 0.f;
+    if (a.bias_starts) {
+      r.bias_lo = clamp_row(a.bias_starts[n], a.biases);
+      r.bias_hi = clamp_row(a.bias_starts[n + 1], a.biases);
+    }
   }
-  r.temperature = a.temperature ? a.temperature[n] : 1.f;
-  r.repetition = a.repetition ? a.repetition[n] : 1.f;
-  r.presence = a.presence ? a.presence[n] : 0.f;
-  r.frequency = a.frequency ? a.frequency[n] : 0.f;
-  if (a.mask) {
-    const int64_t m = a.mask_rows ? a.mask_rows[row] : row;
-    if (m >= 0 && m < a.masks) r.mask = reinterpret_cast<const uint8_t*>(a.mask + m * ((a.V + 31) / 32));
+  if (a.counts) {
+    if (slot < 0 || slot >= a.slots) r.out = true;
+    else r.counts = a.counts + slot * a.V;
   }
-  if (a.bias_starts) {
-    r.bias_lo = clamp_row(a.bias_starts[n], a.biases);
-    r.bias_hi = clamp_row(a.bias_starts[n + 1], a.biases);
-  }
+  if (m >= 0 && m < a.masks) r.mask = reinterpret_cast<const uint8_t*>(a.mask + m * ((a.V + 31) / 32));
   return r;
 }
 
-// Counts of the segment's tokens from the sequence's rows up to this one, and the number (from
-// one) of the entry of the bias list that each has.
-struct Marks {
-  int32_t fed[kSeg];
-  int32_t bias[kSeg];
+// Lists that change a few of a row's tokens: the tokens fed in the sequence's rows up to this one, and
+// its biases, from the last entry on (of a token listed twice the last holds).  A lane an entry, 64 at a
+// time; a wave then goes through those of them that are among its own tokens.
+struct Lists {
+  int64_t fed, biases;   // entries
+  const int32_t* ids;
+  const int32_t* bias_ids;     // the last entry
+  const float* bias_values;
+  int32_t id, bias_id;   // the first 64 of each (-1: none)
+  float bias_value;
+  __device__ __forceinline__ void load(int64_t from) {
+    const int64_t l = from + (threadIdx.x & 63);
+    id = bias_id = -1;
+    if (from < fed) {
+      id = ids[min(l, fed - 1)];
+      id = l < fed ? id : -1;
+    }
+    if (from < biases) {
+      bias_id = bias_ids[-min(l, biases - 1)];
+      bias_value = bias_values[-min(l, biases - 1)];
+      bias_id = l < biases ? bias_id : -1;
+    }
+  }
+  __device__ __forceinline__ Lists(const LogitsArgs& a, const RowOf& r, int64_t row) {
+    fed = a.ids ? row + 1 - r.first : 0;
+    biases = max(r.bias_hi - r.bias_lo, (int64_t)0);
+    ids = a.ids + r.first;
+    bias_ids = a.bias_ids + (r.bias_hi - 1);
+    bias_values = a.bias_values + (r.bias_hi - 1);
+    load(0);
+  }
 };
-__device__ __forceinline__ void mark(const LogitsArgs& a, const RowOf& r, int64_t row, int64_t j0, Marks& m) {
-  if (!a.ids && !a.bias_starts) return;
-  for (int j = threadIdx.x; j < kSeg; j += kThreads) m.fed[j] = m.bias[j] = 0;
-  __syncthreads();
-  const int64_t end = min(j0 + kSeg, a.V);
-  if (a.ids)
-    for (int64_t i = r.first + threadIdx.x; i <= row; i += kThreads) {
-      const int64_t j = a.ids[i];
-      if (j >= j0 && j < end) atomicAdd(&m.fed[j - j0], 1);
-    }
-  for (int64_t i = r.bias_lo + threadIdx.x; i < r.bias_hi; i += kThreads) {
-    const int64_t j = a.bias_ids[i];
-    if (j >= j0 && j < end) atomicMax(&m.bias[j - j0], static_cast<int32_t>(i - r.bias_lo + 1));
-  }
-  __syncthreads();
-}
 
-// Eight tokens' changed logits from token j (-inf past the row)
-template <typename T>
-__device__ __forceinline__ void changed(const LogitsArgs& a, const RowOf& r, int64_t row, int64_t j, const Marks& m, float (&l)[kVec]) {
-#pragma clang fp contract(off)
-  const T* const p = static_cast<const T*>(a.logits) + row * a.stride;
-  const bool whole = j + kVec <= a.V;
+// A thread's eight tokens.  Loads do not branch (a wait for each would follow): a last thread with fewer
+// than eight takes the row's last eight, one without any too, and `keep` says which are its own.  TINY: rows
+// of fewer than eight.
+template <typename T, bool TINY>
+struct Piece {
+  int at;
+  uint32_t keep, bits;   // bits: what the mask allows
   T raw[kVec];
-  int32_t t[kVec] = {};
-  uint32_t bits = 0xff;
-  if (whole) {
-    __builtin_memcpy(raw, p + j, sizeof raw);
-    if (r.counts) __builtin_memcpy(t, r.counts + j, sizeof t);
-  } else {
+  int32_t count[kVec];
+  __device__ __forceinline__ void load_logits(const LogitsArgs& a, int64_t row, int64_t j) {
+    const T* const p = static_cast<const T*>(a.logits) + row * a.stride;
+    if constexpr (TINY) {
+      const int n = static_cast<int>(a.V);
+      at = 0;
+      keep = j == 0 ? (1u << n) - 1 : 0;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      raw[i] = j + i < a.V ? p[j + i] : from_f<T>(-kInf);
-      if (r.counts) t[i] = j + i < a.V ? r.counts[j + i] : 0;
+      for (int i = 0; i < kVec; ++i) raw[i] = p[min(i, n - 1)];
+    } else {
+      at = static_cast<int>(min(j, a.V - kVec));
+      keep = j < a.V ? (0xffu << (j - at)) & 0xff : 0;
+      __builtin_memcpy(raw, p + at, sizeof raw);
     }
   }
-  if (r.mask && j < a.V) bits = r.mask[j >> 3];
-  const int at = threadIdx.x * kVec;
+  __device__ __forceinline__ void load_rest(const LogitsArgs& a, const RowOf& r) {
+    bits = keep;
+    if (r.mask) {
+      const uint32_t lo = r.mask[at >> 3], hi = r.mask[min(at + kVec - 1, static_cast<int>(a.V) - 1) >> 3];
+      bits &= (lo | hi << 8) >> (at & 7);
+    }
+    if (r.counts) {
+      if constexpr (TINY) {
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) {
-    float x = to_f(raw[i]);
-    const int32_t c = (t[i] & 0x7fffffff) + (a.ids ? m.fed[at + i] : 0);
-    if (c | t[i]) {
-      x = x > 0.f ? x / r.repetition : x * r.repetition;
-      if (c) {
-        x = x - r.frequency * static_cast<float>(c);
-        x = x - r.presence;
+        for (int i = 0; i < kVec; ++i) count[i] = r.counts[min(i, static_cast<int>(a.V) - 1)];
+      } else {
+        __builtin_memcpy(count, r.counts + at, sizeof count);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) count[i] = 0;
+    }
+  }
+  // the changed logits; base: the wave's first token
+  __device__ __forceinline__ void changed(const RowOf& r, const Lists& first, int64_t base, float (&l)[kVec]) {
+#pragma clang fp contract(off)
+    for (int64_t from = 0; from < first.fed; from += kWave) {
+      Lists s = first;
+      if (from) s.load(from);
+      for (unsigned long long here = __ballot(static_cast<uint64_t>(s.id - base) < kWaveSpan); here; here &= here - 1) {
+        const int d = lane_int(s.id, __ffsll(here) - 1) - at;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) count[i] += d == i;
       }
     }
-    if (a.bias_starts) {
-      const int32_t b = m.bias[at + i];
-      if (b) x = x + a.bias_values[r.bias_lo + b - 1];
+    int32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      l[i] = to_f(raw[i]);
+      any |= count[i];
     }
-    l[i] = (bits >> i) & 1 ? x : -kInf;
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int32_t c = count[i] & 0x7fffffff;
+        const float x = count[i] ? l[i] > 0.f ? l[i] / r.repetition : l[i] * r.repetition : l[i];
+        const float y = x - r.frequency * static_cast<float>(c);
+        l[i] = c ? y - r.presence : x;
+      }
+    }
+    uint32_t done = 0;
+    for (int64_t from = 0; from < first.biases; from += kWave) {
+      Lists s = first;
+      if (from) s.load(from);
+      for (unsigned long long here = __ballot(static_cast<uint64_t>(s.bias_id - base) < kWaveSpan); here; here &= here - 1) {
+        const int k = __ffsll(here) - 1, d = lane_int(s.bias_id, k) - at;
+        const float value = read_lane(s.bias_value, k);
+        const uint32_t one = d >= 0 && d < kVec ? (1u << d) & ~done : 0;
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) l[i] = one >> i & 1 ? l[i] + value : l[i];
+        done |= one;
+      }
+    }
+    if (bits != 0xff) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) l[i] = bits >> i & 1 ? l[i] : -kInf;
+    }
   }
-}
-
-__device__ __forceinline__ float wave_max(float x) {
+  template <typename TO>
+  __device__ __forceinline__ void store(TO* out, const float (&v)[kVec]) const {
+    TO x[kVec];
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = fmaxf(x, __shfl_xor(x, off, 64));
-  return x;
-}
-__device__ __forceinline__ float wave_add(float x) {
+    for (int i = 0; i < kVec; ++i) x[i] = from_f<TO>(v[i]);
+    if (!TINY && keep == 0xff) {
+      __builtin_memcpy(out + at, x, sizeof x);
+    } else if (keep) {
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
-}
-__device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) x = min(x, __shfl_xor(x, off, 64));
-  return x;
-}
+      for (int i = 0; i < kVec; ++i)
+        if (keep >> i & 1) out[at + i] = x[i];
+    }
+  }
+};
 
 // 1 / temperature as a factor of the base-2 exponential's argument; any temperature gives a
 // number (so that zero times it is zero); not above 0: 1 (the sum only shows NaN then)
@@ -171,115 +240,146 @@ __device__ __forceinline__ float sharpness(float t) {
   if (!(t > 0.f)) return 1.f;
   return fminf(fmaxf(kLog2e / t, 1e-30f), 3e38f);
 }
-// e of l under the largest (which is -inf where nothing is left: l is then -inf too, or NaN)
-__device__ __forceinline__ float under(float l, float top, float k) {
-  return l == top ? (top > -kInf ? 1.f : 0.f) : exp2_hw((l - (top > -kInf ? top : 0.f)) * k);
+// e of l under the largest, and of -inf where nothing is left (`level`: that, or 0)
+__device__ __forceinline__ float under(float l, float top, float level, float k) {
+  return l == top ? (top > -kInf ? 1.f : 0.f) : exp2_hw((l - level) * k);
+}
+__device__ __forceinline__ float level_of(float top) { return top > -kInf ? top : 0.f; }
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) x = min(x, __shfl_xor(x, off, 64));
+  return x;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a) {
-  __shared__ Marks marks;
+// of a segment: CH times eight tokens a thread, a wave's in a row
+template <typename T, int CH, bool TINY>
+__global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a, uint32_t segs) {
   __shared__ float sF[2][kThreads / kWave];
   __shared__ int sI[kThreads / kWave];
-  const int64_t segs = logits_segments(a.V), row = blockIdx.x / segs, seg = blockIdx.x % segs;
-  const RowOf r = row_of(a, row);
-  if (r.seq < 0) return;
-  mark(a, r, row, seg * kSeg, marks);
-  const int64_t j = seg * kSeg + threadIdx.x * kVec;
-  float l[kVec];
-  changed<T>(a, r, row, j, marks, l);
-  const int w = threadIdx.x >> 6;
-  float top = l[0];
+  const uint32_t row = blockIdx.x / segs, seg = blockIdx.x % segs;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t base = (static_cast<int64_t>(seg) * (kThreads / kWave) + w) * (CH * kWaveSpan);
+  Piece<T, TINY> piece[CH];
 #pragma unroll
-  for (int i = 1; i < kVec; ++i) top = fmaxf(top, l[i]);
-  top = wave_max(top == top ? top : -kInf);
-  if ((threadIdx.x & 63) == 0) sF[0][w] = top;
+  for (int c = 0; c < CH; ++c) piece[c].load_logits(a, row, base + c * kWaveSpan + lane * kVec);
+  const RowOf r = row_of(a, row);
+  if (r.out) return;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) piece[c].load_rest(a, r);
+  const Lists lists(a, r, row);
+  float l[CH][kVec], top = -kInf, sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    piece[c].changed(r, lists, base + c * kWaveSpan, l[c]);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) top = fmaxf(top, l[c][i]);
+  }
+  top = wave_max(top);
+  if (lane == 0) sF[0][w] = top;
   __syncthreads();
   top = fmaxf(fmaxf(sF[0][0], sF[0][1]), fmaxf(sF[0][2], sF[0][3]));
-  const float k = sharpness(r.temperature);
-  float sum = 0.f;
-  int first = INT32_MAX;
+  const float k = sharpness(r.temperature), level = level_of(top);
 #pragma unroll
-  for (int i = kVec - 1; i >= 0; --i) {
-    sum += under(l[i], top, k);
-    if (l[i] == top) first = static_cast<int>(j) + i;
-  }
-  sum = wave_add(sum);
-  first = wave_min(first);
-  if ((threadIdx.x & 63) == 0) {
-    sF[1][w] = sum;
-    sI[w] = first;
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) sum += under(l[c][i], top, level, k);
+  sum = wave_sum(sum);
+  if (lane == 0) sF[1][w] = sum;
+  if (!(r.temperature > 0.f)) {
+    int first = INT32_MAX;
+#pragma unroll
+    for (int c = CH - 1; c >= 0; --c)
+#pragma unroll
+      for (int i = kVec - 1; i >= 0; --i)
+        if (l[c][i] == top) first = piece[c].at + i;
+    first = wave_min(first);
+    if (lane == 0) sI[w] = first;
   }
   __syncthreads();
   if (threadIdx.x == 0) {
     Part p;
     p.top = top;
     p.sum = (sF[1][0] + sF[1][1]) + (sF[1][2] + sF[1][3]);
-    p.first = min(min(sI[0], sI[1]), min(sI[2], sI[3]));
+    p.first = !(r.temperature > 0.f) ? min(min(sI[0], sI[1]), min(sI[2], sI[3])) : 0;
     p.unused = 0;
     static_cast<Part*>(a.parts)[blockIdx.x] = p;
   }
 }
 
 // p of a segment from the parts of all, or the changed logits themselves
-template <typename T, typename TO, bool PROBS>
-__global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a) {
-  __shared__ Marks marks;
-  const int64_t segs = logits_segments(a.V), row = blockIdx.x / segs, seg = blockIdx.x % segs;
-  const RowOf r = row_of(a, row);
-  if (r.seq < 0) return;
-  mark(a, r, row, seg * kSeg, marks);
-  const int64_t j = seg * kSeg + threadIdx.x * kVec;
-  float l[kVec];
-  changed<T>(a, r, row, j, marks, l);
+template <typename T, typename TO, int CH, bool TINY, bool PROBS>
+__global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t segs) {
+  const uint32_t row = blockIdx.x / segs, seg = blockIdx.x % segs;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int64_t base = (static_cast<int64_t>(seg) * (kThreads / kWave) + w) * (CH * kWaveSpan);
+  Piece<T, TINY> piece[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) piece[c].load_logits(a, row, base + c * kWaveSpan + lane * kVec);
+  const Part* const parts = static_cast<const Part*>(a.parts) + static_cast<int64_t>(row) * segs;
+  Part p{-kInf, 0.f, INT32_MAX, 0};
   if constexpr (PROBS) {
-    const Part* const parts = static_cast<const Part*>(a.parts) + row * segs;
-    const int lane = threadIdx.x & 63;
-    const float k = sharpness(r.temperature);
-    float top = -kInf, sum = 0.f;
-    int first = INT32_MAX;
-    for (int64_t s = lane; s < segs; s += kWave) top = fmaxf(top, parts[s].top);
-    top = wave_max(top);
-    for (int64_t s = lane; s < segs; s += kWave) {
-      const Part p = parts[s];
-      sum += p.sum * under(p.top, top, k);
-      if (p.sum != p.sum) sum = p.sum;   // (a NaN in a segment that weighs nothing)
-      if (p.top == top) first = min(first, p.first);
-    }
-    sum = wave_add(sum);
-    first = wave_min(first);
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    if (r.temperature > 0.f) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) l[i] = under(l[i], top, k) * f;
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) l[i] = sum != sum ? sum : top > -kInf && j + i == first ? 1.f : 0.f;
-    }
+    const Part x = parts[min(static_cast<uint32_t>(lane), segs - 1)];
+    if (static_cast<uint32_t>(lane) < segs) p = x;
   }
-  TO* const out = static_cast<TO*>(a.out) + row * a.V;
-  TO raw[kVec];
+  const RowOf r = row_of(a, row);
+  if (r.out) return;
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) raw[i] = from_f<TO>(l[i]);
-  if (j + kVec <= a.V) {
-    __builtin_memcpy(out + j, raw, sizeof raw);
-  } else {
+  for (int c = 0; c < CH; ++c) piece[c].load_rest(a, r);
+  const Lists lists(a, r, row);
+  float top = 0.f, level = 0.f, sum = 0.f, f = 0.f, k = 0.f;
+  int first = INT32_MAX;
+  if constexpr (PROBS) {
+    k = sharpness(r.temperature);
+    top = p.top;
+    for (uint32_t s = kWave + lane; s < segs; s += kWave) top = fmaxf(top, parts[s].top);
+    top = wave_max(top);
+    level = level_of(top);
+    auto add = [&](const Part& x) {
+      // (a NaN in a segment that weighs nothing shows too)
+      sum += x.sum == x.sum ? x.sum * under(x.top, top, level, k) : x.sum;
+      if (x.top == top) first = min(first, x.first);
+    };
+    add(p);
+    for (uint32_t s = kWave + lane; s < segs; s += kWave) add(parts[s]);
+    sum = wave_sum(sum);
+    f = sum == 0.f ? 0.f : 1.f / sum;
+    if (!(r.temperature > 0.f)) first = wave_min(first);
+  }
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (j + i < a.V) out[j + i] = raw[i];
+  for (int c = 0; c < CH; ++c) {
+    float l[kVec];
+    piece[c].changed(r, lists, base + c * kWaveSpan, l);
+    if constexpr (PROBS) {
+      if (r.temperature > 0.f) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) l[i] = under(l[i], top, level, k) * f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) l[i] = sum != sum ? sum : top > -kInf && piece[c].at + i == first ? 1.f : 0.f;
+      }
+    }
+    piece[c].store(static_cast<TO*>(a.out) + row * a.V, l);
   }
 }
 
-template <typename T, typename TO>
-hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(a.rows * logits_segments(a.V))), block(kThreads);
+template <typename T, typename TO, int CH, bool TINY>
+hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
+  const int64_t segs = (a.V + CH * kSeg - 1) / (CH * kSeg);
+  const dim3 grid(static_cast<unsigned>(a.rows * segs)), block(kThreads);
   if (!a.probs) {
-    hipLaunchKernelGGL((logits_out<T, TO, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((logits_out<T, TO, CH, TINY, false>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((logits_parts<T>), grid, block, 0, s, a);
-  hipLaunchKernelGGL((logits_out<T, TO, true>), grid, block, 0, s, a);
+  hipLaunchKernelGGL((logits_parts<T, CH, TINY>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
+  hipLaunchKernelGGL((logits_out<T, TO, CH, TINY, true>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
   return hipGetLastError();
+}
+template <typename T, typename TO>
+hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
+  if (a.V < kVec) return logits_at<T, TO, 1, true>(a, s);
+  if (a.rows * ((a.V + 4 * kSeg - 1) / (4 * kSeg)) >= 1024) return logits_at<T, TO, 4, false>(a, s);
+  return logits_at<T, TO, 1, false>(a, s);
 }
 
 constexpr int32_t kPromptBit = INT32_MIN;
