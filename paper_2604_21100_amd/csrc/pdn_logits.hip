@@ -5,8 +5,8 @@
 //   l = l + bias;  -inf where the mask forbids it
 //   p = e / sum(e), e = exp((l - max l) / temperature), 1 where l is the largest
 //
-// Two launches: of every segment of a row the largest l, the sum of e under it, and where
-// the temperature is zero its first place; then each segment again with those of all.
+// One launch with a row in registers, or two: of every segment of a row the largest l, the sum of e under
+// it, and where the temperature is zero its first place; then each token again with those of all.
 // A row's counts come from the table (read along with the logits) and from the few tokens
 // of its own sequence's rows.
 //
@@ -37,37 +37,52 @@ __device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdg
 // a row's sequence and what it has of it
 struct RowOf {
   bool out;             // left out
+  int64_t seq;
   int64_t first;        // its sequence's first row
   const int32_t* counts;
   const uint8_t* mask;
   float temperature, repetition, presence, frequency;
   int64_t bias_lo, bias_hi;
 };
-__device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row) {
+// What a wave reads of all sequences at once, if there are less than 64: a lane a sequence (the loads
+// that a row's others wait for come first, as loads are waited for in their order).
+struct Told {
+  bool all;
+  int32_t start, slot, bias;
+  float temperature, repetition, presence, frequency;
+  __device__ __forceinline__ explicit Told(const LogitsArgs& a) {
+    const int l = threadIdx.x & 63, n = static_cast<int>(min(a.N, (int64_t)kWave)), at = min(l, n), of = min(l, n - 1);
+    all = a.starts && n < kWave;
+    if (!all) return;
+    start = a.starts[at];
+    slot = a.counts && a.slot ? a.slot[of] : of;
+    bias = a.bias_starts ? a.bias_starts[at] : 0;
+    temperature = a.temperature ? a.temperature[of] : 1.f;
+    repetition = a.repetition ? a.repetition[of] : 1.f;
+    presence = a.presence ? a.presence[of] : 0.f;
+    frequency = a.frequency ? a.frequency[of] : 0.f;
+  }
+};
+__device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row, const Told& told) {
   RowOf r{};
   const int l = threadIdx.x & 63;
-  int64_t n, slot = 0;
-  const int64_t m = a.mask ? a.mask_rows ? a.mask_rows[row] : row : -1;
-  const bool told = a.starts && a.N < kWave;   // a lane a sequence: all there is of each is read at once
-  if (told) {
-    const int at = min(l, static_cast<int>(a.N)), of = max(min(l, static_cast<int>(a.N) - 1), 0);
-    const int32_t start = a.starts[at], from = a.counts && a.slot ? a.slot[of] : of, bias = a.bias_starts ? a.bias_starts[at] : 0;
-    const float t = a.temperature ? a.temperature[of] : 1.f, p = a.repetition ? a.repetition[of] : 1.f;
-    const float q = a.presence ? a.presence[of] : 0.f, f = a.frequency ? a.frequency[of] : 0.f;
-    const unsigned long long before = __ballot(l < a.N && clamp_row(start, a.rows) <= row);
-    const int s = before ? 63 - __clzll(before) : -1;
-    r.out = s < 0 || clamp_row(lane_int(start, max(s, 0) + 1), a.rows) <= row;
-    n = max(s, 0);
-    r.first = clamp_row(lane_int(start, static_cast<int>(n)), a.rows);
-    slot = lane_int(from, static_cast<int>(n));
-    r.temperature = read_lane(t, static_cast<int>(n));
-    r.repetition = read_lane(p, static_cast<int>(n));
-    r.presence = read_lane(q, static_cast<int>(n));
-    r.frequency = read_lane(f, static_cast<int>(n));
-    r.bias_lo = clamp_row(lane_int(bias, static_cast<int>(n)), a.biases);
-    r.bias_hi = clamp_row(lane_int(bias, static_cast<int>(n) + 1), a.biases);
+  int64_t slot = 0;
+  if (told.all) {
+    const unsigned long long before = __ballot(l < a.N && clamp_row(told.start, a.rows) <= row);
+    const int n = before ? 63 - __clzll(before) : 0;   // the last sequence that starts at the row or before
+    r.seq = n;
+    r.first = clamp_row(lane_int(told.start, n), a.rows);
+    r.out = !before || clamp_row(lane_int(told.start, n + 1), a.rows) <= row;
+    slot = lane_int(told.slot, n);
+    r.temperature = read_lane(told.temperature, n);
+    r.repetition = read_lane(told.repetition, n);
+    r.presence = read_lane(told.presence, n);
+    r.frequency = read_lane(told.frequency, n);
+    r.bias_lo = clamp_row(lane_int(told.bias, n), a.biases);
+    r.bias_hi = clamp_row(lane_int(told.bias, n + 1), a.biases);
   } else {
-    if (a.starts) {   // the last sequence that starts at the row or before: 64 of them at a time
+    int64_t n;
+    if (a.starts) {   // the same, 64 sequences at a time
       int64_t upto = 0;
       for (int64_t n0 = 0; n0 < a.N; n0 += kWave) {
         const unsigned long long before = __ballot(n0 + l < a.N && clamp_row(a.starts[min(n0 + l, a.N)], a.rows) <= row);
@@ -82,7 +97,8 @@ __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row) {
       r.first = n * each;
       r.out = false;
     }
-    if (a.counts) slot = a.slot ? a.slot[n] : n;
+    r.seq = n;
+    slot = a.counts && a.slot ? a.slot[n] : n;
     r.temperature = a.temperature ? a.temperature[n] : 1.f;
     r.repetition = a.repetition ? a.repetition[n] : 1.f;
     r.presence = a.presence ? a.presence[n] : 0.f;
@@ -96,92 +112,112 @@ __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row) {
     if (slot < 0 || slot >= a.slots) r.out = true;
     else r.counts = a.counts + slot * a.V;
   }
+  const int64_t m = a.mask ? a.mask_rows ? a.mask_rows[row] : row : -1;
   if (m >= 0 && m < a.masks) r.mask = reinterpret_cast<const uint8_t*>(a.mask + m * ((a.V + 31) / 32));
   return r;
 }
 
 // Lists that change a few of a row's tokens: the tokens fed in the sequence's rows up to this one, and
 // its biases, from the last entry on (of a token listed twice the last holds).  A lane an entry, 64 at a
-// time; a wave then goes through those of them that are among its own tokens.
+// time (-1: none); a wave then goes through those of them that are among its own tokens.
 struct Lists {
   int64_t fed, biases;   // entries
   const int32_t* ids;
-  const int32_t* bias_ids;     // the last entry
+  const int32_t* bias_ids;   // the last entry
   const float* bias_values;
-  int32_t id, bias_id;   // the first 64 of each (-1: none)
+  int32_t id, bias_id;       // of the first 64
   float bias_value;
-  __device__ __forceinline__ void load(int64_t from) {
+  __device__ __forceinline__ int32_t fed_id(int64_t from) const {
     const int64_t l = from + (threadIdx.x & 63);
-    id = bias_id = -1;
-    if (from < fed) {
-      id = ids[min(l, fed - 1)];
-      id = l < fed ? id : -1;
-    }
-    if (from < biases) {
-      bias_id = bias_ids[-min(l, biases - 1)];
-      bias_value = bias_values[-min(l, biases - 1)];
-      bias_id = l < biases ? bias_id : -1;
-    }
+    const int32_t x = ids[min(l, fed - 1)];
+    return l < fed ? x : -1;
   }
-  __device__ __forceinline__ Lists(const LogitsArgs& a, const RowOf& r, int64_t row) {
+  __device__ __forceinline__ void bias(int64_t from, int32_t& x, float& value) const {
+    const int64_t l = from + (threadIdx.x & 63);
+    x = bias_ids[-min(l, biases - 1)];
+    value = bias_values[-min(l, biases - 1)];
+    x = l < biases ? x : -1;
+  }
+  __device__ __forceinline__ Lists(const LogitsArgs& a, const RowOf& r, uint32_t row) {
     fed = a.ids ? row + 1 - r.first : 0;
     biases = max(r.bias_hi - r.bias_lo, (int64_t)0);
     ids = a.ids + r.first;
     bias_ids = a.bias_ids + (r.bias_hi - 1);
     bias_values = a.bias_values + (r.bias_hi - 1);
-    load(0);
+    if (fed > 0) id = fed_id(0);
+    if (biases > 0) bias(0, bias_id, bias_value);
   }
 };
 
-// A thread's eight tokens.  Loads do not branch (a wait for each would follow): a last thread with fewer
-// than eight takes the row's last eight, one without any too, and `keep` says which are its own.  TINY: rows
-// of fewer than eight.
-template <typename T, bool TINY>
-struct Piece {
-  int at;
-  uint32_t keep, bits;   // bits: what the mask allows
-  T raw[kVec];
-  int32_t count[kVec];
-  __device__ __forceinline__ void load_logits(const LogitsArgs& a, int64_t row, int64_t j) {
-    const T* const p = static_cast<const T*>(a.logits) + row * a.stride;
+// A thread's eight tokens from j on.  Loads do not branch (a wait for each would follow): a last thread with
+// fewer than eight takes the row's last eight, one without any too, and `keep` says which are its own.  TINY:
+// rows of fewer than eight.
+template <bool TINY>
+struct Place {
+  int at, n;
+  uint32_t keep;
+  __device__ __forceinline__ Place(const LogitsArgs& a, uint32_t j) : n(static_cast<int>(a.V)) {
     if constexpr (TINY) {
-      const int n = static_cast<int>(a.V);
       at = 0;
       keep = j == 0 ? (1u << n) - 1 : 0;
-#pragma unroll
-      for (int i = 0; i < kVec; ++i) raw[i] = p[min(i, n - 1)];
     } else {
-      at = static_cast<int>(min(j, a.V - kVec));
-      keep = j < a.V ? (0xffu << (j - at)) & 0xff : 0;
-      __builtin_memcpy(raw, p + at, sizeof raw);
+      at = static_cast<int>(min(j, static_cast<uint32_t>(n - kVec)));
+      keep = j < static_cast<uint32_t>(n) ? (0xffu << (j - at)) & 0xff : 0;
     }
   }
-  __device__ __forceinline__ void load_rest(const LogitsArgs& a, const RowOf& r) {
-    bits = keep;
-    if (r.mask) {
-      const uint32_t lo = r.mask[at >> 3], hi = r.mask[min(at + kVec - 1, static_cast<int>(a.V) - 1) >> 3];
-      bits &= (lo | hi << 8) >> (at & 7);
-    }
-    if (r.counts) {
-      if constexpr (TINY) {
+  template <typename T>
+  __device__ __forceinline__ void load(const T* row, T (&x)[kVec]) const {
+    if constexpr (TINY) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) count[i] = r.counts[min(i, static_cast<int>(a.V) - 1)];
-      } else {
-        __builtin_memcpy(count, r.counts + at, sizeof count);
-      }
+      for (int i = 0; i < kVec; ++i) x[i] = row[min(i, n - 1)];
+    } else {
+      __builtin_memcpy(x, row + at, sizeof x);
+    }
+  }
+  template <typename TO>
+  __device__ __forceinline__ void store(TO* row, const float (&v)[kVec]) const {
+    TO x[kVec];
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) x[i] = from_f<TO>(v[i]);
+    if (!TINY && keep == 0xff) {
+      __builtin_memcpy(row + at, x, sizeof x);
+    } else if (keep) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        if (keep >> i & 1) row[at + i] = x[i];
+    }
+  }
+};
+
+// Eight tokens of a row with what changes them.
+template <typename T, bool TINY>
+struct Tokens {
+  Place<TINY> place;
+  T raw[kVec];
+  int32_t count[kVec];
+  uint32_t bits[2];   // the mask's bytes at the first and the last of them
+  __device__ __forceinline__ Tokens(const LogitsArgs& a, uint32_t row, uint32_t j) : place(a, j) {
+    place.load(static_cast<const T*>(a.logits) + row * a.stride, raw);
+  }
+  __device__ __forceinline__ void load_rest(const RowOf& r) {
+    if (r.counts) {
+      place.load(r.counts, count);
     } else {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) count[i] = 0;
     }
+    if (r.mask) {
+      bits[0] = r.mask[place.at >> 3];
+      bits[1] = r.mask[(min(place.at + kVec, place.n) - 1) >> 3];
+    }
   }
   // the changed logits; base: the wave's first token
-  __device__ __forceinline__ void changed(const RowOf& r, const Lists& first, int64_t base, float (&l)[kVec]) {
+  __device__ __forceinline__ void changed(const RowOf& r, const Lists& lists, uint32_t base, float (&l)[kVec]) {
 #pragma clang fp contract(off)
-    for (int64_t from = 0; from < first.fed; from += kWave) {
-      Lists s = first;
-      if (from) s.load(from);
-      for (unsigned long long here = __ballot(static_cast<uint64_t>(s.id - base) < kWaveSpan); here; here &= here - 1) {
-        const int d = lane_int(s.id, __ffsll(here) - 1) - at;
+    for (int64_t from = 0; from < lists.fed; from += kWave) {
+      const int32_t id = from ? lists.fed_id(from) : lists.id;
+      for (unsigned long long here = __ballot(static_cast<uint32_t>(id) - base < kWaveSpan); here; here &= here - 1) {
+        const int d = lane_int(id, __ffsll(here) - 1) - place.at;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) count[i] += d == i;
       }
@@ -194,42 +230,32 @@ struct Piece {
     }
     if (any) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
-        const int32_t c = count[i] & 0x7fffffff;
-        const float x = count[i] ? l[i] > 0.f ? l[i] / r.repetition : l[i] * r.repetition : l[i];
-        const float y = x - r.frequency * static_cast<float>(c);
-        l[i] = c ? y - r.presence : x;
-      }
+      for (int i = 0; i < kVec; ++i)
+        if (count[i]) {
+          const int32_t c = count[i] & 0x7fffffff;
+          const float y = l[i] > 0.f ? l[i] / r.repetition : l[i] * r.repetition;
+          const float z = y - r.frequency * static_cast<float>(c);
+          l[i] = c ? z - r.presence : y;
+        }
     }
     uint32_t done = 0;
-    for (int64_t from = 0; from < first.biases; from += kWave) {
-      Lists s = first;
-      if (from) s.load(from);
-      for (unsigned long long here = __ballot(static_cast<uint64_t>(s.bias_id - base) < kWaveSpan); here; here &= here - 1) {
-        const int k = __ffsll(here) - 1, d = lane_int(s.bias_id, k) - at;
-        const float value = read_lane(s.bias_value, k);
+    for (int64_t from = 0; from < lists.biases; from += kWave) {
+      int32_t id = lists.bias_id;
+      float value = lists.bias_value;
+      if (from) lists.bias(from, id, value);
+      for (unsigned long long here = __ballot(static_cast<uint32_t>(id) - base < kWaveSpan); here; here &= here - 1) {
+        const int k = __ffsll(here) - 1, d = lane_int(id, k) - place.at;
+        const float more = read_lane(value, k);
         const uint32_t one = d >= 0 && d < kVec ? (1u << d) & ~done : 0;
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) l[i] = one >> i & 1 ? l[i] + value : l[i];
+        for (int i = 0; i < kVec; ++i) l[i] = one >> i & 1 ? l[i] + more : l[i];
         done |= one;
       }
     }
-    if (bits != 0xff) {
+    const uint32_t on = r.mask ? place.keep & (bits[0] | bits[1] << 8) >> (place.at & 7) : place.keep;
+    if (on != 0xff) {
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) l[i] = bits >> i & 1 ? l[i] : -kInf;
-    }
-  }
-  template <typename TO>
-  __device__ __forceinline__ void store(TO* out, const float (&v)[kVec]) const {
-    TO x[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) x[i] = from_f<TO>(v[i]);
-    if (!TINY && keep == 0xff) {
-      __builtin_memcpy(out + at, x, sizeof x);
-    } else if (keep) {
-#pragma unroll
-      for (int i = 0; i < kVec; ++i)
-        if (keep >> i & 1) out[at + i] = x[i];
+      for (int i = 0; i < kVec; ++i) l[i] = on >> i & 1 ? l[i] : -kInf;
     }
   }
 };
@@ -240,11 +266,20 @@ __device__ __forceinline__ float sharpness(float t) {
   if (!(t > 0.f)) return 1.f;
   return fminf(fmaxf(kLog2e / t, 1e-30f), 3e38f);
 }
-// e of l under the largest, and of -inf where nothing is left (`level`: that, or 0)
-__device__ __forceinline__ float under(float l, float top, float level, float k) {
-  return l == top ? (top > -kInf ? 1.f : 0.f) : exp2_hw((l - level) * k);
+// e of eight l under the largest, `top`.  Where nothing is left that is -inf, and so is every l (or NaN).
+__device__ __forceinline__ float under(float l, float top, float k) {
+  return l == top ? (top > -kInf ? 1.f : 0.f) : exp2_hw((l - (top > -kInf ? top : 0.f)) * k);
 }
-__device__ __forceinline__ float level_of(float top) { return top > -kInf ? top : 0.f; }
+__device__ __forceinline__ void under(const float (&l)[kVec], float top, float k, float (&e)[kVec]) {
+  const float level = top > -kInf ? top : 0.f;
+  if (top == kInf) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) e[i] = under(l[i], top, k);
+  } else {   // (zero times k is zero)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) e[i] = exp2_hw((l[i] - level) * k);
+  }
+}
 
 __device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
@@ -252,134 +287,228 @@ __device__ __forceinline__ int wave_min(int x) {
   return x;
 }
 
-// of a segment: CH times eight tokens a thread, a wave's in a row
-template <typename T, int CH, bool TINY>
-__global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a, uint32_t segs) {
-  __shared__ float sF[2][kThreads / kWave];
-  __shared__ int sI[kThreads / kWave];
+// The first launch: a workgroup a segment of a row, `steps` times kSeg tokens, the next of them loaded ahead.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a, uint32_t segs, uint32_t steps) {
+  __shared__ Part waves[kThreads / kWave];
   const uint32_t row = blockIdx.x / segs, seg = blockIdx.x % segs;
   const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t base = (static_cast<int64_t>(seg) * (kThreads / kWave) + w) * (CH * kWaveSpan);
-  Piece<T, TINY> piece[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) piece[c].load_logits(a, row, base + c * kWaveSpan + lane * kVec);
-  const RowOf r = row_of(a, row);
+  uint32_t base = seg * steps * kSeg + w * kWaveSpan;
+  const Told told(a);
+  Tokens<T, false> next(a, row, base + lane * kVec);
+  const RowOf r = row_of(a, row, told);
   if (r.out) return;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) piece[c].load_rest(a, r);
+  next.load_rest(r);
   const Lists lists(a, r, row);
-  float l[CH][kVec], top = -kInf, sum = 0.f;
+  const float k = sharpness(r.temperature);
+  const bool greedy = !(r.temperature > 0.f);
+  Part mine{-kInf, 0.f, INT32_MAX, 0};   // the thread's
+  for (uint32_t s = 0; s < steps; ++s, base += kSeg) {
+    Tokens<T, false> now = next;
+    // (behind the segment: the row's end, which is not used)
+    next = Tokens<T, false>(a, row, s + 1 < steps ? base + kSeg + lane * kVec : static_cast<uint32_t>(a.V));
+    next.load_rest(r);
+    float l[kVec], e[kVec], top = mine.top;
+    now.changed(r, lists, base, l);
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    piece[c].changed(r, lists, base + c * kWaveSpan, l[c]);
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) top = fmaxf(top, l[c][i]);
-  }
-  top = wave_max(top);
-  if (lane == 0) sF[0][w] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(sF[0][0], sF[0][1]), fmaxf(sF[0][2], sF[0][3]));
-  const float k = sharpness(r.temperature), level = level_of(top);
-#pragma unroll
-  for (int c = 0; c < CH; ++c)
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) sum += under(l[c][i], top, level, k);
-  sum = wave_sum(sum);
-  if (lane == 0) sF[1][w] = sum;
-  if (!(r.temperature > 0.f)) {
-    int first = INT32_MAX;
-#pragma unroll
-    for (int c = CH - 1; c >= 0; --c)
+    for (int i = 0; i < kVec; ++i) top = fmaxf(top, l[i]);
+    if (greedy && top > mine.top) {
 #pragma unroll
       for (int i = kVec - 1; i >= 0; --i)
-        if (l[c][i] == top) first = piece[c].at + i;
-    first = wave_min(first);
-    if (lane == 0) sI[w] = first;
+        if (l[i] == top) mine.first = now.place.at + i;
+    }
+    mine.sum *= under(mine.top, top, k);
+    under(l, top, k, e);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) mine.sum += e[i];
+    mine.top = top;
   }
+  const float most = wave_max(mine.top);
+  const float sum = wave_sum(mine.sum == mine.sum ? mine.sum * under(mine.top, most, k) : mine.sum);   // (a NaN shows, whatever it weighs)
+  const int first = greedy ? wave_min(mine.top == most ? mine.first : INT32_MAX) : 0;
+  if (lane == 0) waves[w] = Part{most, sum, first, 0};
   __syncthreads();
   if (threadIdx.x == 0) {
-    Part p;
-    p.top = top;
-    p.sum = (sF[1][0] + sF[1][1]) + (sF[1][2] + sF[1][3]);
-    p.first = !(r.temperature > 0.f) ? min(min(sI[0], sI[1]), min(sI[2], sI[3])) : 0;
-    p.unused = 0;
+    Part p{fmaxf(fmaxf(waves[0].top, waves[1].top), fmaxf(waves[2].top, waves[3].top)), 0.f, INT32_MAX, 0};
+    for (int i = 0; i < kThreads / kWave; ++i) {
+      p.sum += waves[i].sum == waves[i].sum ? waves[i].sum * under(waves[i].top, p.top, k) : waves[i].sum;
+      if (waves[i].top == p.top) p.first = min(p.first, waves[i].first);
+    }
     static_cast<Part*>(a.parts)[blockIdx.x] = p;
   }
 }
 
-// p of a segment from the parts of all, or the changed logits themselves
-template <typename T, typename TO, int CH, bool TINY, bool PROBS>
-__global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t segs) {
-  const uint32_t row = blockIdx.x / segs, seg = blockIdx.x % segs;
-  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t base = (static_cast<int64_t>(seg) * (kThreads / kWave) + w) * (CH * kWaveSpan);
-  Piece<T, TINY> piece[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) piece[c].load_logits(a, row, base + c * kWaveSpan + lane * kVec);
+// a row's whole from its parts, on every lane of a wave; x: the part of the lane's number
+__device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint32_t segs, float k, bool greedy) {
+  const uint32_t lane = threadIdx.x & 63;
+  float top = lane < segs ? x.top : -kInf;
+  for (uint32_t s = kWave + lane; s < segs; s += kWave) top = fmaxf(top, parts[s].top);
+  Part all{wave_max(top), 0.f, INT32_MAX, 0};
+  auto add = [&](const Part& p) {
+    all.sum += p.sum == p.sum ? p.sum * under(p.top, all.top, k) : p.sum;   // (a NaN shows, whatever it weighs)
+    if (p.top == all.top) all.first = min(all.first, p.first);
+  };
+  if (lane < segs) add(x);
+  for (uint32_t s = kWave + lane; s < segs; s += kWave) add(parts[s]);
+  all.sum = wave_sum(all.sum);
+  if (greedy) all.first = wave_min(all.first);
+  return all;
+}
+
+// The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves.
+template <typename T, typename TO, bool TINY, bool PROBS>
+__global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t windows, uint32_t segs) {
+  const uint32_t row = blockIdx.x / windows, base = blockIdx.x % windows * kSeg + (threadIdx.x >> 6) * kWaveSpan;
+  const uint32_t lane = threadIdx.x & 63;
+  const Told told(a);
   const Part* const parts = static_cast<const Part*>(a.parts) + static_cast<int64_t>(row) * segs;
-  Part p{-kInf, 0.f, INT32_MAX, 0};
-  if constexpr (PROBS) {
-    const Part x = parts[min(static_cast<uint32_t>(lane), segs - 1)];
-    if (static_cast<uint32_t>(lane) < segs) p = x;
-  }
-  const RowOf r = row_of(a, row);
+  Part part{};
+  if constexpr (PROBS) part = parts[min(lane, segs - 1)];
+  Tokens<T, TINY> now(a, row, base + lane * kVec);
+  const RowOf r = row_of(a, row, told);
   if (r.out) return;
-#pragma unroll
-  for (int c = 0; c < CH; ++c) piece[c].load_rest(a, r);
+  now.load_rest(r);
   const Lists lists(a, r, row);
-  float top = 0.f, level = 0.f, sum = 0.f, f = 0.f, k = 0.f;
-  int first = INT32_MAX;
+  const float k = sharpness(r.temperature);
+  const bool greedy = !(r.temperature > 0.f);
+  Part whole{};
+  if constexpr (PROBS) whole = whole_of(parts, part, segs, k, greedy);
+  float l[kVec];
+  now.changed(r, lists, base, l);
   if constexpr (PROBS) {
-    k = sharpness(r.temperature);
-    top = p.top;
-    for (uint32_t s = kWave + lane; s < segs; s += kWave) top = fmaxf(top, parts[s].top);
-    top = wave_max(top);
-    level = level_of(top);
-    auto add = [&](const Part& x) {
-      // (a NaN in a segment that weighs nothing shows too)
-      sum += x.sum == x.sum ? x.sum * under(x.top, top, level, k) : x.sum;
-      if (x.top == top) first = min(first, x.first);
-    };
-    add(p);
-    for (uint32_t s = kWave + lane; s < segs; s += kWave) add(parts[s]);
-    sum = wave_sum(sum);
-    f = sum == 0.f ? 0.f : 1.f / sum;
-    if (!(r.temperature > 0.f)) first = wave_min(first);
+    if (greedy) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        l[i] = whole.sum != whole.sum ? whole.sum : whole.top > -kInf && now.place.at + i == whole.first ? 1.f : 0.f;
+    } else {
+      const float f = whole.sum == 0.f ? 0.f : 1.f / whole.sum;
+      under(l, whole.top, k, l);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) l[i] *= f;
+    }
   }
+  now.place.store(static_cast<TO*>(a.out) + row * a.V, l);
+}
+
+// Both at once: a workgroup a row of up to CH windows of its threads, the changed logits kept in registers.
+template <typename T, typename TO, int THREADS, int CH, bool TINY>
+__global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
+  constexpr int kOneWaves = THREADS / kWave, kOneSeg = THREADS * kVec;
+  __shared__ float tops[kOneWaves], sums[kOneWaves];
+  __shared__ int firsts[kOneWaves];
+  const uint32_t row = blockIdx.x;
+  const int w = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const uint32_t base = w * kWaveSpan;
+  const Told told(a);
+  Tokens<T, TINY> next(a, row, base + lane * kVec);
+  const RowOf r = row_of(a, row, told);
+  if (r.out) return;
+  next.load_rest(r);
+  const Lists lists(a, r, row);
+  const float k = sharpness(r.temperature);
+  const bool greedy = !(r.temperature > 0.f);
+  float l[CH][kVec], top = -kInf, sum = 0.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    float l[kVec];
-    piece[c].changed(r, lists, base + c * kWaveSpan, l);
-    if constexpr (PROBS) {
-      if (r.temperature > 0.f) {
+    Tokens<T, TINY> now = next;
+    if (c + 1 < CH) {
+      next = Tokens<T, TINY>(a, row, base + (c + 1) * kOneSeg + lane * kVec);
+      next.load_rest(r);
+    }
+    now.changed(r, lists, base + c * kOneSeg, l[c]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) l[i] = under(l[i], top, level, k) * f;
-      } else {
+    for (int i = 0; i < kVec; ++i) top = fmaxf(top, l[c][i]);
+  }
+  top = wave_max(top);
+  if (lane == 0) tops[w] = top;
+  __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) l[i] = sum != sum ? sum : top > -kInf && piece[c].at + i == first ? 1.f : 0.f;
+  for (int i = 0; i < kOneWaves; ++i) top = fmaxf(top, tops[i]);
+  if (greedy) {
+    int first = INT32_MAX;
+#pragma unroll
+    for (int c = CH - 1; c >= 0; --c) {
+      const Place<TINY> place(a, base + c * kOneSeg + lane * kVec);
+#pragma unroll
+      for (int i = kVec - 1; i >= 0; --i) {
+        if (l[c][i] == top) first = place.at + i;
+        sum += l[c][i] != l[c][i] ? l[c][i] : 0.f;   // (a NaN shows)
       }
     }
-    piece[c].store(static_cast<TO*>(a.out) + row * a.V, l);
+    first = wave_min(first);
+    if (lane == 0) firsts[w] = first;
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      under(l[c], top, k, l[c]);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) sum += l[c][i];
+    }
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) sums[w] = sum;
+  __syncthreads();
+  sum = 0.f;
+  int first = INT32_MAX;
+#pragma unroll
+  for (int i = 0; i < kOneWaves; ++i) {
+    sum += sums[i];
+    if (greedy) first = min(first, firsts[i]);
+  }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const Place<TINY> place(a, base + c * kOneSeg + lane * kVec);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      l[c][i] = !greedy ? l[c][i] * f : sum != sum ? sum : top > -kInf && place.at + i == first ? 1.f : 0.f;
+    place.store(static_cast<TO*>(a.out) + row * a.V, l[c]);
   }
 }
 
-template <typename T, typename TO, int CH, bool TINY>
+// A row's segments in the first of two launches: about so many workgroups in all, eight to a row or a multiple of it,
+// as workgroups go to the eight L2s in turn: the rows of a sequence then find its counts in one.
+constexpr int64_t kManyBlocks = 4096;
+template <typename T, typename TO, bool TINY>
 hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
-  const int64_t segs = (a.V + CH * kSeg - 1) / (CH * kSeg);
-  const dim3 grid(static_cast<unsigned>(a.rows * segs)), block(kThreads);
-  if (!a.probs) {
-    hipLaunchKernelGGL((logits_out<T, TO, CH, TINY, false>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
+  const int64_t windows = logits_segments(a.V);
+  const dim3 block(kThreads), all(static_cast<unsigned>(a.rows * windows));
+  if (TINY || !a.probs) {
+    hipLaunchKernelGGL((logits_out<T, TO, TINY, false>), all, block, 0, s, a, static_cast<uint32_t>(windows), 0u);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((logits_parts<T, CH, TINY>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
-  hipLaunchKernelGGL((logits_out<T, TO, CH, TINY, true>), grid, block, 0, s, a, static_cast<uint32_t>(segs));
+  const int64_t most = (kManyBlocks / 8 + a.rows - 1) / a.rows * 8;
+  const uint32_t segs = static_cast<uint32_t>(std::min(windows, most)), steps = static_cast<uint32_t>((windows + segs - 1) / segs);
+  hipLaunchKernelGGL((logits_parts<T>), dim3(static_cast<unsigned>(a.rows * segs)), block, 0, s, a, segs, steps);
+  hipLaunchKernelGGL((logits_out<T, TO, false, true>), all, block, 0, s, a, static_cast<uint32_t>(windows), segs);
   return hipGetLastError();
 }
+// One launch up to 16384 tokens, and up to 57344 (what its registers hold) from 96 rows on: it reads the logits once,
+// but a row is one compute unit's.  Two launches | one, us, bf16 with everything on | fp32 logits alone:
+//   rows          1           8            64           128          256          512         1024        2048
+//    2000     14.7  8.0   21.5 11.4   21.3 11.2    21.9 11.5    22.5 12.0    27.9 16.5    28.1 23.9   45.6 47.8
+//    8000     12.1  7.5   13.7  8.4   13.8  8.8    15.0  9.1    19.5 11.0    30.0 17.3    44.3 26.1   79.9 48.3
+//   16000     10.2  8.9   10.9 10.0   12.8 10.4    15.7 12.1    24.7 15.9    39.4 22.2    64.5 36.1    132 74.5
+//   32001      9.4 12.4   10.1 13.7   14.4 16.0    21.6 18.2    35.3 22.7    55.1 41.9    99.5 74.5
+//   50257      8.8 18.4    9.4 20.1   19.2 24.0    30.1 26.7    51.7 33.4    81.1 63.3
+//    2000      6.9  4.5    7.4  4.8    7.6  4.9     8.0  5.1     8.9  5.6    10.3  8.0    13.1 12.9   22.9 25.7
+//   16000      7.6  7.0    7.9  7.3    9.1  8.2    11.9  9.6    19.0 14.3    33.1 22.5    51.8 36.9    114 74.7
+//   50257      7.6 14.6    7.6 15.3   16.4 18.8    26.7 23.0    46.5 34.3    85.9 67.2
+// (1024 threads throughout; up to 2048 tokens take 256.)
 template <typename T, typename TO>
 hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
-  if (a.V < kVec) return logits_at<T, TO, 1, true>(a, s);
-  if (a.rows * ((a.V + 4 * kSeg - 1) / (4 * kSeg)) >= 1024) return logits_at<T, TO, 4, false>(a, s);
-  return logits_at<T, TO, 1, false>(a, s);
+  const dim3 rows(static_cast<unsigned>(a.rows));
+  if (a.probs && a.V <= (a.rows < 96 ? 16384 : 57344)) {
+    if (a.V < kVec) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, true>), rows, dim3(256), 0, s, a);
+    else if (a.V <= 2048) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, false>), rows, dim3(256), 0, s, a);
+    else if (a.V <= 8192) hipLaunchKernelGGL((logits_one<T, TO, 1024, 1, false>), rows, dim3(1024), 0, s, a);
+    else if (a.V <= 16384) hipLaunchKernelGGL((logits_one<T, TO, 1024, 2, false>), rows, dim3(1024), 0, s, a);
+    else if (a.V <= 32768) hipLaunchKernelGGL((logits_one<T, TO, 1024, 4, false>), rows, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((logits_one<T, TO, 1024, 7, false>), rows, dim3(1024), 0, s, a);
+    return hipGetLastError();
+  }
+  if (a.V < kVec) return logits_at<T, TO, true>(a, s);   // (changed logits)
+  return logits_at<T, TO, false>(a, s);
 }
 
 constexpr int32_t kPromptBit = INT32_MIN;
