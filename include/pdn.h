@@ -432,10 +432,10 @@ pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype,
  * Weights, the scale and their gradients are fp32, sums and factors too; the
  * tensors of rows are fp32 or bf16, rounded once when they are written.  They
  * need to be aligned to an element only (16 bytes are faster).  Rows do not
- * depend on each other: a NaN or Inf shows in its own row, and in the gradients of the
- * vectors in its channel.  A row's squares are summed in fp32: a row with a sum past
- * 3.4e38 gives zeros.  Gradients of vectors are summed in one order, so a
- * call's results are the same each time.  No call allocates. */
+ * depend on each other: a NaN or Inf shows in its own row, and in the gradients of
+ * the vectors.  A row's squares are summed in fp32: one whose sum passes 3.4e38 is out
+ * of range (zeros, and gradients that are NaN).  Gradients of vectors are summed in one order, so
+ * a call's results are the same each time.  No call allocates. */
 
 typedef struct {
   int64_t rows, D;      /* rows of D channels; D from 1 to 16384               */
@@ -481,7 +481,8 @@ typedef enum {
 } pdn_act;
 
 typedef struct {
-  int64_t tokens, H;    /* tensors [tokens, H, d], a token's row dense         */
+  int64_t tokens, H;    /* tensors [tokens, H, d], a token's row dense; H below
+                           2^24, H d up to 2^26                                */
   int32_t d;            /* channels of a head; from 1 to 512                   */
   pdn_dtype io;         /* every tensor of rows                                */
   pdn_norm norm;

@@ -131,42 +131,85 @@ __device__ __forceinline__ void block_sum(float (&x)[N], float (*buf)[16][4], in
     for (int k = 0; k < N; ++k) x[k] += b[w][k];
 }
 
-template <int CH, RowKind KIND>
-__device__ __forceinline__ Cols<KIND> cols(int k, int D) {
-  return Cols<KIND>((k * blockDim.x + threadIdx.x) * kVec, D);
+// A workgroup's part of a vector's gradient from its groups of L lanes: a wave's by shuffles, then the waves'
+// (columns of a lane that are another's are zero).
+template <RowKind KIND>
+__device__ __forceinline__ void group_part(float (&v)[kVec], const Cols<KIND>& o, int L, float (*sum)[kWave * kVec], float* part) {
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    for (int off = L; off < kWave; off <<= 1) v[i] += __shfl_xor(v[i], off, 64);
+  const int wave = threadIdx.x / kWave, l = threadIdx.x & 63;
+  __syncthreads();   // (of the last vector's)
+  if (l < L)
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      if (o.keep >> i & 1) sum[wave][o.at + i] = v[i];
+  __syncthreads();
+  for (int j = threadIdx.x; j < o.n; j += blockDim.x) part[j] = (sum[0][j] + sum[1][j]) + (sum[2][j] + sum[3][j]);
 }
 
-template <typename TI, typename TS, int CH, bool POST, RowKind KIND>
-__global__ __launch_bounds__(1024) void rnorm_fwd(RnormArgs a) {
-  __shared__ float buf[2][16][4];
+// The threads of a row: a workgroup, or GROUP: L lanes of one (a power of two) where a row has not
+// more than eight columns for each lane of a wave.
+constexpr int kGroupThreads = 256;
+template <bool GROUP>
+struct Team {
+  int lane, size, L;
+  int64_t first, step;   // rows
+  float (*buf)[16][4];
   int turn = 0;
+  __device__ __forceinline__ Team(int L, float (*buf)[16][4]) : L(L), buf(buf) {
+    const int groups = GROUP ? kGroupThreads / L : 1;
+    lane = GROUP ? threadIdx.x & (L - 1) : threadIdx.x;
+    size = GROUP ? L : blockDim.x;
+    first = blockIdx.x * static_cast<int64_t>(groups) + (GROUP ? threadIdx.x / L : 0);
+    step = gridDim.x * static_cast<int64_t>(groups);
+  }
+  template <int N>
+  __device__ __forceinline__ void sum(float (&x)[N]) {
+    if constexpr (GROUP) {
+#pragma unroll
+      for (int k = 0; k < N; ++k) x[k] = lanes_sum(x[k], L);
+    } else {
+      block_sum(x, buf, turn);
+    }
+  }
+  template <RowKind KIND>
+  __device__ __forceinline__ Cols<KIND> cols(int k, int D) const {
+    return Cols<KIND>((k * size + lane) * kVec, D);
+  }
+};
+
+template <typename TI, typename TS, int CH, bool POST, bool GROUP, RowKind KIND>
+__global__ __launch_bounds__(GROUP ? kGroupThreads : 1024) void rnorm_fwd(RnormArgs a, int L) {
+  __shared__ float buf[2][16][4];
+  Team<GROUP> team(L, buf);
   const int D = static_cast<int>(a.D);
   const float c = 1.f / a.D;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  for (int64_t row = team.first; row < a.rows; row += team.step) {
     const int64_t at = row * a.D;
     Raw<TI> y[CH];
     Raw<TS> x[CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, D);
+      const auto o = team.template cols<KIND>(k, D);
       y[k].load(static_cast<const TI*>(a.y) + at, o);
       if (a.residual) x[k].load(static_cast<const TS*>(a.residual) + at, o);
     }
 #pragma unroll
-    for (int k = 0; k < CH; ++k) y[k].settle(cols<CH, KIND>(k, D));
+    for (int k = 0; k < CH; ++k) y[k].settle(team.template cols<KIND>(k, D));
     float h[CH][kVec], q[1] = {0.f}, ry = 1.f;
     if constexpr (POST) {
 #pragma unroll
       for (int k = 0; k < CH; ++k)
 #pragma unroll
         for (int i = 0; i < kVec; ++i) q[0] += y[k][i] * y[k][i];
-      block_sum(q, buf, turn);
+      team.sum(q);
       ry = factor(q[0], c, a.eps);
       q[0] = 0.f;
     }
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, D);
+      const auto o = team.template cols<KIND>(k, D);
       float v[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) h[k][i] = y[k][i];
@@ -191,11 +234,11 @@ __global__ __launch_bounds__(1024) void rnorm_fwd(RnormArgs a) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) q[0] += h[k][i] * h[k][i];
     }
-    block_sum(q, buf, turn);
+    team.sum(q);
     const float rh = factor(q[0], c, a.eps);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, D);
+      const auto o = team.template cols<KIND>(k, D);
       float v[kVec];
       ld_weight(a.weight, o, v);
 #pragma unroll
@@ -205,20 +248,20 @@ __global__ __launch_bounds__(1024) void rnorm_fwd(RnormArgs a) {
   }
 }
 
-// The backward: a workgroup takes every gridDim-th row and keeps the vectors' gradients of its
-// columns in registers; rnorm_parts of them are summed by sum_parts.  AHEAD: rows of
-// few threads, with the next row loaded while this one waits for its sums, and the vectors
-// in registers.
-constexpr int kAheadThreads = 256;
+// The backward: a team takes every so many-th row and keeps the vectors' gradients of its columns in
+// registers, of D > 8192 two of them in shared memory; the workgroups' (rnorm_parts) are summed by sum_parts.
+// Up to 8192 columns the next row is loaded while this one waits for its sums, and the vectors are
+// in registers, or where a row takes more than 256 threads (and a thread has 128 of those) in shared memory.
 template <typename TI, typename TS, int CH, bool Y, RowKind KIND>
 struct BackRows {   // what a row's step reads
   Raw<TI> du[CH], y[Y ? CH : 1];
   Raw<TS> h[CH], dh[CH];
-  __device__ __forceinline__ void load(const RnormArgs& a, int64_t row) {
+  template <typename TEAM>
+  __device__ __forceinline__ void load(const RnormArgs& a, const TEAM& team, int64_t row) {
     const int64_t at = row * a.D;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
+      const auto o = team.template cols<KIND>(k, static_cast<int>(a.D));
       du[k].load(static_cast<const TI*>(a.du) + at, o);
       h[k].load(static_cast<const TS*>(a.h_in) + at, o);
       if constexpr (Y) {
@@ -227,10 +270,11 @@ struct BackRows {   // what a row's step reads
       if (a.dh) dh[k].load(static_cast<const TS*>(a.dh) + at, o);
     }
   }
-  __device__ __forceinline__ void settle(const RnormArgs& a) {
+  template <typename TEAM>
+  __device__ __forceinline__ void settle(const RnormArgs& a, const TEAM& team) {
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
+      const auto o = team.template cols<KIND>(k, static_cast<int>(a.D));
       du[k].settle(o);
       h[k].settle(o);
       if constexpr (Y) y[k].settle(o);
@@ -238,62 +282,91 @@ struct BackRows {   // what a row's step reads
     }
   }
 };
-// the vectors at this thread's columns
-template <int CH, bool POST, bool SCALE, RowKind KIND>
-struct Vectors {
-  float w[CH][kVec], wp[POST ? CH : 1][kVec], sc[SCALE ? CH : 1][kVec];
-  __device__ __forceinline__ void load(const RnormArgs& a) {
-#pragma unroll
-    for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, static_cast<int>(a.D));
-      ld_weight(a.weight, o, w[k]);
-      if constexpr (POST) ld_weight(a.post_weight, o, wp[k]);
-      if constexpr (SCALE) ld_weight(a.scale, o, sc[k]);
-    }
-  }
-};
-template <typename TI, typename TS, int CH, bool POST, bool SCALE, bool AHEAD, RowKind KIND>
-__global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024, AHEAD ? 3 : 4) void rnorm_bwd(RnormArgs a) {
+constexpr int kBackWaves = 3;   // a SIMD's, where a workgroup has up to 256 threads
+template <typename TI, typename TS, int CH, bool POST, bool SCALE, bool GROUP, int THREADS, RowKind KIND>
+__global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm_bwd(RnormArgs a, int L) {
+  constexpr bool kAhead = CH == 1, kShared = kAhead && THREADS > 256;
+  constexpr int kVectors = 1 + POST + SCALE;
   __shared__ float buf[2][16][4];
-  int turn = 0;
+  __shared__ float kept[CH > 1 && POST ? CH * kVec * THREADS : 1], kept2[CH > 1 && SCALE ? CH * kVec * THREADS : 1];
+  __shared__ floatx4 vectors[kShared ? kVectors * 2 * THREADS : 1];   // (a thread's own places, THREADS apart)
+  Team<GROUP> team(L, buf);
   const int D = static_cast<int>(a.D);
   const float c = 1.f / a.D;
-  float dw[CH][kVec] = {}, dp[POST ? CH : 1][kVec] = {}, ds[SCALE ? CH : 1][kVec] = {};
-  Vectors<CH, POST, SCALE, KIND> v;
-  if constexpr (AHEAD) v.load(a);
+  constexpr bool kRegs = CH == 1;   // (all three gradients in registers)
+  float dw[CH][kVec] = {}, dp[POST && kRegs ? CH : 1][kVec] = {}, ds[SCALE && kRegs ? CH : 1][kVec] = {};
+  float w[kVec], wp[kVec], sc[kVec];
+  // weight (0), post_weight (1), scale (2) at the thread's columns
+  auto of_memory = [&](int which, int k, float (&v)[kVec]) {
+    ld_weight(which == 0 ? a.weight : which == 1 ? a.post_weight : a.scale, team.template cols<KIND>(k, D), v);
+  };
+  auto place = [&](int which, int half) -> floatx4& {
+    return vectors[((which == 2 && !POST ? 1 : which) * 2 + half) * THREADS + threadIdx.x];
+  };
+  auto get = [&](int which, int k, float (&v)[kVec]) {
+    if constexpr (kShared) {
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) v[i] = place(which, i / 4)[i % 4];
+    } else if constexpr (!kAhead) {
+      of_memory(which, k, v);
+    }
+  };
+  if constexpr (kAhead) {
+    of_memory(0, 0, w);
+    if constexpr (POST) of_memory(1, 0, wp);
+    if constexpr (SCALE) of_memory(2, 0, sc);
+    if constexpr (kShared) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        place(0, h) = floatx4{w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]};
+        if constexpr (POST) place(1, h) = floatx4{wp[4 * h], wp[4 * h + 1], wp[4 * h + 2], wp[4 * h + 3]};
+        if constexpr (SCALE) place(2, h) = floatx4{sc[4 * h], sc[4 * h + 1], sc[4 * h + 2], sc[4 * h + 3]};
+      }
+    }
+  } else {   // (likewise)
+#pragma unroll
+    for (int i = 0; i < CH * kVec; ++i) {
+      if constexpr (POST) kept[i * THREADS + threadIdx.x] = 0.f;
+      if constexpr (SCALE) kept2[i * THREADS + threadIdx.x] = 0.f;
+    }
+  }
   BackRows<TI, TS, CH, POST || SCALE, KIND> r;
-  r.load(a, blockIdx.x);
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+  if (team.first < a.rows) r.load(a, team, team.first);
+  for (int64_t row = team.first; row < a.rows; row += team.step) {
     BackRows<TI, TS, CH, POST || SCALE, KIND> next;
-    if constexpr (AHEAD) {
-      r.settle(a);
-      if (row + gridDim.x < a.rows) next.load(a, row + gridDim.x);
+    if constexpr (kAhead) {
+      r.settle(a, team);
+      if (row + team.step < a.rows) next.load(a, team, row + team.step);
     } else {
-      if (row != blockIdx.x) r.load(a, row);
-      v.load(a);
-      r.settle(a);
+      if (row != team.first) r.load(a, team, row);
+      r.settle(a, team);
     }
     const int64_t at = row * a.D;
     float e[POST ? CH : 1][kVec], q[POST ? 3 : 2] = {};
 #pragma unroll
-    for (int k = 0; k < CH; ++k)
+    for (int k = 0; k < CH; ++k) {
+      get(0, k, w);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         q[0] += r.h[k][i] * r.h[k][i];
-        q[1] += r.du[k][i] * v.w[k][i] * r.h[k][i];
+        q[1] += r.du[k][i] * w[i] * r.h[k][i];
         if constexpr (POST) q[2] += r.y[k][i] * r.y[k][i];
       }
-    block_sum(q, buf, turn);
+    }
+    team.sum(q);
     const float rh = factor(q[0], c, a.eps), mh = (rh * q[1] * c) * rh * rh;
     const float ry = POST ? factor(q[POST ? 2 : 0], c, a.eps) : 1.f;
     float p[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = cols<CH, KIND>(k, D);
+      const auto o = team.template cols<KIND>(k, D);
+      get(0, k, w);
+      if constexpr (POST) get(1, k, wp);
+      if constexpr (SCALE) get(2, k, sc);
       float t[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        t[i] = rh * (r.du[k][i] * v.w[k][i]) - r.h[k][i] * mh;
+        t[i] = rh * (r.du[k][i] * w[i]) - r.h[k][i] * mh;
         dw[k][i] += r.du[k][i] * (r.h[k][i] * rh);
         if (a.dh) t[i] += r.dh[k][i];
       }
@@ -302,54 +375,82 @@ __global__ __launch_bounds__(AHEAD ? kAheadThreads : 1024, AHEAD ? 3 : 4) void r
       for (int i = 0; i < kVec; ++i) {
         t[i] *= a.alpha;
         if constexpr (SCALE) {
-          if (a.y) ds[k][i] += t[i] * (POST ? r.y[k][i] * ry * v.wp[POST ? k : 0][i] : r.y[k][i]);
-          t[i] *= v.sc[k][i];
+          if (a.y) {
+            const float x = t[i] * (POST ? r.y[k][i] * ry * wp[i] : r.y[k][i]);
+            if constexpr (kRegs) ds[k][i] += x;
+            else kept2[(k * kVec + i) * THREADS + threadIdx.x] += x;
+          }
+          t[i] *= sc[i];
         }
         if constexpr (POST) {
-          dp[k][i] += t[i] * (r.y[k][i] * ry);
-          e[k][i] = t[i] * v.wp[k][i];
+          const float x = t[i] * (r.y[k][i] * ry);
+          if constexpr (kRegs) dp[k][i] += x;
+          else kept[(k * kVec + i) * THREADS + threadIdx.x] += x;
+          e[k][i] = t[i] * wp[i];
           p[0] += e[k][i] * r.y[k][i];
         }
       }
       if constexpr (!POST) store(static_cast<TI*>(a.dy) + at, o, t);
     }
     if constexpr (POST) {
-      block_sum(p, buf, turn);
+      team.sum(p);
       const float my = (ry * p[0] * c) * ry * ry;
 #pragma unroll
       for (int k = 0; k < CH; ++k) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) e[k][i] = ry * e[k][i] - r.y[k][i] * my;
-        store(static_cast<TI*>(a.dy) + at, cols<CH, KIND>(k, D), e[k]);
+        store(static_cast<TI*>(a.dy) + at, team.template cols<KIND>(k, D), e[k]);
       }
     }
-    if constexpr (AHEAD) r = next;
+    if constexpr (kAhead) r = next;
   }
-#pragma unroll
-  for (int k = 0; k < CH; ++k) {
-    const auto o = cols<CH, KIND>(k, D);
-    float* const part = a.part + blockIdx.x * a.D;
-    const int64_t each = gridDim.x * a.D;
-    if (a.dweight) store(part, o, dw[k]);
+  float* const part = a.part + blockIdx.x * a.D;
+  const int64_t each = gridDim.x * a.D;
+  if constexpr (GROUP) {
+    __shared__ float sum[kGroupThreads / kWave][kWave * kVec];
+    const auto o = team.template cols<KIND>(0, D);
+    if (a.dweight) group_part(dw[0], o, L, sum, part);
     if constexpr (POST) {
-      if (a.dpost_weight) store(part + each, o, dp[k]);
+      if (a.dpost_weight) group_part(dp[0], o, L, sum, part + each);
     }
     if constexpr (SCALE) {
-      if (a.dscale) store(part + 2 * each, o, ds[k]);
+      if (a.dscale) group_part(ds[0], o, L, sum, part + 2 * each);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < CH; ++k) {
+      const auto o = team.template cols<KIND>(k, D);
+      if constexpr (!kRegs) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          if constexpr (POST) dp[0][i] = kept[(k * kVec + i) * THREADS + threadIdx.x];
+          if constexpr (SCALE) ds[0][i] = kept2[(k * kVec + i) * THREADS + threadIdx.x];
+        }
+      }
+      if (a.dweight) store(part, o, dw[k]);
+      if constexpr (POST) {
+        if (a.dpost_weight) store(part + each, o, dp[0]);
+      }
+      if constexpr (SCALE) {
+        if (a.dscale) store(part + 2 * each, o, ds[0]);
+      }
     }
   }
 }
 
-// out[j] = sum over p of part[p][j], for up to three vectors: 16 columns a workgroup, every
-// 64th part a thread, in 64 bits and always in the same order.  What bounds it is
-// latency: sixteen parts are loaded at a time.
+// out[j] = sum over p of part[p][j], for up to three vectors: COLS columns a workgroup, every
+// kSumRows-th part a thread, in 64 bits and always in the same order.  What bounds it is
+// latency: eight parts are loaded at a time.  Columns, 16 | 32, us: 745 parts of 3 x 2048
+// 7.7 | 5.0, 500 of 1001 3.6 | 4.2, 1024 of 128 4.7 | 5.6.
 struct SumArgs {
   const float* part[3];
   float* out[3];
   int64_t parts, width;
 };
-constexpr int kSumCols = 16, kSumRows = 64, kSumDeep = 8;
+constexpr int kSumDeep = 8;
+template <int kSumCols>
 __global__ __launch_bounds__(1024) void sum_parts(SumArgs a) {
+  constexpr int kSumRows = 1024 / kSumCols;
   __shared__ double sum[kSumRows][kSumCols + 1];
   const int c = threadIdx.x % kSumCols, g = threadIdx.x / kSumCols;
   const int64_t j = blockIdx.x * static_cast<int64_t>(kSumCols) + c;
@@ -376,31 +477,43 @@ __global__ __launch_bounds__(1024) void sum_parts(SumArgs a) {
 }
 hipError_t launch_sums(const SumArgs& a, int vectors, hipStream_t s) {
   if (vectors == 0) return hipSuccess;
-  const unsigned blocks = static_cast<unsigned>((a.width + kSumCols - 1) / kSumCols);
-  hipLaunchKernelGGL(sum_parts, dim3(blocks, vectors), dim3(1024), 0, s, a);
+  const bool wide = vectors * a.width >= 4096;
+  const int64_t cols = wide ? 32 : 16;
+  const dim3 grid(static_cast<unsigned>((a.width + cols - 1) / cols), vectors), block(1024);
+  if (wide) hipLaunchKernelGGL(sum_parts<32>, grid, block, 0, s, a);
+  else hipLaunchKernelGGL(sum_parts<16>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
-// threads a row: eight columns each, CH times
+// lanes for n columns, eight each: a power of two
+int lanes_for(int64_t n) {
+  int L = 1;
+  while (L * kVec < n) L *= 2;
+  return L;
+}
+// (D up to 512: rows are groups of a workgroup's lanes, else of 65536 x 512 the backward takes 110 us, of 524288 x 64 654)
+bool grouped(int64_t D) { return D <= kWave * kVec; }
+// a row's threads else: whole waves of eight columns a thread, or twice eight past 8192
 int row_threads(int64_t D) {
-  int t = kWave;
-  while (t < 1024 && t * kVec < D) t *= 2;
-  return t;
+  const int64_t each = D > 1024 * kVec ? 2 * kVec : kVec;
+  return static_cast<int>((D + each * kWave - 1) / (each * kWave) * kWave);
 }
 
-template <typename TI, typename TS, int CH, RowKind KIND>
+template <typename TI, typename TS, int CH, bool GROUP, RowKind KIND>
 hipError_t rnorm_fwd_ch(const RnormArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20))), block(row_threads(a.D));
-  if (a.post_norm) hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, true, KIND>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, false, KIND>), grid, block, 0, s, a);
+  const int L = GROUP ? lanes_for(a.D) : 0, rows = GROUP ? kGroupThreads / L : 1;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((a.rows + rows - 1) / rows, 1 << 20))), block(GROUP ? kGroupThreads : row_threads(a.D));
+  if (a.post_norm) hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, true, GROUP, KIND>), grid, block, 0, s, a, L);
+  else hipLaunchKernelGGL((rnorm_fwd<TI, TS, CH, false, GROUP, KIND>), grid, block, 0, s, a, L);
   return hipGetLastError();
 }
 template <typename TI, typename TS, RowKind KIND>
 hipError_t rnorm_fwd_at(const RnormArgs& a, hipStream_t s) {
   if constexpr (KIND != kFewer) {
-    if (a.D > 1024 * kVec) return rnorm_fwd_ch<TI, TS, 2, KIND>(a, s);
+    if (a.D > 1024 * kVec) return rnorm_fwd_ch<TI, TS, 2, false, KIND>(a, s);
+    if (!grouped(a.D)) return rnorm_fwd_ch<TI, TS, 1, false, KIND>(a, s);
   }
-  return rnorm_fwd_ch<TI, TS, 1, KIND>(a, s);
+  return rnorm_fwd_ch<TI, TS, 1, true, KIND>(a, s);
 }
 template <typename TI, typename TS>
 hipError_t rnorm_fwd_of(const RnormArgs& a, hipStream_t s) {
@@ -409,23 +522,26 @@ hipError_t rnorm_fwd_of(const RnormArgs& a, hipStream_t s) {
                                                                               : rnorm_fwd_at<TI, TS, kFewer>(a, s);
 }
 
-template <typename TI, typename TS, int CH, bool AHEAD, RowKind KIND>
+template <typename TI, typename TS, int CH, bool GROUP, int THREADS, RowKind KIND>
 hipError_t rnorm_bwd_ch(const RnormArgs& a, hipStream_t s) {
-  const dim3 grid(static_cast<unsigned>(rnorm_parts(a.rows, a.D))), block(row_threads(a.D));
+  const int L = GROUP ? lanes_for(a.D) : 0;
+  const dim3 grid(static_cast<unsigned>(rnorm_parts(a.rows, a.D))), block(GROUP ? kGroupThreads : row_threads(a.D));
   const bool scale = a.scale || a.dscale;
-  if (a.post_norm && scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, true, AHEAD, KIND>), grid, block, 0, s, a);
-  else if (a.post_norm) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, false, AHEAD, KIND>), grid, block, 0, s, a);
-  else if (scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, true, AHEAD, KIND>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, false, AHEAD, KIND>), grid, block, 0, s, a);
+  if (a.post_norm && scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, true, GROUP, THREADS, KIND>), grid, block, 0, s, a, L);
+  else if (a.post_norm) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, true, false, GROUP, THREADS, KIND>), grid, block, 0, s, a, L);
+  else if (scale) hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, true, GROUP, THREADS, KIND>), grid, block, 0, s, a, L);
+  else hipLaunchKernelGGL((rnorm_bwd<TI, TS, CH, false, false, GROUP, THREADS, KIND>), grid, block, 0, s, a, L);
   return hipGetLastError();
 }
 template <typename TI, typename TS, RowKind KIND>
 hipError_t rnorm_bwd_at(const RnormArgs& a, hipStream_t s) {
   if constexpr (KIND != kFewer) {
-    if (row_threads(a.D) > kAheadThreads)
-      return a.D > 1024 * kVec ? rnorm_bwd_ch<TI, TS, 2, false, KIND>(a, s) : rnorm_bwd_ch<TI, TS, 1, false, KIND>(a, s);
+    if (a.D > 1024 * kVec) return rnorm_bwd_ch<TI, TS, 2, false, 1024, KIND>(a, s);
+    if (a.D > 512 * kVec) return rnorm_bwd_ch<TI, TS, 1, false, 1024, KIND>(a, s);
+    if (a.D > 256 * kVec) return rnorm_bwd_ch<TI, TS, 1, false, 512, KIND>(a, s);
+    if (!grouped(a.D)) return rnorm_bwd_ch<TI, TS, 1, false, 256, KIND>(a, s);
   }
-  return rnorm_bwd_ch<TI, TS, 1, true, KIND>(a, s);
+  return rnorm_bwd_ch<TI, TS, 1, true, 256, KIND>(a, s);
 }
 template <typename TI, typename TS>
 hipError_t rnorm_bwd_of(const RnormArgs& a, hipStream_t s) {
@@ -461,11 +577,6 @@ __device__ __forceinline__ void gate(float z, float& act, float& slope) {
 // A group of L lanes (a power of two, eight channels a lane) takes a head's row, a workgroup
 // one head of kThreads / L tokens at a time.
 constexpr int kThreads = 256;
-int head_lanes(int d) {
-  int L = 1;
-  while (L * kVec < d) L *= 2;
-  return L;
-}
 template <typename T, int ACT, RowKind KIND>
 __global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L) {
   const Cols<KIND> o((threadIdx.x & (L - 1)) * kVec, a.d);
@@ -507,11 +618,16 @@ __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L) {
   const T* const pdy = static_cast<const T*>(a.dy) + head * a.d;
   float w[kVec], dw[kVec] = {};
   ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, o, w);
+  Raw<T> next[3];   // the next token's
+  auto load = [&](int64_t t) {
+    next[0].load(px + t * a.sx, o);
+    next[1].load(pdy + t * a.sdy, o);
+    if constexpr (ACT != kActNone) next[2].load(pz + t * a.sz, o);
+  };
+  if (first * groups + group < a.M) load(first * groups + group);
   for (int64_t t = first * groups + group; t < a.M; t += each * groups) {
-    Raw<T> x, z, dy;
-    x.load(px + t * a.sx, o);
-    dy.load(pdy + t * a.sdy, o);
-    if constexpr (ACT != kActNone) z.load(pz + t * a.sz, o);
+    Raw<T> x = next[0], dy = next[1], z = next[2];
+    load(min(t + each * groups, a.M - 1));   // (behind the last: not used)
     x.settle(o);
     dy.settle(o);
     if constexpr (ACT != kActNone) z.settle(o);
@@ -535,25 +651,12 @@ __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L) {
     store(static_cast<T*>(a.dx) + t * a.sdx + head * a.d, o, v);
     if constexpr (ACT != kActNone) store(static_cast<T*>(a.dz) + t * a.sdz + head * a.d, o, slope);
   }
-  if (!a.dweight) return;
-  // the groups' sums: over a wave's by shuffles, then over the waves (a window's columns that are
-  // another lane's are zero, and that lane's place is further down)
-#pragma unroll
-  for (int i = 0; i < kVec; ++i)
-    for (int off = L; off < kWave; off <<= 1) dw[i] += __shfl_xor(dw[i], off, 64);
-  const int wave = threadIdx.x / kWave, l = threadIdx.x & 63;
-  if (l < L)
-#pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      if (o.keep >> i & 1) sum[wave][o.at + i] = dw[i];
-  __syncthreads();
-  for (int j = threadIdx.x; j < a.d; j += kThreads)
-    a.part[blockIdx.x * static_cast<int64_t>(a.d) + j] = (sum[0][j] + sum[1][j]) + (sum[2][j] + sum[3][j]);
+  if (a.dweight) group_part(dw, o, L, sum, a.part + blockIdx.x * static_cast<int64_t>(a.d));
 }
 
 template <typename T, RowKind KIND>
 hipError_t hnorm_fwd_at(const HnormArgs& a, hipStream_t s) {
-  const int L = head_lanes(a.d), groups = kThreads / L;
+  const int L = lanes_for(a.d), groups = kThreads / L;
   const int64_t each = std::max<int64_t>(std::min<int64_t>((a.M + groups - 1) / groups, (1 << 20) / a.H), 1);
   const dim3 grid(static_cast<unsigned>(each * a.H)), block(kThreads);
   if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_fwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
@@ -563,7 +666,7 @@ hipError_t hnorm_fwd_at(const HnormArgs& a, hipStream_t s) {
 }
 template <typename T, RowKind KIND>
 hipError_t hnorm_bwd_at(const HnormArgs& a, hipStream_t s) {
-  const int L = head_lanes(a.d);
+  const int L = lanes_for(a.d);
   const dim3 grid(static_cast<unsigned>(hnorm_parts(a.M, a.H, a.d))), block(kThreads);
   if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_bwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
   else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_bwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L);
@@ -584,13 +687,18 @@ hipError_t hnorm_bwd_of(const HnormArgs& a, hipStream_t s) {
 
 // at most so many parts, of as nearly the same number of rows as can be
 int64_t balanced_parts(int64_t rows, int64_t most) {
-  const int64_t each = (rows + most - 1) / most;
-  return each > 0 ? (rows + each - 1) / each : 0;
+  const int64_t each = std::max<int64_t>((rows + most - 1) / most, rows > 512 ? 2 : 1);   // (1048 rows of 1000, everything on: 18.6 us with one each, 14.7)
+  return (rows + each - 1) / each;
 }
 
 }  // namespace
 
-int64_t rnorm_parts(int64_t rows, int64_t) { return balanced_parts(rows, 768); }
+int64_t rnorm_parts(int64_t rows, int64_t D) {
+  const int64_t at_once = grouped(D) ? kGroupThreads / lanes_for(D) : 1;
+  // the workgroups that 256 compute units hold by their registers: 12 waves each up to 256 threads, else 16
+  const int threads = grouped(D) ? kGroupThreads : row_threads(D), waves = threads > 256 ? 16 : 4 * kBackWaves;
+  return balanced_parts((rows + at_once - 1) / at_once, 256 * (waves / (threads / kWave)));
+}
 
 hipError_t launch_rnorm_fwd(const RnormArgs& a, int io_bf16, int stream_bf16, hipStream_t s) {
   if (io_bf16) return stream_bf16 ? rnorm_fwd_of<bf16, bf16>(a, s) : rnorm_fwd_of<bf16, float>(a, s);
@@ -619,7 +727,7 @@ hipError_t launch_rnorm_bwd(const RnormArgs& a, int io_bf16, int stream_bf16, hi
 // a head's tokens in at most so many parts that all heads' are 2048 (H where there are more heads)
 int64_t hnorm_parts(int64_t M, int64_t H, int d) {
   if (M == 0 || H == 0) return 0;
-  const int groups = kThreads / head_lanes(d);
+  const int groups = kThreads / lanes_for(d);
   return H * std::max<int64_t>(std::min<int64_t>((M + groups - 1) / groups, 1024 / H), 1);
 }
 

@@ -37,7 +37,8 @@ pdn_status check_hnorm(const pdn_hnorm* p, int64_t* n) {
   if (p->norm != PDN_NORM_RMS && p->norm != PDN_NORM_L2) return PDN_ERR_VALUE;
   if (p->act != PDN_ACT_NONE && p->act != PDN_ACT_SILU && p->act != PDN_ACT_SIGMOID) return PDN_ERR_VALUE;
   if (!std::isfinite(p->eps) || !(p->eps > 0.f)) return PDN_ERR_VALUE;
-  if (p->H >= (int64_t)1 << 24) return PDN_ERR_SHAPE;   // (a workgroup a head at least)
+  // a workgroup a head at least, and of a weight's gradient one for every 32 of its elements
+  if (p->H >= (int64_t)1 << 24 || p->H * p->d > (int64_t)1 << 26) return PDN_ERR_SHAPE;
   if (!mul_ok(p->tokens, p->H * p->d, n) || *n > kMost) return PDN_ERR_SHAPE;
   return PDN_OK;
 }

@@ -498,7 +498,8 @@ hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
 template <typename T, typename TO>
 hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
   const dim3 rows(static_cast<unsigned>(a.rows));
-  if (a.probs && a.V <= (a.rows < 96 ? 16384 : 57344)) {
+  const bool fits = a.V <= 2048 || a.rows < 1 << 22;   // (a launch holds fewer than 2^32 work items)
+  if (a.probs && fits && a.V <= (a.rows < 96 ? 16384 : 57344)) {
     if (a.V < kVec) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, true>), rows, dim3(256), 0, s, a);
     else if (a.V <= 2048) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, false>), rows, dim3(256), 0, s, a);
     else if (a.V <= 8192) hipLaunchKernelGGL((logits_one<T, TO, 1024, 1, false>), rows, dim3(1024), 0, s, a);

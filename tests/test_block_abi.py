@@ -75,7 +75,7 @@ def test_rnorm_refusals():
 
 
 def test_hnorm_refusals():
-    bad = [(hnorm(tokens=-1), SHAPE), (hnorm(H=-1), SHAPE), (hnorm(d=0), SHAPE), (hnorm(d=513), UNSUP), (hnorm(H=1 << 24), SHAPE),
+    bad = [(hnorm(tokens=-1), SHAPE), (hnorm(H=-1), SHAPE), (hnorm(d=0), SHAPE), (hnorm(d=513), UNSUP), (hnorm(H=1 << 24), SHAPE), (hnorm(H=1 << 21), SHAPE),
            (hnorm(tokens=1 << 45), SHAPE), (hnorm(io=5), DTYPE), (hnorm(norm=2), VALUE), (hnorm(act=3), VALUE), (hnorm(eps=-1.0), VALUE)]
     for p, status in bad:
         assert call_hnorm(p=p) == call_hnorm_bwd(p=p) == status
