@@ -294,3 +294,46 @@ def test_same_bits_streams_and_graphs():
             torch.cuda.synchronize()
             for p, q, e in zip(first, got, eager):
                 assert torch.equal(p, q) and torch.equal(p, e)
+
+
+@pytest.mark.parametrize("rows,D", [(5000, 24), (3300, 300), (1700, 520), (900, 1400), (530, 2056), (520, 3001), (300, 5000), (270, 9000)])
+@pytest.mark.parametrize("io,st", [("bf16", "f32"), ("f32", "f32")])
+def test_backward_over_more_rows_than_parts(rows, D, io, st):
+    """Each width's form with several rows a part: every vector's gradient."""
+    import paper_2604_21100_amd as pdn
+    rng = np.random.default_rng(rows)
+    d, kw = rnorm_inputs(rng, rows, D, io, st, "weight", True, True, True)
+    h, du, dh = d.pop("residual"), seen(rng.standard_normal((rows, D)), io), seen(rng.standard_normal((rows, D)), st)
+    want = bu.rnorm_bwd(du, dh, h, d["y"], d["weight"], True, d["post_weight"], d["scale"], kw["alpha"], kw["eps"])
+    got = pdn.pdn_residual_norm_bwd(put(du, io), put(h, st), put(d["y"], io), dh=put(dh, st), post_norm=True, alpha=kw["alpha"], eps=EPS,
+                                    **{n: put(d[n], "f32") for n in ("weight", "post_weight", "scale")})
+    for n in want:
+        close(got[n], *want[n], {"dy": io, "dresidual": st}.get(n, "f32"), TWO, n)
+
+
+def test_offsets_past_32_bits():
+    """The last rows of tensors of more than 2^31 elements: the bits of a small call."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    g = torch.Generator(device="cuda").manual_seed(7)
+    R, D, H, n = 1_060_000, 2048, 16, 3
+    r = lambda *s: torch.randn(s, generator=g, device="cuda")   # noqa: E731
+    w = r(D)
+    y, x, du = (torch.zeros(R, D, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    for t in (y, x, du):
+        t[-n:] = r(n, D)
+    kw = dict(weight=w, post_norm=True, scale=w)
+    u, h = pdn.pdn_residual_norm(y, x, **kw)
+    us, hs = pdn.pdn_residual_norm(y[-n:], x[-n:], **kw)
+    assert torch.equal(u[-n:], us) and torch.equal(h[-n:], hs) and not u[:-n].any() and not h[:-n].any()
+    a, b = pdn.pdn_residual_norm_bwd(du, h, y, **kw), pdn.pdn_residual_norm_bwd(du[-n:], hs, y[-n:], **kw)
+    for m in ("dy", "dresidual"):
+        assert torch.equal(a[m][-n:], b[m]) and not a[m][:-n].any()
+    heads = lambda t: t.view(-1, H, D // H)   # noqa: E731
+    del a
+    o, os = pdn.pdn_head_norm(heads(x), z=heads(y)), pdn.pdn_head_norm(heads(x[-n:]), z=heads(y[-n:]))
+    assert torch.equal(o[-n:], os) and not o[:-n].any()
+    del o
+    a, b = pdn.pdn_head_norm_bwd(heads(du), heads(x), z=heads(y)), pdn.pdn_head_norm_bwd(heads(du[-n:]), heads(x[-n:]), z=heads(y[-n:]))
+    for m in a:
+        assert torch.equal(a[m][-n:], b[m]) and not a[m][:-n].any()

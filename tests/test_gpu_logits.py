@@ -234,6 +234,51 @@ def test_verification_reads_it():
     assert acc.tolist() == [1, 1] and tok[0] == -1 and tok[1] >= 0
 
 
+@pytest.mark.parametrize("rows,V", [(95, 16385), (96, 16384), (96, 16385), (97, 32769), (96, 57344), (96, 57345), (3, 16384), (3, 16385),
+                                    (5, 2048), (5, 2049), (5, 8192), (5, 8193), (4, 32768), (300, 70000)])
+def test_where_the_forms_meet(rows, V):
+    """One launch or two go by rows and tokens: every token's probability against 64 bits, a greedy row among them."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    g = torch.Generator(device="cuda").manual_seed(V)
+    l = 2 * torch.randn(rows, V, generator=g, device="cuda")
+    l[rows // 2, 5:9] = 50.0
+    T = torch.linspace(0.5, 1.5, rows, device="cuda")
+    T[rows // 2] = 0.0
+    p = pdn.pdn_logits(l, temperature=T)
+    assert p[rows // 2].nonzero().tolist() == [[5]] and p[rows // 2, 5] == 1.0
+    live = torch.arange(rows, device="cuda") != rows // 2
+    arg = (l.double() - l.double().amax(1, keepdim=True)) / T.double()[:, None]
+    e = torch.exp(arg)
+    want = e / e.sum(1, keepdim=True)
+    bound = U * (64 - 4 * arg + (e * -4 * arg).sum(1, keepdim=True) / e.sum(1, keepdim=True)) * want + 2e-38
+    assert ((p.double() - want).abs() <= bound)[live].all()
+
+
+def test_offsets_past_32_bits():
+    """The last rows of tensors of more than 2^31 elements, and of such a table: the bits of a small call."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    R, V, n = 17000, 131072, 2
+    g = torch.Generator(device="cuda").manual_seed(3)
+    l = torch.zeros(R, V, dtype=torch.bfloat16, device="cuda")
+    l[-n:] = torch.randn(n, V, generator=g, device="cuda")
+    table = torch.zeros(R, V, dtype=torch.int32, device="cuda")
+    pdn.pdn_token_counts(i32([3, V - 1, 3]), table, starts=i32([0, 3]), slots=i32([R - 1]))
+    assert table[R - 1].nonzero()[:, 0].tolist() == [3, V - 1] and table[R - 1, 3] == 2 and not table[:R - 1].any()
+    pdn.pdn_token_counts(i32([7]), table, starts=i32([0, 1]), slots=i32([R - 1]), slots_out=i32([R - 2]), prompt=True)
+    assert table[R - 2].nonzero()[:, 0].tolist() == [3, 7, V - 1] and not table[:R - 2].any()
+    kw = dict(repetition=f32([1.5] * R), frequency=f32([0.3] * R), dtype=torch.bfloat16)
+    big = pdn.pdn_logits(l, counts=table, **kw)
+    kw = dict(repetition=f32([1.5] * n), frequency=f32([0.3] * n), dtype=torch.bfloat16)
+    small = pdn.pdn_logits(l[-n:], counts=table, slots=i32([R - 2, R - 1]), **kw)
+    # (sums of as many segments, but not of the same: the same to a step of bf16)
+    assert ((big[-n:].float() - small.float()).abs() <= 2 ** -7 * small.float()).all()
+    assert (big[0].float() - 1 / V).abs().max() <= 2 ** -8 / V
+    assert torch.equal(pdn.pdn_logits(l, counts=table, probs=False, repetition=f32([1.5] * R))[-n:],
+                       pdn.pdn_logits(l[-n:], counts=table, slots=i32([R - 2, R - 1]), probs=False, repetition=f32([1.5] * n)))
+
+
 # ---------------------------------------------------------------- counts
 def ref_counts(table, ids, starts, slots, slots_out, fresh, accepted, prompt):
     new = table.copy()
