@@ -574,22 +574,54 @@ __device__ __forceinline__ void gate(float z, float& act, float& slope) {
   }
 }
 
-// A group of L lanes (a power of two, eight channels a lane) takes a head's row, a workgroup
-// one head of kThreads / L tokens at a time.
+// A group of L lanes (a power of two, eight channels a lane) takes a head's row.  Neighbouring groups take
+// neighbouring heads, so that a workgroup reads whole tokens; with a weight for each head a workgroup stays
+// with one, whose gradient it can sum.
 constexpr int kThreads = 256;
+struct Walk {   // a group's step: so many tokens and heads on
+  int64_t tokens;
+  int32_t heads;
+};
+Walk walk_of(const HnormArgs& a, int64_t blocks) {
+  if (a.head_weight) return Walk{blocks / a.H * (kThreads / lanes_for(a.d)), 0};
+  const int64_t rows = blocks * (kThreads / lanes_for(a.d));
+  return Walk{rows / a.H, static_cast<int32_t>(rows % a.H)};
+}
+struct HeadRow {
+  int64_t t;
+  int32_t head;
+  __device__ __forceinline__ HeadRow(const HnormArgs& a, int L) {
+    const uint32_t group = threadIdx.x / L, groups = kThreads / L, H = static_cast<uint32_t>(a.H);
+    if (a.head_weight) {
+      t = static_cast<int64_t>(blockIdx.x / H) * groups + group;
+      head = blockIdx.x % H;
+    } else {   // (fewer than 2^32 work items, so fewer rows at first)
+      const uint32_t row = blockIdx.x * groups + group;
+      t = row / H;
+      head = row % H;
+    }
+  }
+  __device__ __forceinline__ void next(const HnormArgs& a, const Walk& by) {
+    t += by.tokens;
+    head += by.heads;
+    if (head >= a.H) {
+      head -= static_cast<int32_t>(a.H);
+      ++t;
+    }
+  }
+};
+
 template <typename T, int ACT, RowKind KIND>
-__global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L) {
+__global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L, Walk by) {
   const Cols<KIND> o((threadIdx.x & (L - 1)) * kVec, a.d);
-  const int group = threadIdx.x / L, groups = kThreads / L;
-  const int64_t head = blockIdx.x % a.H, first = blockIdx.x / a.H, each = gridDim.x / a.H;
-  const T* const px = static_cast<const T*>(a.x) + head * a.d;
-  const T* const pz = static_cast<const T*>(a.z) + head * a.d;
+  HeadRow at(a, L);
   float w[kVec];
-  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, o, w);
-  for (int64_t t = first * groups + group; t < a.M; t += each * groups) {
+  ld_weight(a.weight ? a.weight + (a.head_weight ? at.head * a.d : 0) : nullptr, o, w);
+  for (; at.t < a.M; at.next(a, by)) {
     Raw<T> x, z;
-    x.load(px + t * a.sx, o);
-    if constexpr (ACT != kActNone) z.load(pz + t * a.sz, o);
+    const int64_t h = static_cast<int64_t>(at.head) * a.d;
+    x.load(static_cast<const T*>(a.x) + at.t * a.sx + h, o);
+    if constexpr (ACT != kActNone) z.load(static_cast<const T*>(a.z) + at.t * a.sz + h, o);
     x.settle(o);
     float v[kVec], q = 0.f;
 #pragma unroll
@@ -602,32 +634,31 @@ __global__ __launch_bounds__(kThreads) void hnorm_fwd(HnormArgs a, int L) {
       v[i] = x[i] * r * w[i];
       if constexpr (ACT != kActNone) v[i] *= act;
     }
-    store(static_cast<T*>(a.y) + t * a.sy + head * a.d, o, v);
+    store(static_cast<T*>(a.y) + at.t * a.sy + h, o, v);
   }
 }
 
 template <typename T, int ACT, RowKind KIND>
-__global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L) {
+__global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L, Walk by) {
   __shared__ float sum[kThreads / kWave][kWave * kVec];
-  const int col = (threadIdx.x & (L - 1)) * kVec, group = threadIdx.x / L, groups = kThreads / L;
-  const Cols<KIND> o(col, a.d);
-  const int64_t head = blockIdx.x % a.H, first = blockIdx.x / a.H, each = gridDim.x / a.H;
+  const Cols<KIND> o((threadIdx.x & (L - 1)) * kVec, a.d);
   const float c = a.l2 ? 1.f : 1.f / a.d;
-  const T* const px = static_cast<const T*>(a.x) + head * a.d;
-  const T* const pz = static_cast<const T*>(a.z) + head * a.d;
-  const T* const pdy = static_cast<const T*>(a.dy) + head * a.d;
+  HeadRow at(a, L);
   float w[kVec], dw[kVec] = {};
-  ld_weight(a.weight ? a.weight + (a.head_weight ? head * a.d : 0) : nullptr, o, w);
-  Raw<T> next[3];   // the next token's
-  auto load = [&](int64_t t) {
-    next[0].load(px + t * a.sx, o);
-    next[1].load(pdy + t * a.sdy, o);
-    if constexpr (ACT != kActNone) next[2].load(pz + t * a.sz, o);
+  ld_weight(a.weight ? a.weight + (a.head_weight ? at.head * a.d : 0) : nullptr, o, w);
+  Raw<T> next[3];   // the next row's
+  auto load = [&](const HeadRow& r) {
+    const int64_t t = min(r.t, a.M - 1), h = static_cast<int64_t>(r.head) * a.d;   // (behind the last: not used)
+    next[0].load(static_cast<const T*>(a.x) + t * a.sx + h, o);
+    next[1].load(static_cast<const T*>(a.dy) + t * a.sdy + h, o);
+    if constexpr (ACT != kActNone) next[2].load(static_cast<const T*>(a.z) + t * a.sz + h, o);
   };
-  if (first * groups + group < a.M) load(first * groups + group);
-  for (int64_t t = first * groups + group; t < a.M; t += each * groups) {
+  load(at);
+  while (at.t < a.M) {
+    const int64_t t = at.t, h = static_cast<int64_t>(at.head) * a.d;
     Raw<T> x = next[0], dy = next[1], z = next[2];
-    load(min(t + each * groups, a.M - 1));   // (behind the last: not used)
+    at.next(a, by);
+    load(at);
     x.settle(o);
     dy.settle(o);
     if constexpr (ACT != kActNone) z.settle(o);
@@ -648,29 +679,38 @@ __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L) {
       dw[i] += g[i] * (x[i] * r);
       v[i] = r * (g[i] * w[i]) - x[i] * m;
     }
-    store(static_cast<T*>(a.dx) + t * a.sdx + head * a.d, o, v);
-    if constexpr (ACT != kActNone) store(static_cast<T*>(a.dz) + t * a.sdz + head * a.d, o, slope);
+    store(static_cast<T*>(a.dx) + t * a.sdx + h, o, v);
+    if constexpr (ACT != kActNone) store(static_cast<T*>(a.dz) + t * a.sdz + h, o, slope);
   }
   if (a.dweight) group_part(dw, o, L, sum, a.part + blockIdx.x * static_cast<int64_t>(a.d));
 }
 
+// workgroups: at most so many, with a weight for each head as many for each
+int64_t hnorm_blocks(const HnormArgs& a, int64_t most) {
+  const int groups = kThreads / lanes_for(a.d);
+  if (a.head_weight) return a.H * std::max<int64_t>(std::min<int64_t>((a.M + groups - 1) / groups, most / a.H), 1);
+  return std::min<int64_t>((a.M * a.H + groups - 1) / groups, most);
+}
 template <typename T, RowKind KIND>
 hipError_t hnorm_fwd_at(const HnormArgs& a, hipStream_t s) {
-  const int L = lanes_for(a.d), groups = kThreads / L;
-  const int64_t each = std::max<int64_t>(std::min<int64_t>((a.M + groups - 1) / groups, (1 << 20) / a.H), 1);
-  const dim3 grid(static_cast<unsigned>(each * a.H)), block(kThreads);
-  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_fwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
-  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_fwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L);
-  else hipLaunchKernelGGL((hnorm_fwd<T, kActNone, KIND>), grid, block, 0, s, a, L);
+  const int L = lanes_for(a.d);
+  const int64_t blocks = hnorm_blocks(a, 1 << 20);
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
+  const Walk by = walk_of(a, blocks);
+  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_fwd<T, kActSilu, KIND>), grid, block, 0, s, a, L, by);
+  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_fwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L, by);
+  else hipLaunchKernelGGL((hnorm_fwd<T, kActNone, KIND>), grid, block, 0, s, a, L, by);
   return hipGetLastError();
 }
 template <typename T, RowKind KIND>
 hipError_t hnorm_bwd_at(const HnormArgs& a, hipStream_t s) {
   const int L = lanes_for(a.d);
-  const dim3 grid(static_cast<unsigned>(hnorm_parts(a.M, a.H, a.d))), block(kThreads);
-  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_bwd<T, kActSilu, KIND>), grid, block, 0, s, a, L);
-  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_bwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L);
-  else hipLaunchKernelGGL((hnorm_bwd<T, kActNone, KIND>), grid, block, 0, s, a, L);
+  const int64_t blocks = hnorm_parts(a);
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kThreads);
+  const Walk by = walk_of(a, blocks);
+  if (a.act == kActSilu) hipLaunchKernelGGL((hnorm_bwd<T, kActSilu, KIND>), grid, block, 0, s, a, L, by);
+  else if (a.act == kActSigmoid) hipLaunchKernelGGL((hnorm_bwd<T, kActSigmoid, KIND>), grid, block, 0, s, a, L, by);
+  else hipLaunchKernelGGL((hnorm_bwd<T, kActNone, KIND>), grid, block, 0, s, a, L, by);
   return hipGetLastError();
 }
 
@@ -724,18 +764,13 @@ hipError_t launch_rnorm_bwd(const RnormArgs& a, int io_bf16, int stream_bf16, hi
   return launch_sums(sums, n, s);
 }
 
-// a head's tokens in at most so many parts that all heads' are 2048 (H where there are more heads)
-int64_t hnorm_parts(int64_t M, int64_t H, int d) {
-  if (M == 0 || H == 0) return 0;
-  const int groups = kThreads / lanes_for(d);
-  return H * std::max<int64_t>(std::min<int64_t>((M + groups - 1) / groups, 1024 / H), 1);
-}
+int64_t hnorm_parts(const HnormArgs& a) { return a.M == 0 || a.H == 0 ? 0 : hnorm_blocks(a, 1024); }
 
 hipError_t launch_hnorm_fwd(const HnormArgs& a, int io_bf16, hipStream_t s) {
   return io_bf16 ? hnorm_fwd_of<bf16>(a, s) : hnorm_fwd_of<float>(a, s);
 }
 hipError_t launch_hnorm_bwd(const HnormArgs& a, int io_bf16, hipStream_t s) {
-  const int64_t parts = hnorm_parts(a.M, a.H, a.d);
+  const int64_t parts = hnorm_parts(a);
   if (parts > 0) {
     const hipError_t e = io_bf16 ? hnorm_bwd_of<bf16>(a, s) : hnorm_bwd_of<float>(a, s);
     if (e != hipSuccess) return e;

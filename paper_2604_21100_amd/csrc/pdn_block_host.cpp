@@ -197,7 +197,7 @@ pdn_status pdn_head_norm_bwd_workspace_size(const pdn_hnorm* p, size_t* bytes) {
   if (!bytes) return PDN_ERR_NULL;
   int64_t n;
   const pdn_status st = check_hnorm(p, &n);
-  if (st == PDN_OK) *bytes = static_cast<size_t>(hnorm_parts(p->tokens, p->H, p->d) * p->d * 4);
+  if (st == PDN_OK) *bytes = static_cast<size_t>(hnorm_parts(hnorm_args(p)) * p->d * 4);
   return st;
 }
 
@@ -220,7 +220,7 @@ pdn_status pdn_head_norm_bwd(const pdn_hnorm* p, const void* dy, const void* x, 
       !rows_of(dz, p->tokens, row, p->dz_stride, io, &rdz))
     return PDN_ERR_SHAPE;
   if (same_rows(rdy, rdx)) rdy.p = nullptr;   // in place
-  const int64_t needs = dweight ? hnorm_parts(p->tokens, p->H, p->d) * p->d * 4 : 0;
+  const int64_t needs = dweight ? hnorm_parts(hnorm_args(p)) * p->d * 4 : 0;
   const std::array<Rows, 4> ins = {rdy, rx, rz, flat(weight, v)};
   const std::array<Rows, 3> outs = {rdx, rdz, flat(dweight, v)};
   if ((st = check_rows(ins, outs, flat(needs > 0 ? ws : nullptr, static_cast<int64_t>(ws_bytes)))) != PDN_OK) return st;

@@ -348,9 +348,9 @@ struct HnormArgs {
   void* dx;
   void* dz;
   float* dweight;
-  float* part;            // [hnorm_parts / H][H][d] sums of some tokens each
+  float* part;            // [hnorm_parts][d] sums of some rows each; with head_weight [hnorm_parts / H][H][d]
 };
-int64_t hnorm_parts(int64_t M, int64_t H, int d);
+int64_t hnorm_parts(const HnormArgs& a);
 hipError_t launch_hnorm_fwd(const HnormArgs& a, int io_bf16, hipStream_t s);
 hipError_t launch_hnorm_bwd(const HnormArgs& a, int io_bf16, hipStream_t s);
 constexpr int kHnormMaxD = 512;
