@@ -1,6 +1,8 @@
 // Norms around the rule in a block.  Rows are independent; what bounds every call is
 // the reading and writing of its tensors, so each kernel holds a row in registers, reads every
-// tensor once and writes every output once.
+// tensor once and writes every output once.  bf16, of 5.15 TB/s that a copy has: the residual norm of 16384 x 2048
+// rows on an fp32 stream 72 us (5.6 TB/s), its backward with both norms and a scale 81 and 5 for the sums
+// (4.7); norms of 16384 x 16 heads of 128 24 us (5.7), the gated one's backward 69 and 4 (4.6).
 //
 // Residual norm, rows of D channels (r: 1 / sqrt(mean of squares + eps)):
 //   a = y or y r_y w_post     h = residual + alpha s a      u = h r_h w
@@ -26,7 +28,7 @@ namespace {
 constexpr int kVec = 8;
 
 // The eight columns of a thread: from `col` on in a row of n.  Loads must not branch (a wait for
-// each would follow it), so every thread loads eight columns of the row that are there,
+// each would follow it: the backward of 16384 x 2048 rows 104 us, without branches 81), so every thread loads eight columns of the row that are there,
 // and `keep` says which of them are its own: a last thread with fewer than eight takes the row's
 // last eight, one without any the first.  By the row: a multiple of eight columns, more than
 // eight, or fewer (its only thread then loads element by element).
@@ -575,8 +577,9 @@ __device__ __forceinline__ void gate(float z, float& act, float& slope) {
 }
 
 // A group of L lanes (a power of two, eight channels a lane) takes a head's row.  Neighbouring groups take
-// neighbouring heads, so that a workgroup reads whole tokens; with a weight for each head a workgroup stays
-// with one, whose gradient it can sum.
+// neighbouring heads, so that a workgroup reads whole tokens (one head a workgroup: 16 heads of 8, 33, 64 and 128
+// channels, gated backward, 305, 170, 82, 73 us; so 72, 115, 69, 70); with a weight for each head a workgroup
+// stays with one, whose gradient it can sum.
 constexpr int kThreads = 256;
 struct Walk {   // a group's step: so many tokens and heads on
   int64_t tokens;
@@ -736,6 +739,7 @@ int64_t balanced_parts(int64_t rows, int64_t most) {
 int64_t rnorm_parts(int64_t rows, int64_t D) {
   const int64_t at_once = grouped(D) ? kGroupThreads / lanes_for(D) : 1;
   // the workgroups that 256 compute units hold by their registers: 12 waves each up to 256 threads, else 16
+  // (16384 x 2048 rows, everything on: 512 parts 93 us, 768 81, 1024 100)
   const int threads = grouped(D) ? kGroupThreads : row_threads(D), waves = threads > 256 ? 16 : 4 * kBackWaves;
   return balanced_parts((rows + at_once - 1) / at_once, 256 * (waves / (threads / kWave)));
 }

@@ -1,6 +1,6 @@
 // Reductions over a wave's lanes on data-parallel primitives: they run at the rate of the
-// VALU, where a shuffle goes through LDS (a chain of six, twice a row, was what the residual
-// norm's backward waited for: 16384 x 2048 rows, 103 us with shuffles).
+// VALU, where a shuffle goes through LDS (the residual norm's backward, four sums a row: 16384 x 2048
+// rows in 113 us with shuffles, 104 with these).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -10,7 +10,9 @@
 // A row's counts come from the table (read along with the logits) and from the few tokens
 // of its own sequence's rows.
 //
-// What bounds it: reading the logits twice and writing p.
+// What bounds it: reading the logits twice and writing p, for 314 rows of 131072 fp32 logits with penalties and masks
+// 51 us (198 MB; 40 without them, a plain maximum over the rows takes 47) and 74 us (363 MB, 4.9 TB/s; a
+// copy of the logits 62); for a few rows latency, 4.4 and 4.3 us for one of 50257.
 #include <algorithm>
 #include <cmath>
 
@@ -355,7 +357,8 @@ __device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint3
   return all;
 }
 
-// The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves.
+// The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves. No loop:
+// a loop's loads would wait for the stores before them (84 us against 75).
 template <typename T, typename TO, bool TINY, bool PROBS>
 __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t windows, uint32_t segs) {
   const uint32_t row = blockIdx.x / windows, base = blockIdx.x % windows * kSeg + (threadIdx.x >> 6) * kWaveSpan;
@@ -467,7 +470,8 @@ __global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
 }
 
 // A row's segments in the first of two launches: about so many workgroups in all, eight to a row or a multiple of it,
-// as workgroups go to the eight L2s in turn: the rows of a sequence then find its counts in one.
+// as workgroups go to the eight L2s in turn: the rows of a sequence then find its counts in one. (314 rows of
+// 131072: 8 segments 54 us, 16 51.5, 32 55, 13 58.)
 constexpr int64_t kManyBlocks = 4096;
 template <typename T, typename TO, bool TINY>
 hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
@@ -539,7 +543,8 @@ __device__ __forceinline__ SeqOf seq_of(const CountArgs& a, int64_t seq) {
   return s;
 }
 
-// tokens added in place: a workgroup a sequence (whole-number atomics, so any order gives the same)
+// tokens added in place: a workgroup a sequence (whole-number atomics, so any order gives the same); 64 sequences of up to
+// eight tokens 2.4 us, a launch and two dependent reads.
 __global__ __launch_bounds__(kThreads) void counts_add(CountArgs a) {
   const SeqOf s = seq_of(a, blockIdx.x);
   if (s.from < 0) return;
@@ -552,7 +557,8 @@ __global__ __launch_bounds__(kThreads) void counts_add(CountArgs a) {
   }
 }
 
-// a whole row written: a workgroup a segment, its tokens counted in shared memory
+// a whole row written: a workgroup a segment, its tokens counted in shared memory; 16 prompts of up to
+// 2000 tokens into rows of 50257 5.2 us: a few rounds of reads of the prompt, which every segment makes.
 __global__ __launch_bounds__(kThreads) void counts_write(CountArgs a) {
   __shared__ int32_t had[kSeg];
   const int64_t segs = count_segments(a.V), seq = blockIdx.x / segs, j0 = blockIdx.x % segs * kSeg;
