@@ -337,3 +337,36 @@ def test_offsets_past_32_bits():
     a, b = pdn.pdn_head_norm_bwd(heads(du), heads(x), z=heads(y)), pdn.pdn_head_norm_bwd(heads(du[-n:]), heads(x[-n:]), z=heads(y[-n:]))
     for m in a:
         assert torch.equal(a[m][-n:], b[m]) and not a[m][:-n].any()
+
+
+@pytest.mark.parametrize("D", [5, 300, 1000, 1001, 4104, 9001])
+def test_in_place_at_every_width(D):
+    """h in residual's place and dresidual in dh's, in each form of a row: the bits of the calls that do not."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(D)
+    R = 700
+    y, x, du, dh = (torch.randn(R, D, device="cuda") for _ in range(4))
+    w = torch.randn(D, device="cuda")
+    kw = dict(weight=w, post_norm=True, post_weight=w, scale=w)
+    u, h = pdn.pdn_residual_norm(y, x, **kw)
+    a = pdn.pdn_residual_norm_bwd(du, h, y, dh=dh, **kw)
+    u1, h1 = pdn.pdn_residual_norm(y, x, h=x, **kw)
+    assert h1 is x and torch.equal(h, x) and torch.equal(u, u1)
+    b = pdn.pdn_residual_norm_bwd(du, h, y, dh=dh, outputs=dict(dresidual=dh), **kw)
+    assert b["dresidual"] is dh and all(torch.equal(a[n], b[n]) for n in a)
+
+
+@pytest.mark.parametrize("d", [5, 8, 33, 128, 200])
+@pytest.mark.parametrize("each", [False, True])
+def test_head_norm_in_place_at_every_width(d, each):
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(d)
+    M, H = 900, 6
+    x, z, dy = (torch.randn(M, H, d, device="cuda").bfloat16() for _ in range(3))
+    w = torch.randn(H, d, device="cuda") if each else torch.randn(d, device="cuda")
+    y, g = pdn.pdn_head_norm(x, weight=w, z=z), pdn.pdn_head_norm_bwd(dy, x, weight=w, z=z)
+    b = pdn.pdn_head_norm_bwd(dy, x, weight=w, z=z, outputs=dict(dx=dy))
+    assert b["dx"] is dy and all(torch.equal(g[n], b[n]) for n in g)
+    assert pdn.pdn_head_norm(x, weight=w, z=z, y=x) is x and torch.equal(x, y)

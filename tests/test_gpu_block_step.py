@@ -123,3 +123,65 @@ def test_decoding_token_by_token():
     assert rel_err(S2.double().cpu().numpy(), S1.double().cpu().numpy()) <= 1e-4
     a, _ = pdn.pdn_residual_norm(x, weight=w)
     assert torch.equal(a[4:5], pdn.pdn_residual_norm(x[4:5], weight=w)[0])
+
+
+def test_speculating_rounds_in_a_graph():
+    """A layer of a speculating server from the residual stream to the next token and the counts, captured once: rounds of
+    replays give the bits of eager rounds on copies of the same states, other eager calls between them."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(3)
+    N, K, H, d, V, P = 3, 4, 2, 64, 3001, 4
+    M, D, dev = N * K, H * d, "cuda"
+    r = lambda *s: torch.randn(s, device=dev)   # noqa: E731
+    i32 = lambda *a: torch.tensor(a, dtype=torch.int32, device=dev)   # noqa: E731
+    embed, Wi, Wo, head = r(V, D), r(D, 4 * D) / 11, r(D, D) / 11, r(D, V) / 4
+    w, wo, temperature, rep = 1 + 0.1 * r(D), 1 + 0.1 * r(d), torch.tensor([0.0, 0.7, 1.2], device=dev), torch.full((N,), 1.2, device=dev)
+    starts, slots = i32(0, K, 2 * K, 3 * K), i32(2, 0, 3)
+
+    class Server:
+        def __init__(self):
+            self.S, self.tape = torch.zeros(P, H, d, d, device=dev), torch.zeros(P, K, H, pdn.pdn_tape_record(d, d, "scalar", "identity"), device=dev)
+            self.pending, self.counts = torch.zeros(P, H, dtype=torch.int32, device=dev), torch.zeros(P, V, dtype=torch.int32, device=dev)
+            self.accepted, self.token = torch.zeros(N, dtype=torch.int32, device=dev), torch.zeros(N, dtype=torch.int32, device=dev)
+            self.ids, self.beta, self.g = torch.zeros(M, dtype=torch.int32, device=dev), torch.rand(M, H, device=dev), -torch.rand(M, H, device=dev)
+            self.u, self.r, self.p = torch.rand(M, device=dev), torch.rand(N, device=dev), torch.zeros(M, V, device=dev)
+
+        def step(self):
+            h = embed[self.ids.long()]
+            u, _ = pdn.pdn_residual_norm(h, weight=w, want_h=False)
+            q, k, v, z = (a.unflatten(-1, (H, d)) for a in (u @ Wi).split(D, -1))
+            pdn.pdn_head_norm(q, norm="l2", y=q)
+            pdn.pdn_head_norm(k, norm="l2", y=k)
+            o = pdn.pdn_slot_draft(q, k, v, self.beta, self.S, self.tape, self.pending, accepted=self.accepted, starts=starts, slots=slots,
+                                   max_tokens=K, g=self.g, gate="scalar", precond="identity")
+            y = pdn.pdn_head_norm(o, weight=wo, z=z, y=o).view(M, D) @ Wo
+            u, _ = pdn.pdn_residual_norm(y, h, weight=w, alpha=0.5, h=h)
+            pdn.pdn_logits(u @ head, temperature=temperature, repetition=rep, counts=self.counts, slots=slots, ids=self.ids, starts=starts, out=self.p)
+            pdn.pdn_draft_verify(self.p, self.ids, self.u, self.r, starts=starts, accepted=self.accepted, token=self.token)
+            pdn.pdn_token_counts(self.ids, self.counts, starts=starts, slots=slots, accepted=self.accepted)
+
+    a, b = Server(), Server()
+    for m in ("beta", "g"):
+        getattr(b, m).copy_(getattr(a, m))
+    warm = Server()
+    warm.step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.step()
+    for turn in range(5):
+        ids = torch.randint(0, 40, (M,), dtype=torch.int32, device=dev)
+        ids[::K] = a.token.clamp(min=0)
+        u, t = torch.rand(M, device=dev) * 0.1, torch.rand(N, device=dev)
+        for s in (a, b):
+            s.ids.copy_(ids)
+            s.u.copy_(u)
+            s.r.copy_(t)
+        a.step()
+        g.replay()
+        warm.step()
+        torch.cuda.synchronize()
+        for m in ("S", "tape", "pending", "counts", "accepted", "token", "p"):
+            assert torch.equal(getattr(a, m), getattr(b, m)), (turn, m)
+    assert a.counts.sum() >= 5 * N and (a.p.sum(1) - 1).abs().max() < 1e-5
