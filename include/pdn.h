@@ -520,7 +520,8 @@ pdn_status pdn_head_norm_bwd(const pdn_hnorm* problem, const void* dy, const voi
  * each.  Lists on the device are not checked: row numbers are clamped to [0, rows],
  * a sequence whose slot is outside [0, slots) is left out (its rows of `out`, and
  * the table, stay as they were), tokens outside [0, V) count for nothing.  Rows that
- * belong to no sequence stay as they were. */
+ * belong to no sequence stay as they were.  rows (for the counts N) times V / 2048, rounded
+ * up, must be below 2^24. */
 
 typedef struct {
   int64_t rows, V, N;        /* N sequences                                     */

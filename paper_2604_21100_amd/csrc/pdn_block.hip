@@ -559,17 +559,19 @@ __device__ __forceinline__ void gate(float z, float& act, float& slope) {
     act = 1.f;
     slope = 0.f;
   } else {
-    const float x = fabsf(z) > 200.f ? -200.f : -fabsf(z);
-    float e = x * kLog2e;
-    if constexpr (sizeof(T) == 4) {   // (the product's rounding put back: fp32 outputs show it)
+    float e, r;
+    if constexpr (sizeof(T) == 4) {   // (what the product and the reciprocal round off put back: fp32 outputs show it)
+      const float x = fabsf(z) > 200.f ? -200.f : -fabsf(z);
+      e = x * kLog2e;
       const float lo = fmaf(x, kLog2e, -e) + x * 1.925963033e-8f;   // log2(e) = kLog2e + 1.93e-8
       e = exp2_hw(e);
       e = fmaf(e, lo * kLn2, e);
+      r = fast_rcp(1.f + e);
+      r = fmaf(fmaf(-(1.f + e), r, 1.f), r, r);
     } else {
-      e = exp2_hw(e);
+      e = exp2_hw(-fabsf(z) * kLog2e);
+      r = fast_rcp(1.f + e);
     }
-    float r = fast_rcp(1.f + e);
-    r = fmaf(fmaf(-(1.f + e), r, 1.f), r, r);
     const float s = z >= 0.f ? r : e * r, rest = z >= 0.f ? e * r : r;   // sigmoid(z), 1 - sigmoid(z)
     act = ACT == kActSilu ? z * s : s;
     slope = ACT == kActSilu ? s + act * rest : s * rest;
