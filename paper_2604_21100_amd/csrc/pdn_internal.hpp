@@ -375,6 +375,7 @@ struct LogitsArgs {
   const int32_t* mask;
   const int32_t* mask_rows;
   void* parts;            // [rows, logits_segments(V)] of 16 bytes
+  bool passing;           // (set by the launcher: past the caches)
 };
 __host__ __device__ int64_t logits_segments(int64_t V);
 hipError_t launch_logits(const LogitsArgs& a, int in_bf16, int out_bf16, hipStream_t s);

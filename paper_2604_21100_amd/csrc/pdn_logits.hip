@@ -151,6 +151,13 @@ struct Lists {
   }
 };
 
+// Probabilities are written, and logits read for the last time, past the caches, where rows are aligned to the
+// 16 bytes of an access (else an access ends in the next one's line): what is in the caches then is the
+// logits that the second launch still has to read, and the verification reads a row or two of each sequence's
+// only.  With and without, the call | with its verification, us: 314 rows of 131072 81 | 113 and 99 | 126, 64 rows
+// 18 | 32 and 23 | 36; one launch, 512 rows of 16000 19 and 22.  Unaligned, 512 rows of 50257 80 and 67.
+typedef uint32_t Sixteen __attribute__((ext_vector_type(4), aligned(2), may_alias));
+
 // A thread's eight tokens from j on.  Loads do not branch (a wait for each would follow): a last thread with
 // fewer than eight takes the row's last eight, one without any too, and `keep` says which are its own.  TINY:
 // rows of fewer than eight.
@@ -167,22 +174,34 @@ struct Place {
       keep = j < static_cast<uint32_t>(n) ? (0xffu << (j - at)) & 0xff : 0;
     }
   }
-  template <typename T>
+  template <bool PASSING = false, typename T>
   __device__ __forceinline__ void load(const T* row, T (&x)[kVec]) const {
     if constexpr (TINY) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i) x[i] = row[min(i, n - 1)];
+    } else if constexpr (PASSING) {
+      Sixteen q[sizeof x / 16];
+#pragma unroll
+      for (unsigned i = 0; i < sizeof x / 16; ++i) q[i] = __builtin_nontemporal_load(reinterpret_cast<const Sixteen*>(row + at) + i);
+      __builtin_memcpy(x, q, sizeof x);
     } else {
       __builtin_memcpy(x, row + at, sizeof x);
     }
   }
-  template <typename TO>
+  template <bool PASSING, typename TO>
   __device__ __forceinline__ void store(TO* row, const float (&v)[kVec]) const {
     TO x[kVec];
 #pragma unroll
     for (int i = 0; i < kVec; ++i) x[i] = from_f<TO>(v[i]);
     if (!TINY && keep == 0xff) {
-      __builtin_memcpy(row + at, x, sizeof x);
+      if constexpr (PASSING) {
+        Sixteen q[sizeof x / 16];
+        __builtin_memcpy(q, x, sizeof x);
+#pragma unroll
+        for (unsigned i = 0; i < sizeof x / 16; ++i) __builtin_nontemporal_store(q[i], reinterpret_cast<Sixteen*>(row + at) + i);
+      } else {
+        __builtin_memcpy(row + at, x, sizeof x);
+      }
     } else if (keep) {
 #pragma unroll
       for (int i = 0; i < kVec; ++i)
@@ -192,14 +211,14 @@ struct Place {
 };
 
 // Eight tokens of a row with what changes them.
-template <typename T, bool TINY>
+template <typename T, bool TINY, bool LAST = false>   // LAST: the logits are not read again
 struct Tokens {
   Place<TINY> place;
   T raw[kVec];
   int32_t count[kVec];
   uint32_t bits[2];   // the mask's bytes at the first and the last of them
   __device__ __forceinline__ Tokens(const LogitsArgs& a, uint32_t row, uint32_t j) : place(a, j) {
-    place.load(static_cast<const T*>(a.logits) + row * a.stride, raw);
+    place.template load<LAST>(static_cast<const T*>(a.logits) + row * a.stride, raw);
   }
   __device__ __forceinline__ void load_rest(const RowOf& r) {
     if (r.counts) {
@@ -359,7 +378,7 @@ __device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint3
 
 // The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves. No loop:
 // a loop's loads would wait for the stores before them (84 us against 75).
-template <typename T, typename TO, bool TINY, bool PROBS>
+template <typename T, typename TO, bool TINY, bool PROBS, bool PASSING>
 __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t windows, uint32_t segs) {
   const uint32_t row = blockIdx.x / windows, base = blockIdx.x % windows * kSeg + (threadIdx.x >> 6) * kWaveSpan;
   const uint32_t lane = threadIdx.x & 63;
@@ -367,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t wi
   const Part* const parts = static_cast<const Part*>(a.parts) + static_cast<int64_t>(row) * segs;
   Part part{};
   if constexpr (PROBS) part = parts[min(lane, segs - 1)];
-  Tokens<T, TINY> now(a, row, base + lane * kVec);
+  Tokens<T, TINY, PASSING> now(a, row, base + lane * kVec);
   const RowOf r = row_of(a, row, told);
   if (r.out) return;
   now.load_rest(r);
@@ -390,11 +409,11 @@ __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t wi
       for (int i = 0; i < kVec; ++i) l[i] *= f;
     }
   }
-  now.place.store(static_cast<TO*>(a.out) + row * a.V, l);
+  now.place.template store<PASSING>(static_cast<TO*>(a.out) + row * a.V, l);
 }
 
 // Both at once: a workgroup a row of up to CH windows of its threads, the changed logits kept in registers.
-template <typename T, typename TO, int THREADS, int CH, bool TINY>
+template <typename T, typename TO, int THREADS, int CH, bool TINY, bool PASSING>
 __global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
   constexpr int kOneWaves = THREADS / kWave, kOneSeg = THREADS * kVec;
   __shared__ float tops[kOneWaves], sums[kOneWaves];
@@ -465,7 +484,7 @@ __global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
 #pragma unroll
     for (int i = 0; i < kVec; ++i)
       l[c][i] = !greedy ? l[c][i] * f : sum != sum ? sum : top > -kInf && place.at + i == first ? 1.f : 0.f;
-    place.store(static_cast<TO*>(a.out) + row * a.V, l[c]);
+    place.template store<PASSING>(static_cast<TO*>(a.out) + row * a.V, l[c]);
   }
 }
 
@@ -478,40 +497,46 @@ hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
   const int64_t windows = logits_segments(a.V);
   const dim3 block(kThreads), all(static_cast<unsigned>(a.rows * windows));
   if (TINY || !a.probs) {
-    hipLaunchKernelGGL((logits_out<T, TO, TINY, false>), all, block, 0, s, a, static_cast<uint32_t>(windows), 0u);
+    hipLaunchKernelGGL((logits_out<T, TO, TINY, false, false>), all, block, 0, s, a, static_cast<uint32_t>(windows), 0u);
     return hipGetLastError();
   }
   const int64_t most = (kManyBlocks / 8 + a.rows - 1) / a.rows * 8;
   const uint32_t segs = static_cast<uint32_t>(std::min(windows, most)), steps = static_cast<uint32_t>((windows + segs - 1) / segs);
   hipLaunchKernelGGL((logits_parts<T>), dim3(static_cast<unsigned>(a.rows * segs)), block, 0, s, a, segs, steps);
-  hipLaunchKernelGGL((logits_out<T, TO, false, true>), all, block, 0, s, a, static_cast<uint32_t>(windows), segs);
+  if (a.passing) hipLaunchKernelGGL((logits_out<T, TO, false, true, true>), all, block, 0, s, a, static_cast<uint32_t>(windows), segs);
+  else hipLaunchKernelGGL((logits_out<T, TO, false, true, false>), all, block, 0, s, a, static_cast<uint32_t>(windows), segs);
   return hipGetLastError();
 }
-// One launch up to 16384 tokens, and up to 57344 (what its registers hold) from 96 rows on: it reads the logits once,
-// but a row is one compute unit's.  Two launches | one, us, bf16 with everything on | fp32 logits alone:
-//   rows          1           8            64           128          256          512         1024        2048
-//    2000     14.7  8.0   21.5 11.4   21.3 11.2    21.9 11.5    22.5 12.0    27.9 16.5    28.1 23.9   45.6 47.8
-//    8000     12.1  7.5   13.7  8.4   13.8  8.8    15.0  9.1    19.5 11.0    30.0 17.3    44.3 26.1   79.9 48.3
-//   16000     10.2  8.9   10.9 10.0   12.8 10.4    15.7 12.1    24.7 15.9    39.4 22.2    64.5 36.1    132 74.5
-//   32001      9.4 12.4   10.1 13.7   14.4 16.0    21.6 18.2    35.3 22.7    55.1 41.9    99.5 74.5
-//   50257      8.8 18.4    9.4 20.1   19.2 24.0    30.1 26.7    51.7 33.4    81.1 63.3
-//    2000      6.9  4.5    7.4  4.8    7.6  4.9     8.0  5.1     8.9  5.6    10.3  8.0    13.1 12.9   22.9 25.7
-//   16000      7.6  7.0    7.9  7.3    9.1  8.2    11.9  9.6    19.0 14.3    33.1 22.5    51.8 36.9    114 74.7
-//   50257      7.6 14.6    7.6 15.3   16.4 18.8    26.7 23.0    46.5 34.3    85.9 67.2
-// (1024 threads throughout; up to 2048 tokens take 256.)
+// One launch up to 16384 tokens, to 32768 from 80 rows on and to 57344 (what its registers hold) from 128: it reads the
+// logits once, but a row is one compute unit's.  Two launches | one, us, bf16 with everything on, then fp32 logits alone:
+//   rows          1           8            64           96           128          256          512         1024        2048
+//    2000     14.8  7.7   21.4 11.0   21.2 10.9    22.1 11.3    21.8 11.1    22.4 11.5    27.2 14.0    27.1 13.6   44.1 22.1
+//    8000     11.9  7.3   13.5  8.1   13.6  8.5    14.8  8.5    14.8  8.7    18.4  9.7    28.5 15.7    42.4 23.3   78.0 45.1
+//   16000     10.2  8.3   10.9  9.4   12.5  9.7    13.5 10.0    14.8 10.6    23.5 13.8    38.0 19.1    62.3 32.1    125 61.9
+//   32000      9.0 11.6   10.0 12.3   13.2 13.6    16.7 14.5    19.9 15.2    32.3 21.8    53.8 37.9    94.1 67.3
+//   49152      9.1 16.4    9.2 18.1   15.4 20.3    19.5 21.6    23.3 22.4    44.2 34.8    66.7 61.9
+//    2000      6.7  3.7    7.3  4.0    7.6  4.2     7.7  4.3     7.9  4.3     8.7  4.8    10.1  5.3    12.1  6.3   21.5 11.5
+//   16000      7.5  6.4    7.7  6.8    8.6  7.5     9.9  8.0    11.0  8.4    17.3 13.2    29.7 19.5    47.8 35.1    104 71.3
+//   32000      7.6  9.2    7.7  9.3   10.9 10.8    14.0 11.6    16.8 12.6    27.6 24.5    49.9 44.0    82.1 73.8
+//   49152      7.4 12.9    7.7 13.4   12.7 16.4    16.9 17.5    20.0 19.8    42.0 39.7    66.6 73.7
+template <typename T, typename TO, bool PASSING>
+hipError_t one_launch(const LogitsArgs& a, hipStream_t s) {
+  const dim3 rows(static_cast<unsigned>(a.rows));
+  if (a.V <= 2048) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, false, PASSING>), rows, dim3(256), 0, s, a);
+  else if (a.V <= 8192) hipLaunchKernelGGL((logits_one<T, TO, 1024, 1, false, PASSING>), rows, dim3(1024), 0, s, a);
+  else if (a.V <= 16384) hipLaunchKernelGGL((logits_one<T, TO, 1024, 2, false, PASSING>), rows, dim3(1024), 0, s, a);
+  else if (a.V <= 32768) hipLaunchKernelGGL((logits_one<T, TO, 1024, 4, false, PASSING>), rows, dim3(1024), 0, s, a);
+  else hipLaunchKernelGGL((logits_one<T, TO, 1024, 7, false, PASSING>), rows, dim3(1024), 0, s, a);
+  return hipGetLastError();
+}
 template <typename T, typename TO>
 hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
-  const dim3 rows(static_cast<unsigned>(a.rows));
   const bool fits = a.V <= 2048 || a.rows < 1 << 22;   // (a launch holds fewer than 2^32 work items)
-  if (a.probs && fits && a.V <= (a.rows < 96 ? 16384 : 57344)) {
-    if (a.V < kVec) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, true>), rows, dim3(256), 0, s, a);
-    else if (a.V <= 2048) hipLaunchKernelGGL((logits_one<T, TO, 256, 1, false>), rows, dim3(256), 0, s, a);
-    else if (a.V <= 8192) hipLaunchKernelGGL((logits_one<T, TO, 1024, 1, false>), rows, dim3(1024), 0, s, a);
-    else if (a.V <= 16384) hipLaunchKernelGGL((logits_one<T, TO, 1024, 2, false>), rows, dim3(1024), 0, s, a);
-    else if (a.V <= 32768) hipLaunchKernelGGL((logits_one<T, TO, 1024, 4, false>), rows, dim3(1024), 0, s, a);
-    else hipLaunchKernelGGL((logits_one<T, TO, 1024, 7, false>), rows, dim3(1024), 0, s, a);
+  if (a.probs && a.V < kVec) {
+    hipLaunchKernelGGL((logits_one<T, TO, 256, 1, true, false>), dim3(static_cast<unsigned>(a.rows)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
+  if (a.probs && fits && a.V <= (a.rows < 80 ? 16384 : a.rows < 128 ? 32768 : 57344)) return a.passing ? one_launch<T, TO, true>(a, s) : one_launch<T, TO, false>(a, s);
   if (a.V < kVec) return logits_at<T, TO, true>(a, s);   // (changed logits)
   return logits_at<T, TO, false>(a, s);
 }
@@ -585,7 +610,10 @@ __global__ __launch_bounds__(kThreads) void counts_write(CountArgs a) {
 __host__ __device__ int64_t logits_segments(int64_t V) { return (V + kSeg - 1) / kSeg; }
 __host__ __device__ int64_t count_segments(int64_t V) { return (V + kSeg - 1) / kSeg; }
 
-hipError_t launch_logits(const LogitsArgs& a, int in_bf16, int out_bf16, hipStream_t s) {
+hipError_t launch_logits(const LogitsArgs& args, int in_bf16, int out_bf16, hipStream_t s) {
+  LogitsArgs a = args;
+  const int in = in_bf16 ? 2 : 4, out = out_bf16 ? 2 : 4;
+  a.passing = ((reinterpret_cast<uintptr_t>(a.logits) | a.stride * in | reinterpret_cast<uintptr_t>(a.out) | a.V * out) & 15) == 0;
   if (in_bf16) return out_bf16 ? logits_of<bf16, bf16>(a, s) : logits_of<bf16, float>(a, s);
   return out_bf16 ? logits_of<float, bf16>(a, s) : logits_of<float, float>(a, s);
 }

@@ -235,7 +235,8 @@ def test_verification_reads_it():
 
 
 @pytest.mark.parametrize("rows,V", [(95, 16385), (96, 16384), (96, 16385), (97, 32769), (96, 57344), (96, 57345), (3, 16384), (3, 16385),
-                                    (5, 2048), (5, 2049), (5, 8192), (5, 8193), (4, 32768), (300, 70000)])
+                                    (79, 16385), (80, 16385), (80, 32768), (127, 32769), (128, 32769),
+                                    (128, 57344), (128, 57345), (5, 2048), (5, 2049), (5, 8192), (5, 8193), (4, 32768), (300, 70000)])
 def test_where_the_forms_meet(rows, V):
     """One launch or two go by rows and tokens: every token's probability against 64 bits, a greedy row among them."""
     import torch
