@@ -11,8 +11,7 @@
 // of its own sequence's rows.
 //
 // What bounds it: reading the logits twice and writing p, for 314 rows of 131072 fp32 logits with penalties and masks
-// 51 us (198 MB; 40 without them, a plain maximum over the rows takes 47) and 74 us (363 MB, 4.9 TB/s; a
-// copy of the logits 62); for a few rows latency, 4.4 and 4.3 us for one of 50257.
+// 43 us (198 MB, 4.6 TB/s) and 57 us (363 MB, 6.4 TB/s), the vector units 0.73 of the time; for a few rows latency, 4.4 and 4.3 us for one of 50257.
 #include <algorithm>
 #include <cmath>
 
