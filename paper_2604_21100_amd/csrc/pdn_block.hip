@@ -97,6 +97,13 @@ __device__ __forceinline__ void store(T* p, const Cols<KIND>& c, const float (&v
       if (c.keep >> i & 1) p[c.at + i] = x[i];
   }
 }
+// Zero in the columns that are not its own: what enters a row's sum with a vector in it, since the zero
+// of a row there times another column's infinite entry would be a NaN in the whole row.
+template <RowKind KIND>
+__device__ __forceinline__ void settle(const Cols<KIND>& c, float (&v)[kVec]) {
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) v[i] = (KIND == kEights ? c.keep : c.keep >> i & 1) ? v[i] : 0.f;
+}
 // of a vector that may be NULL (= 1)
 template <RowKind KIND>
 __device__ __forceinline__ void ld_weight(const float* p, const Cols<KIND>& c, float (&v)[kVec]) {
@@ -228,10 +235,10 @@ __global__ __launch_bounds__(GROUP ? kGroupThreads : 1024) void rnorm_fwd(RnormA
 #pragma unroll
       for (int i = 0; i < kVec; ++i) h[k][i] *= a.alpha;
       if (a.residual) {
-        x[k].settle(o);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) h[k][i] += x[k][i];
       }
+      settle(o, h[k]);
       if (a.h) store(static_cast<TS*>(a.h) + at, o, h[k]);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) q[0] += h[k][i] * h[k][i];
@@ -314,9 +321,17 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
     }
   };
   if constexpr (kAhead) {
+    const auto o = team.template cols<KIND>(0, D);
     of_memory(0, 0, w);
-    if constexpr (POST) of_memory(1, 0, wp);
-    if constexpr (SCALE) of_memory(2, 0, sc);
+    settle(o, w);
+    if constexpr (POST) {
+      of_memory(1, 0, wp);
+      settle(o, wp);
+    }
+    if constexpr (SCALE) {
+      of_memory(2, 0, sc);
+      settle(o, sc);
+    }
     if constexpr (kShared) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -348,6 +363,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
       get(0, k, w);
+      if constexpr (!kAhead) settle(team.template cols<KIND>(k, D), w);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         q[0] += r.h[k][i] * r.h[k][i];
@@ -389,8 +405,12 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
           if constexpr (kRegs) dp[k][i] += x;
           else kept[(k * kVec + i) * THREADS + threadIdx.x] += x;
           e[k][i] = t[i] * wp[i];
-          p[0] += e[k][i] * r.y[k][i];
         }
+      }
+      if constexpr (POST) {
+        if constexpr (!kAhead) settle(o, e[k]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) p[0] += e[k][i] * r.y[k][i];
       }
       if constexpr (!POST) store(static_cast<TI*>(a.dy) + at, o, t);
     }
@@ -651,6 +671,7 @@ __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L, Walk b
   HeadRow at(a, L);
   float w[kVec], dw[kVec] = {};
   ld_weight(a.weight ? a.weight + (a.head_weight ? at.head * a.d : 0) : nullptr, o, w);
+  if (a.weight) settle(o, w);
   Raw<T> next[3];   // the next row's
   auto load = [&](const HeadRow& r) {
     const int64_t t = min(r.t, a.M - 1), h = static_cast<int64_t>(r.head) * a.d;   // (behind the last: not used)

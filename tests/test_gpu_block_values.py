@@ -1,0 +1,64 @@
+"""The norms around the rule at values where a width's form, a type or a range could show."""
+import numpy as np
+import pytest
+
+from block_util import U
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+@pytest.mark.parametrize("D", [5, 24, 33, 300, 301, 1000, 1001, 1024, 2056, 5001, 9001, 9008])
+def test_an_infinite_entry_of_a_vector(D):
+    """post_weight or scale with one infinite entry: h is infinite in that column and finite elsewhere, and
+    so u (the factor of an infinite sum is zero) NaN there and zero elsewhere, whatever the width's form.
+    In the backward an infinite weight makes the row's second sum infinite, so of rows above zero the gradients are -inf in
+    the other columns."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(D)
+    R = 3
+    y, x, du = (torch.randn(R, D, device="cuda").abs() + 0.5 for _ in range(3))
+    w = torch.rand(D, device="cuda") + 0.5
+    for j in {0, min(7, D - 1), D // 2, D - 2 if D > 1 else 0, D - 1}:
+        v = w.clone()
+        v[j] = INF
+        rest = torch.arange(D, device="cuda") != j
+        for post in (False, True):
+            for kw in ([dict(scale=v)] + ([dict(post_weight=v), dict(post_weight=w, scale=v)] if post else [])):
+                u, h = pdn.pdn_residual_norm(y, x, post_norm=post, **kw)
+                finite = pdn.pdn_residual_norm(y, x, post_norm=post, **{n: torch.where(rest, t, w) for n, t in kw.items()})[1]
+                assert torch.equal(h[:, rest], finite[:, rest]) and (h[:, j] == INF).all(), (j, post, set(kw))
+                assert (u[:, rest] == 0).all() and u[:, j].isnan().all(), (j, post, set(kw))
+        g = pdn.pdn_residual_norm_bwd(du, x, weight=v)
+        assert (g["dresidual"][:, rest] == -INF).all() and g["dresidual"][:, j].isnan().all(), j
+        assert torch.equal(g["dweight"], pdn.pdn_residual_norm_bwd(du, x, weight=w)["dweight"]), j
+        if D > 1:   # (the gradients that do not read the infinite entry; dy's sum over e y has it once)
+            dh = torch.full_like(x, 1e6)   # (t > 0)
+            g = pdn.pdn_residual_norm_bwd(du, x, y, dh=dh, post_norm=True, post_weight=v)
+            f = pdn.pdn_residual_norm_bwd(du, x, y, dh=dh, post_norm=True, post_weight=w)
+            assert (g["dy"][:, rest] == -INF).all() and g["dy"][:, j].isnan().all(), j
+            assert torch.equal(g["dpost_weight"], f["dpost_weight"]) and torch.equal(g["dresidual"], f["dresidual"]), j
+
+
+@pytest.mark.parametrize("d", [5, 24, 33, 64, 200, 201])
+@pytest.mark.parametrize("gated", [False, True])
+def test_an_infinite_entry_of_a_heads_weight(d, gated):
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(d)
+    M, H = 3, 2
+    x, dy, z = (torch.rand(M, H, d, device="cuda") + 0.5 for _ in range(3))
+    z = z if gated else None
+    w = torch.rand(d, device="cuda") + 0.5
+    for j in {0, min(7, d - 1), d // 2, d - 2, d - 1}:
+        v = w.clone()
+        v[j] = INF
+        rest = torch.arange(d, device="cuda") != j
+        y = pdn.pdn_head_norm(x, weight=v, z=z)
+        assert (y[..., j] == INF).all() and torch.equal(y[..., rest], pdn.pdn_head_norm(x, weight=w, z=z)[..., rest])
+        g, f = pdn.pdn_head_norm_bwd(dy, x, weight=v, z=z), pdn.pdn_head_norm_bwd(dy, x, weight=w, z=z)
+        assert (g["dx"][..., rest] == -INF).all() and g["dx"][..., j].isnan().all(), j
+        assert torch.equal(g["dweight"], f["dweight"]), j
+        if gated:
+            assert torch.equal(g["dz"][..., rest], f["dz"][..., rest]) and g["dz"][..., j].isinf().all(), j
