@@ -119,6 +119,10 @@ __device__ __forceinline__ void ld_weight(const float* p, const Cols<KIND>& c, f
 }
 
 __device__ __forceinline__ float factor(float squares, float c, float eps) { return 1.f / sqrtf(squares * c + eps); }
+// in a backward pass: a row whose squares left fp32 has no gradient (a factor of zero would make it zeros)
+__device__ __forceinline__ float factor_back(float squares, float c, float eps) {
+  return squares == __builtin_inff() ? __builtin_nanf("") : factor(squares, c, eps);
+}
 
 // Sums over the workgroup's threads, the same on each of them.  Two buffers in turn: one barrier a sum.
 template <int N>
@@ -372,8 +376,8 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
       }
     }
     team.sum(q);
-    const float rh = factor(q[0], c, a.eps), mh = (rh * q[1] * c) * rh * rh;
-    const float ry = POST ? factor(q[POST ? 2 : 0], c, a.eps) : 1.f;
+    const float rh = factor_back(q[0], c, a.eps), mh = (rh * q[1] * c) * rh * rh;
+    const float ry = POST ? factor_back(q[POST ? 2 : 0], c, a.eps) : 1.f;
     float p[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
@@ -698,7 +702,7 @@ __global__ __launch_bounds__(kThreads) void hnorm_bwd(HnormArgs a, int L, Walk b
       g[i] = ACT == kActNone ? dy[i] : dy[i] * act;
       p += g[i] * w[i] * x[i];
     }
-    const float r = factor(lanes_sum(q, L), c, a.eps), m = (r * lanes_sum(p, L) * c) * r * r;
+    const float r = factor_back(lanes_sum(q, L), c, a.eps), m = (r * lanes_sum(p, L) * c) * r * r;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       slope[i] *= x[i] * r;

@@ -62,3 +62,60 @@ def test_an_infinite_entry_of_a_heads_weight(d, gated):
         assert torch.equal(g["dweight"], f["dweight"]), j
         if gated:
             assert torch.equal(g["dz"][..., rest], f["dz"][..., rest]) and g["dz"][..., j].isinf().all(), j
+
+
+@pytest.mark.parametrize("D", [6, 200, 1000, 2048, 5001, 9000])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_whose_squares_leave_fp32(D, dt):
+    """A row whose sum of squares passes 3.4e38: zeros in the forward, and in the backward NaN, in that
+    row and in the vectors' gradients, not zeros that look like gradients.  Other rows do not see it."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(D)
+    kind = torch.bfloat16 if dt == "bf16" else torch.float32
+    R, at = 4, 2
+    ok = [0, 1, 3]
+    y, h, du, dh = (torch.randn(R, D, device="cuda").to(kind) for _ in range(4))
+    w = torch.rand(D, device="cuda") + 0.5
+    big = torch.full((D,), 1e19, device="cuda").to(kind)   # (squares of 1e38, in range; four of them are not)
+    hb, yb = h.clone(), y.clone()
+    hb[at], yb[at] = big, big
+    u, got = pdn.pdn_residual_norm(torch.zeros_like(hb), hb, weight=w)
+    assert torch.equal(got, hb) and (u[at] == 0).all() and not (u[ok] == 0).all(1).any()
+    a, b = pdn.pdn_residual_norm_bwd(du, h, dh=dh, weight=w), pdn.pdn_residual_norm_bwd(du, hb, dh=dh, weight=w)
+    for n in ("dy", "dresidual"):
+        assert b[n][at].isnan().all() and torch.equal(a[n][ok], b[n][ok]), n
+    assert b["dweight"].isnan().all()
+    kw = dict(weight=w, post_norm=True, post_weight=w, scale=w)
+    u, got = pdn.pdn_residual_norm(yb, h, **kw)
+    assert torch.equal(got[at], h[at])   # (the normed y is zeros)
+    a, b = pdn.pdn_residual_norm_bwd(du, h, y, dh=dh, **kw), pdn.pdn_residual_norm_bwd(du, h, yb, dh=dh, **kw)
+    assert b["dy"][at].isnan().all() and torch.equal(a["dy"][ok], b["dy"][ok])
+    assert torch.equal(a["dresidual"], b["dresidual"]) and torch.equal(a["dweight"], b["dweight"])
+    assert b["dpost_weight"].isnan().all() and b["dscale"].isnan().all()
+
+
+@pytest.mark.parametrize("d", [5, 33, 128, 200])
+@pytest.mark.parametrize("norm", ["rms", "l2"])
+@pytest.mark.parametrize("each", [False, True])
+def test_heads_whose_squares_leave_fp32(d, norm, each):
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(d)
+    M, H = 3, 2
+    for kind in (torch.float32, torch.bfloat16):
+        x, dy, z = (torch.randn(M, H, d, device="cuda").to(kind) for _ in range(3))
+        w = torch.rand(H, d, device="cuda") if each else torch.rand(d, device="cuda")
+        xb = x.clone()
+        xb[1, 1] = 1e19
+        kw = dict(norm=norm, weight=w, z=z)
+        y = pdn.pdn_head_norm(xb, **kw)
+        assert (y[1, 1] == 0).all()
+        a, b = pdn.pdn_head_norm_bwd(dy, x, **kw), pdn.pdn_head_norm_bwd(dy, xb, **kw)
+        for n in ("dx", "dz"):
+            assert b[n][1, 1].isnan().all(), n
+            b[n][1, 1] = a[n][1, 1]
+            assert torch.equal(a[n], b[n]), n
+        assert (b["dweight"][1] if each else b["dweight"]).isnan().all()
+        if each:
+            assert torch.equal(a["dweight"][0], b["dweight"][0])
