@@ -119,3 +119,24 @@ def test_heads_whose_squares_leave_fp32(d, norm, each):
         assert (b["dweight"][1] if each else b["dweight"]).isnan().all()
         if each:
             assert torch.equal(a["dweight"][0], b["dweight"][0])
+
+
+@pytest.mark.parametrize("act", ["silu", "sigmoid"])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_a_weights_gradient_of_gated_rows_is_fp32s(act, dt):
+    """dweight is fp32 for bf16 rows too.  Rows of ones with ones as gradient have a factor of one and a sum of one
+    term, so dweight is act(z) as computed.  Relative roundings, in u = 2^-24: the exponential two (a step), its
+    correction one; 1 + e, its reciprocal, the product with e and that with z one each: 7.  (The argument's own
+    rounding, up to |z| u, is what the correction puts back.)"""
+    import torch
+    import paper_2604_21100_amd as pdn
+    kind = torch.bfloat16 if dt == "bf16" else torch.float32
+    H, d = 512, 128
+    z = torch.linspace(-80, 80, H * d, device="cuda").to(kind).view(1, H, d)
+    one = torch.ones(1, H, d, device="cuda").to(kind)
+    g = pdn.pdn_head_norm_bwd(one, one, weight=torch.ones(H, d, device="cuda"), z=z, act=act, eps=1e-30)
+    x = z.double().cpu().numpy()[0]
+    s = np.where(x >= 0, 1 / (1 + np.exp(-np.abs(x))), np.exp(-np.abs(x)) / (1 + np.exp(-np.abs(x))))
+    want = x * s if act == "silu" else s
+    off = np.abs(g["dweight"].double().cpu().numpy() - want)
+    assert (off <= 8 * U * np.abs(want)).all(), float((off / np.maximum(np.abs(want), 1e-300)).max() / U)
