@@ -280,25 +280,38 @@ struct Tokens {
   }
 };
 
-// 1 / temperature as a factor of the base-2 exponential's argument; any temperature gives a
-// number (so that zero times it is zero); not above 0: 1 (the sum only shows NaN then)
-__device__ __forceinline__ float sharpness(float t) {
-  if (!(t > 0.f)) return 1.f;
-  return fminf(fmaxf(kLog2e / t, 1e-30f), 3e38f);
+// log2(e) / temperature, the factor of the base-2 exponential's argument, from below (k), and the rest of it; both
+// above 0, so that -inf times them is -inf, and numbers, so that zero times them is zero.  A temperature not above 0: 1
+// (the sum only shows NaN then)
+struct Sharpness {
+  float k, rest;
+};
+__device__ __forceinline__ Sharpness sharpness(float t) {
+  constexpr float kTiny = 1.4e-45f;
+  if (!(t > 0.f)) return Sharpness{1.f, kTiny};
+  float k = kLog2e / t;
+  if (k < 1e-30f || k > 1e30f) return Sharpness{fminf(fmaxf(k, 1e-30f), 3e38f), kTiny};   // (such a t has no reciprocal)
+  k = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, k) - 1u);   // (the quotient was rounded)
+  const float rest = (fmaf(-k, t, kLog2e) + 1.925963033e-8f) * fast_rcp(t);   // (log2(e) = kLog2e + 1.93e-8)
+  return Sharpness{read_lane(k, 0), read_lane(rest, 0)};   // (a row's, so a wave's)
 }
+// e^(d / temperature), d <= 0: the argument is rounded once, to 2^-24 of itself (with a rounded k alone 2.2 times that)
+__device__ __forceinline__ float exp_of(float d, const Sharpness& s) { return exp2_hw(fmaf(d, s.k, d * s.rest)); }
 // e of eight l under the largest, `top`.  Where nothing is left that is -inf, and so is every l (or NaN).
-__device__ __forceinline__ float under(float l, float top, float k) {
-  return l == top ? (top > -kInf ? 1.f : 0.f) : exp2_hw((l - (top > -kInf ? top : 0.f)) * k);
+__device__ __forceinline__ float under(float l, float top, const Sharpness& s) {
+  return l == top ? (top > -kInf ? 1.f : 0.f) : exp_of(l - (top > -kInf ? top : 0.f), s);
 }
-__device__ __forceinline__ void under(const float (&l)[kVec], float top, float k, float (&e)[kVec]) {
-  const float level = top > -kInf ? top : 0.f;
-  if (top == kInf) {
+__device__ __forceinline__ void under(const float (&l)[kVec], float top, const Sharpness& s, float (&e)[kVec]) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) e[i] = under(l[i], top, k);
-  } else {   // (zero times k is zero)
+  for (int i = 0; i < kVec; ++i) e[i] = l[i];
+  float level = top > -kInf ? top : 0.f;
+  if (top == kInf) {   // (as if those at infinity were at zero, the others, but for a NaN, below everything)
+    level = 0.f;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) e[i] = exp2_hw((l[i] - level) * k);
+    for (int i = 0; i < kVec; ++i) e[i] = e[i] == kInf ? 0.f : e[i] - kInf;
   }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) e[i] = exp_of(e[i] - level, s);   // (zero times the factor is zero)
 }
 
 __device__ __forceinline__ int wave_min(int x) {
@@ -320,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a, uint32_t 
   if (r.out) return;
   next.load_rest(r);
   const Lists lists(a, r, row);
-  const float k = sharpness(r.temperature);
+  const Sharpness k = sharpness(r.temperature);
   const bool greedy = !(r.temperature > 0.f);
   Part mine{-kInf, 0.f, INT32_MAX, 0};   // the thread's
   for (uint32_t s = 0; s < steps; ++s, base += kSeg) {
@@ -359,7 +372,7 @@ __global__ __launch_bounds__(kThreads) void logits_parts(LogitsArgs a, uint32_t 
 }
 
 // a row's whole from its parts, on every lane of a wave; x: the part of the lane's number
-__device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint32_t segs, float k, bool greedy) {
+__device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint32_t segs, const Sharpness& k, bool greedy) {
   const uint32_t lane = threadIdx.x & 63;
   float top = lane < segs ? x.top : -kInf;
   for (uint32_t s = kWave + lane; s < segs; s += kWave) top = fmaxf(top, parts[s].top);
@@ -390,7 +403,7 @@ __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t wi
   if (r.out) return;
   now.load_rest(r);
   const Lists lists(a, r, row);
-  const float k = sharpness(r.temperature);
+  const Sharpness k = sharpness(r.temperature);
   const bool greedy = !(r.temperature > 0.f);
   Part whole{};
   if constexpr (PROBS) whole = whole_of(parts, part, segs, k, greedy);
@@ -426,7 +439,7 @@ __global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
   if (r.out) return;
   next.load_rest(r);
   const Lists lists(a, r, row);
-  const float k = sharpness(r.temperature);
+  const Sharpness k = sharpness(r.temperature);
   const bool greedy = !(r.temperature > 0.f);
   float l[CH][kVec], top = -kInf, sum = 0.f;
 #pragma unroll
