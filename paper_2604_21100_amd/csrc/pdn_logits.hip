@@ -287,10 +287,10 @@ struct Sharpness {
   float k, rest;
 };
 __device__ __forceinline__ Sharpness sharpness(float t) {
-  constexpr float kTiny = 1.4e-45f;
+  constexpr float kTiny = 1.4e-45f;   // (the smallest: an infinite temperature moves the lowest number by 1e-6)
   if (!(t > 0.f)) return Sharpness{1.f, kTiny};
   float k = kLog2e / t;
-  if (k < 1e-30f || k > 1e30f) return Sharpness{fminf(fmaxf(k, 1e-30f), 3e38f), kTiny};   // (such a t has no reciprocal)
+  if (k < 1e-30f || k > 1e30f) return Sharpness{fminf(fmaxf(k, kTiny), 3e38f), kTiny};   // (such a t may have no reciprocal)
   k = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, k) - 1u);   // (the quotient was rounded)
   const float rest = (fmaf(-k, t, kLog2e) + 1.925963033e-8f) * fast_rcp(t);   // (log2(e) = kLog2e + 1.93e-8)
   return Sharpness{read_lane(k, 0), read_lane(rest, 0)};   // (a row's, so a wave's)

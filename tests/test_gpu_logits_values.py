@@ -35,3 +35,26 @@ def test_probabilities_of_unlikely_tokens(V, rows):
     want = e / e.sum(1, keepdim=True)
     off = (p - want).abs() / want
     assert (off <= (arg + 4) * U).all(), (off / (arg + 4)).max().item() / U
+
+
+@pytest.mark.parametrize("V", [4, 3000, 70000])
+def test_the_largest_temperatures(V):
+    """Temperatures up to the largest number and infinity, over logits as far apart as they are.  1 / T is held to
+    2^-24 down to 1.2e-38 and to 2^-149 below (2e-7 of 1 / 3e38), infinity as 2^-149, which moves a
+    logit of -3.4e38 by 5e-7; a token's e so by 1e-6 at most, and its p by twice that."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    T = [1e29, 1e32, 1e38, 3e38, INF]
+    for forms in (1, 200):
+        temps = T * forms
+        l = torch.full((len(temps), V), -INF, device="cuda")
+        for r, t in enumerate(temps):
+            x = min(t, 1e38)
+            l[r, :4] = f32([0.0, -x, -2 * x, -3.4e38])
+        got = pdn.pdn_logits(l, temperature=f32(temps)).double()
+        e = torch.exp(l.double() / f32(temps).double()[:, None].clamp(max=1e300))
+        want = torch.where(l == -INF, 0.0, e / e.sum(1, keepdim=True))
+        for r, t in enumerate(temps):
+            if t == INF:
+                want[r, :4] = 0.25
+        assert ((got - want).abs() <= 4e-6 * want).all(), (V, forms, ((got - want).abs() / want.clamp(min=1e-300)).max().item())
