@@ -462,7 +462,8 @@ pdn_status pdn_residual_norm(const pdn_rnorm* problem, const void* y, const void
  * none was, its like).  dh: NULL (= 0).  y is needed with post_norm and for dscale.
  * dresidual and the vectors' gradients may be NULL to skip them; a vector that is
  * not given has none (PDN_ERR_VALUE).  dresidual may be dh itself.  `ws`: 256-byte
- * aligned, of at least pdn_residual_norm_bwd_workspace_size bytes. */
+ * aligned, of at least pdn_residual_norm_bwd_workspace_size bytes; none without a
+ * vector's gradient. */
 pdn_status pdn_residual_norm_bwd_workspace_size(const pdn_rnorm* problem, size_t* bytes);
 pdn_status pdn_residual_norm_bwd(const pdn_rnorm* problem, const void* du, const void* dh,
                                  const void* h, const void* y, const float* weight,

@@ -154,7 +154,7 @@ pdn_status pdn_residual_norm_bwd(const pdn_rnorm* p, const void* du, const void*
   for (const float* x : {weight, post_weight, scale, static_cast<const float*>(dweight), static_cast<const float*>(dpost_weight),
                          static_cast<const float*>(dscale)})
     if (!element_aligned(x, 4)) return PDN_ERR_ALIGN;
-  const int64_t v = p->D * 4, needs = rnorm_parts(p->rows, p->D) * v * 3;
+  const int64_t v = p->D * 4, needs = dweight || dpost_weight || dscale ? rnorm_parts(p->rows, p->D) * v * 3 : 0;
   const std::array<Buf, 7> ins = {{{du, n * io}, {dh == dresidual ? nullptr : dh, n * sm}, {h, n * sm}, {y, n * io}, {weight, v},
                                    {post_weight, v}, {scale, v}}};
   const std::array<Buf, 5> outs = {{{dy, n * io}, {dresidual, n * sm}, {dweight, v}, {dpost_weight, v}, {dscale, v}}};

@@ -382,7 +382,7 @@ PyObject* residual_norm_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     size_t bytes = 0, has = 0;
     pdn_status status = function<decltype(&pdn_residual_norm_bwd_workspace_size)>(a[kSizeFn])(&p, &bytes);
     if (status != PDN_OK) return PyLong_FromLong(status);
-    const at::Tensor ws = workspace_of(a[kWorkspace], dev, bytes, &has);
+    const at::Tensor ws = workspace_of(a[kWorkspace], dev, dwp || dpp || dsp ? bytes : 0, &has);
     const auto fn = function<decltype(&pdn_residual_norm_bwd)>(a[kFn]);
     void *const stream = function<void*>(a[kStream]), *const wp = ws.data_ptr();
     Py_BEGIN_ALLOW_THREADS

@@ -140,3 +140,19 @@ def test_a_weights_gradient_of_gated_rows_is_fp32s(act, dt):
     want = x * s if act == "silu" else s
     off = np.abs(g["dweight"].double().cpu().numpy() - want)
     assert (off <= 8 * U * np.abs(want)).all(), float((off / np.maximum(np.abs(want), 1e-300)).max() / U)
+
+
+def test_no_workspace_without_a_vectors_gradient():
+    """The parts are the vectors' gradients': a call that wants none needs no workspace."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    torch.manual_seed(1)
+    du, h, dh, w = torch.randn(700, 640, device="cuda"), torch.randn(700, 640, device="cuda"), torch.randn(700, 640, device="cuda"), torch.randn(640, device="cuda")
+    none = torch.empty(0, dtype=torch.uint8, device="cuda")
+    want = pdn.pdn_residual_norm_bwd(du, h, dh=dh, weight=w)
+    got = pdn.pdn_residual_norm_bwd(du, h, dh=dh, weight=w, want_vectors=False, workspace=none)
+    assert set(got) == {"dy", "dresidual"} and all(torch.equal(got[n], want[n]) for n in got)
+    got = pdn.pdn_residual_norm_bwd(du, h, dh=dh, workspace=none)   # (no vectors at all)
+    assert set(got) == {"dy", "dresidual"}
+    with pytest.raises(pdn.PdnError):
+        pdn.pdn_residual_norm_bwd(du, h, dh=dh, weight=w, workspace=none)
