@@ -680,6 +680,17 @@ def pdn_residual_norm(y, residual=None, *, weight=None, post_norm=False,
         _dtype_number(h_dtype), want_h, u, h)
 
 
+def pdn_residual_norm_bwd_workspace_size(rows: int, D: int) -> int:
+    """Bytes for gradients of vectors (none are needed without)."""
+    n = ctypes.c_size_t(0)
+    p = Rnorm(rows=rows, D=D, alpha=1.0, eps=1.0)
+    st = _lib.pdn_residual_norm_bwd_workspace_size(ctypes.byref(p),
+                                                   ctypes.byref(n))
+    if st != PDN_OK:
+        raise PdnError(st, "pdn_residual_norm_bwd_workspace_size")
+    return n.value
+
+
 def pdn_residual_norm_bwd(du, h, y=None, *, dh=None, weight=None,
                           post_norm=False, post_weight=None, scale=None,
                           alpha=1.0, eps=1e-6, outputs=None,
@@ -710,6 +721,19 @@ def pdn_head_norm(x, *, norm="rms", weight=None, z=None, act=None, eps=1e-6,
     return _call_on(
         "pdn_head_norm", x.device, stream, _pdn_torch.head_norm, _HNORM, x,
         NORMS[norm], weight, z, _act(act, z), eps, y)
+
+
+def pdn_head_norm_bwd_workspace_size(tokens: int, H: int, d: int,
+                                     head_weight: bool = False) -> int:
+    """Bytes for a weight's gradient (none are needed without); head_weight: of
+    a weight [H, d]."""
+    n = ctypes.c_size_t(0)
+    p = Hnorm(tokens=tokens, H=H, d=d, head_weight=head_weight, eps=1.0)
+    st = _lib.pdn_head_norm_bwd_workspace_size(ctypes.byref(p),
+                                               ctypes.byref(n))
+    if st != PDN_OK:
+        raise PdnError(st, "pdn_head_norm_bwd_workspace_size")
+    return n.value
 
 
 def pdn_head_norm_bwd(dy, x, *, norm="rms", weight=None, z=None, act=None,
