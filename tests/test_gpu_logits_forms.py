@@ -1,0 +1,48 @@
+"""pdn_logits with everything on in each of its forms: one launch with one to seven windows a thread, two launches, rows
+aligned to an access and not, in place too."""
+import numpy as np
+import pytest
+
+from test_gpu_logits import Round
+
+pytestmark = pytest.mark.gpu
+
+# rows, vocabulary: windows of one launch (1, 2, 4, 7), then two launches
+FORMS = [(3, 1999), (3, 2000), (3, 7999), (3, 16001), (3, 16000), (90, 20001), (90, 32764), (90, 32760), (130, 40003), (130, 57344), (3, 50257),
+         (5, 70004), (5, 70003), (5, 70008)]
+
+
+def batch(rng, rows):
+    lens = rng.integers(0, 6, rows)
+    ends = np.minimum(np.cumsum(lens), rows)
+    lens = np.diff(np.concatenate([[0], ends]))
+    return [int(n) for n in lens[lens > 0]] + [rows - int(lens.sum())]
+
+
+@pytest.mark.parametrize("rows,V", FORMS)
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+def test_everything_on(rows, V, io):
+    rng = np.random.default_rng(rows + V)
+    r = Round(rng, batch(rng, rows), V, io, pad=[0, 8, 3][V % 3], greedy=True)
+    r.check(rows=range(rows) if rows < 10 else sorted(rng.choice(rows, 10, replace=False)))
+
+
+@pytest.mark.parametrize("rows,V", FORMS)
+@pytest.mark.parametrize("io", ["f32", "bf16"])
+@pytest.mark.parametrize("probs", [True, False])
+def test_in_place(rows, V, io, probs, monkeypatch):
+    """The result in the logits' place: the bits of the call that does not, twice the same."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    rng = np.random.default_rng(rows + V)
+    r = Round(rng, batch(rng, rows), V, io, greedy=True)
+    with monkeypatch.context() as m:
+        m.setattr(pdn, "pdn_logits", lambda logits, **kw: (logits, kw))
+        l, kw = r.call(probs=probs)
+    before = l.clone()
+    want = pdn.pdn_logits(l, dtype=l.dtype, **kw)
+    assert torch.equal(l.view(torch.int16 if io == "bf16" else torch.int32), before.view(torch.int16 if io == "bf16" else torch.int32))
+    for _ in range(2):
+        got = l.clone()
+        assert pdn.pdn_logits(got, out=got, **kw) is got
+        assert torch.equal(got, want)
