@@ -519,18 +519,37 @@ hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
   else hipLaunchKernelGGL((logits_out<T, TO, false, true, false>), all, block, 0, s, a, static_cast<uint32_t>(windows), segs);
   return hipGetLastError();
 }
-// One launch up to 16384 tokens, to 32768 from 80 rows on and to 57344 (what its registers hold) from 128: it reads the
-// logits once, but a row is one compute unit's.  Two launches | one, us, bf16 with everything on, then fp32 logits alone:
-//   rows          1           8            64           96           128          256          512         1024        2048
-//    2000     14.8  7.7   21.4 11.0   21.2 10.9    22.1 11.3    21.8 11.1    22.4 11.5    27.2 14.0    27.1 13.6   44.1 22.1
-//    8000     11.9  7.3   13.5  8.1   13.6  8.5    14.8  8.5    14.8  8.7    18.4  9.7    28.5 15.7    42.4 23.3   78.0 45.1
-//   16000     10.2  8.3   10.9  9.4   12.5  9.7    13.5 10.0    14.8 10.6    23.5 13.8    38.0 19.1    62.3 32.1    125 61.9
-//   32000      9.0 11.6   10.0 12.3   13.2 13.6    16.7 14.5    19.9 15.2    32.3 21.8    53.8 37.9    94.1 67.3
-//   49152      9.1 16.4    9.2 18.1   15.4 20.3    19.5 21.6    23.3 22.4    44.2 34.8    66.7 61.9
-//    2000      6.7  3.7    7.3  4.0    7.6  4.2     7.7  4.3     7.9  4.3     8.7  4.8    10.1  5.3    12.1  6.3   21.5 11.5
-//   16000      7.5  6.4    7.7  6.8    8.6  7.5     9.9  8.0    11.0  8.4    17.3 13.2    29.7 19.5    47.8 35.1    104 71.3
-//   32000      7.6  9.2    7.7  9.3   10.9 10.8    14.0 11.6    16.8 12.6    27.6 24.5    49.9 44.0    82.1 73.8
-//   49152      7.4 12.9    7.7 13.4   12.7 16.4    16.9 17.5    20.0 19.8    42.0 39.7    66.6 73.7
+// Whether one launch: it reads the logits once, but a row is one compute unit's.
+// - Up to 16384 tokens always; to 32768 where no lists change the logits, else from 80 rows on (their work is then more than a
+//   launch).
+// - To 57344, seven windows a thread (which spill 10 to 23 registers), from 128 rows on; past 36000 not for 257 to 1535 aligned rows:
+//   at most 256 are a compute unit's each, some more wait for a second turn of them, and the caches still hold what two launches
+//   read twice, if p is written past them.
+// Two launches | one, us a call (of small ones the host's time), bf16 with everything on, then fp32 logits alone:
+//   rows                1            8           64           96          128          256          512         1024         2048
+//    2000    10.0    6.1  10.5    6.3  11.0    6.2  11.1    6.2  11.3    6.3  12.2    6.4  13.8    7.6  18.1    9.2  27.3   13.0
+//    8000     9.9    6.7  10.8    6.9  10.6    7.3  11.1    7.5  11.4    7.6  15.2    9.0  21.6   11.7  36.0   23.9  70.0   42.4
+//   16000    10.0    8.5  10.5    9.0  11.1    9.8  12.4   10.0  13.6   10.3  20.3   13.0  32.4   19.3  60.6   36.6   123   64.8
+//   32000     9.6   12.4   9.8   12.7  12.9   14.2  15.8   14.4  18.6   15.4  30.9   24.9  52.3   44.2  94.5   82.0   191    148
+//   40000                                           18.1   20.1  21.6   21.8  42.2   34.4  61.2   61.5   116    114   234    202
+//   49152     9.3   18.2   9.9   18.3  15.5   19.8  19.6   21.2  23.2   23.1  44.0   38.7  65.6   71.7   125    128   256    239
+//   57344                                           21.1   22.5  25.8   24.1  47.3   43.3  76.4   80.0   145    143   303    278
+//    2000     8.9    5.8   8.6    5.6   8.3    5.5   8.4    5.5   8.6    5.8   8.9    5.9   8.8    5.7  10.4    6.0  15.2    7.6
+//    8000     8.0    5.7   8.3    5.9   8.5    6.0   8.9    6.0   8.7    5.8   9.8    6.2  13.1    8.3  22.2   15.1  48.4   31.6
+//   16000     8.5    6.0   8.6    5.9   8.9    6.3   8.8    6.5   9.3    7.0  13.3   10.0  20.9   16.5  41.8   32.2  88.8   53.3
+//   32000     9.2    7.2   8.7    7.4   9.7    8.5  10.9    8.9  12.6    9.6  20.2   18.8  39.1   35.3  70.1   61.2   143    112
+//   40000                                           12.3   12.9  14.0   14.1  30.4   29.2  45.8   52.6  85.0   89.5   180    181
+//   49152     8.6   11.1   8.6   11.6  11.3   12.8  13.4   14.6  15.6   15.7  33.2   33.6  52.2   60.8  96.7    107   214    211
+//   57344                                           14.6   14.3  17.2   16.5  35.7   37.0  60.2   69.9   112    121   253    243
+// 512 and 1024 rows of 49152, the other two kinds: bf16 alone 43.7 54.2 and 81.3 93.1, fp32 with everything on 71.1 74.8 and 133 139.
+// Unaligned, 512 rows of 50257: bf16 with everything on 80.5 63.6, fp32 alone 57.8 53.9.
+bool in_one_launch(const LogitsArgs& a) {
+  const bool lists = a.counts || a.ids || a.bias_starts;
+  if (a.V > 2048 && a.rows >= 1 << 22) return false;   // (a launch holds fewer than 2^32 work items)
+  if (a.V <= 16384) return true;
+  if (a.V <= 32768) return !lists || a.rows >= 80;
+  return a.V <= 57344 && a.rows >= 128 && (a.V <= 36000 || a.rows <= 256 || a.rows >= 1536 || !a.passing);
+}
 template <typename T, typename TO, bool PASSING>
 hipError_t one_launch(const LogitsArgs& a, hipStream_t s) {
   const dim3 rows(static_cast<unsigned>(a.rows));
@@ -543,12 +562,11 @@ hipError_t one_launch(const LogitsArgs& a, hipStream_t s) {
 }
 template <typename T, typename TO>
 hipError_t logits_of(const LogitsArgs& a, hipStream_t s) {
-  const bool fits = a.V <= 2048 || a.rows < 1 << 22;   // (a launch holds fewer than 2^32 work items)
   if (a.probs && a.V < kVec) {
     hipLaunchKernelGGL((logits_one<T, TO, 256, 1, true, false>), dim3(static_cast<unsigned>(a.rows)), dim3(256), 0, s, a);
     return hipGetLastError();
   }
-  if (a.probs && fits && a.V <= (a.rows < 80 ? 16384 : a.rows < 128 ? 32768 : 57344)) return a.passing ? one_launch<T, TO, true>(a, s) : one_launch<T, TO, false>(a, s);
+  if (a.probs && in_one_launch(a)) return a.passing ? one_launch<T, TO, true>(a, s) : one_launch<T, TO, false>(a, s);
   if (a.V < kVec) return logits_at<T, TO, true>(a, s);   // (changed logits)
   return logits_at<T, TO, false>(a, s);
 }

@@ -46,3 +46,25 @@ def test_in_place(rows, V, io, probs, monkeypatch):
         got = l.clone()
         assert pdn.pdn_logits(got, out=got, **kw) is got
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows,V", [(1, 32768), (64, 32000), (79, 16385), (80, 16385), (256, 36001), (257, 36000), (257, 36001), (1535, 36001),
+                                    (1536, 36001), (300, 57344)])
+@pytest.mark.parametrize("lists", [False, True])
+def test_where_one_launch_and_two_meet(rows, V, lists):
+    """By rows, tokens and whether lists change the logits: probabilities against 64 bits, with the bound of block_util."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    from block_util import U
+    g = torch.Generator(device="cuda").manual_seed(rows + V)
+    l = 2 * torch.randn(rows, V, generator=g, device="cuda")
+    T = torch.linspace(0.5, 1.5, rows, device="cuda")
+    ids = torch.randint(0, V, (rows,), generator=g, device="cuda")
+    p = pdn.pdn_logits(l, temperature=T, **(dict(ids=ids.int(), presence=torch.full((rows,), 0.5, device="cuda")) if lists else {}))
+    if lists:
+        l[torch.arange(rows, device="cuda"), ids] -= 0.5
+    arg = (l.double() - l.double().amax(1, keepdim=True)) / T.double()[:, None]
+    e = torch.exp(arg)
+    want = e / e.sum(1, keepdim=True)
+    bound = U * (64 - 4 * arg + (e * -4 * arg).sum(1, keepdim=True) / e.sum(1, keepdim=True)) * want + 2e-38
+    assert ((p.double() - want).abs() <= bound).all()
