@@ -83,15 +83,19 @@ __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row, const 
     r.bias_hi = clamp_row(lane_int(told.bias, n + 1), a.biases);
   } else {
     int64_t n;
-    if (a.starts) {   // the same, 64 sequences at a time
-      int64_t upto = 0;
-      for (int64_t n0 = 0; n0 < a.N; n0 += kWave) {
-        const unsigned long long before = __ballot(n0 + l < a.N && clamp_row(a.starts[min(n0 + l, a.N)], a.rows) <= row);
-        if (before) upto = n0 + 64 - __clzll(before);
+    if (a.starts) {   // the same, of every 64^k-th sequence first (all of them 64 at a time: 16384 rows of 1000, one a sequence, 503 us, so 35)
+      int shift = 0;
+      while ((int64_t)kWave << shift < a.N) shift += 6;
+      n = 0;
+      bool any = true;
+      for (; shift >= 0; shift -= 6) {
+        const int64_t at = n + ((int64_t)l << shift);
+        const unsigned long long before = __ballot(at < a.N && clamp_row(a.starts[min(at, a.N)], a.rows) <= row);
+        any = any && before;
+        if (before) n += (int64_t)(63 - __clzll(before)) << shift;
       }
-      n = max(upto - 1, (int64_t)0);
       r.first = clamp_row(a.starts[n], a.rows);
-      r.out = upto == 0 || clamp_row(a.starts[n + 1], a.rows) <= row;
+      r.out = !any || clamp_row(a.starts[n + 1], a.rows) <= row;
     } else {
       const uint32_t each = static_cast<uint32_t>(a.rows) / static_cast<uint32_t>(a.N);
       n = static_cast<uint32_t>(row) / each;

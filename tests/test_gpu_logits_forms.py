@@ -68,3 +68,27 @@ def test_where_one_launch_and_two_meet(rows, V, lists):
     want = e / e.sum(1, keepdim=True)
     bound = U * (64 - 4 * arg + (e * -4 * arg).sum(1, keepdim=True) / e.sum(1, keepdim=True)) * want + 2e-38
     assert ((p.double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("N", [63, 64, 65, 4095, 4096, 4097, 5000, 270_000])
+@pytest.mark.parametrize("rows_before", [0, 3])
+def test_a_rows_sequence_among_many(N, rows_before):
+    """Sequences of no, one and a few rows, each with a temperature of its own; rows before the first and behind the
+    last belong to none."""
+    import torch
+    import paper_2604_21100_amd as pdn
+    from block_util import U
+    g = torch.Generator(device="cuda").manual_seed(N)
+    lens = torch.randint(0, 4, (N,), generator=g, device="cuda")
+    starts = rows_before + torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), torch.cumsum(lens, 0)])
+    rows, V = int(starts[-1]) + 2, 12
+    l = torch.randn(rows, V, generator=g, device="cuda")
+    T = 0.3 + torch.rand(N, generator=g, device="cuda")
+    out = torch.full((rows, V), 5.0, device="cuda")
+    pdn.pdn_logits(l, temperature=T, starts=starts.int(), out=out)
+    assert (out[:rows_before] == 5.0).all() and (out[-2:] == 5.0).all()
+    own = slice(rows_before, rows - 2)
+    arg = (l[own].double() - l[own].double().amax(1, keepdim=True)) / torch.repeat_interleave(T.double(), lens)[:, None]
+    e = torch.exp(arg)
+    want = e / e.sum(1, keepdim=True)
+    assert ((out[own].double() - want).abs() <= U * (64 - 4 * arg + (e * -4 * arg).sum(1, keepdim=True)) * want).all()
