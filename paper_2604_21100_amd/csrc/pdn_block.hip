@@ -129,8 +129,7 @@ template <int N>
 __device__ __forceinline__ void block_sum(float (&x)[N], float (*buf)[16][4], int& turn) {
 #pragma unroll
   for (int k = 0; k < N; ++k) x[k] = wave_sum(x[k]);
-  const int waves = blockDim.x >> 6;
-  if (waves == 1) return;
+  const int waves = blockDim.x >> 6;   // (two at least)
   float(*const b)[4] = buf[turn & 1];
   ++turn;
   if ((threadIdx.x & 63) == 0)

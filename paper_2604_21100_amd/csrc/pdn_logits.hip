@@ -38,7 +38,6 @@ __device__ __forceinline__ int lane_int(int x, int lane) { return __builtin_amdg
 // a row's sequence and what it has of it
 struct RowOf {
   bool out;             // left out
-  int64_t seq;
   int64_t first;        // its sequence's first row
   const int32_t* counts;
   const uint8_t* mask;
@@ -71,7 +70,6 @@ __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row, const 
   if (told.all) {
     const unsigned long long before = __ballot(l < a.N && clamp_row(told.start, a.rows) <= row);
     const int n = before ? 63 - __clzll(before) : 0;   // the last sequence that starts at the row or before
-    r.seq = n;
     r.first = clamp_row(lane_int(told.start, n), a.rows);
     r.out = !before || clamp_row(lane_int(told.start, n + 1), a.rows) <= row;
     slot = lane_int(told.slot, n);
@@ -102,7 +100,6 @@ __device__ __forceinline__ RowOf row_of(const LogitsArgs& a, int64_t row, const 
       r.first = n * each;
       r.out = false;
     }
-    r.seq = n;
     slot = a.counts && a.slot ? a.slot[n] : n;
     r.temperature = a.temperature ? a.temperature[n] : 1.f;
     r.repetition = a.repetition ? a.repetition[n] : 1.f;
