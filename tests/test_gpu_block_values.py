@@ -126,7 +126,7 @@ def test_heads_whose_squares_leave_fp32(d, norm, each):
 def test_a_weights_gradient_of_gated_rows_is_fp32s(act, dt):
     """dweight is fp32 for bf16 rows too.  Rows of ones with ones as gradient have a factor of one and a sum of one
     term, so dweight is act(z) as computed.  Relative roundings, in u = 2^-24: the exponential two (a step), its
-    correction one; 1 + e, its reciprocal, the product with e and that with z one each: 7.  (The argument's own
+    correction one; 1 + e, its reciprocal (two where it is the hardware's alone), the product with e and that with z one each: 7 or 8.  (The argument's own
     rounding, up to |z| u, is what the correction puts back.)"""
     import torch
     import paper_2604_21100_amd as pdn
