@@ -1,8 +1,8 @@
 // Norms around the rule in a block.  Rows are independent; what bounds every call is
 // the reading and writing of its tensors, so each kernel holds a row in registers, reads every
 // tensor once and writes every output once.  bf16, of 5.15 TB/s that a copy has: the residual norm of 16384 x 2048
-// rows on an fp32 stream 72 us (5.6 TB/s), its backward with both norms and a scale 81 and 5 for the sums
-// (4.7); norms of 16384 x 16 heads of 128 24 us (5.7), the gated one's backward 69 and 4 (4.6).
+// rows on an fp32 stream 73 us (5.5 TB/s), its backward with both norms and a scale 84 and 5 for the sums
+// (4.5); norms of 16384 x 16 heads of 128 24 us (5.7), the gated one's backward 70 and 5 (4.5).
 //
 // Residual norm, rows of D channels (r: 1 / sqrt(mean of squares + eps)):
 //   a = y or y r_y w_post     h = residual + alpha s a      u = h r_h w
@@ -28,7 +28,7 @@ namespace {
 constexpr int kVec = 8;
 
 // The eight columns of a thread: from `col` on in a row of n.  Loads must not branch (a wait for
-// each would follow it: the backward of 16384 x 2048 rows 104 us, without branches 81), so every thread loads eight columns of the row that are there,
+// each would follow it, which took the backward of 16384 x 2048 rows 1.3 times as long), so every thread loads eight columns of the row that are there,
 // and `keep` says which of them are its own: a last thread with fewer than eight takes the row's
 // last eight, one without any the first.  By the row: a multiple of eight columns, more than
 // eight, or fewer (its only thread then loads element by element).
@@ -38,9 +38,12 @@ template <RowKind KIND>
 struct Cols {
   int at, n;
   uint32_t keep;   // bit i: column at + i
-  __device__ __forceinline__ Cols(int col, int n) : n(n) {
+  __device__ __forceinline__ Cols(int col, int n, bool whole = false) : n(n) {   // whole: eight of them are there for sure
     const bool on = col < n;
-    if constexpr (KIND == kEights) {
+    if (whole) {
+      at = col;
+      keep = 0xff;
+    } else if constexpr (KIND == kEights) {
       at = on ? col : 0;
       keep = on ? 0xff : 0;
     } else if constexpr (KIND == kMore) {
@@ -97,12 +100,16 @@ __device__ __forceinline__ void store(T* p, const Cols<KIND>& c, const float (&v
       if (c.keep >> i & 1) p[c.at + i] = x[i];
   }
 }
-// Zero in the columns that are not its own: what enters a row's sum with a vector in it, since the zero
+// x, or zero in a column that is not its own: what enters a row's sum with a vector in it, since the zero
 // of a row there times another column's infinite entry would be a NaN in the whole row.
+template <RowKind KIND>
+__device__ __forceinline__ float own(const Cols<KIND>& c, int i, float x) {
+  return (KIND == kEights ? c.keep : c.keep >> i & 1) ? x : 0.f;
+}
 template <RowKind KIND>
 __device__ __forceinline__ void settle(const Cols<KIND>& c, float (&v)[kVec]) {
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) v[i] = (KIND == kEights ? c.keep : c.keep >> i & 1) ? v[i] : 0.f;
+  for (int i = 0; i < kVec; ++i) v[i] = own(c, i, v[i]);
 }
 // of a vector that may be NULL (= 1)
 template <RowKind KIND>
@@ -185,9 +192,10 @@ struct Team {
       block_sum(x, buf, turn);
     }
   }
-  template <RowKind KIND>
+  // the k-th eight columns of a thread, of CH (of several all but the last are whole: row_threads)
+  template <RowKind KIND, int CH>
   __device__ __forceinline__ Cols<KIND> cols(int k, int D) const {
-    return Cols<KIND>((k * size + lane) * kVec, D);
+    return Cols<KIND>((k * size + lane) * kVec, D, k + 1 < CH);
   }
 };
 
@@ -203,12 +211,12 @@ __global__ __launch_bounds__(GROUP ? kGroupThreads : 1024) void rnorm_fwd(RnormA
     Raw<TS> x[CH];
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, D);
+      const auto o = team.template cols<KIND, CH>(k, D);
       y[k].load(static_cast<const TI*>(a.y) + at, o);
       if (a.residual) x[k].load(static_cast<const TS*>(a.residual) + at, o);
     }
 #pragma unroll
-    for (int k = 0; k < CH; ++k) y[k].settle(team.template cols<KIND>(k, D));
+    for (int k = 0; k < CH; ++k) y[k].settle(team.template cols<KIND, CH>(k, D));
     float h[CH][kVec], q[1] = {0.f}, ry = 1.f;
     if constexpr (POST) {
 #pragma unroll
@@ -221,7 +229,7 @@ __global__ __launch_bounds__(GROUP ? kGroupThreads : 1024) void rnorm_fwd(RnormA
     }
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, D);
+      const auto o = team.template cols<KIND, CH>(k, D);
       float v[kVec];
 #pragma unroll
       for (int i = 0; i < kVec; ++i) h[k][i] = y[k][i];
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(GROUP ? kGroupThreads : 1024) void rnorm_fwd(RnormA
     const float rh = factor(q[0], c, a.eps);
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, D);
+      const auto o = team.template cols<KIND, CH>(k, D);
       float v[kVec];
       ld_weight(a.weight, o, v);
 #pragma unroll
@@ -273,7 +281,7 @@ struct BackRows {   // what a row's step reads
     const int64_t at = row * a.D;
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, static_cast<int>(a.D));
+      const auto o = team.template cols<KIND, CH>(k, static_cast<int>(a.D));
       du[k].load(static_cast<const TI*>(a.du) + at, o);
       h[k].load(static_cast<const TS*>(a.h_in) + at, o);
       if constexpr (Y) {
@@ -286,7 +294,7 @@ struct BackRows {   // what a row's step reads
   __device__ __forceinline__ void settle(const RnormArgs& a, const TEAM& team) {
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, static_cast<int>(a.D));
+      const auto o = team.template cols<KIND, CH>(k, static_cast<int>(a.D));
       du[k].settle(o);
       h[k].settle(o);
       if constexpr (Y) y[k].settle(o);
@@ -299,6 +307,9 @@ template <typename TI, typename TS, int CH, bool POST, bool SCALE, bool GROUP, i
 __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm_bwd(RnormArgs a, int L) {
   constexpr bool kAhead = CH == 1, kShared = kAhead && THREADS > 256;
   constexpr int kVectors = 1 + POST + SCALE;
+  // Where other columns' entries are made zero: once, or in rows of two times eight columns for each, in their products or as they
+  // are loaded (what spills less: 2048 x 16384 with both norms and a scale 186 | 196 us, without the scale 188 | 156).
+  constexpr bool kProducts = !kAhead && SCALE;
   __shared__ float buf[2][16][4];
   __shared__ float kept[CH > 1 && POST ? CH * kVec * THREADS : 1], kept2[CH > 1 && SCALE ? CH * kVec * THREADS : 1];
   __shared__ floatx4 vectors[kShared ? kVectors * 2 * THREADS : 1];   // (a thread's own places, THREADS apart)
@@ -310,7 +321,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
   float w[kVec], wp[kVec], sc[kVec];
   // weight (0), post_weight (1), scale (2) at the thread's columns
   auto of_memory = [&](int which, int k, float (&v)[kVec]) {
-    ld_weight(which == 0 ? a.weight : which == 1 ? a.post_weight : a.scale, team.template cols<KIND>(k, D), v);
+    ld_weight(which == 0 ? a.weight : which == 1 ? a.post_weight : a.scale, team.template cols<KIND, CH>(k, D), v);
   };
   auto place = [&](int which, int half) -> floatx4& {
     return vectors[((which == 2 && !POST ? 1 : which) * 2 + half) * THREADS + threadIdx.x];
@@ -321,10 +332,11 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
       for (int i = 0; i < kVec; ++i) v[i] = place(which, i / 4)[i % 4];
     } else if constexpr (!kAhead) {
       of_memory(which, k, v);
+      if constexpr (!kProducts) settle(team.template cols<KIND, CH>(k, D), v);
     }
   };
   if constexpr (kAhead) {
-    const auto o = team.template cols<KIND>(0, D);
+    const auto o = team.template cols<KIND, CH>(0, D);
     of_memory(0, 0, w);
     settle(o, w);
     if constexpr (POST) {
@@ -365,12 +377,13 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
     float e[POST ? CH : 1][kVec], q[POST ? 3 : 2] = {};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
+      const auto o = team.template cols<KIND, CH>(k, D);
       get(0, k, w);
-      if constexpr (!kAhead) settle(team.template cols<KIND>(k, D), w);
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
+        const float g = r.du[k][i] * w[i];
         q[0] += r.h[k][i] * r.h[k][i];
-        q[1] += r.du[k][i] * w[i] * r.h[k][i];
+        q[1] += (kProducts ? own(o, i, g) : g) * r.h[k][i];
         if constexpr (POST) q[2] += r.y[k][i] * r.y[k][i];
       }
     }
@@ -380,7 +393,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
     float p[1] = {0.f};
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, D);
+      const auto o = team.template cols<KIND, CH>(k, D);
       get(0, k, w);
       if constexpr (POST) get(1, k, wp);
       if constexpr (SCALE) get(2, k, sc);
@@ -408,12 +421,8 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
           if constexpr (kRegs) dp[k][i] += x;
           else kept[(k * kVec + i) * THREADS + threadIdx.x] += x;
           e[k][i] = t[i] * wp[i];
+          p[0] += (kProducts ? own(o, i, e[k][i]) : e[k][i]) * r.y[k][i];
         }
-      }
-      if constexpr (POST) {
-        if constexpr (!kAhead) settle(o, e[k]);
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) p[0] += e[k][i] * r.y[k][i];
       }
       if constexpr (!POST) store(static_cast<TI*>(a.dy) + at, o, t);
     }
@@ -424,7 +433,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
       for (int k = 0; k < CH; ++k) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) e[k][i] = ry * e[k][i] - r.y[k][i] * my;
-        store(static_cast<TI*>(a.dy) + at, team.template cols<KIND>(k, D), e[k]);
+        store(static_cast<TI*>(a.dy) + at, team.template cols<KIND, CH>(k, D), e[k]);
       }
     }
     if constexpr (kAhead) r = next;
@@ -433,7 +442,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
   const int64_t each = gridDim.x * a.D;
   if constexpr (GROUP) {
     __shared__ float sum[kGroupThreads / kWave][kWave * kVec];
-    const auto o = team.template cols<KIND>(0, D);
+    const auto o = team.template cols<KIND, CH>(0, D);
     if (a.dweight) group_part(dw[0], o, L, sum, part);
     if constexpr (POST) {
       if (a.dpost_weight) group_part(dp[0], o, L, sum, part + each);
@@ -444,7 +453,7 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
   } else {
 #pragma unroll
     for (int k = 0; k < CH; ++k) {
-      const auto o = team.template cols<KIND>(k, D);
+      const auto o = team.template cols<KIND, CH>(k, D);
       if constexpr (!kRegs) {
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
@@ -607,7 +616,7 @@ __device__ __forceinline__ void gate(float z, float& act, float& slope) {
 
 // A group of L lanes (a power of two, eight channels a lane) takes a head's row.  Neighbouring groups take
 // neighbouring heads, so that a workgroup reads whole tokens (one head a workgroup: 16 heads of 8, 33, 64 and 128
-// channels, gated backward, 305, 170, 82, 73 us; so 72, 115, 69, 70); with a weight for each head a workgroup
+// channels, gated backward of 2^25 elements, 304, 171, 82, 74 us; so 76, 113, 73, 71); with a weight for each head a workgroup
 // stays with one, whose gradient it can sum.
 constexpr int kThreads = 256;
 struct Walk {   // a group's step: so many tokens and heads on
@@ -769,7 +778,7 @@ int64_t balanced_parts(int64_t rows, int64_t most) {
 int64_t rnorm_parts(int64_t rows, int64_t D) {
   const int64_t at_once = grouped(D) ? kGroupThreads / lanes_for(D) : 1;
   // the workgroups that 256 compute units hold by their registers: 12 waves each up to 256 threads, else 16
-  // (16384 x 2048 rows, everything on: 512 parts 93 us, 768 81, 1024 100)
+  // (everything on, so, with 512 parts and with 1024: 16384 x 2048 bf16 rows 89, 83 and 100 us, 20000 x 1600 82, 88 and 97)
   const int threads = grouped(D) ? kGroupThreads : row_threads(D), waves = threads > 256 ? 16 : 4 * kBackWaves;
   return balanced_parts((rows + at_once - 1) / at_once, 256 * (waves / (threads / kWave)));
 }
