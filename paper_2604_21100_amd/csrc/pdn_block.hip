@@ -421,8 +421,12 @@ __global__ __launch_bounds__(THREADS, THREADS > 256 ? 4 : kBackWaves) void rnorm
           if constexpr (kRegs) dp[k][i] += x;
           else kept[(k * kVec + i) * THREADS + threadIdx.x] += x;
           e[k][i] = t[i] * wp[i];
-          p[0] += (kProducts ? own(o, i, e[k][i]) : e[k][i]) * r.y[k][i];
+          if constexpr (!kAhead) p[0] += (kProducts ? own(o, i, e[k][i]) : e[k][i]) * r.y[k][i];
         }
+      }
+      if constexpr (POST && kAhead) {   // (apart, as it spills less: fp32 8192 x 4096, everything on, 180 us, else 205)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) p[0] += e[k][i] * r.y[k][i];
       }
       if constexpr (!POST) store(static_cast<TI*>(a.dy) + at, o, t);
     }
@@ -777,9 +781,13 @@ int64_t balanced_parts(int64_t rows, int64_t most) {
 
 int64_t rnorm_parts(int64_t rows, int64_t D) {
   const int64_t at_once = grouped(D) ? kGroupThreads / lanes_for(D) : 1;
-  // the workgroups that 256 compute units hold by their registers: 12 waves each up to 256 threads, else 16
-  // (everything on, so, with 512 parts and with 1024: 16384 x 2048 bf16 rows 89, 83 and 100 us, 20000 x 1600 82, 88 and 97)
-  const int threads = grouped(D) ? kGroupThreads : row_threads(D), waves = threads > 256 ? 16 : 4 * kBackWaves;
+  // the workgroups that 256 compute units hold by their registers: 12 waves each up to 256 threads, else 16.  Aligned rows
+  // in which hardly a lane is without columns wait for memory alone, and ten waves ask for enough.  Twelve | ten, us, everything
+  // on: bf16 16384 x 2048 88 | 81, fp32 161 | 153, bf16 33554 x 1000 90 | 88; else 55924 x 600 96 | 104, 111848 x 300 114 | 142, bf16 on an
+  // fp32 stream 32784 x 2047 255 | 274; without norm and scale 20971 x 1600 66 | 76.
+  const int threads = grouped(D) ? kGroupThreads : row_threads(D);
+  const bool full = D % kVec == 0 && D > (kVec - 1) * (grouped(D) ? lanes_for(D) : threads);
+  const int waves = threads > 256 ? 16 : full ? 10 : 4 * kBackWaves;
   return balanced_parts((rows + at_once - 1) / at_once, 256 * (waves / (threads / kWave)));
 }
 
