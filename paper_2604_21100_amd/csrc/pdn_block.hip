@@ -1,8 +1,8 @@
 // Norms around the rule in a block.  Rows are independent; what bounds every call is
 // the reading and writing of its tensors, so each kernel holds a row in registers, reads every
 // tensor once and writes every output once.  bf16, of 5.15 TB/s that a copy has: the residual norm of 16384 x 2048
-// rows on an fp32 stream 73 us (5.5 TB/s), its backward with both norms and a scale 84 and 5 for the sums
-// (4.5); norms of 16384 x 16 heads of 128 24 us (5.7), the gated one's backward 70 and 5 (4.5).
+// rows on an fp32 stream 73 us (5.5 TB/s), its backward with both norms and a scale 77 and 5 for the sums
+// (4.9); norms of 16384 x 16 heads of 128 24 us (5.7), the gated one's backward 70 and 5 (4.5).
 //
 // Residual norm, rows of D channels (r: 1 / sqrt(mean of squares + eps)):
 //   a = y or y r_y w_post     h = residual + alpha s a      u = h r_h w

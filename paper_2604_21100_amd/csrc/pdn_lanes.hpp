@@ -1,6 +1,6 @@
 // Reductions over a wave's lanes on data-parallel primitives: they run at the rate of the
-// VALU, where a shuffle goes through LDS (the residual norm's backward, four sums a row: 16384 x 2048
-// rows in 113 us with shuffles, 104 with these).
+// VALU, where a shuffle goes through LDS (the residual norm's backward with everything on, four sums a row,
+// 16384 x 2048 rows: of bf16 as long with shuffles, of fp32 4 % longer).
 #pragma once
 
 #include <hip/hip_runtime.h>

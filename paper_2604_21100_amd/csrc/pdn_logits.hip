@@ -11,7 +11,7 @@
 // of its own sequence's rows.
 //
 // What bounds it: reading the logits twice and writing p, for 314 rows of 131072 fp32 logits with penalties and masks
-// 43 us (198 MB, 4.6 TB/s) and 57 us (363 MB, 6.4 TB/s), the vector units 0.73 of the time; for a few rows latency, 4.4 and 4.3 us for one of 50257.
+// 44 us (198 MB, 4.5 TB/s) and 58 us (363 MB, 6.3 TB/s), the vector units 0.75 of the time; for a few rows latency, 4.5 and 4.3 us for one of 50257.
 #include <algorithm>
 #include <cmath>
 
@@ -154,8 +154,9 @@ struct Lists {
 // Probabilities are written, and logits read for the last time, past the caches, where rows are aligned to the
 // 16 bytes of an access (else an access ends in the next one's line): what is in the caches then is the
 // logits that the second launch still has to read, and the verification reads a row or two of each sequence's
-// only.  With and without, the call | with its verification, us: 314 rows of 131072 81 | 113 and 99 | 126, 64 rows
-// 18 | 32 and 23 | 36; one launch, 512 rows of 16000 19 and 22.  Unaligned, 512 rows of 50257 80 and 67.
+// only.  With and without, fp32 rows with penalties and masks, the call | with its verification, us: 314 of 131072
+// 100 | 119 and 112 | 132, 64 of them 35 | 50 and 37 | 52; one launch, 314 of 16000 13.5 | 23 and 16.4 | 26.  Unaligned rows took 1.2
+// times as long with it.
 typedef uint32_t Sixteen __attribute__((ext_vector_type(4), aligned(2), may_alias));
 
 // A thread's eight tokens from j on.  Loads do not branch (a wait for each would follow): a last thread with
@@ -389,8 +390,8 @@ __device__ __forceinline__ Part whole_of(const Part* parts, const Part& x, uint3
   return all;
 }
 
-// The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves. No loop:
-// a loop's loads would wait for the stores before them (84 us against 75).
+// The second launch: p of a window of kSeg tokens from the parts of all, or the changed logits themselves. No loop
+// (two windows a workgroup: 58.3 us for 314 rows of 131072, so 57.5).
 template <typename T, typename TO, bool TINY, bool PROBS, bool PASSING>
 __global__ __launch_bounds__(kThreads) void logits_out(LogitsArgs a, uint32_t windows, uint32_t segs) {
   const uint32_t row = blockIdx.x / windows, base = blockIdx.x % windows * kSeg + (threadIdx.x >> 6) * kWaveSpan;
@@ -503,7 +504,7 @@ __global__ __launch_bounds__(THREADS) void logits_one(LogitsArgs a) {
 
 // A row's segments in the first of two launches: about so many workgroups in all, eight to a row or a multiple of it,
 // as workgroups go to the eight L2s in turn: the rows of a sequence then find its counts in one. (314 rows of
-// 131072: 8 segments 54 us, 16 51.5, 32 55, 13 58.)
+// 131072: 8 segments 43.3 us, 16 44.2, 32 51.4, 13 51.6.)
 constexpr int64_t kManyBlocks = 4096;
 template <typename T, typename TO, bool TINY>
 hipError_t logits_at(const LogitsArgs& a, hipStream_t s) {
