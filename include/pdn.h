@@ -434,8 +434,9 @@ pdn_status pdn_draft_verify(int64_t N, int64_t rows, int64_t V, pdn_dtype dtype,
  * need to be aligned to an element only (16 bytes are faster).  Rows do not
  * depend on each other: a NaN or Inf shows in its own row, and in the gradients of
  * the vectors.  A row's squares are summed in fp32: one whose sum passes 3.4e38 is out
- * of range (its norm is zeros; the gradients through that norm, and of the vectors on it, are NaN).  Gradients of vectors are summed in one order, so
- * a call's results are the same each time.  No call allocates. */
+ * of range (its norm is zeros; the gradients through that norm, and of the vectors on
+ * it, are NaN).  Gradients of vectors are summed in one order, so a call's results are
+ * the same each time.  No call allocates. */
 
 typedef struct {
   int64_t rows, D;      /* rows of D channels; D from 1 to 16384               */
